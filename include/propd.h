@@ -308,6 +308,137 @@ PROPD_API propd_status propd_commit_path(const propd_tree *tree, propd_dtype dt,
                                void *hip_stream);
 
 /*
+ * A bounded K/V cache with shared heads: what a decoding loop needs when the model's query heads share
+ * K/V heads and the generation is longer than the cache.  A step then is
+ *   propd_rotary             positions of the tree's nodes into q and k
+ *   propd_grouped_attention  the nodes over the cached rows, with lse
+ *   propd_accept_path        (any of the calls above that shape the tree fit in between)
+ *   propd_cache_observe      what the accepted nodes paid to every cached row, and the new rows' positions
+ *   propd_commit_path        with H = H_kv
+ *   propd_cache_evict        the rows that were paid least go, where there are more than `budget`
+ * Positions.  seq_lens[b] rows of a sequence's cache are in use, dropped[b] >= 0 positions of the sequence have no
+ * row any more (NULL: none), so its next position - that of the tree's root - is P = seq_lens[b] + dropped[b]; a node's is
+ * P + its depth, taken from its ancestor set.  position [B,H_kv,L_max] holds the position of every cached row, per
+ * K/V head, in any order; NULL: row j has position dropped[b] + j.  A negative entry marks a row that nobody sees.
+ * Positions have to be below 2^30.
+ *
+ * How scores are made of products, for query position p_i and key position p_j:
+ *     s = scale * <q_i, k_j>;  cap > 0: s = cap * tanh(s / cap);  slopes: s = s - slopes[h] * (p_i - p_j)
+ * and which keys a query sees: cached rows with 0 <= p_j <= p_i, nodes of its ancestor set; of both
+ * only those with p_i - p_j < window where window > 0.
+ */
+typedef struct propd_score_rule {
+  float scale;          /* > 0                                                       */
+  float cap;            /* 0: scores are not capped; otherwise 2^-10 .. 1024          */
+  int32_t window;       /* 0: no window; >= 0                                        */
+  const float *slopes;  /* [H] or NULL: bias per position of distance, finite        */
+} propd_score_rule;
+
+/*
+ * Tree attention with shared K/V heads.  Query head h reads K/V head h / (H / H_kv); otherwise as
+ * propd_tree_attention, with the rule above:
+ *     out[b,h,i,:] = softmax_j(s_ij) . v_j,   lse[b,h,i] = log sum_j exp(s_ij)
+ * A single token per sequence is a tree of one node.  A row that sees nothing (only possible where a node's set lacks the
+ * node itself) gets zeros, lse -inf.  A key that a query does not see does not touch its result, whatever it holds.
+ *
+ *   H, H_kv    H a multiple of H_kv
+ *   dt, d      PROPD_BF16 or PROPD_F32, d in {64, 128}.  Scores, softmax and sums are fp32; PROPD_BF16 rounds the weights to
+ *              bf16 before they meet V, and the result.
+ *   q, out     [B,H,T_max,d]        k_tree, v_tree  [B,H_kv,T_max,d]
+ *   k_cache, v_cache  [B,H_kv,L_max,d]; rows >= seq_lens[b] are never used
+ *   position, dropped  see above; either may be NULL
+ *   tree       n_nodes and anc are read
+ *   lse        [B,H,T_max] fp32 or NULL
+ *   out and lse rows i >= n_nodes[b] are left untouched
+ *   workspace  propd_workspace_bytes(PROPD_WS_GROUPED_ATTENTION, B, T_max, H, d, L_max, 0, 0) bytes
+ * q, k_cache, v_cache, k_tree, v_tree, out, anc and workspace must be 16-byte aligned.
+ */
+PROPD_API propd_status propd_grouped_attention(const propd_tree *tree, propd_dtype dt, int32_t H, int32_t H_kv, int32_t d,
+                                     const propd_score_rule *rule, const void *q, const void *k_cache, const void *v_cache,
+                                     const void *k_tree, const void *v_tree, const int32_t *seq_lens,
+                                     const int32_t *position, const int32_t *dropped, int32_t L_max, void *out, float *lse,
+                                     void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * What the accepted nodes paid to every row of the cache, between acceptance and commit of a step.  With the
+ * path's nodes n_0 (the root), ..., n_{a-1} = accept_path[b,0..a-1], a = accept_len[b], at positions P, ..., P + a - 1,
+ * L = seq_lens[b] and the scores and the visibility of `rule` (node n_r sees the path up to itself):
+ *     paid[j] = sum over r and the query heads h of the K/V head of exp(s_rj - lse[b,h,n_r])
+ *     weight_out[b,hk,j] = decay * weight[b,hk,j] + paid[j]      position_out[b,hk,j] = position[b,hk,j]     j < L
+ *     weight_out[b,hk,L+r] = paid[n_r]                           position_out[b,hk,L+r] = P + r              r < a
+ * so that the rows that propd_commit_path appends next have their entries.  Rows that do not fit (L + r >= L_max) are
+ * left out, as by the commit; seq_lens[b] + dropped[b] then falls behind by as many.  Entries from there on
+ * are left untouched.
+ *
+ *   q          [B,H,T_max,d]   of the tree that the path indexes     lse  [B,H,T_max], as left by the attention
+ *   k_tree     [B,H_kv,T_max,d]     k_cache  [B,H_kv,L_max,d]
+ *   accept_len, accept_path, path_stride   as written by propd_accept_path.  accept_len is clamped to [0, path_stride]; a path
+ *              entry outside [0, n_nodes[b]) pays nothing and its row gets weight 0 and position -1
+ *   position   with position_out, or both NULL: rows in the order of their positions
+ *   weight_out, position_out  may be weight and position themselves, but must not overlap them otherwise
+ *   decay      0 < decay <= 1
+ *   tree       n_nodes is read
+ * Every sum is made by one wave in a fixed order.  No workspace.  q, k_cache and k_tree must be 16-byte aligned.
+ */
+PROPD_API propd_status propd_cache_observe(const propd_tree *tree, propd_dtype dt, int32_t H, int32_t H_kv, int32_t d,
+                                 const propd_score_rule *rule, float decay, const int32_t *accept_len,
+                                 const int32_t *accept_path, int32_t path_stride, const void *q, const float *lse,
+                                 const void *k_cache, const void *k_tree, const int32_t *seq_lens, const int32_t *dropped,
+                                 const int32_t *position, const float *weight, int32_t L_max, int32_t *position_out,
+                                 float *weight_out, void *hip_stream);
+
+/* Per-row state of a cache, see above. */
+typedef struct propd_cache_rows {
+  int32_t *seq_lens;  /* [B]                  */
+  int32_t *dropped;   /* [B]                  */
+  int32_t *position;  /* [B,H_kv,L_max]       */
+  float *weight;      /* [B,H_kv,L_max] fp32  */
+} propd_cache_rows;
+
+/*
+ * Eviction: of every sequence with more than `budget` rows each K/V head keeps `budget` of them,
+ * the first of this order:
+ *   rows with position >= P - recent or position < sinks (P = seq_lens[b] + dropped[b]), by rising row;
+ *   then the others by falling weight, equal weights (0 and -0 are equal) by rising row;
+ *   then rows with weight NaN or -inf, and rows with a negative position whatever else holds, by rising row.
+ * The kept rows at or beyond `budget` move to the places below it that became free, both in rising order: the k-th of
+ * the ones to the k-th of the others.  K, V, position and weight move together, no other row changes,
+ * and what lies at or beyond the new length is left as it was.
+ *     rows_out->seq_lens[b] = min(L, budget),  rows_out->dropped[b] = dropped[b] + L - that
+ * Sequences of at most `budget` rows stay as they are.
+ *
+ *   k_cache, v_cache  [B,H_kv,L_max,d] in place; d * sizeof a multiple of 16, 16-byte aligned
+ *   rows, rows_out    host structs of device arrays, all of them given.  Each array of rows_out may be that of rows, in place, or another one: it
+ *                     then gets the entries of the rows kept (position and weight below the new length, nothing else)
+ *   budget            1..L_max     recent, sinks  >= 0
+ *   workspace         propd_workspace_bytes(PROPD_WS_CACHE_EVICT, B, 0, H_kv, 0, L_max, 0, 0) bytes, 16-byte aligned
+ */
+PROPD_API propd_status propd_cache_evict(int32_t B, propd_dtype dt, int32_t H_kv, int32_t d, int32_t L_max, int32_t budget,
+                               int32_t recent, int32_t sinks, void *k_cache, void *v_cache, const propd_cache_rows *rows,
+                               const propd_cache_rows *rows_out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Rotary positions of one or several axes (for instance time, height and width), for the nodes of a tree or the
+ * rows of a prompt.  Pair c of every head is turned by the angle
+ *     start[b, axis_of[c]] + offset[b, axis_of[c], s]   times   inv_freq[c],   c < rot / 2
+ * (positions as 64-bit sums, angles in 64 bits):  (x, y) -> (x cos - y sin, y cos + x sin).
+ *   rot        channels that turn, a multiple of 16, <= d; the others are copied.  Pair c is channels c and c + rot/2, or,
+ *              with adjacent != 0, channels 2c and 2c + 1
+ *   inv_freq   [rot/2] fp32
+ *   n_axes     >= 1         axis_of  [rot/2], clamped to [0, n_axes); NULL: all 0
+ *   start      [B,n_axes] or NULL: zeros
+ *   offset     [B,offset_axes,S], offset_axes 1 (the same for all axes, for instance a tree's depth) or n_axes
+ *   n_rows     [B] or NULL: rows s >= n_rows[b] are left untouched
+ *   q [B,H,S,d], k [B,H_kv,S,d] or NULL (with H_kv = 0);  q_out, k_out  of the same shape, q and k themselves or not overlapping
+ *   dt         PROPD_BF16 or PROPD_F32, d a multiple of 8; results are fp32, rounded once
+ * q, k, q_out and k_out must be 16-byte aligned.
+ */
+PROPD_API propd_status propd_rotary(propd_dtype dt, int32_t B, int32_t S, int32_t H, int32_t H_kv, int32_t d, int32_t rot,
+                          int32_t adjacent, int32_t n_axes, const int32_t *axis_of, const float *inv_freq,
+                          const int32_t *start, const int32_t *offset, int32_t offset_axes, const int32_t *n_rows, const void *q,
+                          const void *k, void *q_out, void *k_out, void *hip_stream);
+
+/*
  * Dynamic token-tree generation (Section 4.2): the controller that picks the tree size from
  * measured iteration times and measured head accuracies.  HOST code: every pointer below is
  * a host pointer, nothing is enqueued on a stream, no device is touched.  It is meant to run
@@ -374,7 +505,9 @@ PROPD_API propd_status propd_controller_best_size(const void *state, double now,
 typedef enum {
   PROPD_WS_TREE_ATTENTION = 0,
   PROPD_WS_EARLY_PRUNE = 1,
-  PROPD_WS_ACCEPT_PATH = 2
+  PROPD_WS_ACCEPT_PATH = 2,
+  PROPD_WS_GROUPED_ATTENTION = 3,
+  PROPD_WS_CACHE_EVICT = 4 /* H is the number of K/V heads */
 } propd_ws_kind;
 PROPD_API size_t propd_workspace_bytes(propd_ws_kind which, int32_t B, int32_t T_max, int32_t H, int32_t d,
                              int32_t L_max, int32_t hidden, int32_t vocab);

@@ -24,12 +24,12 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpropd.so")
 
 PROPD_F32, PROPD_BF16 = 0, 1
-WS_TREE_ATTENTION, WS_EARLY_PRUNE, WS_ACCEPT_PATH = 0, 1, 2
+WS_TREE_ATTENTION, WS_EARLY_PRUNE, WS_ACCEPT_PATH, WS_GROUPED_ATTENTION, WS_CACHE_EVICT = 0, 1, 2, 3, 4
 MAX_TREE = 128
 MAX_PAYLOADS = 8
 
 EXPORTS = ("propd_tree_mask", "propd_validate_tree", "propd_tree_attention", "propd_early_prune", "propd_accept_path",
-           "propd_accept_path_static", "propd_early_prune_prob", "propd_commit_path", "propd_workspace_bytes", "propd_status_string",
+           "propd_accept_path_static", "propd_early_prune_prob", "propd_commit_path", "propd_grouped_attention", "propd_cache_observe", "propd_cache_evict", "propd_rotary", "propd_workspace_bytes", "propd_status_string",
            "propd_controller_bytes", "propd_controller_init", "propd_controller_observe_time",
            "propd_controller_observe_hit", "propd_controller_fit", "propd_controller_build_tree",
            "propd_controller_best_size")
@@ -50,6 +50,14 @@ class _Payload(ctypes.Structure):
     _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("row_bytes", ctypes.c_size_t),
                 ("outer", ctypes.c_int64), ("stride_b", ctypes.c_int64),
                 ("stride_outer", ctypes.c_int64), ("stride_t", ctypes.c_int64)]
+
+
+class _ScoreRule(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("cap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p)]
+
+
+class _CacheRows(ctypes.Structure):
+    _fields_ = [("seq_lens", ctypes.c_void_p), ("dropped", ctypes.c_void_p), ("position", ctypes.c_void_p), ("weight", ctypes.c_void_p)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -114,6 +122,17 @@ def load_library() -> ctypes.CDLL:
     lib.propd_commit_path.restype = ctypes.c_int
     lib.propd_commit_path.argtypes = [ctypes.POINTER(_Tree), ctypes.c_int, i32, i32, vp, vp, i32, vp,
                                       vp, vp, vp, vp, i32, vp, vp, i32, vp]
+    rule, rows, f32 = ctypes.POINTER(_ScoreRule), ctypes.POINTER(_CacheRows), ctypes.c_float
+    lib.propd_grouped_attention.restype = ctypes.c_int
+    lib.propd_grouped_attention.argtypes = [ctypes.POINTER(_Tree), ctypes.c_int, i32, i32, i32, rule, vp, vp, vp, vp, vp, vp, vp, vp,
+                                            i32, vp, vp, vp, sz, vp]
+    lib.propd_cache_observe.restype = ctypes.c_int
+    lib.propd_cache_observe.argtypes = [ctypes.POINTER(_Tree), ctypes.c_int, i32, i32, i32, rule, f32, vp, vp, i32, vp, vp, vp, vp,
+                                        vp, vp, vp, vp, i32, vp, vp, vp]
+    lib.propd_cache_evict.restype = ctypes.c_int
+    lib.propd_cache_evict.argtypes = [i32, ctypes.c_int, i32, i32, i32, i32, i32, i32, vp, vp, rows, rows, vp, sz, vp]
+    lib.propd_rotary.restype = ctypes.c_int
+    lib.propd_rotary.argtypes = [ctypes.c_int, i32, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
     lib.propd_workspace_bytes.restype = sz
     lib.propd_workspace_bytes.argtypes = [ctypes.c_int, i32, i32, i32, i32, i32, i32, i32]
     dbl, pd = ctypes.c_double, ctypes.POINTER(ctypes.c_double)
@@ -494,6 +513,170 @@ def propd_commit_path(tree: Tree, accept_len: torch.Tensor, accept_path: torch.T
         _ptr(next_token), _ptr(k_tree), _ptr(v_tree), _ptr(k_cache), _ptr(v_cache), L_max,
         _ptr(seq_lens), _ptr(out), out_stride, _stream()), "propd_commit_path")
     return out
+
+
+# ---- a bounded K/V cache with shared heads (see propd.h)
+
+def _all_dev(device: torch.device, **named) -> None:
+    """Contiguous GPU tensors on `device`, the current one: each a tensor (or None) with its type and, if given, its shape."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise TypeError("the tensors have to be on the current GPU")
+    for name, (t, dtype, shape) in named.items():
+        if t is None:
+            continue
+        _dev(t, dtype, name)
+        if t.device != device:
+            raise TypeError(f"{name}: on another device")
+        if shape is not None and tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _same_or_apart(out: Optional[torch.Tensor], src: Optional[torch.Tensor], name: str) -> None:
+    if out is None or src is None or out.data_ptr() == src.data_ptr():
+        return
+    if out.data_ptr() < src.data_ptr() + src.nbytes and src.data_ptr() < out.data_ptr() + out.nbytes:
+        raise ValueError(f"{name}: overlaps the input without being the same")
+
+
+def _apart(out: Optional[torch.Tensor], name: str, *others: Optional[torch.Tensor]) -> None:
+    for t in others:
+        if out is not None and t is not None and out.nbytes and t.nbytes and out.data_ptr() < t.data_ptr() + t.nbytes and \
+                t.data_ptr() < out.data_ptr() + out.nbytes:
+            raise ValueError(f"{name}: overlaps another argument")
+
+
+@dataclass
+class CacheRows:
+    """Per-row state of a bounded cache (``propd_cache_rows``)."""
+    seq_lens: torch.Tensor                   # int32 [B]            rows in use
+    dropped: Optional[torch.Tensor] = None   # int32 [B]            positions that have no row any more
+    position: Optional[torch.Tensor] = None  # int32 [B,H_kv,L_max]
+    weight: Optional[torch.Tensor] = None    # float32 [B,H_kv,L_max]
+
+    def _c(self) -> _CacheRows:
+        return _CacheRows(_ptr(self.seq_lens), _ptr(self.dropped), _ptr(self.position), _ptr(self.weight))
+
+
+def _shared_heads(tree: Tree, q: torch.Tensor, k_tree: torch.Tensor, k_cache: torch.Tensor):
+    if q.dim() != 4 or k_tree.dim() != 4 or k_cache.dim() != 4:
+        raise ValueError("q, k_tree and k_cache have four dimensions")
+    B, H, T_max, d = q.shape
+    H_kv, L_max = k_tree.shape[1], k_cache.shape[2]
+    if tree.B != B or tree.T_max != T_max:
+        raise ValueError("tree and q disagree on B or T_max")
+    if H_kv < 1 or H % H_kv:
+        raise ValueError("the query heads must be a multiple of the K/V heads")
+    return B, H, H_kv, T_max, d, L_max
+
+
+def propd_grouped_attention(tree: Tree, q, k_cache, v_cache, k_tree, v_tree, seq_lens, scale: float, cap: float = 0.0,
+                            window: int = 0, slopes: Optional[torch.Tensor] = None, position: Optional[torch.Tensor] = None,
+                            dropped: Optional[torch.Tensor] = None, want_lse: bool = False, out: Optional[torch.Tensor] = None,
+                            lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """-> out [B,H,T_max,d], or (out, lse) if ``want_lse`` or an ``lse`` tensor is given."""
+    B, H, H_kv, T_max, d, L_max = _shared_heads(tree, q, k_tree, k_cache)
+    dt, i32, f32 = _dt(q), torch.int32, torch.float32
+    cache, rows = (B, H_kv, L_max, d), (B, H_kv, T_max, d)
+    if lse is None and want_lse:
+        lse = torch.empty((B, H, T_max), dtype=f32, device=q.device)
+    if out is None:
+        out = torch.empty_like(q)
+    _all_dev(q.device, q=(q, q.dtype, None), k_cache=(k_cache, q.dtype, cache), v_cache=(v_cache, q.dtype, cache),
+             k_tree=(k_tree, q.dtype, rows), v_tree=(v_tree, q.dtype, rows), seq_lens=(seq_lens, i32, (B,)),
+             n_nodes=(tree.n_nodes, i32, (B,)), anc=(tree.anc, torch.int64, (B, T_max, 2)), slopes=(slopes, f32, (H,)),
+             position=(position, i32, cache[:3]), dropped=(dropped, i32, (B,)), out=(out, q.dtype, q.shape), lse=(lse, f32, q.shape[:3]))
+    _apart(out, "out", q, k_cache, v_cache, k_tree, v_tree, lse)
+    ws = _workspace(workspace_bytes(WS_GROUPED_ATTENTION, B, T_max, H, d, L_max), q.device, workspace)
+    c_tree, rule = tree._c(), _ScoreRule(scale, cap, window, _ptr(slopes))
+    _check(load_library().propd_grouped_attention(
+        ctypes.byref(c_tree), dt, H, H_kv, d, ctypes.byref(rule), _ptr(q), _ptr(k_cache) if L_max else None,
+        _ptr(v_cache) if L_max else None, _ptr(k_tree), _ptr(v_tree), _ptr(seq_lens), _ptr(position) if L_max else None, _ptr(dropped),
+        L_max, _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream()), "propd_grouped_attention")
+    return out if lse is None else (out, lse)
+
+
+def propd_cache_observe(tree: Tree, accept_len: torch.Tensor, accept_path: torch.Tensor, q: torch.Tensor, lse: torch.Tensor,
+                        k_cache: torch.Tensor, k_tree: torch.Tensor, rows: CacheRows, scale: float, cap: float = 0.0, window: int = 0,
+                        slopes: Optional[torch.Tensor] = None, decay: float = 1.0, weight_out: Optional[torch.Tensor] = None,
+                        position_out: Optional[torch.Tensor] = None) -> None:
+    """Adds what the accepted nodes paid to every row to ``rows.weight``, and sets weight and position of the rows that the
+    commit is about to append; IN PLACE unless ``weight_out`` (``position_out``) is given.  Between acceptance and commit."""
+    B, H, H_kv, T_max, d, L_max = _shared_heads(tree, q, k_tree, k_cache)
+    dt, i32, f32 = _dt(q), torch.int32, torch.float32
+    weight_out = rows.weight if weight_out is None else weight_out
+    position_out = rows.position if position_out is None else position_out
+    if rows.weight is None:
+        raise ValueError("rows.weight is needed")
+    if accept_path.dim() != 2:
+        raise ValueError("accept_path has two dimensions")
+    state = (B, H_kv, L_max)
+    _all_dev(q.device, q=(q, q.dtype, None), k_cache=(k_cache, q.dtype, (B, H_kv, L_max, d)), k_tree=(k_tree, q.dtype, (B, H_kv, T_max, d)),
+             lse=(lse, f32, (B, H, T_max)), n_nodes=(tree.n_nodes, i32, (B,)), accept_len=(accept_len, i32, (B,)),
+             accept_path=(accept_path, i32, (B, accept_path.shape[1])), seq_lens=(rows.seq_lens, i32, (B,)), dropped=(rows.dropped, i32, (B,)),
+             position=(rows.position, i32, state), weight=(rows.weight, f32, state), slopes=(slopes, f32, (H,)),
+             weight_out=(weight_out, f32, state), position_out=(position_out, i32, state))
+    _same_or_apart(weight_out, rows.weight, "weight_out")
+    _same_or_apart(position_out, rows.position, "position_out")
+    c_tree, rule = tree._c(), _ScoreRule(scale, cap, window, _ptr(slopes))
+    _check(load_library().propd_cache_observe(
+        ctypes.byref(c_tree), dt, H, H_kv, d, ctypes.byref(rule), decay, _ptr(accept_len), _ptr(accept_path), accept_path.shape[1],
+        _ptr(q), _ptr(lse), _ptr(k_cache), _ptr(k_tree), _ptr(rows.seq_lens), _ptr(rows.dropped), _ptr(rows.position), _ptr(rows.weight),
+        L_max, _ptr(position_out), _ptr(weight_out), _stream()), "propd_cache_observe")
+
+
+def propd_cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, rows: CacheRows, budget: int, recent: int, sinks: int = 0,
+                      rows_out: Optional[CacheRows] = None, workspace: Optional[torch.Tensor] = None) -> None:
+    """Down to ``budget`` rows per K/V head, IN PLACE; the per-row state too unless ``rows_out`` is given."""
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache has four dimensions")
+    B, H_kv, L_max, d = k_cache.shape
+    dt, i32, f32 = _dt(k_cache), torch.int32, torch.float32
+    rows_out = rows if rows_out is None else rows_out
+    for r, which in ((rows, "rows"), (rows_out, "rows_out")):
+        for name, dtype, shape in (("seq_lens", i32, (B,)), ("dropped", i32, (B,)), ("position", i32, (B, H_kv, L_max)),
+                                   ("weight", f32, (B, H_kv, L_max))):
+            if getattr(r, name) is None:
+                raise ValueError(f"{which}.{name} is needed")
+            _all_dev(k_cache.device, **{f"{which}.{name}": (getattr(r, name), dtype, shape)})
+            _same_or_apart(getattr(rows_out, name), getattr(rows, name), f"rows_out.{name}")
+    _all_dev(k_cache.device, k_cache=(k_cache, k_cache.dtype, None), v_cache=(v_cache, k_cache.dtype, k_cache.shape))
+    _apart(v_cache, "v_cache", k_cache)
+    ws = _workspace(workspace_bytes(WS_CACHE_EVICT, B, 0, H_kv, L_max=L_max), k_cache.device, workspace)
+    c_rows, c_out = rows._c(), rows_out._c()
+    _check(load_library().propd_cache_evict(
+        B, dt, H_kv, d, L_max, budget, recent, sinks, _ptr(k_cache), _ptr(v_cache), ctypes.byref(c_rows), ctypes.byref(c_out), _ptr(ws),
+        ws.numel() * ws.element_size(), _stream()), "propd_cache_evict")
+
+
+def propd_rotary(q: torch.Tensor, k: Optional[torch.Tensor], inv_freq: torch.Tensor, offset: torch.Tensor,
+                 start: Optional[torch.Tensor] = None, axis_of: Optional[torch.Tensor] = None, n_rows: Optional[torch.Tensor] = None,
+                 adjacent: bool = False, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """-> (q_out, k_out).  ``offset`` is int32 [B,S] (all axes alike) or [B,n_axes,S], ``start`` int32 [B,n_axes]; twice as many
+    channels turn as ``inv_freq`` has entries.  ``q_out`` may be ``q``, and ``k_out`` ``k``."""
+    if q.dim() != 4 or (k is not None and k.dim() != 4) or offset.dim() not in (2, 3) or inv_freq.dim() != 1:
+        raise ValueError("q and k have four dimensions, offset two or three, inv_freq one")
+    B, H, S, d = q.shape
+    H_kv = 0 if k is None else k.shape[1]
+    n_axes = start.shape[-1] if start is not None else offset.shape[1] if offset.dim() == 3 else 1
+    offset_axes = offset.shape[1] if offset.dim() == 3 else 1
+    dt, i32 = _dt(q), torch.int32
+    q_out = torch.empty_like(q) if q_out is None else q_out
+    k_out = torch.empty_like(k) if k_out is None and k is not None else k_out
+    if (k is None) != (k_out is None):
+        raise ValueError("k_out without k")
+    pairs = inv_freq.shape[0]
+    kv = None if k is None else (B, H_kv, S, d)
+    _all_dev(q.device, q=(q, q.dtype, None), k=(k, q.dtype, kv), q_out=(q_out, q.dtype, q.shape), k_out=(k_out, q.dtype, kv),
+             inv_freq=(inv_freq, torch.float32, None), offset=(offset, i32, (B, offset_axes, S) if offset.dim() == 3 else (B, S)),
+             start=(start, i32, (B, n_axes)), axis_of=(axis_of, i32, (pairs,)), n_rows=(n_rows, i32, (B,)))
+    _same_or_apart(q_out, q, "q_out")
+    _same_or_apart(k_out, k, "k_out")
+    _apart(q_out, "q_out", k, k_out)
+    _apart(k_out, "k_out", q)
+    _check(load_library().propd_rotary(dt, B, S, H, H_kv, d, 2 * pairs, int(adjacent), n_axes, _ptr(axis_of), _ptr(inv_freq), _ptr(start),
+                                       _ptr(offset), offset_axes, _ptr(n_rows), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _stream()),
+           "propd_rotary")
+    return q_out, k_out
 
 
 class Controller:

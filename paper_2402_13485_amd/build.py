@@ -15,7 +15,8 @@ MARSHAL_PATH = os.path.join(HERE, "_marshal.so")
 MARSHAL_SOURCE = "marshal.cpp"
 HEADER = os.path.join(HERE, os.pardir, "include", "propd.h")
 SOURCES = ["tree_mask.hip", "tree_attention.hip", "early_prune.hip", "accept_path.hip",
-           "commit_path.hip", "tree_controller.hip"]
+           "commit_path.hip", "tree_controller.hip", "grouped_attention.hip", "cache_observe.hip", "cache_evict.hip",
+           "rotary.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",  # no packed-fp32 codegen
@@ -27,7 +28,8 @@ FLAGS = [
 # by hand).  A register that is saved to scratch memory or to an accumulation register while such a load
 # is on its way is saved before the value is there, and the load then lands in a register that
 # holds something else by that time, an address for instance.
-HAND_WAITED = ("tree_attn_bf16_kernel", "early_head_bf16_kernel")
+HAND_WAITED = {"tree_attn_bf16_kernel": "tree_attention.hip", "early_head_bf16_kernel": "early_prune.hip",
+               "grouped_attn_bf16_kernel": "grouped_attention.hip"}  # and the source that has them
 
 
 def unsafe_kernels(remarks: str) -> list:
@@ -42,7 +44,8 @@ def unsafe_kernels(remarks: str) -> list:
                 seen.add(kernel)
                 if len(used) != 3 or any(used.values()):
                     found.append(f"{name}: {used}")
-    return found + [f"{kernel}: no resource usage reported" for kernel in HAND_WAITED if kernel not in seen]
+    return found + [f"{kernel}: no resource usage reported" for kernel, source in HAND_WAITED.items()
+                    if kernel not in seen and source in SOURCES]
 
 
 def has_marshal() -> bool:

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/propd.h"
 
 namespace propd {
@@ -82,9 +84,23 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 inline bool launch_ok() { return hipGetLastError() == hipSuccess; }
 
+// Lets a kernel use this much LDS.  The setting belongs to the device that is current; `set` remembers for which (the first 64)
+// it was made, for calls from several threads.
+inline bool allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &set) {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return false;
+  const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0ull;
+  if (set.load() & bit) return true;
+  if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return false;
+  set.fetch_or(bit);
+  return true;
+}
+
 // scratch sizes (host arithmetic), defined next to the kernels that use the scratch
 size_t early_prune_workspace_bytes(int B, int T_max, int vocab);
 size_t tree_attention_workspace_bytes(int B, int H, int L_max, int T_max);
 size_t accept_path_workspace_bytes(int B, int T_max);
+size_t grouped_attention_workspace_bytes(int B, int H, int L_max, int T_max);
+size_t cache_evict_workspace_bytes(int B, int H_kv, int L_max);
 
 }  // namespace propd

@@ -1,0 +1,696 @@
+// Tree attention whose K/V heads are shared by several query heads, with capped and biased scores, a window and cached
+// rows at positions of their own.
+//
+// bf16 path.  A unit is a (sequence, K/V head, block of 128 query columns): the nodes of all query heads that read
+// the K/V head lie side by side, column r is node r % T of head r / T, so that a K or V row is read once for all of them.
+//   - A workgroup takes one range of a unit's 32-row stages of K and V (cached rows, then tree rows) and streams it through
+//     a ring in LDS by direct loads; its four waves own 32 columns each.
+//   - S^T = K . Q^T by the 32x32x16 products, so that a lane owns a column: the softmax statistics, the query's
+//     position, slope and ancestor set are per-lane scalars, and the weights, rounded to bf16, are the B
+//     operand of O^T += V^T . P^T (V^T by the transposing LDS read).  The scores of stage i + 1 are multiplied in front
+//     of the softmax of stage i.
+//   - A unit is cut into as many ranges as the chip needs (plan_ranges); partial results are merged by a second kernel, in
+//     the order of the ranges.
+#include "attention_device.h"
+#include "score_rule.h"
+
+namespace propd {
+
+constexpr int kGroupThreads = 256;
+constexpr int kGroupSlots = 2048;  // partial results of a call, at most
+
+struct GroupedParams {
+  const uint16_t *q, *k_cache, *v_cache, *k_tree, *v_tree;
+  uint16_t *out;
+  float *lse;
+  const int32_t *seq_lens, *n_nodes, *position, *dropped;
+  const uint64_t *anc;
+  const float *slopes;
+  int B, H, H_kv, group, T_max, L_max;
+  int blocks;           // blocks of 128 columns of a unit's tree of T_max nodes
+  int window;           // window_of
+  float scale_log2e, cap_in, cap_log2e;  // cap_in: 2 scale log2(e) / cap
+  float *part_o;        // [slots][4 waves][16 blocks][64 lanes][4]
+  float *part_ml;       // [slots][4 waves][m | l][64 lanes]
+  int32_t *records;     // [B * H_kv * blocks][4]: first slot, slots between pieces, pieces (1: no merge), nodes
+  int slots, resident;  // partial results there is room for; workgroups that run at once
+  int may_split;
+};
+
+__device__ __forceinline__ Lengths lengths_of(const GroupedParams &p, int b) {
+  return lengths_of(p.seq_lens, p.n_nodes, p.dropped, p.L_max, p.T_max, b);
+}
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Stages of a unit of a sequence: cached rows from `first_stage` on (a window hides those before it where rows
+// lie in the order of their positions), then tree rows.
+struct Stages {
+  int first, cached, tree;
+};
+__device__ __forceinline__ Stages stages_of(int L, int T, int window, bool in_order) {
+  Stages s;
+  const int row = in_order && L > window ? L - window + 1 : 0;  // the first row that the root sees
+  s.first = row / kStageRows;
+  s.cached = (L + kStageRows - 1) / kStageRows - s.first;
+  s.cached = s.cached < 0 ? 0 : s.cached;
+  s.tree = (T + kStageRows - 1) / kStageRows;
+  return s;
+}
+
+// n / d rounded up for any n >= 1, d >= 1: at least 1, off by one at most far beyond 2^20 (the same value wherever it is asked for)
+__device__ __forceinline__ int pieces_of(int n, int d) {
+  const int x = (int)(((float)n + (float)d - .5f) * __builtin_amdgcn_rcpf((float)d));
+  return x < 1 ? 1 : (x > n ? n : x);
+}
+
+// How the units are cut.  Every workgroup works the same plan out from the lengths: a range is at most `most` stages, a
+// unit of s stages has pieces_of(s, most) of them, equally long.  Candidates for `most` are what makes the ranges of all units
+// fill 1, 2, 3 or 4 rounds of the workgroups that run at once, and longer ones; the cost of one is its rounds times
+// (its longest range + kRangeCost), and kMergeCost where any unit is cut.
+constexpr int kCandidates = 16, kLeastStages = 2;
+constexpr float kRangeCost = 4.f, kMergeCost = 4.f;
+
+struct Plan {
+  int most;      // stages of a range
+  int n_ranges;  // of the call
+};
+
+template <class StagesOf>
+__device__ __forceinline__ Plan plan_ranges(const GroupedParams &p, StagesOf &&lane_units) {
+  const int lane = threadIdx.x & 63;
+  auto sum = [](int x, int y) { return x + y; };
+  auto larger = [](int x, int y) { return x > y ? x : y; };
+  float total = 0.f;
+  int units = 0, longest = 1;
+  for (int b0 = 0; b0 < p.B; b0 += kWave) {
+    int s, u;
+    lane_units(b0 + lane, s, u);
+    // products of two numbers below 2^24 in float: only the cost depends on them
+    float t = (float)s * (float)u;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, kWave);
+    total += t;
+    units += __builtin_amdgcn_readlane(wave_scan_i32(u, 0, sum), 63);
+    longest = larger(longest, __builtin_amdgcn_readlane(wave_scan_i32(s, 0, larger), 63));
+  }
+  Plan plan = {longest, units};
+  if (!p.may_split) return plan;
+  const float G = (float)p.resident;
+  // candidate of this lane: rounds 1 (eight lengths), 2 (four), 3 and 4 (two each)
+  const int c = lane & (kCandidates - 1), round = c < 8 ? 1 : c < 12 ? 2 : c < 14 ? 3 : 4;
+  const int step = c < 8 ? c : c < 12 ? c - 8 : c & 1;
+  float most_f = ceilf(total / (G * (float)round) * (1.f + .125f * (float)step));
+  most_f = fminf(fmaxf(most_f, (float)kLeastStages), (float)longest);
+  const int most_l = (int)most_f;
+  float ranges_l = 0.f;  // of the call with this lane's candidate
+  for (int b0 = 0; b0 < p.B; b0 += kWave) {
+    int s, u;
+    lane_units(b0 + lane, s, u);
+    const int here = p.B - b0 < kWave ? p.B - b0 : kWave;
+    for (int i = 0; i < here; ++i)
+      ranges_l += (float)__builtin_amdgcn_readlane(u, i) * (float)pieces_of(__builtin_amdgcn_readlane(s, i), most_l);
+  }
+  const bool cut = ranges_l > (float)units;
+  const float longest_range = ceilf((float)longest / (float)pieces_of(longest, most_l));
+  float cost = ceilf(ranges_l / G) * (longest_range + kRangeCost) + kMergeCost;
+  if (!cut || ranges_l > (float)p.slots) cost = INFINITY;  // not cut: `whole`
+  const float whole = ceilf((float)units / G) * ((float)longest + kRangeCost);
+  float least = cost;
+#pragma unroll
+  for (int o = kCandidates / 2; o > 0; o >>= 1) least = fminf(least, __shfl_xor(least, o, kWave));
+  least = __uint_as_float(uniform(__float_as_uint(least)));
+  if (!(least < whole)) return plan;
+  const int pick = __builtin_ctzll(__ballot(cost == least));
+  plan.most = __builtin_amdgcn_readlane(most_l, pick);
+  plan.n_ranges = (int)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ranges_l), pick));
+  return plan;
+}
+
+// A lane's columns of the result, and where they lie.
+__device__ __forceinline__ size_t column_row(const GroupedParams &p, int b, int hk, int column, int T) {
+  const int g = column / T, i = column - g * T;
+  return ((size_t)b * p.H + hk * p.group + g) * p.T_max + i;
+}
+
+// One direct load of a wave: 64 lanes x 4 bytes, contiguous in LDS.
+__device__ __forceinline__ void dma4(const void *src, uint32_t lds_at) {
+  __builtin_amdgcn_global_load_lds((global_void *)src, (lds_void *)(uintptr_t)lds_at, 4, 0, 0);
+}
+
+// kCap: capped scores.  kPlace: positions take part (a window, a bias, or rows at positions of their own).
+template <int D, bool kCap, bool kPlace>
+__global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(GroupedParams p) {
+  using G_ = Geo<D>;
+  constexpr int kRowBytes = G_::kRowBytes, kHalfStage = G_::kHalfStage, kStageBytes = G_::kStageBytes;
+  constexpr int kMb = G_::kMb, kLoads = G_::kLoads, kQf = D / 16;
+  constexpr int NS = D == 128 ? 4 : 6, kAhead = NS - 2;  // two stages are in use by the math, the rest is in flight
+  constexpr bool kRaw = !kCap && !kPlace;                // the softmax scale is applied inside the exponent
+  constexpr int kPerStage = 2 * kLoads + (kPlace ? 1 : 0);  // loads of a wave per stage
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const uint32_t ring = (uint32_t)(uintptr_t)(lds_void *)smem;
+  const uint32_t place_ring = ring + NS * kStageBytes;               // [NS][4 waves][64] positions
+  int32_t *const tree_place = reinterpret_cast<int32_t *>(smem + NS * kStageBytes + (kPlace ? NS * 1024 : 0));  // [128]
+  __shared__ int s_any[2];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int l32 = lane & 31, g = lane >> 5;
+  const bool in_order = p.position == nullptr;
+
+  auto lane_units = [&](int b, int &s, int &u) {
+    s = u = 0;
+    if (b < p.B) {
+      const Lengths n = lengths_of(p, b);
+      const Stages st = stages_of(n.L, n.T, p.window, in_order);
+      s = st.cached + st.tree;
+      u = p.H_kv * ((p.group * n.T + 127) / 128);
+    }
+  };
+  const Plan plan = plan_ranges(p, lane_units);
+
+  // ---- where a lane reads in a stage: K as the A operand (row l32, chunk 2 ks + g), V^T by transposing reads
+  uint32_t k_rd[kQf], v_rd[kMb][2];
+#pragma unroll
+  for (int ks = 0; ks < kQf; ++ks) k_rd[ks] = ring + l32 * kRowBytes + (((2 * ks + g) ^ G_::k_key(l32)) << 4);
+#pragma unroll
+  for (int mb = 0; mb < kMb; ++mb)
+#pragma unroll
+    for (int hi = 0; hi < 2; ++hi) {
+      const int r = 4 * g + 8 * hi + ((lane & 15) >> 2);
+      const int chunk = mb * 4 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      v_rd[mb][hi] = ring + kHalfStage + r * kRowBytes + ((chunk ^ G_::v_key(r)) << 4) + 8 * (lane & 1);
+    }
+  const int ld_row = G_::kLdRows * wave + lane / G_::kChunks;
+  const int k_lane_chunk = ((lane % G_::kChunks) ^ G_::k_key(ld_row)) << 4;
+  const int v_lane_chunk = ((lane % G_::kChunks) ^ G_::v_key(ld_row)) << 4;
+  if (tid < 2) s_any[tid] = 0;
+  int n_any = 0;
+
+  // ---- ranges.  The blocks of a unit read the same rows: they run next to each other on one XCD (workgroups go to the 8
+  //      XCDs in turn), so that the rows come from its L2 but for the first time.
+  const int span = 8 * p.blocks, padded = (plan.n_ranges + span - 1) / span * span;
+  for (int at = blockIdx.x; at < padded; at += gridDim.x) {
+    const int in_span = at % span, range = at - in_span + in_span % 8 * p.blocks + in_span / 8;
+    if (range >= plan.n_ranges) continue;
+    // the sequence of the range, and the ranges before that sequence
+    int b = 0, first_range = 0;
+    for (int b0 = 0, before = 0; b0 < p.B; b0 += kWave) {
+      int s, u;
+      lane_units(b0 + lane, s, u);
+      const int mine = u * (s > 0 ? pieces_of(s, plan.most) : 0);
+      const int incl = wave_scan_i32(mine, 0, [](int x, int y) { return x + y; });
+      const uint64_t le = __ballot(b0 + lane < p.B && before + incl - mine <= range);
+      if (le == 0) break;
+      const int src = __popcll(le) - 1;
+      b = b0 + src;
+      first_range = __builtin_amdgcn_readlane(before + incl - mine, src);
+      before += __builtin_amdgcn_readlane(incl, 63);
+    }
+    b = uniform(b);
+    Lengths n = lengths_of(p, b);
+    n.L = uniform(n.L), n.T = uniform(n.T), n.P = uniform(n.P), n.dropped = uniform(n.dropped);
+    const Stages st = stages_of(n.L, n.T, p.window, in_order);
+    const int L = n.L, T = n.T, columns = p.group * T, n_blocks = (columns + 127) / 128, n_all = st.cached + st.tree;
+    const int P = pieces_of(n_all, plan.most);
+    int rest = range - first_range;
+    const int block = rest % n_blocks;
+    rest /= n_blocks;
+    const int piece = rest % P, hk = rest / P;
+    const int quot = n_all / P, extra = n_all - quot * P;
+    const int s0 = piece * quot + (piece < extra ? piece : extra), n_st = quot + (piece < extra ? 1 : 0);
+    const size_t unit = (size_t)b * p.H_kv + hk;
+
+    // ---- this lane's column
+    const int column = block * 128 + wave * 32 + l32;
+    const bool active = block * 128 + wave * 32 < columns, there = column < columns;
+    const int col = there ? column : 0;  // lanes past the last column take the first: valid memory, never stored
+    const int head = col / T, node = col - head * T;
+    const size_t row_out = ((size_t)b * p.H + hk * p.group + head) * p.T_max + node;
+    u32x4 qf[kQf];
+    {
+      const uint16_t *src = p.q + row_out * D + g * 8;
+#pragma unroll
+      for (int ks = 0; ks < kQf; ++ks) qf[ks] = *reinterpret_cast<const u32x4 *>(src + ks * 16);
+    }
+    const u32x4 ancv = *reinterpret_cast<const u32x4 *>(p.anc + ((size_t)b * p.T_max + node) * 2);
+    const uint64_t anc_lo = ((uint64_t)ancv.y << 32) | ancv.x, anc_hi = ((uint64_t)ancv.w << 32) | ancv.z;
+    Sight sight = {0, 0, 0};
+    float slope = 0.f;
+    if constexpr (kPlace) {
+      sight = sight_of(n.P + __popcll(anc_lo) + __popcll(anc_hi) - 1, p.window);
+      slope = p.slopes ? p.slopes[hk * p.group + head] * kLog2e : 0.f;
+    }
+    __builtin_amdgcn_s_barrier();  // the range before is done with the ring and the table
+    if constexpr (kPlace) {
+      if (tid < T) {
+        const uint64_t *a = p.anc + ((size_t)b * p.T_max + tid) * 2;
+        tree_place[tid] = n.P + __popcll(a[0]) + __popcll(a[1]) - 1;
+      } else if (tid < 128) {
+        tree_place[tid] = 0;
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // seen by all behind the first stage's barrier
+    }
+
+    // ---- loader: see attention_device.h for the layout.  Rows past the last valid one re-read that row: finite
+    //      data that the mask discards (K) or that meets a zero weight (V).
+    auto issue = [&](int x, int slot) {
+      const int s = s0 + x;
+      const bool tree = s >= st.cached;
+      const int row0 = (tree ? s - st.cached : s + st.first) * kStageRows, left = (tree ? T : L) - row0;
+      const size_t base = unit * (size_t)(tree ? p.T_max : p.L_max) + row0;
+      const unsigned char *k = reinterpret_cast<const unsigned char *>(tree ? p.k_tree : p.k_cache) + base * kRowBytes;
+      const unsigned char *v = reinterpret_cast<const unsigned char *>(tree ? p.v_tree : p.v_cache) + base * kRowBytes;
+      unsigned char *dst = smem + slot * kStageBytes + wave * 1024;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        int row = 4 * G_::kLdRows * i + ld_row;
+        row = row < left ? row : left - 1;
+        __builtin_amdgcn_global_load_lds((global_void *)(k + row * kRowBytes + k_lane_chunk), (lds_void *)(dst + i * 4096), 16, 0, 2 /* nt */);
+        __builtin_amdgcn_global_load_lds((global_void *)(v + row * kRowBytes + v_lane_chunk), (lds_void *)(dst + kHalfStage + i * 4096), 16, 0, 2);
+      }
+      if constexpr (kPlace) {  // tree stages and rows in order need none; the count of loads stays the same
+        const int row = l32 < left ? l32 : left - 1;
+        const int32_t *src = in_order || tree ? p.seq_lens + b : p.position + base + row;
+        dma4(src, place_ring + slot * 1024 + wave * 256);
+      }
+    };
+    auto start = [&]() {
+#pragma unroll
+      for (int x = 0; x < kAhead; ++x)
+        if (x < n_st) issue(x, x);
+    };
+    auto slot_of = [](int x) { return (int)((unsigned)x % (unsigned)NS); };
+    // Stage x is there for all waves, and its place kAhead stages on is free: everyone is done with stage x - 2.  A wave's
+    // loads complete in order, so that at most the younger stages' loads outstanding means that stage x has landed.
+    auto acquire = [&](int x) {
+      int younger = n_st - 1 - x;
+      younger = younger < kAhead - 1 ? younger : kAhead - 1;
+      if constexpr (kAhead > 3) {
+        if (younger == 3) wait_vmem<3 * kPerStage>();
+      }
+      if constexpr (kAhead > 2) {
+        if (younger == 2) wait_vmem<2 * kPerStage>();
+      }
+      if (younger == 1) wait_vmem<kPerStage>();
+      if (younger <= 0) wait_vmem<0>();
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (x + kAhead < n_st) issue(x + kAhead, slot_of(x + kAhead));
+    };
+
+    float m_run, l_run;
+    f32x16 o_acc[kMb];
+    u32x2 vt[2][2 * kMb];
+    auto scores = [&](int x) -> f32x16 {
+      const uint32_t so = (uint32_t)slot_of(x) * kStageBytes;
+      f32x16 acc;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < kQf; ++ks) {
+        const bf16x8 a = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>((uintptr_t)(k_rd[ks] + so));
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, qf[ks]), acc, 0, 0, 0);
+      }
+      return acc;
+    };
+    auto read_v = [&](int x, auto half) __attribute__((always_inline)) {
+      constexpr int kHalf = decltype(half)::value;
+      const uint32_t so = (uint32_t)slot_of(x) * kStageBytes;
+#pragma unroll
+      for (int mb = 0; mb < kMb; ++mb) {
+        vt[kHalf][2 * mb] = lds_read_tr16<16 * kRowBytes * kHalf>(v_rd[mb][0] + so);
+        vt[kHalf][2 * mb + 1] = lds_read_tr16<16 * kRowBytes * kHalf>(v_rd[mb][1] + so);
+      }
+    };
+    // Values of V that are not finite: out of the V registers of 16 rows, and what they add to O to it.
+    auto take_out = [&](const uint32_t (&pw)[8], auto half) __attribute__((always_inline)) {
+      constexpr int kHalf = decltype(half)::value;
+#pragma unroll
+      for (int mb = 0; mb < kMb; ++mb) {
+        uint32_t v4[4] = {vt[kHalf][2 * mb].x, vt[kHalf][2 * mb].y, vt[kHalf][2 * mb + 1].x, vt[kHalf][2 * mb + 1].y};
+        u32x4 code, seen;  // seen: 1 for a weight
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t w2 = pw[4 * kHalf + x];
+          seen[x] = (w2 & 0xffffu ? 0x3f80u : 0u) | (w2 >> 16 ? 0x3f800000u : 0u);
+          code[x] = take_not_finite(v4[x]);
+        }
+        vt[kHalf][2 * mb] = u32x2{v4[0], v4[1]};
+        vt[kHalf][2 * mb + 1] = u32x2{v4[2], v4[3]};
+        f32x16 codes;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) codes[r] = 0.f;
+        codes = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, code), __builtin_bit_cast(bf16x8, seen), codes, 0, 0, 0);
+        mfma_settle();  // O too: its last products came before
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o_acc[mb][r] += not_finite_sum(codes[r]);
+      }
+    };
+    // a new running maximum is adopted only when it exceeds the reference by 2^8 in the exponent: weights then exceed 1, by a
+    // factor that fp32 sums and bf16 weights hold, and O is hardly ever scaled
+    const float tau = kRaw ? fminf(8.f / p.scale_log2e, 1e38f) : 8.f;
+
+    // The weights of stage i from its products, and what they add to O.
+    auto take_stage = [&](int i, float (&sc)[16], auto with_care) __attribute__((always_inline)) {
+      constexpr bool kCareful = decltype(with_care)::value;
+      const int s = s0 + i;
+      const bool tree = s >= st.cached;
+      const int j0 = (tree ? s - st.cached : s + st.first) * kStageRows;
+      int n_valid = (tree ? T : L) - j0;
+      n_valid = n_valid > kStageRows ? kStageRows : n_valid;
+      // ---- scores in the exponent's (log2) domain.  Register r holds row j0 + 8 * (r / 4) + 4 * g + r % 4.
+      if constexpr (kCap) {
+        // cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float e = fast_exp2(sc[r] * p.cap_in);
+          sc[r] = fmaf(-2.f * p.cap_log2e, __builtin_amdgcn_rcpf(e + 1.f), p.cap_log2e);
+        }
+      } else if constexpr (kPlace) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] *= p.scale_log2e;
+      }
+      if constexpr (kPlace) {
+        if (in_order && !tree) {
+          const int back = sight.p_i - (n.dropped + j0 + 4 * g);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int dist = back - (8 * (r >> 2) + (r & 3));
+            sc[r] = (unsigned)dist <= (unsigned)sight.reach ? fmaf(-slope, (float)dist, sc[r]) : -INFINITY;
+          }
+        } else {
+          const uint32_t from = tree ? (uint32_t)(uintptr_t)(lds_void *)(tree_place + j0)
+                                     : place_ring + (uint32_t)slot_of(i) * 1024 + wave * 256;
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            typedef __attribute__((ext_vector_type(4))) int i32x4;
+            const i32x4 at4 = *reinterpret_cast<const __attribute__((address_space(3))) i32x4 *>((uintptr_t)(from + 32 * q4 + 16 * g));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int r = 4 * q4 + j;
+              sc[r] = in_sight(sight, at4[j]) ? fmaf(-slope, (float)(sight.p_i - at4[j]), sc[r]) : -INFINITY;
+            }
+          }
+        }
+      }
+      if (tree || n_valid < kStageRows) {  // uniform
+        uint32_t vis = n_valid >= 32 ? ~0u : ((1u << n_valid) - 1u);
+        const uint64_t word = j0 >= 64 ? anc_hi : anc_lo;  // tree stages start at 0, 32, 64, 96
+        vis &= tree ? (uint32_t)(word >> (j0 & 32)) : ~0u;
+        vis >>= 4 * g;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] = ((vis >> (8 * (r >> 2) + (r & 3))) & 1u) ? sc[r] : -INFINITY;
+      }
+      float m_blk = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) m_blk = fmaxf(m_blk, sc[r]);
+      {  // the other half of the stage's rows is in the lane 32 away
+        uint32_t lo = __float_as_uint(m_blk), hi = lo;
+        swap_halves(lo, hi);
+        m_blk = fmaxf(__uint_as_float(lo), __uint_as_float(hi));
+      }
+      if (__builtin_amdgcn_ballot_w64(m_blk > m_run + tau) != 0) {
+        const float m_new = fmaxf(m_run, m_blk), m_safe = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = fast_exp2((m_run - m_safe) * (kRaw ? p.scale_log2e : 1.f));
+        l_run *= alpha;
+        mfma_settle();
+#pragma unroll
+        for (int mb = 0; mb < kMb; ++mb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o_acc[mb][r] *= alpha;
+        m_run = m_new;
+      }
+      const float neg_m = -(m_run == -INFINITY ? 0.f : m_run) * (kRaw ? p.scale_log2e : 1.f);
+      read_v(i, std::integral_constant<int, 0>{});
+      uint32_t pw[8];
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        const float p0 = fast_exp2(kRaw ? fmaf(sc[r], p.scale_log2e, neg_m) : sc[r] + neg_m);
+        const float p1 = fast_exp2(kRaw ? fmaf(sc[r + 1], p.scale_log2e, neg_m) : sc[r + 1] + neg_m);
+        pw[r >> 1] = cvt_pk_bf16(p0, p1);
+        l_run += p0 + p1;  // of the weights as they are: lse is an fp32 result
+      }
+      read_v(i, std::integral_constant<int, 1>{});
+      static_for_i<2>([&](auto half) __attribute__((always_inline)) {
+        constexpr int kHalf = decltype(half)::value;
+        wait_lds<kHalf == 0 ? 2 * kMb : 0>(vt[kHalf]);
+        if constexpr (kCareful) take_out(pw, half);
+        const u32x4 pv = {pw[4 * kHalf], pw[4 * kHalf + 1], pw[4 * kHalf + 2], pw[4 * kHalf + 3]};
+#pragma unroll
+        for (int mb = 0; mb < kMb; ++mb) {
+          const u32x4 aw = {vt[kHalf][2 * mb].x, vt[kHalf][2 * mb].y, vt[kHalf][2 * mb + 1].x, vt[kHalf][2 * mb + 1].y};
+          o_acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, aw), __builtin_bit_cast(bf16x8, pv), o_acc[mb], 0, 0, 0);
+        }
+      });
+    };
+    auto clear = [&]() {
+      m_run = -INFINITY;
+      l_run = 0.f;
+#pragma unroll
+      for (int mb = 0; mb < kMb; ++mb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o_acc[mb][r] = 0.f;
+    };
+
+    start();
+    clear();
+    acquire(0);
+    if (active) {
+      f32x16 raw = scores(0);
+      for (int i = 0; i < n_st; ++i) {
+        mfma_settle();  // raw was written by products of the iteration before
+        float sc[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] = raw[r];
+        if (i + 1 < n_st) {
+          acquire(i + 1);
+          raw = scores(i + 1);
+        }
+        take_stage(i, sc, std::false_type{});
+      }
+      mfma_settle();
+    } else {
+      for (int i = 1; i < n_st; ++i) acquire(i);  // columns beyond the last: loads and barriers only
+    }
+    // Zero weights times values of V that are not finite: such a range is done once more, with care.
+    ++n_any;
+    int *word = s_any + (n_any & 1);
+    if (active && __builtin_amdgcn_ballot_w64(has_nan(o_acc)) != 0) *word = n_any;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (uniform(*word) == n_any) {
+      start();
+      clear();
+      for (int i = 0; i < n_st; ++i) {
+        acquire(i);
+        if (!active) continue;
+        const f32x16 raw = scores(i);
+        mfma_settle();
+        float sc[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] = raw[r];
+        take_stage(i, sc, std::true_type{});
+        mfma_settle();
+      }
+    }
+
+    // ---- results
+    l_run += __shfl_xor(l_run, 32, kWave);
+    if constexpr (kRaw) m_run *= p.scale_log2e;
+    if (tid == 0 && piece == 0)
+      *reinterpret_cast<u32x4 *>(p.records + 4 * (unit * p.blocks + block)) =
+          u32x4{(uint32_t)range, (uint32_t)n_blocks, (uint32_t)P, (uint32_t)T};
+    if (there && P == 1) {
+      const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : l_run;  // NaN stays
+#pragma unroll
+      for (int mb = 0; mb < kMb; ++mb) store_out_block<false>(p.out + row_out * D, o_acc[mb], inv, g, mb);
+      if (p.lse && g == 0) p.lse[row_out] = (m_run + __builtin_amdgcn_logf(l_run)) * kLn2;
+    } else if (there) {
+#pragma unroll
+      for (int mb = 0; mb < kMb; ++mb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          *reinterpret_cast<f32x4 *>(p.part_o + part_o_index(range, wave, 4 * mb + q4, lane)) =
+              f32x4{o_acc[mb][4 * q4], o_acc[mb][4 * q4 + 1], o_acc[mb][4 * q4 + 2], o_acc[mb][4 * q4 + 3]};
+      p.part_ml[part_ml_index(range, wave, 0, lane)] = m_run;
+      p.part_ml[part_ml_index(range, wave, 1, lane)] = l_run;
+    }
+  }
+}
+
+// A result to be merged with factor f: left out where the factor is zero (an infinity would be NaN).
+__device__ __forceinline__ float counted(float o, float f) { return f == 0.f ? 0.f : o; }
+
+// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the pieces s of a unit, in their order.  One wave per 32 columns
+// and 32-wide block of d, eight pieces requested together.
+template <int D>
+__global__ __launch_bounds__(kWave) void grouped_attn_merge_kernel(GroupedParams p) {
+  constexpr int kMb = Geo<D>::kMb, N = 8;
+  const int mb = blockIdx.x % kMb, wave = blockIdx.x / kMb % 4;
+  const unsigned item = blockIdx.x / (4 * kMb);
+  const int block = (int)(item % (unsigned)p.blocks);
+  const size_t unit = item / (unsigned)p.blocks;
+  const int b = (int)(unit / p.H_kv), hk = (int)(unit - (size_t)b * p.H_kv);
+  int T = p.n_nodes[b];
+  T = T < 1 ? 1 : (T > p.T_max ? p.T_max : T);
+  const int columns = p.group * T;
+  if (block * 128 + wave * 32 >= columns) return;
+  const u32x4 record = *reinterpret_cast<const u32x4 *>(p.records + 4 * (unit * p.blocks + block));
+  const int first = (int)record.x, stride = (int)record.y, P = (int)record.z;
+  if (P <= 1) return;
+  const int lane = threadIdx.x, g = lane >> 5, column = block * 128 + wave * 32 + (lane & 31);
+  const bool there = column < columns;
+  const int ln = there ? lane : 0;  // lanes past the last column read lane 0's data and store nothing
+  f32x16 acc;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+  float M = -INFINITY, total = 0.f;
+  for (int s0 = 0; s0 < P; s0 += N) {
+    f32x4 o[N][4];
+    float m[N], l[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const size_t slot = first + (size_t)(s0 + k < P ? s0 + k : P - 1) * stride;
+      m[k] = p.part_ml[part_ml_index(slot, wave, 0, ln)];
+      l[k] = p.part_ml[part_ml_index(slot, wave, 1, ln)];
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) o[k][q4] = *reinterpret_cast<const f32x4 *>(p.part_o + part_o_index(slot, wave, 4 * mb + q4, ln));
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (s0 + k >= P) break;  // uniform
+      const float M_new = fmaxf(M, m[k]), M_safe = M_new == -INFINITY ? 0.f : M_new;
+      const float a_old = fast_exp2(M - M_safe), a_new = fast_exp2(m[k] - M_safe);
+      total = total * a_old + l[k] * a_new;
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[4 * q4 + j] = counted(acc[4 * q4 + j], a_old) * a_old + counted(o[k][q4][j], a_new) * a_new;
+      M = M_new;
+    }
+  }
+  if (!there) return;
+  const size_t row = column_row(p, b, hk, column, T);
+  const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
+  store_out_block<false>(p.out + row * D, acc, inv, g, mb);
+  if (p.lse && mb == 0 && g == 0) p.lse[row] = (M + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
+// ------------------------------------------------------------------------------------
+// host side
+// ------------------------------------------------------------------------------------
+static int grouped_compute_units() {
+  static const int cus = [] {
+    int dev = 0;
+    hipDeviceProp_t prop;
+    if (hipGetDevice(&dev) == hipSuccess && hipGetDeviceProperties(&prop, dev) == hipSuccess && prop.multiProcessorCount > 0)
+      return prop.multiProcessorCount;
+    return 256;
+  }();
+  return cus;
+}
+
+// Slots for partial results: no more than ranges of kLeastStages stages, a bound that needs no device.
+static long long grouped_slots(int B, int H, int T_max, int L_max) {
+  const long long stages = (L_max + kStageRows - 1ll) / kStageRows + (T_max + kStageRows - 1) / kStageRows;
+  const long long most = (long long)B * H * stages;
+  return most < kGroupSlots ? most : kGroupSlots;
+}
+
+size_t grouped_attention_workspace_bytes(int B, int H, int L_max, int T_max) {
+  const size_t slots = (size_t)grouped_slots(B, H, T_max, L_max);
+  return align_up(slots * kPartOFloats * 4, 256) + align_up(slots * kPartMlFloats * 4, 256) + align_up((size_t)B * H * 16, 256);
+}
+
+template <int D, bool kCap, bool kPlace>
+static bool launch_grouped(const GroupedParams &p, unsigned grid, hipStream_t st) {
+  constexpr int NS = D == 128 ? 4 : 6;
+  constexpr int lds_bytes = NS * Geo<D>::kStageBytes + (kPlace ? NS * 1024 + 512 : 0);
+  static std::atomic<uint64_t> set{0};
+  if (!allow_lds(reinterpret_cast<const void *>(&grouped_attn_bf16_kernel<D, kCap, kPlace>), lds_bytes, set)) return false;
+  hipLaunchKernelGGL((grouped_attn_bf16_kernel<D, kCap, kPlace>), dim3(grid), dim3(kGroupThreads), lds_bytes, st, p);
+  if (!launch_ok()) return false;
+  if (!p.may_split) return true;
+  hipLaunchKernelGGL(grouped_attn_merge_kernel<D>, dim3((unsigned)p.B * (unsigned)p.H_kv * (unsigned)p.blocks * 4u * Geo<D>::kMb),
+                     dim3(kWave), 0, st, p);
+  return launch_ok();
+}
+
+template <int D>
+static bool launch_grouped(const GroupedParams &p, bool cap, bool place, unsigned grid, hipStream_t st) {
+  return cap ? (place ? launch_grouped<D, true, true>(p, grid, st) : launch_grouped<D, true, false>(p, grid, st))
+             : (place ? launch_grouped<D, false, true>(p, grid, st) : launch_grouped<D, false, false>(p, grid, st));
+}
+
+#include "grouped_attention_f32.h"
+
+}  // namespace propd
+
+extern "C" propd_status propd_grouped_attention(const propd_tree *tree, propd_dtype dt, int32_t H, int32_t H_kv, int32_t d,
+                                                const propd_score_rule *rule, const void *q, const void *k_cache,
+                                                const void *v_cache, const void *k_tree, const void *v_tree,
+                                                const int32_t *seq_lens, const int32_t *position, const int32_t *dropped,
+                                                int32_t L_max, void *out, float *lse, void *workspace,
+                                                size_t workspace_bytes, void *hip_stream) {
+  using namespace propd;
+  if (!tree || tree->B < 1 || tree->T_max < 1 || tree->T_max > PROPD_MAX_TREE || H < 1 || H_kv < 1 || H % H_kv != 0 || L_max < 0 ||
+      !score_rule_ok(rule) || !tree->n_nodes || !tree->anc || !q || !k_tree || !v_tree || !seq_lens || !out ||
+      (L_max > 0 && (!k_cache || !v_cache)))
+    return PROPD_ERR_INVALID_ARG;
+  if (dt != PROPD_BF16 && dt != PROPD_F32) return PROPD_ERR_INVALID_ARG;
+  if (d != 64 && d != 128) return PROPD_ERR_UNSUPPORTED;
+  for (const void *ptr : {q, k_cache, v_cache, k_tree, v_tree, (const void *)out, (const void *)tree->anc, (const void *)workspace})
+    if (reinterpret_cast<uintptr_t>(ptr) % 16 != 0) return PROPD_ERR_INVALID_ARG;
+  const long long nodes = (long long)tree->B * H * tree->T_max;
+  if (nodes > (1ll << 30) || (long long)tree->B * H > (1ll << 24)) return PROPD_ERR_UNSUPPORTED;
+  if (!workspace || workspace_bytes < grouped_attention_workspace_bytes(tree->B, H, L_max, tree->T_max)) return PROPD_ERR_WORKSPACE;
+  hipStream_t st = as_stream(hip_stream);
+  GroupedParams p;
+  p.q = reinterpret_cast<const uint16_t *>(q);
+  p.k_cache = reinterpret_cast<const uint16_t *>(k_cache);
+  p.v_cache = reinterpret_cast<const uint16_t *>(v_cache);
+  p.k_tree = reinterpret_cast<const uint16_t *>(k_tree);
+  p.v_tree = reinterpret_cast<const uint16_t *>(v_tree);
+  p.out = reinterpret_cast<uint16_t *>(out);
+  p.lse = lse;
+  p.seq_lens = seq_lens;
+  p.n_nodes = tree->n_nodes;
+  p.position = L_max > 0 ? position : nullptr;
+  p.dropped = dropped;
+  p.anc = tree->anc;
+  p.slopes = rule->slopes;
+  p.B = tree->B;
+  p.H = H;
+  p.H_kv = H_kv;
+  p.group = H / H_kv;
+  p.T_max = tree->T_max;
+  p.L_max = L_max;
+  p.blocks = (p.group * p.T_max + 127) / 128;
+  p.window = window_of(rule);
+  p.scale_log2e = rule->scale * kLog2e;
+  p.cap_in = rule->cap > 0.f ? 2.f * rule->scale * kLog2e / rule->cap : 0.f;
+  p.cap_log2e = rule->cap * kLog2e;
+  const bool cap = rule->cap > 0.f, place = p.position || rule->window > 0 || rule->slopes;
+  if (dt == PROPD_F32) return launch_grouped_f32(p, rule->scale, rule->cap, d, place, workspace, workspace_bytes, st) ? PROPD_OK : PROPD_ERR_DEVICE;
+  const size_t slots = (size_t)grouped_slots(tree->B, H, tree->T_max, L_max);
+  char *ws = reinterpret_cast<char *>(workspace);
+  p.part_o = reinterpret_cast<float *>(ws);
+  ws += align_up(slots * kPartOFloats * 4, 256);
+  p.part_ml = reinterpret_cast<float *>(ws);
+  ws += align_up(slots * kPartMlFloats * 4, 256);
+  p.records = reinterpret_cast<int32_t *>(ws);
+  p.slots = (int)slots;
+  p.resident = 2 * grouped_compute_units();
+  // with so many units that they fill the chip four times over none is cut
+  p.may_split = (long long)p.B * H_kv < 4ll * p.resident ? 1 : 0;
+  const long long units = (long long)p.B * H_kv * p.blocks;
+  const long long stages = (L_max + kStageRows - 1ll) / kStageRows + (p.T_max + kStageRows - 1) / kStageRows;
+  long long grid = p.may_split ? units * stages : units;
+  grid = (grid + 8ll * p.blocks - 1) / (8ll * p.blocks) * (8ll * p.blocks);
+  if (grid > p.resident) grid = p.resident;
+  return (d == 64 ? launch_grouped<64>(p, cap, place, (unsigned)grid, st) : launch_grouped<128>(p, cap, place, (unsigned)grid, st))
+             ? PROPD_OK
+             : PROPD_ERR_DEVICE;
+}

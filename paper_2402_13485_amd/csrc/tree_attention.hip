@@ -1436,6 +1436,7 @@ extern "C" size_t propd_workspace_bytes(propd_ws_kind which, int32_t B, int32_t 
                                         int32_t d, int32_t L_max, int32_t hidden, int32_t vocab) {
   (void)d;
   (void)hidden;
+  if (which == PROPD_WS_CACHE_EVICT) return B < 1 || H < 1 || L_max < 1 ? 0 : propd::cache_evict_workspace_bytes(B, H, L_max);
   if (B < 1 || T_max < 1 || T_max > PROPD_MAX_TREE) return 0;
   switch (which) {
     case PROPD_WS_TREE_ATTENTION:
@@ -1446,6 +1447,11 @@ extern "C" size_t propd_workspace_bytes(propd_ws_kind which, int32_t B, int32_t 
       return propd::early_prune_workspace_bytes(B, T_max, vocab);
     case PROPD_WS_ACCEPT_PATH:
       return propd::accept_path_workspace_bytes(B, T_max);
+    case PROPD_WS_GROUPED_ATTENTION:
+      if (H < 1 || L_max < 0) return 0;
+      return propd::grouped_attention_workspace_bytes(B, H, L_max, T_max);
+    case PROPD_WS_CACHE_EVICT:
+      break;  // above
   }
   return 0;
 }

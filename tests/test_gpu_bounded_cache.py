@@ -1,0 +1,531 @@
+"""The calls of a bounded cache with shared heads on the GPU against the float64 definitions of oracle/bounded_cache.py.
+
+Tolerances.  A score is off by at most `score_error` (products, sums, cap and bias in fp32), a softmax weight by that
+and a few units of 2^-24 relative, bf16 weights by half a step (2^-8) more, a sum of n by n * 2^-24; what an error of
+the weights counts against is sum_j p_j |v_j|.  A bf16 result is rounded by half a step at the end."""
+import numpy as np
+import pytest
+import torch
+
+from cache_util import f64, make_inputs, poison, rule_of, score_error, slopes_of
+from gpu_util import host_f64, sentinel_like, to_dev, to_host
+from oracle import bounded_cache as ref
+from paper_2402_13485_amd import synth
+from test_gpu_parity import pb  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def dev_rule(rule):
+    return dict(scale=rule["scale"], cap=rule["cap"], window=rule["window"], slopes=None if rule["slopes"] is None else to_dev(rule["slopes"]))
+
+
+def dev_tree(pb, x):
+    nn, par = to_dev(x["n_nodes"]), to_dev(x["parent"])
+    depth, anc = pb.propd_tree_mask(nn, par)
+    return pb.Tree(n_nodes=nn, parent=par, depth=depth, anc=anc)
+
+
+def optional(a):
+    return None if a is None else to_dev(a)
+
+
+def run_attention(pb, x, rule, tree=None, want_lse=True):
+    out, lse = to_dev(sentinel_like(x["q"])), to_dev(sentinel_like(np.zeros(x["q"].shape[:3], np.float32)))
+    pb.propd_grouped_attention(tree or dev_tree(pb, x), *(to_dev(x[n]) for n in ("q", "k_cache", "v_cache", "k_tree", "v_tree", "seq_lens")),
+                               dropped=to_dev(x["dropped"]), position=optional(x["position"]), out=out, lse=lse if want_lse else None, **dev_rule(rule))
+    torch.cuda.synchronize()
+    return to_host(out), to_host(lse)
+
+
+def check_attention(x, rule, out, lse, rows=None):
+    want, want_lse, mag = ref.grouped_attention(x["n_nodes"], x["parent"], *(f64(x[n]) for n in ("q", "k_cache", "v_cache", "k_tree", "v_tree")),
+                                                x["seq_lens"], x["dropped"], x["position"], rule)
+    bf16 = x["dtype"] == "bf16"
+    keys = int(x["seq_lens"].max()) + x["q"].shape[2]
+    e = score_error(x, rule, x["q"].shape[3])
+    share = 2 * e + (keys + 16) * U + (2.0 ** -8 if bf16 else 0.0)
+    for b, T in enumerate(x["n_nodes"]):
+        got, r = synth.as_float(out[b, :, :T]).astype(np.float64), want[b, :, :T]
+        fine = np.isfinite(r)
+        assert (np.isfinite(got) == fine).all(), (b, np.argwhere(np.isfinite(got) != fine)[:5])
+        with np.errstate(invalid="ignore"):
+            bound = share * mag[b, :, :T] + (2.0 ** -8 if bf16 else U) * np.abs(r) + 1e-37
+            assert (np.abs(got - r)[fine] <= bound[fine]).all(), float((np.abs(got - r) / bound)[fine].max())
+        bound = e + (keys + 16) * U + 4 * U * np.abs(want_lse[b, :, :T])
+        assert (np.abs(lse[b, :, :T] - want_lse[b, :, :T]) <= bound).all(), float((np.abs(lse[b, :, :T] - want_lse[b, :, :T]) / bound).max())
+        assert (out[b, :, T:] == sentinel_like(x["q"])[b, :, T:]).all() and (lse[b, :, T:] == 12345.5).all()
+
+
+# rule: cap, window, slopes
+RULES = {"plain": (0.0, 0, False), "cap": (3.0, 0, False), "window": (0.0, 37, False), "bias": (0.0, 0, True), "all": (20.0, 50, True)}
+
+
+def make_rule(name, H, d):
+    cap, window, slopes = RULES[name]
+    return rule_of(d, cap, window, slopes_of(H) if slopes else None)
+
+
+# ---- grouped attention
+
+@pytest.mark.parametrize("placed", [False, True])
+@pytest.mark.parametrize("name", list(RULES))
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+def test_attention_rules(pb, dtype, d, name, placed):
+    """Every rule and both kinds of positions: ragged lengths, an empty cache, a tree of one node, NaN in padding and holes."""
+    rng = np.random.default_rng(len(name) + d)
+    H, Hk = 6, 2
+    shapes = [synth.random_tree(rng, 45), synth.chain_tree(1), synth.rank_product_tree(20, 4), synth.random_tree(rng, 13)]
+    x = make_inputs(rng, dtype, H, Hk, d, shapes, [131, 64, 0, 33], T_max=47, L_max=140, placed=placed, holes=0.1)
+    rule = make_rule(name, H, d)
+    check_attention(x, rule, *run_attention(pb, x, rule))
+
+
+@pytest.mark.parametrize("H,Hk,T,L", [(1, 1, 1, 0), (1, 1, 1, 1), (8, 8, 3, 31), (8, 1, 1, 700), (40, 8, 1, 97), (5, 1, 128, 64), (16, 2, 128, 95),
+                                      (64, 2, 16, 40), (3, 3, 128, 32), (8, 4, 64, 1100)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_heads_and_lengths(pb, dtype, H, Hk, T, L):
+    """One to 32 query heads to a K/V head, one column to several blocks of 128, one key to many ranges."""
+    rng = np.random.default_rng(H + T + L)
+    x = make_inputs(rng, dtype, H, Hk, 128, [synth.random_tree(rng, T)], [L], L_max=L + 5)
+    rule = rule_of(128)
+    check_attention(x, rule, *run_attention(pb, x, rule))
+
+
+@pytest.mark.parametrize("B", [65, 130])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_many_sequences(pb, dtype, B):
+    rng = np.random.default_rng(B)
+    shapes = [synth.random_tree(rng, int(rng.integers(1, 9))) for _ in range(B)]
+    x = make_inputs(rng, dtype, 4, 2, 64, shapes, rng.integers(0, 90, B).tolist())
+    rule = make_rule("all", 4, 64)
+    check_attention(x, rule, *run_attention(pb, x, rule))
+
+
+@pytest.mark.parametrize("window", [1, 2, 31, 32, 33, 200])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_window_edges(pb, dtype, window):
+    """Windows that end on, before and behind a tile's edge, shorter than the tree is deep, longer than everything."""
+    rng = np.random.default_rng(window)
+    x = make_inputs(rng, dtype, 4, 2, 128, [synth.chain_tree(40), synth.random_tree(rng, 40)], [130, 17])
+    rule = rule_of(128, window=window)
+    check_attention(x, rule, *run_attention(pb, x, rule))
+
+
+@pytest.mark.parametrize("where", ["hole", "window", "stranger"])
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_hidden_rows_may_hold_anything(pb, dtype, value, where):
+    """K and V rows that a query does not see: rows without a position, behind the window, other branches of the tree.
+    (Those of other branches are seen by their own nodes, whose results are not finite then.)"""
+    rng = np.random.default_rng(11)
+    x = make_inputs(rng, dtype, 4, 2, 128, [synth.star_tree(20), synth.star_tree(40)], [100, 75], placed=where == "hole", holes=0.0)
+    bits = synth.from_float(np.full(1, value, np.float32), dtype)[0]
+    rule = rule_of(128, window=30 if where == "window" else 0)
+    for name in ("k", "v"):
+        if where == "hole":
+            x["position"][:, :, 5:9] = -1
+            x[name + "_cache"][:, :, 5:9] = bits
+        elif where == "window":
+            x[name + "_cache"][:, :, 3:7] = bits
+    if where == "stranger":
+        x["v_tree"][:, :, 9, 3] = bits
+    check_attention(x, rule, *run_attention(pb, x, rule))
+
+
+def test_attention_without_lse_is_the_same(pb):
+    rng = np.random.default_rng(12)
+    x = make_inputs(rng, "bf16", 8, 2, 128, [synth.random_tree(rng, 30)] * 3, [300, 20, 111])
+    out, _ = run_attention(pb, x, rule_of(128))
+    again, lse = run_attention(pb, x, rule_of(128), want_lse=False)
+    assert (out == again).all() and (lse == 12345.5).all()
+
+
+def test_attention_of_one_group_is_the_tree_attention(pb):
+    """Against propd_tree_attention: both round the same sums, in other orders."""
+    rng = np.random.default_rng(13)
+    x = make_inputs(rng, "bf16", 8, 8, 128, [synth.random_tree(rng, 60), synth.random_tree(rng, 22)], [500, 77], T_max=64)
+    out = synth.as_float(run_attention(pb, x, rule_of(128))[0])
+    other = host_f64(pb.propd_tree_attention(dev_tree(pb, x), *(to_dev(x[n]) for n in ("q", "k_cache", "v_cache", "k_tree", "v_tree", "seq_lens")),
+                                             rule_of(128)["scale"]))
+    for b, T in enumerate(x["n_nodes"]):
+        # each within half a step of the weights (of sums of |V| below 4) and of the result
+        assert np.abs(out[b, :, :T] - other[b, :, :T]).max() <= 2 * (4 * 2.0 ** -8 + 2.0 ** -8 * np.abs(other[b, :, :T]).max())
+
+
+def test_attention_moving_maximum(pb):
+    """Scores that rise from row to row: the softmax reference moves again and again, O is scaled."""
+    rng = np.random.default_rng(14)
+    x = make_inputs(rng, "bf16", 4, 2, 128, [synth.random_tree(rng, 33)], [400])
+    ramp = synth.as_float(x["k_cache"]).copy()
+    ramp[..., 0] = np.linspace(-60, 60, 400)
+    x["k_cache"] = synth.from_float(ramp, "bf16")
+    q = synth.as_float(x["q"]).copy()
+    q[..., 0] = 9.0
+    x["q"] = synth.from_float(q, "bf16")
+    for name in ("plain", "all"):
+        rule = make_rule(name, 4, 128)
+        check_attention(x, rule, *run_attention(pb, x, rule))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_replayed_from_a_graph_and_on_another_stream(pb, dtype):
+    """Two captured graphs with workspaces of their own, replayed in turn between eager calls, the second one's inputs rewritten
+    in place; every result is the eager one's, bit for bit."""
+    rng = np.random.default_rng(15)
+    xs = [make_inputs(rng, dtype, 8, 2, 128, [synth.random_tree(rng, 40)] * 2, lens, L_max=600) for lens in ([600, 45], [130, 599])]
+    rule = dev_rule(make_rule("all", 8, 128))
+    trees = [dev_tree(pb, x) for x in xs]
+    args = [[to_dev(x[n]) for n in ("q", "k_cache", "v_cache", "k_tree", "v_tree", "seq_lens")] for x in xs]
+    call = lambda i, out, lse, ws: pb.propd_grouped_attention(trees[i], *args[i], out=out, lse=lse, workspace=ws, **rule)
+    eager = [call(i, torch.zeros_like(args[i][0]), torch.zeros(2, 8, 40, device="cuda"), None) for i in (0, 1)]
+    nbytes = pb.workspace_bytes(pb.WS_GROUPED_ATTENTION, 2, 40, 8, 128, 600)
+    held = [(torch.zeros_like(args[i][0]), torch.zeros(2, 8, 40, device="cuda"), torch.empty(nbytes, dtype=torch.uint8, device="cuda")) for i in (0, 1)]
+    side, graphs = torch.cuda.Stream(), []
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            call(i, *held[i])
+        graphs.append(graph)
+    for turn in range(4):
+        for i in (0, 1):
+            held[i][0].zero_(), held[i][1].zero_()
+            graphs[i].replay()
+            call(1 - i, torch.zeros_like(args[0][0]), None, None)
+            torch.cuda.synchronize()
+            assert torch.equal(held[i][0], eager[i][0]) and torch.equal(held[i][1], eager[i][1]), (turn, i)
+
+
+def test_attention_cache_beyond_32_bits(pb):
+    """K/V offsets of the last units lie past 2^31 and 2^32 bytes."""
+    H, Hk, L_max, d = 4, 2, 4200000, 128  # 1.07 GB per unit of K
+    B = 3
+    k = torch.zeros((B, Hk, L_max, d), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    lens = [70, 33, 4199990]
+    k[:, :, :64].normal_(generator=gen), v[:, :, :64].normal_(generator=gen)
+    k[2, :, -64:].normal_(generator=gen), v[2, :, -64:].normal_(generator=gen)
+    small = torch.randn((4, B, H, 5, d), generator=gen, device="cuda").bfloat16()
+    q, kt, vt = small[0], small[1][:, :Hk].contiguous(), small[2][:, :Hk].contiguous()
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    parent = torch.tensor([[-1, 0, 1, 2, 3]] * B, dtype=torch.int32, device="cuda")
+    nn = torch.full((B,), 5, dtype=torch.int32, device="cuda")
+    depth, anc = pb.propd_tree_mask(nn, parent)
+    # a window: the last 200 positions only, so that the definition has few rows to look at
+    out, lse = pb.propd_grouped_attention(pb.Tree(nn, parent, anc=anc), q, k, v, kt, vt, seq, 0.09, window=200, want_lse=True)
+    for b in range(B):
+        first = max(0, lens[b] - 300)
+        x = dict(dtype="bf16", n_nodes=np.array([5], np.int32), parent=parent[:1].cpu().numpy(), seq_lens=np.array([lens[b] - first], np.int32),
+                 dropped=np.array([first], np.int32), position=None)
+        for name, t in (("q", q), ("k_cache", k[:, :, first:lens[b]]), ("v_cache", v[:, :, first:lens[b]]), ("k_tree", kt), ("v_tree", vt)):
+            x[name] = to_host(t[b:b + 1].contiguous())
+        check_attention(x, dict(scale=float(np.float32(0.09)), cap=0.0, window=200, slopes=None), to_host(out[b:b + 1]), to_host(lse[b:b + 1]))
+
+
+# ---- accumulated weights
+
+def observe_case(rng, dtype, H, Hk, d, lens, a, T=24, L_max=None, placed=True, stride=8, holes=0.1):
+    shapes = [synth.random_tree(rng, T, max_depth=stride) for _ in lens]
+    x = make_inputs(rng, dtype, H, Hk, d, shapes, lens, L_max=L_max, placed=placed, holes=holes)
+    B, L_max = len(lens), x["k_cache"].shape[2]
+    x["accept_len"] = np.zeros(B, np.int32)
+    x["accept_path"] = np.full((B, stride), -1, np.int32)
+    for b in range(B):
+        node = int(rng.integers(0, T))
+        path = ref.root_path(x["parent"][b], node)[:min(stride, a[b])]
+        x["accept_len"][b], x["accept_path"][b, :len(path)] = len(path), path
+    x["weight"] = np.exp(rng.normal(size=(B, Hk, L_max))).astype(np.float32)
+    x["lse"] = rng.uniform(0.5, 6.0, size=(B, H, T)).astype(np.float32)
+    return x
+
+
+def run_observe(pb, x, rule, decay, in_place=False):
+    rows = pb.CacheRows(to_dev(x["seq_lens"]), to_dev(x["dropped"]), optional(x["position"]), to_dev(x["weight"]))
+    weight = rows.weight if in_place else to_dev(sentinel_like(x["weight"]))
+    position = None if rows.position is None else rows.position if in_place else to_dev(sentinel_like(x["position"]))
+    given = {} if in_place else dict(weight_out=weight, position_out=position)
+    pb.propd_cache_observe(dev_tree(pb, x), to_dev(x["accept_len"]), to_dev(x["accept_path"]), to_dev(x["q"]), to_dev(x["lse"]), to_dev(x["k_cache"]),
+                           to_dev(x["k_tree"]), rows, decay=decay, **given, **dev_rule(rule))
+    torch.cuda.synchronize()
+    return to_host(weight), None if position is None else to_host(position)
+
+
+def check_observe(x, rule, decay, weight, position, start=None, start_position=None):
+    start = sentinel_like(x["weight"]) if start is None else start
+    start_position = x["position"] if x["position"] is None else sentinel_like(x["position"]) if start_position is None else start_position
+    want, want_position, paid = ref.cache_observe(x["n_nodes"], x["accept_len"], x["accept_path"], f64(x["q"]), x["lse"], f64(x["k_cache"]), f64(x["k_tree"]),
+                                                  x["seq_lens"], x["dropped"], x["position"], x["weight"], rule, float(np.float32(decay)), start, start_position)
+    n = x["q"].shape[1] // x["k_tree"].shape[1] * x["accept_path"].shape[1]
+    with np.errstate(invalid="ignore"):
+        # the exponent s - lse is off by the score's error and a few roundings of it (|s| and lse below 40 here)
+        bound = paid * (2 * score_error(x, rule, x["q"].shape[3]) + (n + 16 + 4 * 40) * U) + 4 * U * np.abs(want)
+    assert (np.abs(weight - want) <= bound).all(), float(np.max(np.abs(weight - want) / (bound + 1e-30)))
+    if x["position"] is not None:
+        assert (position == want_position).all()
+
+
+@pytest.mark.parametrize("placed", [False, True])
+@pytest.mark.parametrize("name", list(RULES))
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+def test_observe_rules(pb, dtype, d, name, placed):
+    """Ragged lengths, an empty cache, no accepted node, a cache with too little room; entries that are not written stay."""
+    rng = np.random.default_rng(d + len(name))
+    x = observe_case(rng, dtype, 6, 2, d, [131, 0, 33, 139, 64], [8, 3, 1, 8, 0], L_max=140, placed=placed)
+    rule = make_rule(name, 6, d)
+    check_observe(x, rule, 0.75, *run_observe(pb, x, rule, 0.75))
+
+
+@pytest.mark.parametrize("H,Hk,L", [(1, 1, 1), (40, 8, 17), (8, 1, 700), (64, 2, 129), (16, 16, 2100)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_observe_heads_and_lengths_in_place(pb, dtype, H, Hk, L):
+    rng = np.random.default_rng(H + L)
+    x = observe_case(rng, dtype, H, Hk, 128, [L, L // 2], [4, 7], L_max=L + 9, stride=20)
+    rule = make_rule("plain", H, 128)
+    weight, position = run_observe(pb, x, rule, 1.0, in_place=True)
+    check_observe(x, rule, 1.0, weight, position, x["weight"], x["position"])
+
+
+def test_observe_many_tiles(pb):
+    """Enough rows for several tiles per wave."""
+    rng = np.random.default_rng(21)
+    for dtype in ("bf16", "f32"):
+        x = observe_case(rng, dtype, 8, 8, 64, [2500, 2399, 7, 2300, 2500, 2450, 2448, 2447], [3] * 8, L_max=2500)
+        rule = make_rule("bias", 8, 64)
+        check_observe(x, rule, 0.9, *run_observe(pb, x, rule, 0.9))
+
+
+def test_observe_bad_path_entries_pay_nothing(pb):
+    rng = np.random.default_rng(22)
+    x = observe_case(rng, "bf16", 4, 2, 128, [50, 20, 10], [1, 1, 1], L_max=70)
+    x["accept_path"][:, :5] = [[0, -5, 3, 24, 7], [99, 1, 2, 3, 4], [0, 1, 2, 1 << 30, -1]]
+    x["accept_len"][:] = [5, 4, 1000]
+    rule = make_rule("all", 4, 128)
+    weight, position = run_observe(pb, x, rule, 1.0)
+    check_observe(x, rule, 1.0, weight, position)
+    assert (position[0, :, 51] == -1).all() and (weight[0, :, 53] == 0).all()
+
+
+# ---- eviction
+
+def evict_case(rng, dtype, Hk, d, lens, L_max, ties):
+    B = len(lens)
+    x = dict(dtype=dtype, seq_lens=np.array(lens, np.int32), dropped=rng.integers(0, 3 * L_max, B).astype(np.int32))
+    x["k"], x["v"] = (synth.from_float(rng.normal(size=(B, Hk, L_max, d)).astype(np.float32), dtype) for _ in range(2))
+    x["position"] = np.stack([[rng.permutation(max(L_max, int(n + m)))[:L_max] for _ in range(Hk)] for n, m in zip(lens, x["dropped"])]).astype(np.int32)
+    w = rng.normal(size=(B, Hk, L_max)).astype(np.float32)
+    x["weight"] = np.round(2 * w) / 2 if ties else np.exp(w)  # negative ones and -0 among them
+    return x
+
+
+def run_evict(pb, x, budget, recent, sinks, in_place):
+    rows = pb.CacheRows(*(to_dev(x[n]) for n in ("seq_lens", "dropped", "position", "weight")))
+    out = rows if in_place else pb.CacheRows(*(to_dev(sentinel_like(x[n])) for n in ("seq_lens", "dropped", "position", "weight")))
+    k, v = to_dev(x["k"]), to_dev(x["v"])
+    pb.propd_cache_evict(k, v, rows, budget, recent, sinks, rows_out=None if in_place else out)
+    torch.cuda.synchronize()
+    want = {n: (x[n] if in_place else sentinel_like(x[n])).copy() for n in ("seq_lens", "dropped", "position", "weight")}
+    k_ref, v_ref = x["k"].copy(), x["v"].copy()
+    ref.cache_evict(k_ref, v_ref, x["seq_lens"], x["dropped"], x["position"], x["weight"], budget, recent, sinks, want)
+    same = lambda a, b: (a.view(np.uint8) == b.view(np.uint8)).all()
+    for n, a in want.items():
+        assert same(to_host(getattr(out, n)), a), n
+    assert same(to_host(k), k_ref) and same(to_host(v), v_ref)
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("ties", [False, True])
+@pytest.mark.parametrize("budget,recent,sinks", [(1, 0, 0), (64, 7, 2), (65, 65, 65), (100, 1000000, 0), (199, 0, 4), (200, 3, 0)])
+def test_evict_small(pb, budget, recent, sinks, ties, in_place):
+    """Lengths below, at and above the budget, an empty cache; everything protected; all four per-row arrays, K and V bit for bit."""
+    rng = np.random.default_rng(budget)
+    x = evict_case(rng, "bf16", 3, 128, [200, budget, 0, min(200, budget + 1), 150], 200, ties)
+    run_evict(pb, x, budget, recent, sinks, in_place)
+
+
+@pytest.mark.parametrize("dtype,d,L,budget", [("f32", 4, 1025, 1024), ("bf16", 64, 4096, 1000), ("f32", 64, 4097, 2048), ("bf16", 8, 16384, 5000),
+                                              ("bf16", 8, 16385, 16000), ("f32", 12, 40000, 30000), ("bf16", 1024, 130, 70)])
+@pytest.mark.parametrize("ties", [False, True])
+def test_evict_long(pb, dtype, d, L, budget, ties):
+    """All forms of the search: keys in registers, few and many, and read again; rows of 16 bytes to 2 KB."""
+    rng = np.random.default_rng(L)
+    x = evict_case(rng, dtype, 2, d, [L, L - 3], L, ties)
+    run_evict(pb, x, budget, 17, 4, True)
+
+
+def test_evict_odd_weights_and_holes(pb):
+    """NaN, infinities, zeros of both signs, subnormals, equal weights; rows without a position go first."""
+    rng = np.random.default_rng(31)
+    x = evict_case(rng, "bf16", 2, 64, [300, 280], 300, False)
+    x["weight"][:, :, :60] = np.tile(np.array([np.nan, np.inf, -np.inf, 0.0, -0.0, 1e-45], np.float32), 10)
+    x["weight"][:, :, 60:200] = 1.5
+    x["position"][:, :, 100:150:3] = -np.arange(1, 18)
+    x["position"][0, 0, 7] = -2 ** 31
+    for budget in (30, 61, 120, 270):
+        run_evict(pb, x, budget, 20, 3, True)
+
+
+def test_evict_all_alike(pb):
+    x = evict_case(np.random.default_rng(32), "bf16", 2, 64, [3000, 2900], 3000, False)
+    x["weight"][:] = 0
+    run_evict(pb, x, 1234, 0, 0, True)
+
+
+# ---- rotary positions
+
+def check_rotary(pb, rng, dtype, B, S, H, Hk, d, pairs, axes, shared, adjacent, ragged, in_place, far=100000):
+    q, k = (synth.from_float(rng.normal(size=(B, h, S, d)).astype(np.float32), dtype) for h in (H, Hk))
+    inv = (1e4 ** (-np.arange(pairs) / pairs)).astype(np.float32)
+    offset = rng.integers(-5, 5000, (B, S) if shared else (B, axes, S)).astype(np.int32)
+    start = rng.integers(0, far, (B, axes)).astype(np.int32)
+    axis_of = rng.integers(0, axes, pairs).astype(np.int32) if axes > 1 else None
+    n_rows = rng.integers(0, S + 1, B).astype(np.int32) if ragged else None
+    dq, dk = to_dev(q), to_dev(k)
+    oq, ok = (dq, dk) if in_place else (to_dev(sentinel_like(q)), to_dev(sentinel_like(k)))
+    pb.propd_rotary(dq, dk, to_dev(inv), to_dev(offset), start=to_dev(start), axis_of=optional(axis_of), n_rows=optional(n_rows), adjacent=adjacent,
+                    q_out=oq, k_out=ok)
+    torch.cuda.synchronize()
+    for x, out in ((q, oq), (k, ok)):
+        base = x if in_place else sentinel_like(x)
+        want = ref.rotary(f64(x), inv, offset, start, axis_of, n_rows, adjacent, f64(base))
+        got = host_f64(out)
+        # cos and sin are 1.2e-7 off at most (angles reduced in 64 bits), products and sum round twice
+        size = np.abs(f64(x)).max()
+        bound = 2 * size * (1.2e-7 + 2 * U) + (2.0 ** -8 if dtype == "bf16" else U) * np.abs(want)
+        assert (np.abs(got - want) <= bound).all(), float((np.abs(got - want) / bound).max())
+        for b in range(B):
+            n = int(n_rows[b]) if ragged else S
+            assert (to_host(out)[b, :, n:] == base[b, :, n:]).all()
+            assert (to_host(out)[b, :, :n, 2 * pairs:] == x[b, :, :n, 2 * pairs:]).all()
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,S,H,Hk,d,pairs,axes,shared", [(1, 1, 1, 1, 16, 8, 1, True), (3, 17, 5, 1, 128, 64, 3, False), (2, 33, 4, 2, 64, 16, 1, True),
+                                                          (2, 130, 8, 8, 72, 32, 4, True), (1, 700, 40, 8, 128, 32, 2, False)])
+def test_rotary(pb, B, S, H, Hk, d, pairs, axes, shared, dtype, adjacent, in_place):
+    check_rotary(pb, np.random.default_rng(S + d), dtype, B, S, H, Hk, d, pairs, axes, shared, adjacent, S > 20, in_place)
+
+
+def test_rotary_far_positions_and_no_keys(pb):
+    rng = np.random.default_rng(41)
+    check_rotary(pb, rng, "f32", 2, 40, 2, 1, 64, 32, 1, True, False, False, False, far=2 ** 31 - 1)
+    q = rng.normal(size=(1, 2, 5, 32)).astype(np.float32)
+    inv, offset = np.ones(16, np.float32), np.arange(5, dtype=np.int32)[None]
+    out, none = pb.propd_rotary(to_dev(q), None, to_dev(inv), to_dev(offset))
+    want = ref.rotary(f64(q), inv, offset, None, None, None, False, np.zeros(q.shape))
+    assert none is None and np.abs(host_f64(out) - want).max() < 2e-6
+
+
+def test_rotary_axes_outside_are_clamped(pb):
+    rng = np.random.default_rng(42)
+    q = rng.normal(size=(1, 2, 7, 32)).astype(np.float32)
+    inv, offset = np.ones(16, np.float32), rng.integers(0, 99, (1, 2, 7)).astype(np.int32)
+    axis_of = np.array([-3, 9] * 8, np.int32)
+    out = host_f64(pb.propd_rotary(to_dev(q), None, to_dev(inv), to_dev(offset), axis_of=to_dev(axis_of))[0])
+    want = ref.rotary(f64(q), inv, offset, None, np.clip(axis_of, 0, 1), None, False, np.zeros(q.shape))
+    assert np.abs(out - want).max() < 2e-6
+
+
+# ---- together
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_steps_of_a_bounded_cache(pb, dtype):
+    """Six steps as a decoding loop makes them: positions into q and k, attention over what is left of the cache, acceptance, the
+    accepted nodes' weights, commit, eviction.  After each call the state is compared with the definitions' own."""
+    rng = np.random.default_rng(51)
+    B, H, Hk, d, T, L_max, budget, vocab, pairs = 2, 6, 2, 64, 12, 48, 30, 19, 32
+    rule = make_rule("all", H, d)
+    inv = (1e4 ** (-np.arange(pairs) / pairs)).astype(np.float32)
+    zeros = lambda *s: synth.from_float(np.zeros(s, np.float32), dtype)
+    x = dict(dtype=dtype, seq_lens=np.array([26, 3], np.int32), dropped=np.zeros(B, np.int32),
+             position=np.tile(np.arange(L_max, dtype=np.int32), (B, Hk, 1)), weight=np.zeros((B, Hk, L_max), np.float32),
+             k_cache=synth.from_float(rng.normal(size=(B, Hk, L_max, d)).astype(np.float32), dtype), v_cache=zeros(B, Hk, L_max, d))
+    rows = pb.CacheRows(*(to_dev(x[n]) for n in ("seq_lens", "dropped", "position", "weight")))
+    k_dev, v_dev = to_dev(x["k_cache"]), to_dev(x["v_cache"])
+    evicted = 0
+    for step in range(6):
+        shapes = [synth.random_tree(rng, T, max_depth=5) for _ in range(B)]
+        n_nodes, parent, depth = synth.pad_trees(shapes, T)
+        x.update(n_nodes=n_nodes, parent=parent)
+        raw = {n: synth.from_float(rng.normal(size=(B, h, T, d)).astype(np.float32), dtype) for n, h in (("q", H), ("k_tree", Hk), ("v_tree", Hk))}
+        token = rng.integers(0, vocab, (B, T)).astype(np.int32)
+        logits = rng.normal(size=(B, T, vocab)).astype(np.float32)
+        for b in range(B):  # the model follows a path to some node
+            path = ref.root_path(parent[b], int(rng.integers(T // 2, T)))
+            for i, j in zip(path, path[1:]):
+                logits[b, i, token[b, j]] = 9.0
+        tree = dev_tree(pb, x)
+        tree.token = to_dev(token)
+        start = (x["seq_lens"] + x["dropped"]).astype(np.int32)
+        q_dev, kt_dev = pb.propd_rotary(to_dev(raw["q"]), to_dev(raw["k_tree"]), to_dev(inv), tree.depth, start=to_dev(start[:, None]))
+        vt_dev = to_dev(raw["v_tree"])
+        for n, t in (("q", q_dev), ("k_tree", kt_dev)):  # compared here, then taken over with its roundings
+            want = ref.rotary(f64(raw[n]), inv, depth, start[:, None], None, None, False, np.zeros(raw[n].shape))
+            assert np.abs(host_f64(t) - want).max() <= 2.0 ** -8 * np.abs(want).max() + 1e-5
+            x[n] = to_host(t)
+        x["v_tree"] = raw["v_tree"]
+        out, lse = pb.propd_grouped_attention(tree, q_dev, k_dev, v_dev, kt_dev, vt_dev, rows.seq_lens, position=rows.position, dropped=rows.dropped,
+                                              want_lse=True, **dev_rule(rule))
+        check_attention(x, rule, to_host(out), to_host(lse))
+        a, path, nxt = pb.propd_accept_path(tree, to_dev(logits), path_stride=6)
+        x.update(accept_len=to_host(a), accept_path=to_host(path), lse=to_host(lse))
+        pb.propd_cache_observe(tree, a, path, q_dev, lse, k_dev, kt_dev, rows, decay=0.9, **dev_rule(rule))
+        weight, position = to_host(rows.weight), to_host(rows.position)
+        check_observe(x, rule, 0.9, weight, position, x["weight"], x["position"])
+        x.update(weight=weight, position=position)
+        pb.propd_commit_path(tree, a, path, nxt, kt_dev, vt_dev, k_dev, v_dev, rows.seq_lens)
+        for b in range(B):
+            for r in range(int(x["accept_len"][b])):
+                for n in ("k", "v"):
+                    x[n + "_cache"][b, :, x["seq_lens"][b] + r] = x[n + "_tree"][b, :, x["accept_path"][b, r]]
+        x["seq_lens"] = x["seq_lens"] + x["accept_len"]
+        assert (to_host(rows.seq_lens) == x["seq_lens"]).all()
+        pb.propd_cache_evict(k_dev, v_dev, rows, budget, recent=4, sinks=2)
+        new = {n: x[n].copy() for n in ("seq_lens", "dropped", "position", "weight")}
+        ref.cache_evict(x["k_cache"], x["v_cache"], x["seq_lens"], x["dropped"], x["position"], x["weight"], budget, 4, 2, new)
+        x.update(new)
+        evicted = int(x["dropped"].sum())
+        for n, t in (("k_cache", k_dev), ("v_cache", v_dev), ("seq_lens", rows.seq_lens), ("dropped", rows.dropped), ("position", rows.position), ("weight", rows.weight)):
+            assert (to_host(t) == x[n]).all(), (step, n)
+        assert (to_host(rows.seq_lens) <= budget).all()
+    assert evicted > 0
+
+
+# ---- refusals that need tensors
+
+def test_overlaps_shapes_and_devices_are_refused(pb):
+    rng = np.random.default_rng(61)
+    x = observe_case(rng, "f32", 4, 2, 64, [20, 9], [3, 3], L_max=30)
+    tree, t = dev_tree(pb, x), {n: to_dev(x[n]) for n in ("q", "k_cache", "v_cache", "k_tree", "v_tree", "seq_lens", "dropped", "position", "weight", "lse",
+                                                          "accept_len", "accept_path")}
+    attention = lambda **kw: pb.propd_grouped_attention(**{**dict(tree=tree, q=t["q"], k_cache=t["k_cache"], v_cache=t["v_cache"], k_tree=t["k_tree"],
+                                                                  v_tree=t["v_tree"], seq_lens=t["seq_lens"], scale=0.1), **kw})
+    for kw in (dict(out=t["q"]), dict(out=t["q"][:1]), dict(lse=t["lse"][:1]), dict(slopes=torch.zeros(3, device="cuda")), dict(v_cache=t["v_cache"][:, :, 1:].contiguous()),
+               dict(position=t["position"][:, :1].contiguous()), dict(dropped=t["dropped"][:1]), dict(seq_lens=t["seq_lens"][:1])):
+        with pytest.raises(ValueError):
+            attention(**kw)
+    for kw in (dict(q=t["q"].half()), dict(v_cache=t["v_cache"].cpu()), dict(k_tree=t["k_tree"].transpose(2, 3)), dict(position=t["position"].long()),
+               dict(seq_lens=t["seq_lens"].cpu())):
+        with pytest.raises(TypeError):
+            attention(**kw)
+    with pytest.raises(pb.PropdError):
+        attention(cap=-1.0)
+    both = torch.zeros(2 * t["weight"].numel(), device="cuda")
+    n = t["weight"].numel()
+    rows = pb.CacheRows(t["seq_lens"], t["dropped"], t["position"], both[:n].view(2, 2, 30))
+    with pytest.raises(ValueError):
+        pb.propd_cache_observe(tree, t["accept_len"], t["accept_path"], t["q"], t["lse"], t["k_cache"], t["k_tree"], rows, 0.1,
+                               weight_out=both[4:n + 4].view(2, 2, 30))
+    with pytest.raises(ValueError):
+        pb.propd_cache_evict(t["k_cache"], t["k_cache"], rows, 5, 0)
+    with pytest.raises(ValueError):
+        pb.propd_cache_evict(t["k_cache"], t["v_cache"], pb.CacheRows(t["seq_lens"]), 5, 0)
+    inv, offset = torch.ones(32, device="cuda"), torch.zeros((2, 24), dtype=torch.int32, device="cuda")
+    for kw in (dict(q_out=t["k_tree"]), dict(k_out=t["q"]), dict(k=None, k_out=t["k_tree"].clone()), dict(start=torch.zeros((1, 1), dtype=torch.int32, device="cuda"))):
+        with pytest.raises(ValueError):
+            pb.propd_rotary(**{**dict(q=t["q"], k=t["k_tree"], inv_freq=inv, offset=offset), **kw})

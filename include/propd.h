@@ -324,7 +324,7 @@ PROPD_API propd_status propd_commit_path(const propd_tree *tree, propd_dtype dt,
  *
  * How scores are made of products, for query position p_i and key position p_j:
  *     s = scale * <q_i, k_j>;  cap > 0: s = cap * tanh(s / cap);  slopes: s = s - slopes[h] * (p_i - p_j)
- * and which keys a query sees: cached rows with 0 <= p_j <= p_i, nodes of its ancestor set; of both
+ * and which keys a query sees: cached rows with 0 <= p_j < P, nodes of its ancestor set; of both
  * only those with p_i - p_j < window where window > 0.
  */
 typedef struct propd_score_rule {

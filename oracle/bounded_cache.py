@@ -46,7 +46,7 @@ def grouped_attention(n_nodes, parent, q, k_cache, v_cache, k_tree, v_tree, seq_
                 p_i = now + len(path) - 1
                 back = np.concatenate((p_i - at, len(path) - 1 - np.arange(len(path))))
                 seen = in_window(back, rule)
-                seen[:L] &= (at >= 0) & (at <= p_i)
+                seen[:L] &= (at >= 0) & (at < now)
                 # (only what the node sees is looked at: hidden rows may hold anything)
                 k = np.concatenate((k_cache[b, hk, :L], k_tree[b, hk, path]))[seen]
                 v = np.concatenate((v_cache[b, hk, :L], v_tree[b, hk, path]))[seen]
@@ -79,7 +79,7 @@ def cache_observe(n_nodes, accept_len, accept_path, q, lse, k_cache, k_tree, seq
                 places = [x for x in range(r + 1) if path[x] is not None]
                 back = np.concatenate((now + r - at, r - np.array(places)))
                 seen = in_window(back, rule)
-                seen[:L] &= (at >= 0) & (at <= now + r)
+                seen[:L] &= (at >= 0) & (at < now)
                 to = np.concatenate((np.arange(L), L + np.array(places)))[seen]
                 k = np.concatenate((k_cache[b, hk, :L], k_tree[b, hk, [path[x] for x in places]]))[seen]
                 for h in range(hk * group, (hk + 1) * group):

@@ -75,7 +75,8 @@ def _init_marshal(lib: ctypes.CDLL) -> None:
         return
     native.init(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
         "propd_tree_mask", "propd_tree_attention", "propd_early_prune", "propd_early_prune_prob", "propd_accept_path",
-        "propd_commit_path", "propd_workspace_bytes")))
+        "propd_commit_path", "propd_workspace_bytes", "propd_grouped_attention", "propd_cache_observe", "propd_cache_evict",
+        "propd_rotary")))
     _marshal = native
 
 
@@ -574,6 +575,12 @@ def propd_grouped_attention(tree: Tree, q, k_cache, v_cache, k_tree, v_tree, seq
                             dropped: Optional[torch.Tensor] = None, want_lse: bool = False, out: Optional[torch.Tensor] = None,
                             lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """-> out [B,H,T_max,d], or (out, lse) if ``want_lse`` or an ``lse`` tensor is given."""
+    native = _native()
+    if native is not None:
+        r = native.grouped_attention(tree.n_nodes, tree.parent, tree.token, tree.depth, tree.anc, q, k_cache, v_cache, k_tree, v_tree, seq_lens,
+                                     scale, cap, window, slopes, position, dropped, want_lse, out, lse, workspace, _stream)
+        if r is not None:
+            return _done(r, "propd_grouped_attention")
     B, H, H_kv, T_max, d, L_max = _shared_heads(tree, q, k_tree, k_cache)
     dt, i32, f32 = _dt(q), torch.int32, torch.float32
     cache, rows = (B, H_kv, L_max, d), (B, H_kv, T_max, d)
@@ -601,6 +608,14 @@ def propd_cache_observe(tree: Tree, accept_len: torch.Tensor, accept_path: torch
                         position_out: Optional[torch.Tensor] = None) -> None:
     """Adds what the accepted nodes paid to every row to ``rows.weight``, and sets weight and position of the rows that the
     commit is about to append; IN PLACE unless ``weight_out`` (``position_out``) is given.  Between acceptance and commit."""
+    native = _native()
+    if native is not None:
+        r = native.cache_observe(tree.n_nodes, tree.parent, tree.token, tree.depth, tree.anc, accept_len, accept_path, q, lse, k_cache, k_tree,
+                                 rows.seq_lens, rows.dropped, rows.position, rows.weight, scale, cap, window, slopes, decay, weight_out,
+                                 position_out, _stream)
+        if r is not None:
+            _done(None if r is True else r, "propd_cache_observe")
+            return
     B, H, H_kv, T_max, d, L_max = _shared_heads(tree, q, k_tree, k_cache)
     dt, i32, f32 = _dt(q), torch.int32, torch.float32
     weight_out = rows.weight if weight_out is None else weight_out
@@ -627,6 +642,14 @@ def propd_cache_observe(tree: Tree, accept_len: torch.Tensor, accept_path: torch
 def propd_cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, rows: CacheRows, budget: int, recent: int, sinks: int = 0,
                       rows_out: Optional[CacheRows] = None, workspace: Optional[torch.Tensor] = None) -> None:
     """Down to ``budget`` rows per K/V head, IN PLACE; the per-row state too unless ``rows_out`` is given."""
+    native = _native()
+    if native is not None:
+        to = rows if rows_out is None else rows_out
+        r = native.cache_evict(k_cache, v_cache, rows.seq_lens, rows.dropped, rows.position, rows.weight, to.seq_lens, to.dropped, to.position,
+                               to.weight, budget, recent, sinks, workspace, _stream)
+        if r is not None:
+            _done(None if r is True else r, "propd_cache_evict")
+            return
     if k_cache.dim() != 4:
         raise ValueError("k_cache has four dimensions")
     B, H_kv, L_max, d = k_cache.shape
@@ -653,6 +676,11 @@ def propd_rotary(q: torch.Tensor, k: Optional[torch.Tensor], inv_freq: torch.Ten
                  adjacent: bool = False, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """-> (q_out, k_out).  ``offset`` is int32 [B,S] (all axes alike) or [B,n_axes,S], ``start`` int32 [B,n_axes]; twice as many
     channels turn as ``inv_freq`` has entries.  ``q_out`` may be ``q``, and ``k_out`` ``k``."""
+    native = _native()
+    if native is not None:
+        r = native.rotary(q, k, inv_freq, offset, start, axis_of, n_rows, adjacent, q_out, k_out, _stream)
+        if r is not None:
+            return _done(r, "propd_rotary")
     if q.dim() != 4 or (k is not None and k.dim() != 4) or offset.dim() not in (2, 3) or inv_freq.dim() != 1:
         raise ValueError("q and k have four dimensions, offset two or three, inv_freq one")
     B, H, S, d = q.shape

@@ -42,7 +42,7 @@ __device__ __forceinline__ uint32_t rank_key(float weight, int position, int nex
 template <int KEYS, int BITS>
 __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(EvictParams p) {
   constexpr int kBins = (1 << BITS) - 1;
-  __shared__ int s_count[2][kSelectWaves][kBins + 1];
+  __shared__ int s_count[2][kBins][kSelectWaves];
   __shared__ int s_total[3][kSelectWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int unit = blockIdx.x, b = unit / p.H_kv;
@@ -88,9 +88,10 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(EvictParam
     }
   };
 
-  // ---- the largest threshold that `budget` keys reach.  (Rows past L have key 0, which every threshold but 0 leaves out.)
+  // ---- the largest threshold that `budget` keys reach, or one that exactly as many do.  (Rows past L have key 0, which every
+  //      threshold tried leaves out.)
   uint32_t threshold = 0u;
-  int reached = L, above = 0;  // keys >= threshold, keys > threshold
+  int above = 0;  // keys > threshold
   for (int shift = 32 - BITS, turn = 0; shift >= 0; shift -= BITS, turn ^= 1) {
     int count[kBins];
 #pragma unroll
@@ -101,35 +102,47 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(EvictParam
     });
     if (lane == 0)
 #pragma unroll
-      for (int t = 0; t < kBins; ++t) s_count[turn][wave][t] = count[t];
+      for (int t = 0; t < kBins; ++t) s_count[turn][t][wave] = count[t];
     __syncthreads();
+    // The sums over the waves, four thresholds at a time: a row of 16 lanes adds up one threshold's.  (48 reads and additions per
+    // thread instead took 1.2 us per round.)
     int best = 0;  // counts fall with t
+    bool exact = false;
 #pragma unroll
-    for (int t = 0; t < kBins; ++t) {
-      int all = 0;
+    for (int t0 = 0; t0 < kBins; t0 += 4) {
+      const int t = t0 + (lane >> 4);
+      int all = s_count[turn][t < kBins ? t : 0][lane & 15];
+      all += __builtin_amdgcn_update_dpp(0, all, 0x128, 0xf, 0xf, false);  // row_ror:8, 4, 2, 1
+      all += __builtin_amdgcn_update_dpp(0, all, 0x124, 0xf, 0xf, false);
+      all += __builtin_amdgcn_update_dpp(0, all, 0x122, 0xf, 0xf, false);
+      all += __builtin_amdgcn_update_dpp(0, all, 0x121, 0xf, 0xf, false);
 #pragma unroll
-      for (int w = 0; w < kSelectWaves; ++w) all += s_count[turn][w][t];
-      if (all >= budget) {
-        best = t + 1;
-        reached = all;
-      } else if (best == t) {
-        above = all;  // of the next threshold, which too few keys reach
+      for (int k = 0; k < 4; ++k) {
+        if (t0 + k >= kBins) continue;
+        const int sum = __builtin_amdgcn_readlane(all, 16 * k);
+        if (sum >= budget) best = t0 + k + 1;
+        else if (best == t0 + k) above = sum;  // the first that too few keys reach
+        exact = exact || sum == budget;
       }
     }
     threshold += (uint32_t)best << shift;
+    if (exact) {  // the keys from here on are the ones that stay.  (Equal counts: any of these thresholds has the same keys.)
+      threshold -= 1u;
+      above = budget;
+      break;
+    }
   }
-  (void)reached;
-  // `above` is the count of the last threshold tried that too few keys reach; behind the last round (shift 0) that is
-  // threshold + 1, unless all of that round's were reached: then an earlier round's, which is the same number.
+  // Otherwise `above` is the count of the least threshold that too few keys reach, which is threshold + 1 by now.
 
   // ---- which of the keys equal to the threshold stay: the first ones
-  auto before = [&](int which, int mine) {  // the waves in front of this one
-    if (lane == 0) s_total[which][wave] = mine;
-    __syncthreads();
-    int sum = 0;
-#pragma unroll
-    for (int w = 0; w < kSelectWaves; ++w) sum += w < wave ? s_total[which][w] : 0;
-    return sum;
+  auto sum_before = [&](int which) {  // of the waves in front of this one
+    int x = s_total[which][lane & 15];
+    x = (lane & 15) < wave ? x : 0;
+    x += __builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x124, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x122, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x121, 0xf, 0xf, false);
+    return __builtin_amdgcn_readfirstlane(x);
   };
   const uint64_t below = (1ull << lane) - 1ull;
   const int wanted = budget - above;
@@ -137,7 +150,9 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(EvictParam
   for_keys([&](int i, uint32_t key) __attribute__((always_inline)) {
     equal += __popcll(__ballot(start + kWave * i + lane < L && key == threshold));
   });
-  const int equal_before = before(0, equal);
+  if (lane == 0) s_total[0][wave] = equal;
+  __syncthreads();
+  const int equal_before = sum_before(0);
   auto for_rows = [&](auto &&f) __attribute__((always_inline)) {  // f(row, whether it is kept)
     int seen = equal_before;
     for_keys([&](int i, uint32_t key) __attribute__((always_inline)) {
@@ -153,10 +168,12 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(EvictParam
     holes += __popcll(__ballot(j < budget && !keep));
     late += __popcll(__ballot(j >= budget && keep));
   });
-  if (lane == 0) s_total[2][wave] = late;
-  int hole = before(1, holes), row = 0;
-#pragma unroll
-  for (int w = 0; w < kSelectWaves; ++w) row += w < wave ? s_total[2][w] : 0;
+  if (lane == 0) {
+    s_total[1][wave] = holes;
+    s_total[2][wave] = late;
+  }
+  __syncthreads();
+  int hole = sum_before(1), row = sum_before(2);
   int32_t *const free_places = p.lists + (size_t)unit * 2 * p.room, *const moving = free_places + p.room;
   for_rows([&](int j, bool keep) __attribute__((always_inline)) {
     const uint64_t h = __ballot(j < budget && !keep), m = __ballot(j >= budget && keep);

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kObserveThreads) void cache_observe_kernel(ObserveP
         if (p.cap > 0.f) s = capped(s, p.cap, p.inv_cap);
         s = fmaf(-slope[j], (float)(sight[j].p_i - at[x]), s);
         const float w = __builtin_amdgcn_exp2f((s - lse[j]) * kLog2e);
-        const bool seen = place[j] >= 0 && in_sight(sight[j], at[x]) && (!own || key[x] <= place[j]);
+        const bool seen = place[j] >= 0 && in_sight(sight[j], at[x]) && (own ? key[x] <= place[j] : at[x] < n.P);
         paid[x] += seen ? w : 0.f;
       }
     }

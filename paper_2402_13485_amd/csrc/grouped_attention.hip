@@ -64,17 +64,31 @@ __device__ __forceinline__ int pieces_of(int n, int d) {
   return x < 1 ? 1 : (x > n ? n : x);
 }
 
-// How the units are cut.  Every workgroup works the same plan out from the lengths: a range is at most `most` stages, a
-// unit of s stages has pieces_of(s, most) of them, equally long.  Candidates for `most` are what makes the ranges of all units
-// fill 1, 2, 3 or 4 rounds of the workgroups that run at once, and longer ones; the cost of one is its rounds times
-// (its longest range + kRangeCost), and kMergeCost where any unit is cut.
-constexpr int kCandidates = 16, kLeastStages = 2;
-constexpr float kRangeCost = 4.f, kMergeCost = 4.f;
-
+// How the units are cut.  Every workgroup works the same plan out from the lengths.
+//   All sequences alike: as many whole units as there are workgroups that run at once, as often as that goes, then the units
+//     left over in `pieces` ranges each, piece by piece.
+//   Otherwise: a range is at most `most` stages, a unit of s stages has pieces_of(s, most) of them, equally long.
+// The time of a plan is counted in stages of a workgroup that has a compute unit to itself (plan_time); the lanes try a candidate each.
 struct Plan {
-  int most;      // stages of a range
+  bool alike;
+  int whole;     // alike: units done whole, first
+  int left;      // alike: units left over
+  int stages;    // alike: of a unit
+  int per_sequence;  // alike: units
+  int pieces;    // alike
+  int most;      // otherwise: stages of a range
   int n_ranges;  // of the call
 };
+
+constexpr float kShared = 1.6f;      // a stage of a workgroup that shares its compute unit with another one
+constexpr float kRangeCost = 6.f;    // per range: the first loads, the result
+constexpr float kMergeCost = 6.f;    // where any unit is cut: another kernel
+constexpr float kPieceCost = .03f;   // per range of a cut unit: its partial result, written and read
+__device__ __forceinline__ float rounds_time(float ranges, float longest, float resident) {
+  const float full = floorf(ranges / resident), rest = ranges - full * resident;
+  return full * (longest * kShared + kRangeCost) +
+         (rest > 0.f ? longest * (rest > .5f * resident ? kShared : 1.f) + kRangeCost : 0.f);
+}
 
 template <class StagesOf>
 __device__ __forceinline__ Plan plan_ranges(const GroupedParams &p, StagesOf &&lane_units) {
@@ -82,11 +96,17 @@ __device__ __forceinline__ Plan plan_ranges(const GroupedParams &p, StagesOf &&l
   auto sum = [](int x, int y) { return x + y; };
   auto larger = [](int x, int y) { return x > y ? x : y; };
   float total = 0.f;
-  int units = 0, longest = 1;
+  int units = 0, longest = 1, s_first = 0, u_first = 0;
+  bool alike = true;
   for (int b0 = 0; b0 < p.B; b0 += kWave) {
     int s, u;
     lane_units(b0 + lane, s, u);
-    // products of two numbers below 2^24 in float: only the cost depends on them
+    if (b0 == 0) {
+      s_first = uniform(s);
+      u_first = uniform(u);
+    }
+    alike = alike && __ballot(b0 + lane < p.B && (s != s_first || u != u_first)) == 0;
+    // products of two numbers below 2^24 in float: only the choice depends on them
     float t = (float)s * (float)u;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, kWave);
@@ -94,36 +114,48 @@ __device__ __forceinline__ Plan plan_ranges(const GroupedParams &p, StagesOf &&l
     units += __builtin_amdgcn_readlane(wave_scan_i32(u, 0, sum), 63);
     longest = larger(longest, __builtin_amdgcn_readlane(wave_scan_i32(s, 0, larger), 63));
   }
-  Plan plan = {longest, units};
+  Plan plan = {alike, 0, units, s_first, u_first, 1, longest, units};
   if (!p.may_split) return plan;
   const float G = (float)p.resident;
-  // candidate of this lane: rounds 1 (eight lengths), 2 (four), 3 and 4 (two each)
-  const int c = lane & (kCandidates - 1), round = c < 8 ? 1 : c < 12 ? 2 : c < 14 ? 3 : 4;
-  const int step = c < 8 ? c : c < 12 ? c - 8 : c & 1;
-  float most_f = ceilf(total / (G * (float)round) * (1.f + .125f * (float)step));
-  most_f = fminf(fmaxf(most_f, (float)kLeastStages), (float)longest);
-  const int most_l = (int)most_f;
-  float ranges_l = 0.f;  // of the call with this lane's candidate
-  for (int b0 = 0; b0 < p.B; b0 += kWave) {
-    int s, u;
-    lane_units(b0 + lane, s, u);
-    const int here = p.B - b0 < kWave ? p.B - b0 : kWave;
-    for (int i = 0; i < here; ++i)
-      ranges_l += (float)__builtin_amdgcn_readlane(u, i) * (float)pieces_of(__builtin_amdgcn_readlane(s, i), most_l);
+  float ranges = 0.f, range = 0.f;
+  int pieces = 1, most = longest, whole = 0;
+  if (alike) {
+    // lanes 0..31: all units in 1..32 pieces; 32..63: the ones left over behind full rounds of whole units
+    whole = lane < 32 ? 0 : units / p.resident * p.resident;
+    pieces = (lane & 31) + 1;
+    pieces = pieces < s_first ? pieces : s_first;
+    ranges = (float)(units - whole) * (float)pieces;
+    range = ceilf((float)s_first / (float)pieces);
+  } else {
+    // what fills 1 (32 lanes), 2 (16), 3 and 4 (8) rounds of the workgroups that run at once, and longer ranges
+    const int round = lane < 32 ? 1 : lane < 48 ? 2 : lane < 56 ? 3 : 4, step = lane < 32 ? lane : lane < 48 ? lane - 32 : lane & 7;
+    const float most_f = ceilf(total / (G * (float)round) * (1.f + .0625f * (float)step));
+    most = (int)fminf(fmaxf(most_f, 1.f), (float)longest);
+    for (int b0 = 0; b0 < p.B; b0 += kWave) {
+      int s, u;
+      lane_units(b0 + lane, s, u);
+      const int here = p.B - b0 < kWave ? p.B - b0 : kWave;
+      for (int i = 0; i < here; ++i)
+        ranges += (float)__builtin_amdgcn_readlane(u, i) * (float)pieces_of(__builtin_amdgcn_readlane(s, i), most);
+    }
+    range = ceilf((float)longest / (float)pieces_of(longest, most));
   }
-  const bool cut = ranges_l > (float)units;
-  const float longest_range = ceilf((float)longest / (float)pieces_of(longest, most_l));
-  float cost = ceilf(ranges_l / G) * (longest_range + kRangeCost) + kMergeCost;
-  if (!cut || ranges_l > (float)p.slots) cost = INFINITY;  // not cut: `whole`
-  const float whole = ceilf((float)units / G) * ((float)longest + kRangeCost);
+  const bool cut = alike ? pieces > 1 && whole < units : ranges > (float)units;
+  float cost = (float)(whole / p.resident) * ((float)longest * kShared + kRangeCost) + rounds_time(ranges, range, G) +
+               (cut ? kMergeCost + kPieceCost * ranges : 0.f);
+  if ((cut && ranges > (float)p.slots) || (!cut && !alike)) cost = INFINITY;
+  const float uncut = rounds_time((float)units, (float)longest, G);
   float least = cost;
 #pragma unroll
-  for (int o = kCandidates / 2; o > 0; o >>= 1) least = fminf(least, __shfl_xor(least, o, kWave));
+  for (int o = 32; o > 0; o >>= 1) least = fminf(least, __shfl_xor(least, o, kWave));
   least = __uint_as_float(uniform(__float_as_uint(least)));
-  if (!(least < whole)) return plan;
+  if (!(least < uncut)) return plan;
   const int pick = __builtin_ctzll(__ballot(cost == least));
-  plan.most = __builtin_amdgcn_readlane(most_l, pick);
-  plan.n_ranges = (int)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ranges_l), pick));
+  plan.whole = __builtin_amdgcn_readlane(whole, pick);
+  plan.left = units - plan.whole;
+  plan.pieces = __builtin_amdgcn_readlane(pieces, pick);
+  plan.most = __builtin_amdgcn_readlane(most, pick);
+  plan.n_ranges = plan.whole + (int)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ranges), pick));
   return plan;
 }
 
@@ -149,8 +181,10 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
   constexpr int kPerStage = 2 * kLoads + (kPlace ? 1 : 0);  // loads of a wave per stage
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const uint32_t ring = (uint32_t)(uintptr_t)(lds_void *)smem;
-  const uint32_t place_ring = ring + NS * kStageBytes;               // [NS][4 waves][64] positions
-  int32_t *const tree_place = reinterpret_cast<int32_t *>(smem + NS * kStageBytes + (kPlace ? NS * 1024 : 0));  // [128]
+  const uint32_t place_ring = ring + NS * kStageBytes;  // [NS][4 waves][64] positions
+  // places: positions less that of the root, as numbers that are exact where they matter
+  float *const stage_place = reinterpret_cast<float *>(smem + NS * kStageBytes + NS * 1024);  // [4 waves][32], of the stage at work
+  float *const tree_place = stage_place + 4 * 32;                                             // [128], of the tree's nodes
   __shared__ int s_any[2];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -187,35 +221,58 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
   int n_any = 0;
 
   // ---- ranges.  The blocks of a unit read the same rows: they run next to each other on one XCD (workgroups go to the 8
-  //      XCDs in turn), so that the rows come from its L2 but for the first time.
-  const int span = 8 * p.blocks, padded = (plan.n_ranges + span - 1) / span * span;
-  for (int at = blockIdx.x; at < padded; at += gridDim.x) {
-    const int in_span = at % span, range = at - in_span + in_span % 8 * p.blocks + in_span / 8;
-    if (range >= plan.n_ranges) continue;
-    // the sequence of the range, and the ranges before that sequence
-    int b = 0, first_range = 0;
-    for (int b0 = 0, before = 0; b0 < p.B; b0 += kWave) {
-      int s, u;
-      lane_units(b0 + lane, s, u);
-      const int mine = u * (s > 0 ? pieces_of(s, plan.most) : 0);
-      const int incl = wave_scan_i32(mine, 0, [](int x, int y) { return x + y; });
-      const uint64_t le = __ballot(b0 + lane < p.B && before + incl - mine <= range);
-      if (le == 0) break;
-      const int src = __popcll(le) - 1;
-      b = b0 + src;
-      first_range = __builtin_amdgcn_readlane(before + incl - mine, src);
-      before += __builtin_amdgcn_readlane(incl, 63);
+  //      XCDs in turn), so that the rows come from its L2 but for the first time.  What does not fill a span stays in order.
+  const int span = 8 * p.blocks;
+  for (int at = blockIdx.x; at < plan.n_ranges; at += gridDim.x) {
+    const int part0 = at < plan.whole ? 0 : plan.whole, part_n = at < plan.whole ? plan.whole : plan.n_ranges - plan.whole;
+    const int local = at - part0, in_span = local % span;
+    const int range = local < part_n / span * span ? local - in_span + in_span % 8 * p.blocks + in_span / 8 : local;  // within its part
+    int b = 0, block, hk, piece = 0, P = 1, first_slot = 0, stride = 1;
+    if (plan.alike) {
+      int u = part0 + range;
+      if (part0 == plan.whole && at >= plan.whole) {
+        P = plan.pieces;
+        piece = range / plan.left;
+        first_slot = range - piece * plan.left;
+        stride = plan.left;
+        u = plan.whole + first_slot;
+      }
+      b = u / plan.per_sequence;
+      const int in_sequence = u - b * plan.per_sequence, n_blocks = plan.per_sequence / p.H_kv;
+      hk = in_sequence / n_blocks;
+      block = in_sequence - hk * n_blocks;
+    } else {
+      // the sequence of the range, and the ranges before that sequence
+      int first_range = 0, P_b = 1, u_b = 1;
+      for (int b0 = 0, before = 0; b0 < p.B; b0 += kWave) {
+        int s, u;
+        lane_units(b0 + lane, s, u);
+        const int cuts = s > 0 ? pieces_of(s, plan.most) : 0, mine = u * cuts;
+        const int incl = wave_scan_i32(mine, 0, [](int x, int y) { return x + y; });
+        const uint64_t le = __ballot(b0 + lane < p.B && before + incl - mine <= range);
+        if (le == 0) break;
+        const int src = __popcll(le) - 1;
+        b = b0 + src;
+        first_range = __builtin_amdgcn_readlane(before + incl - mine, src);
+        P_b = __builtin_amdgcn_readlane(cuts, src);
+        u_b = __builtin_amdgcn_readlane(u, src);
+        before += __builtin_amdgcn_readlane(incl, 63);
+      }
+      const int n_blocks = u_b / p.H_kv;
+      int rest = range - first_range;
+      block = rest % n_blocks;
+      rest /= n_blocks;
+      P = P_b;
+      piece = rest % P;
+      hk = rest / P;
+      stride = n_blocks;
+      first_slot = range - piece * n_blocks;
     }
     b = uniform(b);
     Lengths n = lengths_of(p, b);
     n.L = uniform(n.L), n.T = uniform(n.T), n.P = uniform(n.P), n.dropped = uniform(n.dropped);
     const Stages st = stages_of(n.L, n.T, p.window, in_order);
-    const int L = n.L, T = n.T, columns = p.group * T, n_blocks = (columns + 127) / 128, n_all = st.cached + st.tree;
-    const int P = pieces_of(n_all, plan.most);
-    int rest = range - first_range;
-    const int block = rest % n_blocks;
-    rest /= n_blocks;
-    const int piece = rest % P, hk = rest / P;
+    const int L = n.L, T = n.T, columns = p.group * T, n_all = st.cached + st.tree, slot_of_piece = first_slot + piece * stride;
     const int quot = n_all / P, extra = n_all - quot * P;
     const int s0 = piece * quot + (piece < extra ? piece : extra), n_st = quot + (piece < extra ? 1 : 0);
     const size_t unit = (size_t)b * p.H_kv + hk;
@@ -234,19 +291,24 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
     }
     const u32x4 ancv = *reinterpret_cast<const u32x4 *>(p.anc + ((size_t)b * p.T_max + node) * 2);
     const uint64_t anc_lo = ((uint64_t)ancv.y << 32) | ancv.x, anc_hi = ((uint64_t)ancv.w << 32) | ancv.z;
-    Sight sight = {0, 0, 0};
-    float slope = 0.f;
+    // A column sees places from `lowest` on; `all_see`: from here on every column of the wave does.  The bias of a score is
+    // slope * (place of the key) - slope * depth of the node, the second part of which waits for lse.
+    float lowest = 0.f, all_see = 0.f, slope = 0.f, shift = 0.f;
     if constexpr (kPlace) {
-      sight = sight_of(n.P + __popcll(anc_lo) + __popcll(anc_hi) - 1, p.window);
+      const int depth = __popcll(anc_lo) + __popcll(anc_hi) - 1;
+      lowest = (float)(sight_of(n.P + depth, p.window).lowest - n.P);
       slope = p.slopes ? p.slopes[hk * p.group + head] * kLog2e : 0.f;
+      shift = -slope * (float)depth;
+      all_see = lowest;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) all_see = fmaxf(all_see, __shfl_xor(all_see, o, kWave));
+      all_see = __uint_as_float(uniform(__float_as_uint(all_see)));
     }
     __builtin_amdgcn_s_barrier();  // the range before is done with the ring and the table
     if constexpr (kPlace) {
-      if (tid < T) {
-        const uint64_t *a = p.anc + ((size_t)b * p.T_max + tid) * 2;
-        tree_place[tid] = n.P + __popcll(a[0]) + __popcll(a[1]) - 1;
-      } else if (tid < 128) {
-        tree_place[tid] = 0;
+      if (tid < 128) {
+        const uint64_t *a = p.anc + ((size_t)b * p.T_max + (tid < T ? tid : 0)) * 2;
+        tree_place[tid] = (float)(__popcll(a[0]) + __popcll(a[1]) - 1);
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // seen by all behind the first stage's barrier
     }
@@ -372,24 +434,41 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       }
       if constexpr (kPlace) {
         if (in_order && !tree) {
-          const int back = sight.p_i - (n.dropped + j0 + 4 * g);
+          const float first = (float)(j0 - L + 4 * g);  // row j of the cache has place j - L
+          if (p.slopes) {  // uniform, as the next
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int dist = back - (8 * (r >> 2) + (r & 3));
-            sc[r] = (unsigned)dist <= (unsigned)sight.reach ? fmaf(-slope, (float)dist, sc[r]) : -INFINITY;
+            for (int r = 0; r < 16; ++r) sc[r] = fmaf(slope, first + (float)(8 * (r >> 2) + (r & 3)), sc[r]);
+          }
+          if ((float)(j0 - L) < all_see) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[r] = first + (float)(8 * (r >> 2) + (r & 3)) >= lowest ? sc[r] : -INFINITY;
           }
         } else {
-          const uint32_t from = tree ? (uint32_t)(uintptr_t)(lds_void *)(tree_place + j0)
-                                     : place_ring + (uint32_t)slot_of(i) * 1024 + wave * 256;
+          const float *from = tree ? tree_place + j0 : stage_place + 32 * wave;
+          bool all = true;
+          if (tree) {
+            all = 0.f >= all_see;
+          } else {
+            // the 32 positions become places; a row without one, or that is not before the root, lies below everything
+            const int at = *reinterpret_cast<const __attribute__((address_space(3))) int *>((uintptr_t)(place_ring + (uint32_t)slot_of(i) * 1024 + wave * 256 + 4 * l32));
+            const float place = (unsigned)at < (unsigned)n.P ? (float)(at - n.P) : -0x1p31f;
+            stage_place[32 * wave + l32] = place;
+            all = __ballot(place < all_see) == 0;
+          }
+          float place[16];
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
-            typedef __attribute__((ext_vector_type(4))) int i32x4;
-            const i32x4 at4 = *reinterpret_cast<const __attribute__((address_space(3))) i32x4 *>((uintptr_t)(from + 32 * q4 + 16 * g));
+            const f32x4 at4 = *reinterpret_cast<const f32x4 *>(from + 8 * q4 + 4 * g);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int r = 4 * q4 + j;
-              sc[r] = in_sight(sight, at4[j]) ? fmaf(-slope, (float)(sight.p_i - at4[j]), sc[r]) : -INFINITY;
-            }
+            for (int j = 0; j < 4; ++j) place[4 * q4 + j] = at4[j];
+          }
+          if (p.slopes) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[r] = fmaf(slope, place[r], sc[r]);
+          }
+          if (!all) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[r] = place[r] >= lowest ? sc[r] : -INFINITY;
           }
         }
       }
@@ -498,9 +577,10 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
     // ---- results
     l_run += __shfl_xor(l_run, 32, kWave);
     if constexpr (kRaw) m_run *= p.scale_log2e;
+    if constexpr (kPlace) m_run += shift;
     if (tid == 0 && piece == 0)
       *reinterpret_cast<u32x4 *>(p.records + 4 * (unit * p.blocks + block)) =
-          u32x4{(uint32_t)range, (uint32_t)n_blocks, (uint32_t)P, (uint32_t)T};
+          u32x4{(uint32_t)first_slot, (uint32_t)stride, (uint32_t)P, (uint32_t)T};
     if (there && P == 1) {
       const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : l_run;  // NaN stays
 #pragma unroll
@@ -511,10 +591,10 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       for (int mb = 0; mb < kMb; ++mb)
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4)
-          *reinterpret_cast<f32x4 *>(p.part_o + part_o_index(range, wave, 4 * mb + q4, lane)) =
+          *reinterpret_cast<f32x4 *>(p.part_o + part_o_index(slot_of_piece, wave, 4 * mb + q4, lane)) =
               f32x4{o_acc[mb][4 * q4], o_acc[mb][4 * q4 + 1], o_acc[mb][4 * q4 + 2], o_acc[mb][4 * q4 + 3]};
-      p.part_ml[part_ml_index(range, wave, 0, lane)] = m_run;
-      p.part_ml[part_ml_index(range, wave, 1, lane)] = l_run;
+      p.part_ml[part_ml_index(slot_of_piece, wave, 0, lane)] = m_run;
+      p.part_ml[part_ml_index(slot_of_piece, wave, 1, lane)] = l_run;
     }
   }
 }
@@ -522,12 +602,15 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
 // A result to be merged with factor f: left out where the factor is zero (an infinity would be NaN).
 __device__ __forceinline__ float counted(float o, float f) { return f == 0.f ? 0.f : o; }
 
-// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the pieces s of a unit, in their order.  One wave per 32 columns
-// and 32-wide block of d, eight pieces requested together.
-template <int D>
-__global__ __launch_bounds__(kWave) void grouped_attn_merge_kernel(GroupedParams p) {
-  constexpr int kMb = Geo<D>::kMb, N = 8;
-  const int mb = blockIdx.x % kMb, wave = blockIdx.x / kMb % 4;
+// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the pieces s of a unit, always in the same order.  A workgroup has 32
+// columns of a unit and a 32-wide block of d.  W waves take the pieces in turn, N of them requested together, and meet
+// through LDS: with few units there are many pieces, and what costs is the chain of their loads (33 pieces of 8 units, one
+// wave with a load after the other: 9.7 us).
+template <int D, int W, int N>
+__global__ __launch_bounds__(W *kWave) void grouped_attn_merge_kernel(GroupedParams p) {
+  constexpr int kMb = Geo<D>::kMb;
+  __shared__ float s_part[W > 1 ? W - 1 : 1][18][kWave];
+  const int mb = blockIdx.x % kMb, group = blockIdx.x / kMb % 4;
   const unsigned item = blockIdx.x / (4 * kMb);
   const int block = (int)(item % (unsigned)p.blocks);
   const size_t unit = item / (unsigned)p.blocks;
@@ -535,40 +618,62 @@ __global__ __launch_bounds__(kWave) void grouped_attn_merge_kernel(GroupedParams
   int T = p.n_nodes[b];
   T = T < 1 ? 1 : (T > p.T_max ? p.T_max : T);
   const int columns = p.group * T;
-  if (block * 128 + wave * 32 >= columns) return;
+  if (block * 128 + group * 32 >= columns) return;
   const u32x4 record = *reinterpret_cast<const u32x4 *>(p.records + 4 * (unit * p.blocks + block));
   const int first = (int)record.x, stride = (int)record.y, P = (int)record.z;
   if (P <= 1) return;
-  const int lane = threadIdx.x, g = lane >> 5, column = block * 128 + wave * 32 + (lane & 31);
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 5, column = block * 128 + group * 32 + (lane & 31);
   const bool there = column < columns;
   const int ln = there ? lane : 0;  // lanes past the last column read lane 0's data and store nothing
   f32x16 acc;
 #pragma unroll
   for (int r = 0; r < 16; ++r) acc[r] = 0.f;
   float M = -INFINITY, total = 0.f;
-  for (int s0 = 0; s0 < P; s0 += N) {
+  auto join = [&](const f32x16 &o, float m, float l) {
+    const float M_new = fmaxf(M, m), M_safe = M_new == -INFINITY ? 0.f : M_new;
+    const float a_old = fast_exp2(M - M_safe), a_new = fast_exp2(m - M_safe);
+    total = total * a_old + l * a_new;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = counted(acc[r], a_old) * a_old + counted(o[r], a_new) * a_new;
+    M = M_new;
+  };
+  for (int s0 = wave; s0 < P; s0 += N * W) {
     f32x4 o[N][4];
     float m[N], l[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const size_t slot = first + (size_t)(s0 + k < P ? s0 + k : P - 1) * stride;
-      m[k] = p.part_ml[part_ml_index(slot, wave, 0, ln)];
-      l[k] = p.part_ml[part_ml_index(slot, wave, 1, ln)];
+      const size_t slot = first + (size_t)(s0 + k * W < P ? s0 + k * W : P - 1) * stride;  // past the last: that once more, not used
+      m[k] = p.part_ml[part_ml_index(slot, group, 0, ln)];
+      l[k] = p.part_ml[part_ml_index(slot, group, 1, ln)];
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) o[k][q4] = *reinterpret_cast<const f32x4 *>(p.part_o + part_o_index(slot, wave, 4 * mb + q4, ln));
+      for (int q4 = 0; q4 < 4; ++q4) o[k][q4] = *reinterpret_cast<const f32x4 *>(p.part_o + part_o_index(slot, group, 4 * mb + q4, ln));
     }
+    __builtin_amdgcn_sched_barrier(0);  // all of them are requested first
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      if (s0 + k >= P) break;  // uniform
-      const float M_new = fmaxf(M, m[k]), M_safe = M_new == -INFINITY ? 0.f : M_new;
-      const float a_old = fast_exp2(M - M_safe), a_new = fast_exp2(m[k] - M_safe);
-      total = total * a_old + l[k] * a_new;
+      if (s0 + k * W < P) {  // uniform
+        f32x16 x;
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4)
+        for (int r = 0; r < 16; ++r) x[r] = o[k][r / 4][r % 4];
+        join(x, m[k], l[k]);
+      }
+    }
+  }
+  if constexpr (W > 1) {
+    if (wave > 0) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          acc[4 * q4 + j] = counted(acc[4 * q4 + j], a_old) * a_old + counted(o[k][q4][j], a_new) * a_new;
-      M = M_new;
+      for (int r = 0; r < 16; ++r) s_part[wave - 1][r][lane] = acc[r];
+      s_part[wave - 1][16][lane] = M;
+      s_part[wave - 1][17][lane] = total;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < W - 1; ++w) {
+      f32x16 x;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = s_part[w][r][lane];
+      join(x, s_part[w][16][lane], s_part[w][17][lane]);
     }
   }
   if (!there) return;
@@ -607,14 +712,16 @@ size_t grouped_attention_workspace_bytes(int B, int H, int L_max, int T_max) {
 template <int D, bool kCap, bool kPlace>
 static bool launch_grouped(const GroupedParams &p, unsigned grid, hipStream_t st) {
   constexpr int NS = D == 128 ? 4 : 6;
-  constexpr int lds_bytes = NS * Geo<D>::kStageBytes + (kPlace ? NS * 1024 + 512 : 0);
+  constexpr int lds_bytes = NS * Geo<D>::kStageBytes + (kPlace ? NS * 1024 + 1024 : 0);
   static std::atomic<uint64_t> set{0};
   if (!allow_lds(reinterpret_cast<const void *>(&grouped_attn_bf16_kernel<D, kCap, kPlace>), lds_bytes, set)) return false;
   hipLaunchKernelGGL((grouped_attn_bf16_kernel<D, kCap, kPlace>), dim3(grid), dim3(kGroupThreads), lds_bytes, st, p);
   if (!launch_ok()) return false;
   if (!p.may_split) return true;
-  hipLaunchKernelGGL(grouped_attn_merge_kernel<D>, dim3((unsigned)p.B * (unsigned)p.H_kv * (unsigned)p.blocks * 4u * Geo<D>::kMb),
-                     dim3(kWave), 0, st, p);
+  const unsigned units = (unsigned)p.B * (unsigned)p.H_kv * (unsigned)p.blocks;
+  const dim3 merge(units * 4u * Geo<D>::kMb);
+  if (units <= 96) hipLaunchKernelGGL((grouped_attn_merge_kernel<D, 4, 8>), merge, dim3(4 * kWave), 0, st, p);
+  else hipLaunchKernelGGL((grouped_attn_merge_kernel<D, 1, 4>), merge, dim3(kWave), 0, st, p);
   return launch_ok();
 }
 
@@ -688,7 +795,6 @@ extern "C" propd_status propd_grouped_attention(const propd_tree *tree, propd_dt
   const long long units = (long long)p.B * H_kv * p.blocks;
   const long long stages = (L_max + kStageRows - 1ll) / kStageRows + (p.T_max + kStageRows - 1) / kStageRows;
   long long grid = p.may_split ? units * stages : units;
-  grid = (grid + 8ll * p.blocks - 1) / (8ll * p.blocks) * (8ll * p.blocks);
   if (grid > p.resident) grid = p.resident;
   return (d == 64 ? launch_grouped<64>(p, cap, place, (unsigned)grid, st) : launch_grouped<128>(p, cap, place, (unsigned)grid, st))
              ? PROPD_OK

@@ -119,6 +119,7 @@ __device__ __forceinline__ void grouped_f32_range(const GroupedParamsF32 &p, int
           at[r] = n.P + __popcll(anc[2 * j]) + __popcll(anc[2 * j + 1]) - 1;
         } else {
           at[r] = in_order ? n.dropped + j : place[(unsigned)j];
+          at[r] = at[r] < n.P ? at[r] : -1;
         }
       }
     }

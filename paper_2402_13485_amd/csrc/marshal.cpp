@@ -12,6 +12,7 @@
 // do.  No state is kept but the addresses of the entry points.
 #include <ATen/ATen.h>
 #include <Python.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <memory>
@@ -29,6 +30,10 @@ struct Entries {
   decltype(&propd_accept_path) accept_path = nullptr;
   decltype(&propd_commit_path) commit_path = nullptr;
   decltype(&propd_workspace_bytes) workspace_bytes = nullptr;
+  decltype(&propd_grouped_attention) grouped_attention = nullptr;
+  decltype(&propd_cache_observe) cache_observe = nullptr;
+  decltype(&propd_cache_evict) cache_evict = nullptr;
+  decltype(&propd_rotary) rotary = nullptr;
 };
 
 struct NotThis {};  // the Python code takes over
@@ -213,8 +218,8 @@ void take(PyObject *o, E &entry) {
 }
 
 PyObject *py_init(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  if (n != 7) {
-    PyErr_SetString(PyExc_TypeError, "init: seven addresses");
+  if (n != 11) {
+    PyErr_SetString(PyExc_TypeError, "init: eleven addresses");
     return nullptr;
   }
   take(a[0], entries.tree_mask);
@@ -224,6 +229,10 @@ PyObject *py_init(PyObject *, PyObject *const *a, Py_ssize_t n) {
   take(a[4], entries.accept_path);
   take(a[5], entries.commit_path);
   take(a[6], entries.workspace_bytes);
+  take(a[7], entries.grouped_attention);
+  take(a[8], entries.cache_observe);
+  take(a[9], entries.cache_evict);
+  take(a[10], entries.rotary);
   if (PyErr_Occurred()) return nullptr;
   Py_RETURN_NONE;
 }
@@ -410,9 +419,190 @@ PyObject *py_commit_path(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// ---- a bounded cache with shared heads: all tensors contiguous on one GPU, the current one (binding._all_dev)
+struct Device {
+  c10::Device device;
+  explicit Device(const at::Tensor &t) : device(t.device()) {
+    need(device.is_cuda() && c10::impl::VirtualGuardImpl(device.type()).getDevice() == device);
+  }
+  const at::Tensor &operator()(PyObject *o, at::ScalarType type, at::IntArrayRef shape) const {
+    const at::Tensor &t = tensor(o);
+    need(t.device() == device && t.scalar_type() == type && t.is_contiguous() && t.sizes() == shape);
+    return t;
+  }
+  // None where the argument may be left out
+  template <class T>
+  T *optional(PyObject *o, at::ScalarType type, at::IntArrayRef shape) const {
+    return o == Py_None ? nullptr : (T *)(*this)(o, type, shape).data_ptr();
+  }
+};
+
+bool overlap(const at::Tensor &x, const at::Tensor &y) {
+  const char *a = (const char *)x.data_ptr(), *b = (const char *)y.data_ptr();
+  return a < b + y.nbytes() && b < a + x.nbytes();
+}
+
+void same_or_apart(const at::Tensor &out, const at::Tensor &in) { need(out.data_ptr() == in.data_ptr() || !overlap(out, in)); }
+
+// grouped_attention(*tree, q, k_cache, v_cache, k_tree, v_tree, seq_lens, scale, cap, window, slopes, position, dropped, want_lse, out, lse,
+// workspace, stream) -> out or (out, lse)
+PyObject *py_grouped_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded([&]() -> Owned {
+    need(n == 22);
+    const at::Tensor &q = tensor(a[5]), &kt0 = tensor(a[8]), &kc0 = tensor(a[6]);
+    const propd_dtype dt = type_of(q);
+    const at::ScalarType type = q.scalar_type();
+    need(q.dim() == 4 && kt0.dim() == 4 && kc0.dim() == 4 && q.is_contiguous());
+    const Device on(q);
+    const int64_t B = q.size(0), H = q.size(1), T = q.size(2), d = q.size(3), Hk = kt0.size(1), L = kc0.size(2);
+    need(Hk >= 1 && H % Hk == 0);
+    const at::Tensor &kc = on(a[6], type, {B, Hk, L, d}), &vc = on(a[7], type, {B, Hk, L, d});
+    const at::Tensor &kt = on(a[8], type, {B, Hk, T, d}), &vt = on(a[9], type, {B, Hk, T, d}), &seq = on(a[10], at::kInt, {B});
+    on(a[0], at::kInt, {B});
+    on(a[4], at::kLong, {B, T, 2});
+    const propd_tree tree = tree_of(a);
+    need(tree.B == B && tree.T_max == T);
+    propd_score_rule rule;
+    rule.scale = real(a[11]);
+    rule.cap = real(a[12]);
+    rule.window = whole32(a[13]);
+    rule.slopes = on.optional<float>(a[14], at::kFloat, {H});
+    int32_t *position = on.optional<int32_t>(a[15], at::kInt, {B, Hk, L}), *dropped = on.optional<int32_t>(a[16], at::kInt, {B});
+    const bool want = truth(a[17]) || a[19] != Py_None;
+    at::Tensor out, lse;
+    {
+      const Unlocked u;
+      if (a[18] == Py_None) out = at::empty_like(q);
+      if (want && a[19] == Py_None) lse = at::empty({B, H, T}, q.options().dtype(at::kFloat));
+    }
+    if (a[18] != Py_None) out = on(a[18], type, q.sizes());
+    if (a[19] != Py_None) lse = on(a[19], at::kFloat, {B, H, T});
+    for (const at::Tensor *t : {&q, &kc, &vc, &kt, &vt}) need(!overlap(out, *t));
+    need(!want || !overlap(out, lse));
+    const Workspace w = workspace(a[20], entries.workspace_bytes(PROPD_WS_GROUPED_ATTENTION, tree.B, tree.T_max, size32(H), size32(d),
+                                                                 size32(L), 0, 0), q);
+    Owned o = a[18] != Py_None ? object(a[18]) : object(out);
+    Owned result = want ? tuple_of(std::move(o), a[19] != Py_None ? object(a[19]) : object(lse)) : std::move(o);
+    call(entries.grouped_attention, &tree, dt, size32(H), size32(Hk), size32(d), &rule, q.data_ptr(), L ? kc.data_ptr() : nullptr,
+         L ? vc.data_ptr() : nullptr, kt.data_ptr(), vt.data_ptr(), (const int32_t *)seq.data_ptr(), L ? position : nullptr, dropped, size32(L),
+         out.data_ptr(), want ? (float *)lse.data_ptr() : nullptr, w.ptr, w.bytes, stream_of(a[21]));
+    return result;
+  });
+}
+
+// cache_observe(*tree, accept_len, accept_path, q, lse, k_cache, k_tree, seq_lens, dropped, position, weight, scale, cap, window, slopes, decay,
+// weight_out, position_out, stream) -> True
+PyObject *py_cache_observe(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded([&]() -> Owned {
+    need(n == 23);
+    const at::Tensor &q = tensor(a[7]), &kc0 = tensor(a[9]), &kt0 = tensor(a[10]), &path0 = tensor(a[6]);
+    const propd_dtype dt = type_of(q);
+    const at::ScalarType type = q.scalar_type();
+    need(q.dim() == 4 && kt0.dim() == 4 && kc0.dim() == 4 && path0.dim() == 2 && q.is_contiguous());
+    const Device on(q);
+    const int64_t B = q.size(0), H = q.size(1), T = q.size(2), d = q.size(3), Hk = kt0.size(1), L = kc0.size(2), P = path0.size(1);
+    need(Hk >= 1 && H % Hk == 0);
+    on(a[0], at::kInt, {B});
+    const propd_tree tree = tree_of(a);
+    need(tree.B == B && tree.T_max == T);
+    const at::Tensor &len = on(a[5], at::kInt, {B}), &path = on(a[6], at::kInt, {B, P}), &lse = on(a[8], at::kFloat, {B, H, T});
+    const at::Tensor &kc = on(a[9], type, {B, Hk, L, d}), &kt = on(a[10], type, {B, Hk, T, d}), &seq = on(a[11], at::kInt, {B});
+    int32_t *dropped = on.optional<int32_t>(a[12], at::kInt, {B}), *position = on.optional<int32_t>(a[13], at::kInt, {B, Hk, L});
+    const at::Tensor &weight = on(a[14], at::kFloat, {B, Hk, L});
+    propd_score_rule rule;
+    rule.scale = real(a[15]);
+    rule.cap = real(a[16]);
+    rule.window = whole32(a[17]);
+    rule.slopes = on.optional<float>(a[18], at::kFloat, {H});
+    const float decay = real(a[19]);
+    const at::Tensor &weight_out = a[20] == Py_None ? weight : on(a[20], at::kFloat, {B, Hk, L});
+    int32_t *position_out = a[21] == Py_None ? position : on.optional<int32_t>(a[21], at::kInt, {B, Hk, L});
+    same_or_apart(weight_out, weight);
+    if (position && a[21] != Py_None) same_or_apart(tensor(a[21]), tensor(a[13]));
+    Owned result = object(Py_True);
+    call(entries.cache_observe, &tree, dt, size32(H), size32(Hk), size32(d), &rule, decay, (const int32_t *)len.data_ptr(),
+         (const int32_t *)path.data_ptr(), size32(P), q.data_ptr(), (const float *)lse.data_ptr(), kc.data_ptr(), kt.data_ptr(),
+         (const int32_t *)seq.data_ptr(), dropped, position, (const float *)weight.data_ptr(), size32(L), position_out,
+         (float *)weight_out.data_ptr(), stream_of(a[22]));
+    return result;
+  });
+}
+
+// cache_evict(k_cache, v_cache, seq_lens, dropped, position, weight, the same four for the results, budget, recent, sinks, workspace, stream) -> True
+PyObject *py_cache_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded([&]() -> Owned {
+    need(n == 15);
+    const at::Tensor &k = tensor(a[0]);
+    const propd_dtype dt = type_of(k);
+    need(k.dim() == 4 && k.is_contiguous());
+    const Device on(k);
+    const at::Tensor &v = on(a[1], k.scalar_type(), k.sizes());
+    need(!overlap(k, v));
+    const int64_t B = k.size(0), Hk = k.size(1), L = k.size(2), d = k.size(3);
+    propd_cache_rows rows[2];
+    for (int i = 0; i < 2; ++i) {
+      rows[i].seq_lens = (int32_t *)on(a[2 + 4 * i], at::kInt, {B}).data_ptr();
+      rows[i].dropped = (int32_t *)on(a[3 + 4 * i], at::kInt, {B}).data_ptr();
+      rows[i].position = (int32_t *)on(a[4 + 4 * i], at::kInt, {B, Hk, L}).data_ptr();
+      rows[i].weight = (float *)on(a[5 + 4 * i], at::kFloat, {B, Hk, L}).data_ptr();
+    }
+    for (int i = 2; i < 6; ++i) same_or_apart(tensor(a[4 + i]), tensor(a[i]));
+    const int32_t budget = whole32(a[10]), recent = whole32(a[11]), sinks = whole32(a[12]);
+    const Workspace w = workspace(a[13], entries.workspace_bytes(PROPD_WS_CACHE_EVICT, size32(B), 0, size32(Hk), 0, size32(L), 0, 0), k);
+    Owned result = object(Py_True);
+    call(entries.cache_evict, size32(B), dt, size32(Hk), size32(d), size32(L), budget, recent, sinks, k.data_ptr(), v.data_ptr(),
+         (const propd_cache_rows *)&rows[0], (const propd_cache_rows *)&rows[1], w.ptr, w.bytes, stream_of(a[14]));
+    return result;
+  });
+}
+
+// rotary(q, k, inv_freq, offset, start, axis_of, n_rows, adjacent, q_out, k_out, stream) -> (q_out, k_out)
+PyObject *py_rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded([&]() -> Owned {
+    need(n == 11);
+    const at::Tensor &q = tensor(a[0]), &inv = tensor(a[2]), &off = tensor(a[3]);
+    const propd_dtype dt = type_of(q);
+    const at::ScalarType type = q.scalar_type();
+    need(q.dim() == 4 && q.is_contiguous() && inv.dim() == 1 && (off.dim() == 2 || off.dim() == 3));
+    const Device on(q);
+    const int64_t B = q.size(0), H = q.size(1), S = q.size(2), d = q.size(3), pairs = inv.size(0);
+    const bool keys = a[1] != Py_None, each = off.dim() == 3;
+    need(keys ? tensor(a[1]).dim() == 4 : a[9] == Py_None);
+    const int64_t Hk = keys ? tensor(a[1]).size(1) : 0, offset_axes = each ? off.size(1) : 1;
+    need(a[4] == Py_None || tensor(a[4]).dim() == 2);
+    const int64_t axes = a[4] != Py_None ? tensor(a[4]).size(1) : offset_axes;
+    on(a[2], at::kFloat, {pairs});
+    if (each) on(a[3], at::kInt, {B, offset_axes, S});
+    else on(a[3], at::kInt, {B, S});
+    const int32_t *start = on.optional<int32_t>(a[4], at::kInt, {B, axes}), *axis_of = on.optional<int32_t>(a[5], at::kInt, {pairs});
+    const int32_t *n_rows = on.optional<int32_t>(a[6], at::kInt, {B});
+    const bool adjacent = truth(a[7]);
+    at::Tensor k, q_out, k_out;
+    if (keys) k = on(a[1], type, {B, Hk, S, d});
+    {
+      const Unlocked u;
+      if (a[8] == Py_None) q_out = at::empty_like(q);
+      if (keys && a[9] == Py_None) k_out = at::empty_like(k);
+    }
+    if (a[8] != Py_None) q_out = on(a[8], type, q.sizes());
+    if (a[9] != Py_None) k_out = on(a[9], type, k.sizes());
+    same_or_apart(q_out, q);
+    if (keys) {
+      same_or_apart(k_out, k);
+      need(!overlap(q_out, k) && !overlap(q_out, k_out) && !overlap(k_out, q));
+    }
+    Owned result = tuple_of(a[8] != Py_None ? object(a[8]) : object(q_out), a[9] != Py_None ? object(a[9]) : object(k_out));
+    call(entries.rotary, dt, size32(B), size32(S), size32(H), size32(Hk), size32(d), size32(2 * pairs), (int32_t)adjacent, size32(axes), axis_of,
+         (const float *)inv.data_ptr(), start, (const int32_t *)off.data_ptr(), size32(offset_axes), n_rows, q.data_ptr(),
+         keys ? k.data_ptr() : nullptr, q_out.data_ptr(), keys ? k_out.data_ptr() : nullptr, stream_of(a[10]));
+    return result;
+  });
+}
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(init),        METHOD(tree_mask),   METHOD(tree_attention), METHOD(early_prune),
-                         METHOD(accept_path), METHOD(commit_path), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(accept_path), METHOD(commit_path), METHOD(grouped_attention), METHOD(cache_observe),
+                         METHOD(cache_evict), METHOD(rotary),      {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -126,7 +126,8 @@ def test_attention_hidden_rows_may_hold_anything(pb, dtype, value, where):
     rule = rule_of(128, window=30 if where == "window" else 0)
     for name in ("k", "v"):
         if where == "hole":
-            x["position"][:, :, 5:9] = -1
+            x["position"][:, :, 5:8] = -1
+            x["position"][:, :, 8] = (x["seq_lens"] + x["dropped"] + 3)[:, None]  # not before the root
             x[name + "_cache"][:, :, 5:9] = bits
         elif where == "window":
             x[name + "_cache"][:, :, 3:7] = bits
@@ -529,3 +530,54 @@ def test_overlaps_shapes_and_devices_are_refused(pb):
     for kw in (dict(q_out=t["k_tree"]), dict(k_out=t["q"]), dict(k=None, k_out=t["k_tree"].clone()), dict(start=torch.zeros((1, 1), dtype=torch.int32, device="cuda"))):
         with pytest.raises(ValueError):
             pb.propd_rotary(**{**dict(q=t["q"], k=t["k_tree"], inv_freq=inv, offset=offset), **kw})
+
+
+# ---- native and Python marshalling
+
+def test_marshalling_in_python_is_the_same(pb, monkeypatch):
+    """Outputs bit for bit, made by the call and given, and the errors of what is refused."""
+    from test_gpu_marshal import both, flat
+    rng = np.random.default_rng(71)
+    x = observe_case(rng, "bf16", 4, 2, 64, [20, 9], [3, 3], L_max=30)
+    tree, t = dev_tree(pb, x), {n: to_dev(x[n]) for n in ("q", "k_cache", "v_cache", "k_tree", "v_tree", "seq_lens", "dropped", "position", "weight", "lse",
+                                                          "accept_len", "accept_path")}
+    full = pb.Tree(torch.full_like(tree.n_nodes, 24), tree.parent, anc=tree.anc)
+    slopes, inv, offset = torch.rand(4, device="cuda"), torch.rand(16, device="cuda"), torch.zeros((2, 24), dtype=torch.int32, device="cuda")
+    start, axis_of = torch.ones((2, 3), dtype=torch.int32, device="cuda"), torch.zeros(16, dtype=torch.int32, device="cuda")
+    rows = lambda: pb.CacheRows(*(t[n].clone() for n in ("seq_lens", "dropped", "position", "weight")))
+    att = lambda **k: pb.propd_grouped_attention(full, t["q"], t["k_cache"], t["v_cache"], t["k_tree"], t["v_tree"], t["seq_lens"], 0.125, **k)
+
+    def observe(r, decay=0.5, **k):
+        pb.propd_cache_observe(tree, t["accept_len"], t["accept_path"], t["q"], t["lse"], t["k_cache"], t["k_tree"], r, 0.125, decay=decay, **k)
+        return [r, *k.values()]
+
+    def evict(budget=7, **k):
+        kc, vc, r = t["k_cache"].clone(), t["v_cache"].clone(), rows()
+        pb.propd_cache_evict(kc, vc, r, budget, 2, 1, **k)
+        return [kc, vc, r, *(v for v in k.values() if not torch.is_tensor(v))]
+    zero = lambda: torch.zeros_like(t["weight"])
+    good = [lambda: att(out=torch.zeros_like(t["q"])), lambda: att(want_lse=True, cap=5.0, window=9, slopes=slopes),
+            lambda: att(position=t["position"], dropped=t["dropped"], lse=torch.zeros_like(t["lse"]), workspace=torch.empty(1 << 27, dtype=torch.uint8, device="cuda")),
+            lambda: observe(rows()), lambda: observe(rows(), cap=5.0, window=9, slopes=slopes, weight_out=zero(), position_out=torch.zeros_like(t["position"])),
+            lambda: observe(pb.CacheRows(t["seq_lens"], weight=t["weight"].clone())), lambda: evict(),
+            lambda: evict(rows_out=pb.CacheRows(*(torch.zeros_like(t[n]) for n in ("seq_lens", "dropped", "position", "weight")))),
+            lambda: pb.propd_rotary(t["q"], t["k_tree"], inv, offset), lambda: pb.propd_rotary(t["q"], None, inv, offset, adjacent=True)[0],
+            lambda: pb.propd_rotary(t["q"].clone(), t["k_tree"], inv, offset, start=start, axis_of=axis_of, n_rows=tree.n_nodes, q_out=torch.zeros_like(t["q"]),
+                                    k_out=torch.zeros_like(t["k_tree"]))]
+    for n, call in enumerate(good):
+        native, python = both(pb, monkeypatch, call)
+        assert type(native) is type(python), (n, native, python)
+        native, python = flat(native), flat(python)
+        assert len(native) == len(python) > 0, n
+        for a, b in zip(native, python):
+            # (bits: the first calls see the NaN of the rows without a position, and give NaN)
+            assert a.shape == b.shape and a.dtype == b.dtype and a.contiguous().view(torch.uint8).equal(b.contiguous().view(torch.uint8)), n
+    cpu = {k: v.cpu() for k, v in t.items()}
+    bad = [lambda: att(cap=-1.0), lambda: att(window=-1), lambda: att(window=1.5), lambda: att(slopes=slopes[:3]), lambda: att(lse=cpu["lse"]), lambda: att(out=t["q"]),
+           lambda: att(workspace=torch.empty(8, dtype=torch.uint8, device="cuda")), lambda: observe(rows(), decay=2.0), lambda: observe(pb.CacheRows(t["seq_lens"])),
+           lambda: observe(rows(), weight_out=cpu["weight"]), lambda: evict(budget=0), lambda: evict(budget="7"), lambda: evict(rows_out=pb.CacheRows(t["seq_lens"])),
+           lambda: pb.propd_rotary(t["q"], t["k_tree"], inv[:3], offset), lambda: pb.propd_rotary(t["q"], cpu["k_tree"], inv, offset),
+           lambda: pb.propd_rotary(t["q"], t["k_tree"], inv, offset[:1]), lambda: pb.propd_rotary(t["q"], t["k_tree"], inv, offset, q_out=t["k_tree"])]
+    for n, call in enumerate(bad):
+        native, python = both(pb, monkeypatch, call)
+        assert isinstance(native, Exception) and type(native) is type(python) and str(native) == str(python), (n, native, python)

@@ -215,8 +215,8 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       v_rd[mb][hi] = ring + kHalfStage + r * kRowBytes + ((chunk ^ G_::v_key(r)) << 4) + 8 * (lane & 1);
     }
   const int ld_row = G_::kLdRows * wave + lane / G_::kChunks;
-  const int k_lane_chunk = ((lane % G_::kChunks) ^ G_::k_key(ld_row)) << 4;
-  const int v_lane_chunk = ((lane % G_::kChunks) ^ G_::v_key(ld_row)) << 4;
+  const uint32_t k_lane = ld_row * kRowBytes + (((lane % G_::kChunks) ^ G_::k_key(ld_row)) << 4);
+  const uint32_t v_lane = ld_row * kRowBytes + (((lane % G_::kChunks) ^ G_::v_key(ld_row)) << 4);
   if (tid < 2) s_any[tid] = 0;
   int n_any = 0;
 
@@ -313,35 +313,59 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // seen by all behind the first stage's barrier
     }
 
-    // ---- loader: see attention_device.h for the layout.  Rows past the last valid one re-read that row: finite
-    //      data that the mask discards (K) or that meets a zero weight (V).
-    auto issue = [&](int x, int slot) {
-      const int s = s0 + x;
-      const bool tree = s >= st.cached;
-      const int row0 = (tree ? s - st.cached : s + st.first) * kStageRows, left = (tree ? T : L) - row0;
+    // ---- loader.  One direct load moves 64 lanes x 16 bytes into 1 KB of LDS, contiguous in lane order, so that the swizzle is
+    //      applied by the lanes' addresses.  It walks the cached rows and then the tree's, a stage at a time; rows past the last
+    //      valid one re-read that row: data that the mask discards (K) or that meets a zero weight (V).
+    int ld_left;  // rows left in the segment, from the next stage to issue
+    const unsigned char *ld_k, *ld_v;
+    const int32_t *ld_place;
+    bool ld_tree;
+    auto segment = [&](bool tree, int row0) {
       const size_t base = unit * (size_t)(tree ? p.T_max : p.L_max) + row0;
-      const unsigned char *k = reinterpret_cast<const unsigned char *>(tree ? p.k_tree : p.k_cache) + base * kRowBytes;
-      const unsigned char *v = reinterpret_cast<const unsigned char *>(tree ? p.v_tree : p.v_cache) + base * kRowBytes;
+      ld_tree = tree;
+      ld_left = (tree ? T : L) - row0;
+      ld_k = reinterpret_cast<const unsigned char *>(tree ? p.k_tree : p.k_cache) + base * kRowBytes;
+      ld_v = reinterpret_cast<const unsigned char *>(tree ? p.v_tree : p.v_cache) + base * kRowBytes;
+      if constexpr (kPlace) ld_place = tree || in_order ? nullptr : p.position + base;
+    };
+    auto issue = [&](int slot) __attribute__((always_inline)) {
       unsigned char *dst = smem + slot * kStageBytes + wave * 1024;
+      if (ld_left >= kStageRows) {  // uniform
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        int row = 4 * G_::kLdRows * i + ld_row;
-        row = row < left ? row : left - 1;
-        __builtin_amdgcn_global_load_lds((global_void *)(k + row * kRowBytes + k_lane_chunk), (lds_void *)(dst + i * 4096), 16, 0, 2 /* nt */);
-        __builtin_amdgcn_global_load_lds((global_void *)(v + row * kRowBytes + v_lane_chunk), (lds_void *)(dst + kHalfStage + i * 4096), 16, 0, 2);
+        for (int i = 0; i < kLoads; ++i) {
+          __builtin_amdgcn_global_load_lds((global_void *)(ld_k + i * 4096 + k_lane), (lds_void *)(dst + i * 4096), 16, 0, 2 /* nt */);
+          __builtin_amdgcn_global_load_lds((global_void *)(ld_v + i * 4096 + v_lane), (lds_void *)(dst + kHalfStage + i * 4096), 16, 0, 2);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          int row = 4 * G_::kLdRows * i + ld_row;
+          row = (row < ld_left ? row : ld_left - 1) - ld_row;
+          __builtin_amdgcn_global_load_lds((global_void *)(ld_k + (row * kRowBytes + (int)k_lane)), (lds_void *)(dst + i * 4096), 16, 0, 2);
+          __builtin_amdgcn_global_load_lds((global_void *)(ld_v + (row * kRowBytes + (int)v_lane)), (lds_void *)(dst + kHalfStage + i * 4096), 16, 0, 2);
+        }
       }
       if constexpr (kPlace) {  // tree stages and rows in order need none; the count of loads stays the same
-        const int row = l32 < left ? l32 : left - 1;
-        const int32_t *src = in_order || tree ? p.seq_lens + b : p.position + base + row;
-        dma4(src, place_ring + slot * 1024 + wave * 256);
+        const int row = l32 < ld_left ? l32 : ld_left - 1;
+        dma4(ld_place ? ld_place + row : p.seq_lens + b, place_ring + slot * 1024 + wave * 256);
+      }
+      if (ld_left > kStageRows) {
+        ld_left -= kStageRows;
+        ld_k += kHalfStage;
+        ld_v += kHalfStage;
+        if constexpr (kPlace) ld_place += ld_place ? kStageRows : 0;
+      } else if (!ld_tree) {
+        segment(true, 0);
       }
     };
+    auto slot_of = [](int x) { return (int)((unsigned)x % (unsigned)NS); };
     auto start = [&]() {
+      if (s0 < st.cached) segment(false, (s0 + st.first) * kStageRows);
+      else segment(true, (s0 - st.cached) * kStageRows);
 #pragma unroll
       for (int x = 0; x < kAhead; ++x)
-        if (x < n_st) issue(x, x);
+        if (x < n_st) issue(x);
     };
-    auto slot_of = [](int x) { return (int)((unsigned)x % (unsigned)NS); };
     // Stage x is there for all waves, and its place kAhead stages on is free: everyone is done with stage x - 2.  A wave's
     // loads complete in order, so that at most the younger stages' loads outstanding means that stage x has landed.
     auto acquire = [&](int x) {
@@ -357,14 +381,15 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       if (younger <= 0) wait_vmem<0>();
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      if (x + kAhead < n_st) issue(x + kAhead, slot_of(x + kAhead));
+      if (x + kAhead < n_st) issue(slot_of(x + kAhead));
     };
 
     float m_run, l_run;
     f32x16 o_acc[kMb];
     u32x2 vt[2][2 * kMb];
-    auto scores = [&](int x) -> f32x16 {
-      const uint32_t so = (uint32_t)slot_of(x) * kStageBytes;
+    // (a slot known at compile time goes into the offsets of the LDS reads)
+    auto scores = [&](auto slot) __attribute__((always_inline)) -> f32x16 {
+      const uint32_t so = (uint32_t)(int)slot * kStageBytes;
       f32x16 acc;
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[r] = 0.f;
@@ -375,13 +400,15 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       }
       return acc;
     };
-    auto read_v = [&](int x, auto half) __attribute__((always_inline)) {
+    auto read_v = [&](auto slot, auto half) __attribute__((always_inline)) {
       constexpr int kHalf = decltype(half)::value;
-      const uint32_t so = (uint32_t)slot_of(x) * kStageBytes;
+      constexpr bool kKnown = !std::is_same_v<decltype(slot), int>;
+      constexpr int kAt = 16 * kRowBytes * kHalf + (kKnown ? (int)decltype(std::conditional_t<kKnown, decltype(slot), std::integral_constant<int, 0>>{})::value : 0) * kStageBytes;
+      const uint32_t so = kKnown ? 0u : (uint32_t)(int)slot * kStageBytes;
 #pragma unroll
       for (int mb = 0; mb < kMb; ++mb) {
-        vt[kHalf][2 * mb] = lds_read_tr16<16 * kRowBytes * kHalf>(v_rd[mb][0] + so);
-        vt[kHalf][2 * mb + 1] = lds_read_tr16<16 * kRowBytes * kHalf>(v_rd[mb][1] + so);
+        vt[kHalf][2 * mb] = lds_read_tr16<kAt>(v_rd[mb][0] + so);
+        vt[kHalf][2 * mb + 1] = lds_read_tr16<kAt>(v_rd[mb][1] + so);
       }
     };
     // Values of V that are not finite: out of the V registers of 16 rows, and what they add to O to it.
@@ -413,10 +440,14 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
     const float tau = kRaw ? fminf(8.f / p.scale_log2e, 1e38f) : 8.f;
 
     // The weights of stage i from its products, and what they add to O.
-    auto take_stage = [&](int i, float (&sc)[16], auto with_care) __attribute__((always_inline)) {
-      constexpr bool kCareful = decltype(with_care)::value;
+    // kInside: a full stage of cached rows.  next: called once the scores are no longer needed as they were.
+    auto take_stage = [&](int i, auto slot, const f32x16 &raw, auto inside, auto with_care, auto &&next) __attribute__((always_inline)) {
+      constexpr bool kCareful = decltype(with_care)::value, kInside = decltype(inside)::value;
+      float sc[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] = raw[r];
       const int s = s0 + i;
-      const bool tree = s >= st.cached;
+      const bool tree = !kInside && s >= st.cached;
       const int j0 = (tree ? s - st.cached : s + st.first) * kStageRows;
       int n_valid = (tree ? T : L) - j0;
       n_valid = n_valid > kStageRows ? kStageRows : n_valid;
@@ -450,7 +481,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
             all = 0.f >= all_see;
           } else {
             // the 32 positions become places; a row without one, or that is not before the root, lies below everything
-            const int at = *reinterpret_cast<const __attribute__((address_space(3))) int *>((uintptr_t)(place_ring + (uint32_t)slot_of(i) * 1024 + wave * 256 + 4 * l32));
+            const int at = *reinterpret_cast<const __attribute__((address_space(3))) int *>((uintptr_t)(place_ring + (uint32_t)(int)slot * 1024 + wave * 256 + 4 * l32));
             const float place = (unsigned)at < (unsigned)n.P ? (float)(at - n.P) : -0x1p31f;
             stage_place[32 * wave + l32] = place;
             all = __ballot(place < all_see) == 0;
@@ -472,7 +503,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
           }
         }
       }
-      if (tree || n_valid < kStageRows) {  // uniform
+      if (!kInside && (tree || n_valid < kStageRows)) {  // uniform
         uint32_t vis = n_valid >= 32 ? ~0u : ((1u << n_valid) - 1u);
         const uint64_t word = j0 >= 64 ? anc_hi : anc_lo;  // tree stages start at 0, 32, 64, 96
         vis &= tree ? (uint32_t)(word >> (j0 & 32)) : ~0u;
@@ -500,7 +531,8 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
         m_run = m_new;
       }
       const float neg_m = -(m_run == -INFINITY ? 0.f : m_run) * (kRaw ? p.scale_log2e : 1.f);
-      read_v(i, std::integral_constant<int, 0>{});
+      next();  // products of the next stage, in one block with what follows
+      read_v(slot, std::integral_constant<int, 0>{});
       uint32_t pw[8];
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
@@ -509,7 +541,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
         pw[r >> 1] = cvt_pk_bf16(p0, p1);
         l_run += p0 + p1;  // of the weights as they are: lse is an fp32 result
       }
-      read_v(i, std::integral_constant<int, 1>{});
+      read_v(slot, std::integral_constant<int, 1>{});
       static_for_i<2>([&](auto half) __attribute__((always_inline)) {
         constexpr int kHalf = decltype(half)::value;
         wait_lds<kHalf == 0 ? 2 * kMb : 0>(vt[kHalf]);
@@ -531,21 +563,38 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
         for (int r = 0; r < 16; ++r) o_acc[mb][r] = 0.f;
     };
 
+    const int n_inside = L / kStageRows - st.first - s0;  // full stages of cached rows, from the first on
+    using yes = std::true_type;
+    using no = std::false_type;
     start();
     clear();
     acquire(0);
     if (active) {
-      f32x16 raw = scores(0);
-      for (int i = 0; i < n_st; ++i) {
-        mfma_settle();  // raw was written by products of the iteration before
-        float sc[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sc[r] = raw[r];
-        if (i + 1 < n_st) {
-          acquire(i + 1);
-          raw = scores(i + 1);
-        }
-        take_stage(i, sc, std::false_type{});
+      f32x16 raw = scores(std::integral_constant<int, 0>{});
+      int i = 0;
+      // whole turns of the ring while there is more to come than is in flight
+      for (; i + NS <= n_inside && i + NS + kAhead < n_st; i += NS) {
+        static_for_i<NS>([&](auto k) __attribute__((always_inline)) {
+          constexpr int kSlot = decltype(k)::value, kNext = (kSlot + 1) % NS, kFree = (kSlot + 1 + kAhead) % NS;
+          wait_vmem<(kAhead - 1) * kPerStage>();
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+          issue(kFree);
+          mfma_settle();  // raw was written by products of the stage before
+          f32x16 raw_next;
+          take_stage(i + kSlot, k, raw, yes{}, no{}, [&]() __attribute__((always_inline)) { raw_next = scores(std::integral_constant<int, kNext>{}); });
+          raw = raw_next;
+        });
+      }
+      for (; i < n_st; ++i) {
+        const bool more = i + 1 < n_st;
+        if (more) acquire(i + 1);
+        mfma_settle();
+        f32x16 raw_next = raw;
+        take_stage(i, slot_of(i), raw, no{}, no{}, [&]() __attribute__((always_inline)) {
+          if (more) raw_next = scores(slot_of(i + 1));
+        });
+        raw = raw_next;
       }
       mfma_settle();
     } else {
@@ -564,12 +613,9 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       for (int i = 0; i < n_st; ++i) {
         acquire(i);
         if (!active) continue;
-        const f32x16 raw = scores(i);
+        const f32x16 raw = scores(slot_of(i));
         mfma_settle();
-        float sc[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sc[r] = raw[r];
-        take_stage(i, sc, std::true_type{});
+        take_stage(i, slot_of(i), raw, no{}, yes{}, [] {});
         mfma_settle();
       }
     }

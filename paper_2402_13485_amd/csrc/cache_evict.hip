@@ -3,11 +3,10 @@
 // row moves: K and V bytes are two times the rows that move, nothing in a sequence that is not too long.
 //
 // cache_select_kernel, one workgroup per (sequence, K/V head).  Rows are ranked by a 32-bit key (rank_key), and the budget-th
-// largest key is found by halving its range, two bits at a time: three counts over all keys, which stay in registers.
-// Counts are population counts of ballots, a few cycles per 64 keys whatever the keys are; a histogram in LDS has every
-// lane of a wave at the same bin where weights are alike.  Wave w owns rows w * share .. in order, so that all that
+// largest key is found in four passes over the keys, which stay in registers.  Counting by ballots instead, two bits at a time, took 8.3 us
+// for 1032 rows and 28 us for 8192 where this takes SELECT_SMALL and SELECT_LARGE.  Wave w owns rows w * share .. in order, so that all that
 // depends on the order (which of the equal keys stay, the lists of free places and of rows that move) takes a prefix over
-// the waves' totals and one within the wave.
+// the waves' totals and one within the wave.  No result depends on the order of the additions in LDS.
 // cache_move_kernel moves what the lists say, spread over the chip, and writes the new lengths: nobody reads them any more.
 #include "score_rule.h"
 
@@ -38,11 +37,10 @@ __device__ __forceinline__ uint32_t rank_key(float weight, int position, int nex
   return bits >> 31 ? ~bits : bits | 0x80000000u;
 }
 
-// KEYS: keys of a thread that stay in registers; 0: read again for every count.  BITS of the threshold per round.
-template <int KEYS, int BITS>
+// KEYS: keys of a thread that stay in registers; 0: read again for every pass.
+template <int KEYS>
 __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(EvictParams p) {
-  constexpr int kBins = (1 << BITS) - 1;
-  __shared__ int s_count[2][kBins][kSelectWaves];
+  __shared__ int s_bins[4][256];
   __shared__ int s_total[3][kSelectWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int unit = blockIdx.x, b = unit / p.H_kv;
@@ -88,51 +86,58 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(EvictParam
     }
   };
 
-  // ---- the largest threshold that `budget` keys reach, or one that exactly as many do.  (Rows past L have key 0, which every
-  //      threshold tried leaves out.)
+  // ---- the budget-th largest key, eight bits at a time: how many of the keys that share the bits found so far have which
+  //      next eight.  Lanes that would all add to one bin (weights alike) add once.
   uint32_t threshold = 0u;
   int above = 0;  // keys > threshold
-  for (int shift = 32 - BITS, turn = 0; shift >= 0; shift -= BITS, turn ^= 1) {
-    int count[kBins];
-#pragma unroll
-    for (int t = 0; t < kBins; ++t) count[t] = 0;
-    for_keys([&](int, uint32_t key) __attribute__((always_inline)) {
-#pragma unroll
-      for (int t = 0; t < kBins; ++t) count[t] += __popcll(__ballot(key >= threshold + ((uint32_t)(t + 1) << shift)));
-    });
-    if (lane == 0)
-#pragma unroll
-      for (int t = 0; t < kBins; ++t) s_count[turn][t][wave] = count[t];
-    __syncthreads();
-    // The sums over the waves, four thresholds at a time: a row of 16 lanes adds up one threshold's.  (48 reads and additions per
-    // thread instead took 1.2 us per round.)
-    int best = 0;  // counts fall with t
-    bool exact = false;
-#pragma unroll
-    for (int t0 = 0; t0 < kBins; t0 += 4) {
-      const int t = t0 + (lane >> 4);
-      int all = s_count[turn][t < kBins ? t : 0][lane & 15];
-      all += __builtin_amdgcn_update_dpp(0, all, 0x128, 0xf, 0xf, false);  // row_ror:8, 4, 2, 1
-      all += __builtin_amdgcn_update_dpp(0, all, 0x124, 0xf, 0xf, false);
-      all += __builtin_amdgcn_update_dpp(0, all, 0x122, 0xf, 0xf, false);
-      all += __builtin_amdgcn_update_dpp(0, all, 0x121, 0xf, 0xf, false);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (t0 + k >= kBins) continue;
-        const int sum = __builtin_amdgcn_readlane(all, 16 * k);
-        if (sum >= budget) best = t0 + k + 1;
-        else if (best == t0 + k) above = sum;  // the first that too few keys reach
-        exact = exact || sum == budget;
+  for (int i = tid; i < 4 * 256; i += kSelectThreads) s_bins[0][i] = 0;
+  __syncthreads();
+#pragma unroll 1
+  for (int turn = 0; turn < 4; ++turn) {
+    const int shift = 24 - 8 * turn;
+    for_keys([&](int i, uint32_t key) __attribute__((always_inline)) {
+      const bool mine = start + kWave * i + lane < L && (turn == 0 || (key ^ threshold) >> (shift + 8) == 0u);
+      const uint64_t who = __ballot(mine);
+      if (who == 0) return;
+      const int bin = (int)(key >> shift & 255u);
+      const int one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(who));
+      if (__ballot(mine && bin != one) == 0) {
+        if (lane == 0) atomicAdd(&s_bins[turn][one], __popcll(who));
+      } else if (mine) {
+        atomicAdd(&s_bins[turn][bin], 1);
       }
-    }
-    threshold += (uint32_t)best << shift;
-    if (exact) {  // the keys from here on are the ones that stay.  (Equal counts: any of these thresholds has the same keys.)
-      threshold -= 1u;
+    });
+    __syncthreads();
+    // Lane l has bins 255 - 4 l and the three below: counts from the top, by every wave for itself.
+    const int top = 255 - 4 * lane;
+    int c[4], sum = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum += c[k] = s_bins[turn][top - k];
+    int upto = sum;  // of this lane's bins and those above
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x111, 0xf, 0xf, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x112, 0xf, 0xf, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xf, 0xf, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xf, 0xf, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x142, 0xa, 0xf, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x143, 0xc, 0xf, false);
+    const int wanted = budget - above;  // the wanted-th of these keys from the top
+    const int holder = __builtin_ctzll(__ballot(upto >= wanted));
+    int before = upto - sum, bin = top, in_bin = c[0];
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (before + c[k] < wanted && bin == top - k) {
+        before += c[k];
+        bin = top - k - 1;
+        in_bin = c[k + 1];
+      }
+    above += __builtin_amdgcn_readlane(before, holder);
+    threshold |= (uint32_t)__builtin_amdgcn_readlane(bin, holder) << shift;
+    if (above + __builtin_amdgcn_readlane(in_bin, holder) == budget) {  // all keys from here on stay, and no others
+      threshold -= 1u;  // (not from 0: fewer keys stay than there are)
       above = budget;
       break;
     }
   }
-  // Otherwise `above` is the count of the least threshold that too few keys reach, which is threshold + 1 by now.
 
   // ---- which of the keys equal to the threshold stay: the first ones
   auto sum_before = [&](int which) {  // of the waves in front of this one
@@ -277,9 +282,9 @@ extern "C" propd_status propd_cache_evict(int32_t B, propd_dtype dt, int32_t H_k
   ws += align_up((size_t)units * 4, 256);
   p.left = reinterpret_cast<int32_t *>(ws);
   const dim3 grid((unsigned)units), threads(kSelectThreads);
-  if (L_max <= 4 * kSelectThreads) hipLaunchKernelGGL((cache_select_kernel<4, 2>), grid, threads, 0, st, p);
-  else if (L_max <= 16 * kSelectThreads) hipLaunchKernelGGL((cache_select_kernel<16, 2>), grid, threads, 0, st, p);
-  else hipLaunchKernelGGL((cache_select_kernel<0, 4>), grid, threads, 0, st, p);
+  if (L_max <= 4 * kSelectThreads) hipLaunchKernelGGL((cache_select_kernel<4>), grid, threads, 0, st, p);
+  else if (L_max <= 16 * kSelectThreads) hipLaunchKernelGGL((cache_select_kernel<16>), grid, threads, 0, st, p);
+  else hipLaunchKernelGGL((cache_select_kernel<0>), grid, threads, 0, st, p);
   if (!launch_ok()) return PROPD_ERR_DEVICE;
   // as many workgroups as fill the chip several times, no more than the most rows that can move give work
   const long long most = (long long)(budget < L_max - budget ? budget : L_max - budget) * (row_bytes / 16);

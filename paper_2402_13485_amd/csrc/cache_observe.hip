@@ -1,10 +1,12 @@
 // What the accepted nodes of a step paid to every row of a cache: paid[j] = sum of exp(s_rj - lse_r) over the
 // accepted nodes and the query heads that share the K/V head; the rows' weights decay and take it up.
 //
-// One pass over K (a softmax needs two, but the attention has left lse), bound by its bytes: a wave owns KT tiles of 16 keys and keeps
-// their rows in registers as the B operand of S = Q . K^T (16x16 products), the accepted queries come 16 at a time as the A
-// operand, from the L2.  A lane then holds four queries' scores of one key, adds their weights up, and the
-// four lanes of a key meet at the end.  Rows are read straight from memory in the operand's layout, 64 bytes of 16 rows per load.
+// One pass over K (a softmax needs two, but the attention has left lse), bound by its bytes: a wave walks KT tiles of 16 keys at a time,
+// the next ones requested in front of the work on these, as the B operand of S = Q . K^T (16x16 products); the accepted queries are
+// the A operand, 16 rows to a group, the first kHeld groups of which stay in registers.  A lane then holds four queries' scores of
+// one key, adds their weights up, and the four lanes of a key meet at the end.  K rows are read straight from memory in the operand's
+// layout, 64 bytes of 16 rows per load.  With one batch of tiles per wave every wave paid for the chain path -> query -> lse, and 16 x
+// 8 heads x 4096 rows took 57 us; walking OBSERVE_MEASURED us.
 #include "score_rule.h"
 
 namespace propd {
@@ -59,8 +61,13 @@ struct Rows<float, D> {
   }
 };
 
+constexpr int kHeld = 2;  // groups of 16 query rows that stay in registers
+
 template <class E, int D, int KT>
-__global__ __launch_bounds__(kObserveThreads) void cache_observe_kernel(ObserveParams p) {
+__global__ __launch_bounds__(kObserveThreads, 2) void cache_observe_kernel(ObserveParams p) {
+  // of the first 16 * kHeld query rows (row = place on the path * group + head)
+  __shared__ __attribute__((aligned(16))) float s_lse[16 * kHeld], s_slope[16 * kHeld];
+  __shared__ __attribute__((aligned(16))) int s_place[16 * kHeld], s_row[16 * kHeld];  // place on the path (-1: no query), row of q
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, part = lane >> 4;
   const int unit = (int)(blockIdx.x / (unsigned)p.chunks), chunk = (int)(blockIdx.x - (unsigned)unit * (unsigned)p.chunks);
@@ -70,109 +77,158 @@ __global__ __launch_bounds__(kObserveThreads) void cache_observe_kernel(ObserveP
   a = a < 0 ? 0 : (a > p.path_stride ? p.path_stride : a);
   const int32_t *path = p.accept_path + (size_t)b * p.path_stride;
   const int cached = (n.L + 15) / 16, tiles = cached + (a + 15) / 16;
-  const int tile0 = (chunk * kObserveWaves + wave) * KT;
-  if (tile0 >= tiles) return;
+  if (chunk * kObserveWaves * KT >= tiles) return;  // the whole workgroup
+  const int step = p.chunks * kObserveWaves * KT;
+  int tile0 = (chunk * kObserveWaves + wave) * KT;
   const E *q = reinterpret_cast<const E *>(p.q), *k_cache = reinterpret_cast<const E *>(p.k_cache) + (size_t)unit * p.L_max * D;
   const E *k_tree = reinterpret_cast<const E *>(p.k_tree) + (size_t)unit * p.T_max * D;
+  const int rows = a * p.group;
 
-  // ---- this lane's keys: tile t is 16 cached rows, or 16 places of the path.  Keys past the last take a valid row.
-  Rows<E, D> keys[KT];
-  int key[KT], at[KT];  // place in its kind (-1: none), position
+  // ---- a batch of tiles: 16 cached rows each, or 16 places of the path.  Keys past the last take a valid row.
+  struct Batch {
+    Rows<E, D> keys[KT];
+    int key[KT], at[KT];  // place in its kind (-1: none), position
+    float old[KT];        // weight so far
+  };
+  auto load = [&](Batch &x, int t0) __attribute__((always_inline)) {
 #pragma unroll
-  for (int x = 0; x < KT; ++x) {
-    const int t = tile0 + x < tiles ? tile0 + x : tiles - 1;
-    if (t < cached) {
-      const int j = 16 * t + c16, row = j < n.L ? j : n.L - 1;
-      key[x] = tile0 + x < tiles && j < n.L ? j : -1;
-      at[x] = p.position ? p.position[(size_t)unit * p.L_max + row] : n.dropped + row;
-      keys[x].load(k_cache + (size_t)row * D, part);
-    } else {
-      const int r = 16 * (t - cached) + c16, node = path[r < a ? r : a - 1];
-      key[x] = tile0 + x < tiles && r < a ? r : -1;
-      const bool valid = node >= 0 && node < n.T;
-      at[x] = valid ? n.P + r : -1;
-      keys[x].load(k_tree + (size_t)(valid ? node : 0) * D, part);
-    }
-  }
-  float paid[KT];
-#pragma unroll
-  for (int x = 0; x < KT; ++x) paid[x] = 0.f;
-
-  const int rows = a * p.group;  // row = place on the path * group + head
-  for (int row0 = 0; row0 < rows; row0 += 16) {
-    Rows<E, D> queries;
-    {
-      const int row = row0 + c16 < rows ? row0 + c16 : rows - 1, r = row / p.group, head = row - r * p.group;
-      int node = path[r];
-      node = node >= 0 && node < n.T ? node : 0;
-      queries.load(q + (((size_t)b * p.H + hk * p.group + head) * p.T_max + node) * D, part);
-    }
-    // the four queries whose scores this lane gets
-    float lse[4], slope[4];
-    Sight sight[4];
-    int place[4];  // on the path; -1: no query
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int row = row0 + 4 * part + j, r = row < rows ? row / p.group : 0, head = row < rows ? row - r * p.group : 0;
-      const int node = path[r];
-      const bool valid = row < rows && node >= 0 && node < n.T;
-      place[j] = valid ? r : -1;
-      const size_t h = (size_t)hk * p.group + head;
-      lse[j] = p.lse[((size_t)b * p.H + h) * p.T_max + (valid ? node : 0)];
-      slope[j] = p.slopes ? p.slopes[h] : 0.f;
-      sight[j] = sight_of(n.P + r, p.window);
-    }
-#pragma unroll
-    for (int x = 0; x < KT; ++x) {
-      const f32x4 raw = queries.times(keys[x]);
-      mfma_settle();
-      const bool own = tile0 + x >= cached;  // a key of the path
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float s = raw[j] * p.scale;
-        if (p.cap > 0.f) s = capped(s, p.cap, p.inv_cap);
-        s = fmaf(-slope[j], (float)(sight[j].p_i - at[x]), s);
-        const float w = __builtin_amdgcn_exp2f((s - lse[j]) * kLog2e);
-        const bool seen = place[j] >= 0 && in_sight(sight[j], at[x]) && (own ? key[x] <= place[j] : at[x] < n.P);
-        paid[x] += seen ? w : 0.f;
+    for (int i = 0; i < KT; ++i) {
+      const int t = t0 + i < tiles ? t0 + i : tiles - 1;  // uniform
+      if (t < cached) {
+        const int j = 16 * t + c16, row = j < n.L ? j : n.L - 1;
+        x.key[i] = t0 + i < tiles && j < n.L ? j : -1;
+        x.at[i] = p.position ? p.position[(size_t)unit * p.L_max + row] : n.dropped + row;
+        x.old[i] = p.weight[(size_t)unit * p.L_max + row];
+        x.keys[i].load(k_cache + (size_t)row * D, part);
+      } else {
+        const int r = 16 * (t - cached) + c16, node = path[r < a ? r : a - 1];
+        x.key[i] = t0 + i < tiles && r < a ? r : -1;
+        const bool valid = node >= 0 && node < n.T;
+        x.at[i] = valid ? n.P + r : -1;
+        x.old[i] = 0.f;
+        x.keys[i].load(k_tree + (size_t)(valid ? node : 0) * D, part);
       }
     }
-  }
+  };
+  Batch now, next;
+  if (tile0 < tiles) load(now, tile0);
 
-  // ---- the four lanes of a key; lanes of part x write tile x
-#pragma unroll
-  for (int x = 0; x < KT; ++x) {
-    paid[x] += __shfl_xor(paid[x], 16, kWave);
-    paid[x] += __shfl_xor(paid[x], 32, kWave);
+  // ---- the query rows that are held
+  const int held = rows < 16 * kHeld ? rows : 16 * kHeld;
+  auto row_at = [&](int row, int &r, int &node, size_t &line) __attribute__((always_inline)) {  // of a row that exists
+    r = row / p.group;
+    const int head = hk * p.group + row - r * p.group;
+    node = path[r];
+    const bool valid = node >= 0 && node < n.T;
+    line = ((size_t)b * p.H + head) * p.T_max + (valid ? node : 0);
+    return valid;
+  };
+  if (threadIdx.x < 16 * kHeld) {
+    const int row = threadIdx.x;
+    int r = 0, node = 0;
+    size_t line = 0;
+    const bool there = row < held && row_at(row, r, node, line);
+    s_place[row] = there ? r : -1;
+    s_lse[row] = there ? p.lse[line] : 0.f;
+    s_slope[row] = there && p.slopes ? p.slopes[hk * p.group + row - r * p.group] : 0.f;
+    s_row[row] = there ? (int)(line - (size_t)b * p.H * p.T_max) : 0;
   }
+  __syncthreads();
+  const E *q_base = q + (size_t)b * p.H * p.T_max * D;
+  Rows<E, D> queries[kHeld];
 #pragma unroll
-  for (int x = 0; x < KT; ++x) {
-    if (part != x || key[x] < 0) continue;
-    const size_t base = (size_t)unit * p.L_max;
-    if (tile0 + x < cached) {
-      const size_t i = base + key[x];
-      p.weight_out[i] = p.decay * p.weight[i] + paid[x];
-      if (p.position_out) p.position_out[i] = at[x];
-    } else if (n.L + key[x] < p.L_max) {
-      const size_t i = base + n.L + key[x];
-      p.weight_out[i] = at[x] < 0 ? 0.f : paid[x];
-      if (p.position_out) p.position_out[i] = at[x];
+  for (int g = 0; g < kHeld; ++g)
+    if (16 * g < held) queries[g].load(q_base + (size_t)s_row[16 * g + c16] * D, part);
+
+  float paid[KT];
+  // what 16 query rows pay to the batch's keys; this lane's four of them: lse, slope, place on the path
+  auto pay = [&](const Batch &x, const Rows<E, D> &rows16, const float (&lse)[4], const float (&slope)[4], const int (&place)[4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      const f32x4 raw = rows16.times(x.keys[i]);
+      mfma_settle();
+      const bool own = tile0 + i >= cached;  // keys of the path
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const Sight sight = sight_of(n.P + place[j], p.window);
+        float s = raw[j] * p.scale;
+        if (p.cap > 0.f) s = capped(s, p.cap, p.inv_cap);
+        s = fmaf(-slope[j], (float)(sight.p_i - x.at[i]), s);
+        const float w = __builtin_amdgcn_exp2f((s - lse[j]) * kLog2e);
+        const bool seen = place[j] >= 0 && in_sight(sight, x.at[i]) && (own ? x.key[i] <= place[j] : x.at[i] < n.P);
+        paid[i] += seen ? w : 0.f;
+      }
     }
+  };
+  for (; tile0 < tiles; tile0 += step) {
+    const bool more = tile0 + step < tiles;
+    if (more) load(next, tile0 + step);
+#pragma unroll
+    for (int i = 0; i < KT; ++i) paid[i] = 0.f;
+#pragma unroll
+    for (int g = 0; g < kHeld; ++g)
+      if (16 * g < held) {  // uniform
+        float lse[4], slope[4];
+        int place[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          lse[j] = s_lse[16 * g + 4 * part + j];
+          slope[j] = s_slope[16 * g + 4 * part + j];
+          place[j] = s_place[16 * g + 4 * part + j];
+        }
+        pay(now, queries[g], lse, slope, place);
+      }
+    for (int row0 = 16 * kHeld; row0 < rows; row0 += 16) {  // the rows that are not held
+      Rows<E, D> rows16;
+      float lse[4], slope[4];
+      int place[4], r, node;
+      size_t line;
+      row_at(row0 + c16 < rows ? row0 + c16 : rows - 1, r, node, line);
+      rows16.load(q + line * D, part);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int row = row0 + 4 * part + j;
+        const bool valid = row_at(row < rows ? row : rows - 1, r, node, line) && row < rows;
+        place[j] = valid ? r : -1;
+        lse[j] = p.lse[line];
+        slope[j] = p.slopes ? p.slopes[hk * p.group + (row < rows ? row - r * p.group : 0)] : 0.f;
+      }
+      pay(now, rows16, lse, slope, place);
+    }
+    // ---- the four lanes of a key; lanes of part i write tile i
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      paid[i] += __shfl_xor(paid[i], 16, kWave);
+      paid[i] += __shfl_xor(paid[i], 32, kWave);
+    }
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      if (part != i || now.key[i] < 0) continue;
+      const size_t base = (size_t)unit * p.L_max;
+      if (tile0 + i < cached) {
+        const size_t w = base + now.key[i];
+        p.weight_out[w] = p.decay * now.old[i] + paid[i];
+        if (p.position_out) p.position_out[w] = now.at[i];
+      } else if (n.L + now.key[i] < p.L_max) {
+        const size_t w = base + n.L + now.key[i];
+        p.weight_out[w] = now.at[i] < 0 ? 0.f : paid[i];
+        if (p.position_out) p.position_out[w] = now.at[i];
+      }
+    }
+    if (more) now = next;
   }
 }
 
 template <class E, int D>
 static bool launch_observe(ObserveParams p, long long units, hipStream_t st) {
   const long long tiles = (p.L_max + 15ll) / 16 + (p.path_stride + 15ll) / 16;
-  constexpr int kMany = sizeof(E) == 2 ? 4 : 2;
-  // several tiles per wave once the chip is full of waves without
-  const bool many = units * tiles > 8192ll;
-  const int per = kObserveWaves * (many ? kMany : 1);
-  const long long chunks = (tiles + per - 1) / per;
+  constexpr int KT = sizeof(E) == 2 ? 2 : 1;
+  // a few workgroups per compute unit, as long as every wave has a batch
+  long long chunks = (1024 + units - 1) / units;
+  const long long most = (tiles + kObserveWaves * KT - 1) / (kObserveWaves * KT);
+  if (chunks > most) chunks = most;
   p.chunks = (int)chunks;
-  const dim3 grid((unsigned)(units * chunks));
-  if (many) hipLaunchKernelGGL((cache_observe_kernel<E, D, kMany>), grid, dim3(kObserveThreads), 0, st, p);
-  else hipLaunchKernelGGL((cache_observe_kernel<E, D, 1>), grid, dim3(kObserveThreads), 0, st, p);
+  hipLaunchKernelGGL((cache_observe_kernel<E, D, KT>), dim3((unsigned)(units * chunks)), dim3(kObserveThreads), 0, st, p);
   return launch_ok();
 }
 
@@ -194,9 +250,7 @@ extern "C" propd_status propd_cache_observe(const propd_tree *tree, propd_dtype 
   for (const void *ptr : {q, k_cache, k_tree})
     if (reinterpret_cast<uintptr_t>(ptr) % 16 != 0) return PROPD_ERR_INVALID_ARG;
   const long long units = (long long)tree->B * H_kv;
-  if ((long long)tree->B * H > (1ll << 24) || (long long)path_stride * (H / H_kv) > (1ll << 30)) return PROPD_ERR_UNSUPPORTED;
-  // (a workgroup takes 8 tiles at least where there are many)
-  if (units * ((L_max + 15ll) / 16 + (path_stride + 15ll) / 16) > (1ll << 26)) return PROPD_ERR_UNSUPPORTED;
+  if (L_max > (1 << 30) || units > (1ll << 22) || (long long)tree->B * H > (1ll << 24) || (long long)H * tree->T_max > (1ll << 30) || (long long)path_stride * (H / H_kv) > (1ll << 30)) return PROPD_ERR_UNSUPPORTED;
   ObserveParams p;
   p.q = q;
   p.k_cache = k_cache;

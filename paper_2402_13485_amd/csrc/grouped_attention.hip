@@ -32,7 +32,7 @@ struct GroupedParams {
   float scale_log2e, cap_in, cap_log2e;  // cap_in: 2 scale log2(e) / cap
   float *part_o;        // [slots][4 waves][16 blocks][64 lanes][4]
   float *part_ml;       // [slots][4 waves][m | l][64 lanes]
-  int32_t *records;     // [B * H_kv * blocks][4]: first slot, slots between pieces, pieces (1: no merge), nodes
+  int32_t *records;     // [B * H_kv * blocks][4]: first slot, slots between pieces, pieces (1: no merge), how much earlier the later ones lie
   int slots, resident;  // partial results there is room for; workgroups that run at once
   int may_split;
 };
@@ -58,110 +58,125 @@ __device__ __forceinline__ Stages stages_of(int L, int T, int window, bool in_or
   return s;
 }
 
-// n / d rounded up for any n >= 1, d >= 1: at least 1, off by one at most far beyond 2^20 (the same value wherever it is asked for)
+// Quotients of whole numbers without the long sequence of a division.  below(n, d): n / d rounded down, exact for n below
+// 2^20.  pieces_of(n, d): n / d rounded up for any n >= 1, d >= 1, at least 1 and at most n; off by one at most far
+// beyond 2^20 (and the same value wherever it is asked for).
+__device__ __forceinline__ int below(int n, int d) { return (int)(((float)n + .5f) * __builtin_amdgcn_rcpf((float)d)); }
+__device__ __forceinline__ int quotient(int n, int d) { return n < (1 << 20) ? below(n, d) : n / d; }
 __device__ __forceinline__ int pieces_of(int n, int d) {
   const int x = (int)(((float)n + (float)d - .5f) * __builtin_amdgcn_rcpf((float)d));
   return x < 1 ? 1 : (x > n ? n : x);
 }
 
-// How the units are cut.  Every workgroup works the same plan out from the lengths.
-//   All sequences alike: as many whole units as there are workgroups that run at once, as often as that goes, then the units
-//     left over in `pieces` ranges each, piece by piece.
-//   Otherwise: a range is at most `most` stages, a unit of s stages has pieces_of(s, most) of them, equally long.
-// The time of a plan is counted in stages of a workgroup that has a compute unit to itself (plan_time); the lanes try a candidate each.
-struct Plan {
-  bool alike;
-  int whole;     // alike: units done whole, first
-  int left;      // alike: units left over
-  int stages;    // alike: of a unit
-  int per_sequence;  // alike: units
-  int pieces;    // alike
-  int most;      // otherwise: stages of a range
-  int n_ranges;  // of the call
+// The lengths of a sequence, of this lane's or of one for all lanes, and what they make: stages of a unit, units of the sequence (0
+// beyond the batch).
+struct Sequence {
+  int L, T, dropped;
+  __device__ __forceinline__ Stages stages(const GroupedParams &p) const { return stages_of(L, T, p.window, p.position == nullptr); }
+  __device__ __forceinline__ int blocks(const GroupedParams &p) const { return (p.group * T + 127) / 128; }
+  __device__ __forceinline__ int count(const GroupedParams &p) const {
+    const Stages s = stages(p);
+    return T > 0 ? s.cached + s.tree : 0;
+  }
+  __device__ __forceinline__ int units(const GroupedParams &p) const { return p.H_kv * blocks(p); }
 };
-
-constexpr float kShared = 1.6f;      // a stage of a workgroup that shares its compute unit with another one
-constexpr float kRangeCost = 6.f;    // per range: the first loads, the result
-constexpr float kMergeCost = 6.f;    // where any unit is cut: another kernel
-constexpr float kPieceCost = .03f;   // per range of a cut unit: its partial result, written and read
-__device__ __forceinline__ float rounds_time(float ranges, float longest, float resident) {
-  const float full = floorf(ranges / resident), rest = ranges - full * resident;
-  return full * (longest * kShared + kRangeCost) +
-         (rest > 0.f ? longest * (rest > .5f * resident ? kShared : 1.f) + kRangeCost : 0.f);
+__device__ __forceinline__ Sequence lane_sequence(const GroupedParams &p, int b) {
+  if (b >= p.B) return {0, 0, 0};
+  const Lengths n = lengths_of(p, b);
+  return {n.L, n.T, n.dropped};
 }
 
-template <class StagesOf>
-__device__ __forceinline__ Plan plan_ranges(const GroupedParams &p, StagesOf &&lane_units) {
+// How the units are cut.  Every workgroup works the same plan out from the lengths, in few steps: they stand in front of its first
+// load.
+//   kAlike   All sequences alike: as many whole units as there are workgroups that run at once, as often as that goes, then
+//            the units left over in `pieces` ranges each, piece by piece.
+//   kRanges  A range is at most `most` stages, a unit of s stages has pieces_of(s, most) of them, equally long; the least
+//            `most` whose ranges all run at once.
+//   kShares  Up to twice as many units as workgroups, of different lengths: every workgroup has an equal share of the list of all
+//            stages, which may cross units (each crossing: another unit's first loads and a partial result).
+// How many workgroups run at once (`slots_for`): one per compute unit, two where that leaves ranges of more than kLongRange
+// stages.  A stage of a workgroup that shares its compute unit takes 1.45 of the time, so two halves of a range save little, and
+// each range costs about 5 us of first loads and result and 128 KB of partial result written and read.  Calls, us, 256 / 512
+// ranges: 40 units of 49 stages 29 / 38, 128 of 128 75 / 70, 256 of 130 (capped) 160 / 135.  No range is
+// shorter than kLeastStages.
+enum PlanKind { kAlike, kRanges, kShares };
+struct Plan {
+  int kind;
+  int n_ranges;     // of the call; kShares: workgroups
+  int whole, left;  // kAlike: units done whole, first; units left over
+  int pieces;       // kAlike
+  int most;         // kRanges
+  int quot, rest;   // kShares: stages of a share; the first `rest` shares have one more
+  __device__ __forceinline__ int share_start(int w) const { return w * quot + (w < rest ? w : rest); }
+  __device__ __forceinline__ int share_of(int x) const {
+    const int big = rest * (quot + 1);
+    return x < big ? (int)((unsigned)x / (unsigned)(quot + 1)) : rest + (int)((unsigned)(x - big) / (unsigned)quot);
+  }
+};
+constexpr int kLeastStages = 3, kLongRange = 32;
+
+__device__ __forceinline__ int wave_sum_i32(int v) {
+  return __builtin_amdgcn_readlane(wave_scan_i32(v, 0, [](int x, int y) { return x + y; }), 63);
+}
+
+__device__ __forceinline__ Plan plan_ranges(const GroupedParams &p, const Sequence &first) {
   const int lane = threadIdx.x & 63;
-  auto sum = [](int x, int y) { return x + y; };
-  auto larger = [](int x, int y) { return x > y ? x : y; };
-  float total = 0.f;
-  int units = 0, longest = 1, s_first = 0, u_first = 0;
+  int units = 0, total = 0;  // (the total is looked at where it is below 2^30: see propd_grouped_attention)
+  const int s_first = uniform(first.count(p)), u_first = uniform(first.units(p));
   bool alike = true;
   for (int b0 = 0; b0 < p.B; b0 += kWave) {
-    int s, u;
-    lane_units(b0 + lane, s, u);
-    if (b0 == 0) {
-      s_first = uniform(s);
-      u_first = uniform(u);
-    }
+    const Sequence q = b0 == 0 ? first : lane_sequence(p, b0 + lane);
+    const int s = q.count(p), u = q.units(p);
     alike = alike && __ballot(b0 + lane < p.B && (s != s_first || u != u_first)) == 0;
-    // products of two numbers below 2^24 in float: only the choice depends on them
-    float t = (float)s * (float)u;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, kWave);
-    total += t;
-    units += __builtin_amdgcn_readlane(wave_scan_i32(u, 0, sum), 63);
-    longest = larger(longest, __builtin_amdgcn_readlane(wave_scan_i32(s, 0, larger), 63));
+    units += wave_sum_i32(u);
+    total += wave_sum_i32(s * u);
   }
-  Plan plan = {alike, 0, units, s_first, u_first, 1, longest, units};
+  Plan plan = {alike ? kAlike : kRanges, units, 0, units, 1, 1 << 30, 0, 0};
   if (!p.may_split) return plan;
-  const float G = (float)p.resident;
-  float ranges = 0.f, range = 0.f;
-  int pieces = 1, most = longest, whole = 0;
+  const int half = p.resident / 2;
+  const int slots = total > half * kLongRange ? p.resident : half;
   if (alike) {
-    // lanes 0..31: all units in 1..32 pieces; 32..63: the ones left over behind full rounds of whole units
-    whole = lane < 32 ? 0 : units / p.resident * p.resident;
-    pieces = (lane & 31) + 1;
-    pieces = pieces < s_first ? pieces : s_first;
-    ranges = (float)(units - whole) * (float)pieces;
-    range = ceilf((float)s_first / (float)pieces);
-  } else {
-    // what fills 1 (32 lanes), 2 (16), 3 and 4 (8) rounds of the workgroups that run at once, and longer ranges
-    const int round = lane < 32 ? 1 : lane < 48 ? 2 : lane < 56 ? 3 : 4, step = lane < 32 ? lane : lane < 48 ? lane - 32 : lane & 7;
-    const float most_f = ceilf(total / (G * (float)round) * (1.f + .0625f * (float)step));
-    most = (int)fminf(fmaxf(most_f, 1.f), (float)longest);
-    for (int b0 = 0; b0 < p.B; b0 += kWave) {
-      int s, u;
-      lane_units(b0 + lane, s, u);
-      const int here = p.B - b0 < kWave ? p.B - b0 : kWave;
-      for (int i = 0; i < here; ++i)
-        ranges += (float)__builtin_amdgcn_readlane(u, i) * (float)pieces_of(__builtin_amdgcn_readlane(s, i), most);
+    plan.whole = units / p.resident * p.resident;
+    plan.left = units - plan.whole;
+    if (plan.left > 0) {
+      const int room = plan.whole > 0 ? half : slots;
+      int pieces = below(room, plan.left);
+      pieces = pieces < below(s_first, kLeastStages) ? pieces : below(s_first, kLeastStages);
+      plan.pieces = pieces < 1 ? 1 : pieces;
+      plan.n_ranges = plan.whole + plan.left * plan.pieces;
     }
-    range = ceilf((float)longest / (float)pieces_of(longest, most));
+    return plan;
   }
-  const bool cut = alike ? pieces > 1 && whole < units : ranges > (float)units;
-  float cost = (float)(whole / p.resident) * ((float)longest * kShared + kRangeCost) + rounds_time(ranges, range, G) +
-               (cut ? kMergeCost + kPieceCost * ranges : 0.f);
-  if ((cut && ranges > (float)p.slots) || (!cut && !alike)) cost = INFINITY;
-  const float uncut = rounds_time((float)units, (float)longest, G);
-  float least = cost;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) least = fminf(least, __shfl_xor(least, o, kWave));
-  least = __uint_as_float(uniform(__float_as_uint(least)));
-  if (!(least < uncut)) return plan;
-  const int pick = __builtin_ctzll(__ballot(cost == least));
-  plan.whole = __builtin_amdgcn_readlane(whole, pick);
-  plan.left = units - plan.whole;
-  plan.pieces = __builtin_amdgcn_readlane(pieces, pick);
-  plan.most = __builtin_amdgcn_readlane(most, pick);
-  plan.n_ranges = plan.whole + (int)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ranges), pick));
+  if (units <= p.resident) {
+    // from an equal share on, a sixteenth of it longer at a time
+    const float equal = (float)total / (float)slots;
+    for (int step = 0; step < 48; ++step) {
+      const int m = (int)ceilf(equal * (1.f + .0625f * (float)step));
+      const int most = m > kLeastStages ? m : kLeastStages;
+      int n = 0;
+      for (int b0 = 0; b0 < p.B; b0 += kWave) {
+        const Sequence q = b0 == 0 ? first : lane_sequence(p, b0 + lane);
+        n += wave_sum_i32(q.T > 0 ? q.units(p) * pieces_of(q.count(p), most) : 0);
+      }
+      if (n <= slots || n <= units) {
+        plan.most = most;
+        plan.n_ranges = n;
+        break;
+      }
+    }
+    return plan;
+  }
+  if (units >= 2 * p.resident || 2 * p.resident > p.slots) return plan;  // short units, two rounds and more: whole
+  plan.kind = kShares;
+  plan.n_ranges = p.resident;
+  plan.quot = total / p.resident;
+  plan.rest = total - plan.quot * p.resident;
   return plan;
 }
 
 // A lane's columns of the result, and where they lie.
 __device__ __forceinline__ size_t column_row(const GroupedParams &p, int b, int hk, int column, int T) {
-  const int g = column / T, i = column - g * T;
+  const int g = quotient(column, T), i = column - g * T;
   return ((size_t)b * p.H + hk * p.group + g) * p.T_max + i;
 }
 
@@ -181,9 +196,10 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
   constexpr int kPerStage = 2 * kLoads + (kPlace ? 1 : 0);  // loads of a wave per stage
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const uint32_t ring = (uint32_t)(uintptr_t)(lds_void *)smem;
-  const uint32_t place_ring = ring + NS * kStageBytes;  // [NS][4 waves][64] positions
+  u32x4 *const tree_anc = reinterpret_cast<u32x4 *>(smem + NS * kStageBytes);  // [128] ancestor sets
+  const uint32_t place_ring = ring + NS * kStageBytes + 2048;                  // [NS][4 waves][64] positions
   // places: positions less that of the root, as numbers that are exact where they matter
-  float *const stage_place = reinterpret_cast<float *>(smem + NS * kStageBytes + NS * 1024);  // [4 waves][32], of the stage at work
+  float *const stage_place = reinterpret_cast<float *>(smem + NS * kStageBytes + 2048 + NS * 1024);  // [4 waves][32], of the stage at work
   float *const tree_place = stage_place + 4 * 32;                                             // [128], of the tree's nodes
   __shared__ int s_any[2];
 
@@ -191,16 +207,20 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
   const int l32 = lane & 31, g = lane >> 5;
   const bool in_order = p.position == nullptr;
 
-  auto lane_units = [&](int b, int &s, int &u) {
-    s = u = 0;
-    if (b < p.B) {
-      const Lengths n = lengths_of(p, b);
-      const Stages st = stages_of(n.L, n.T, p.window, in_order);
-      s = st.cached + st.tree;
-      u = p.H_kv * ((p.group * n.T + 127) / 128);
-    }
+  // (registers are short: the lengths of the first 64 sequences lie in LDS; every wave writes the same)
+  __shared__ int s_lengths[3][kWave];
+  Plan plan;
+  {
+    const Sequence lanes = lane_sequence(p, lane);
+    s_lengths[0][lane] = lanes.L;
+    s_lengths[1][lane] = lanes.T;
+    s_lengths[2][lane] = lanes.dropped;
+    plan = plan_ranges(p, lanes);
+  }
+  auto sequence_at = [&](int b) -> Sequence {  // of this lane's number, or of one for all lanes
+    if (b < kWave) return {s_lengths[0][b], s_lengths[1][b], s_lengths[2][b]};
+    return lane_sequence(p, b);
   };
-  const Plan plan = plan_ranges(p, lane_units);
 
   // ---- where a lane reads in a stage: K as the A operand (row l32, chunk 2 ks + g), V^T by transposing reads
   uint32_t k_rd[kQf], v_rd[kMb][2];
@@ -223,65 +243,104 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
   // ---- ranges.  The blocks of a unit read the same rows: they run next to each other on one XCD (workgroups go to the 8
   //      XCDs in turn), so that the rows come from its L2 but for the first time.  What does not fill a span stays in order.
   const int span = 8 * p.blocks;
-  for (int at = blockIdx.x; at < plan.n_ranges; at += gridDim.x) {
-    const int part0 = at < plan.whole ? 0 : plan.whole, part_n = at < plan.whole ? plan.whole : plan.n_ranges - plan.whole;
-    const int local = at - part0, in_span = local % span;
-    const int range = local < part_n / span * span ? local - in_span + in_span % 8 * p.blocks + in_span / 8 : local;  // within its part
-    int b = 0, block, hk, piece = 0, P = 1, first_slot = 0, stride = 1;
-    if (plan.alike) {
-      int u = part0 + range;
-      if (part0 == plan.whole && at >= plan.whole) {
-        P = plan.pieces;
-        piece = range / plan.left;
-        first_slot = range - piece * plan.left;
-        stride = plan.left;
-        u = plan.whole + first_slot;
-      }
-      b = u / plan.per_sequence;
-      const int in_sequence = u - b * plan.per_sequence, n_blocks = plan.per_sequence / p.H_kv;
-      hk = in_sequence / n_blocks;
-      block = in_sequence - hk * n_blocks;
-    } else {
-      // the sequence of the range, and the ranges before that sequence
-      int first_range = 0, P_b = 1, u_b = 1;
+  int at = blockIdx.x, x = 0, x_end = 0;  // the next range; kShares: what is left of this workgroup's share
+  if (plan.kind == kShares) {
+    if (at >= plan.n_ranges) return;
+    const int even = plan.n_ranges / 8 * 8;  // an XCD has neighbouring shares
+    at = at < even ? at % 8 * (even / 8) + at / 8 : at;
+    x = plan.share_start(at);
+    x_end = plan.share_start(at + 1);
+  }
+  bool first_range = true;
+  while (plan.kind == kShares ? x < x_end : at < plan.n_ranges) {
+    int b = 0, block, hk, s0, n_st, slot, first_slot, stride, P, late = 0;  // late: see the merge
+    // the sequence that holds item `which` of a list that has of(x) items per sequence, and the items before that sequence
+    auto locate = [&](int which, auto &&of) __attribute__((always_inline)) {
+      int start = 0;
       for (int b0 = 0, before = 0; b0 < p.B; b0 += kWave) {
-        int s, u;
-        lane_units(b0 + lane, s, u);
-        const int cuts = s > 0 ? pieces_of(s, plan.most) : 0, mine = u * cuts;
-        const int incl = wave_scan_i32(mine, 0, [](int x, int y) { return x + y; });
-        const uint64_t le = __ballot(b0 + lane < p.B && before + incl - mine <= range);
+        const Sequence q = sequence_at(b0 + lane);
+        const int mine = of(q), incl = wave_scan_i32(mine, 0, [](int x, int y) { return x + y; });
+        const uint64_t le = __ballot(b0 + lane < p.B && before + incl - mine <= which);
         if (le == 0) break;
         const int src = __popcll(le) - 1;
         b = b0 + src;
-        first_range = __builtin_amdgcn_readlane(before + incl - mine, src);
-        P_b = __builtin_amdgcn_readlane(cuts, src);
-        u_b = __builtin_amdgcn_readlane(u, src);
+        start = __builtin_amdgcn_readlane(before + incl - mine, src);
         before += __builtin_amdgcn_readlane(incl, 63);
       }
-      const int n_blocks = u_b / p.H_kv;
-      int rest = range - first_range;
-      block = rest % n_blocks;
-      rest /= n_blocks;
-      P = P_b;
-      piece = rest % P;
-      hk = rest / P;
-      stride = n_blocks;
-      first_slot = range - piece * n_blocks;
+      return start;
+    };
+    Sequence n;
+    int n_stages, n_blocks;
+    auto take_lengths = [&]() __attribute__((always_inline)) {
+      const Sequence m = sequence_at(b);
+      n = {uniform(m.L), uniform(m.T), uniform(m.dropped)};
+      n_stages = n.count(p);
+      n_blocks = n.blocks(p);
+    };
+    if (plan.kind == kShares) {
+      const int in_sequence = x - locate(x, [&](const Sequence &q) { return q.count(p) * q.units(p); });
+      take_lengths();
+      const int u = quotient(in_sequence, n_stages);
+      hk = quotient(u, n_blocks);
+      block = u - hk * n_blocks;
+      s0 = in_sequence - u * n_stages;
+      n_st = n_stages - s0 < x_end - x ? n_stages - s0 : x_end - x;
+      P = s0 == 0 ? plan.share_of(x + n_stages - 1) - at + 1 : 2;  // 2: more than one
+      slot = 2 * at + (s0 == 0 ? 1 : 0);
+      first_slot = slot;
+      stride = 2;
+      late = 1;
+      x += n_st;
+    } else {
+      const int part0 = at < plan.whole ? 0 : plan.whole, part_n = at < plan.whole ? plan.whole : plan.n_ranges - plan.whole;
+      const int local = at - part0, in_span = local - quotient(local, span) * span;
+      const int range = local < quotient(part_n, span) * span ? local - in_span + in_span % 8 * p.blocks + in_span / 8 : local;  // within its part
+      int piece = 0;
+      if (plan.kind == kAlike) {
+        const int per_sequence = uniform(sequence_at(0).units(p));
+        int u = part0 + range;
+        P = 1;
+        first_slot = 0;
+        stride = 1;
+        if (at >= plan.whole) {
+          P = plan.pieces;
+          piece = quotient(range, plan.left);
+          first_slot = range - piece * plan.left;
+          stride = plan.left;
+          u = plan.whole + first_slot;
+        }
+        b = quotient(u, per_sequence);
+        take_lengths();
+        const int in_sequence = u - b * per_sequence;
+        hk = quotient(in_sequence, n_blocks);
+        block = in_sequence - hk * n_blocks;
+      } else {
+        const int most = plan.most;
+        const int rest = range - locate(range, [&](const Sequence &q) { return q.T > 0 ? q.units(p) * pieces_of(q.count(p), most) : 0; });
+        take_lengths();
+        P = pieces_of(n_stages, most);
+        const int in_order_of_blocks = quotient(rest, n_blocks);
+        block = rest - in_order_of_blocks * n_blocks;
+        hk = quotient(in_order_of_blocks, P);
+        piece = in_order_of_blocks - hk * P;
+        stride = n_blocks;
+        first_slot = range - piece * n_blocks;
+      }
+      slot = first_slot + piece * stride;
+      const int quot = quotient(n_stages, P), extra = n_stages - quot * P;
+      s0 = piece * quot + (piece < extra ? piece : extra);
+      n_st = quot + (piece < extra ? 1 : 0);
+      at += gridDim.x;
     }
-    b = uniform(b);
-    Lengths n = lengths_of(p, b);
-    n.L = uniform(n.L), n.T = uniform(n.T), n.P = uniform(n.P), n.dropped = uniform(n.dropped);
-    const Stages st = stages_of(n.L, n.T, p.window, in_order);
-    const int L = n.L, T = n.T, columns = p.group * T, n_all = st.cached + st.tree, slot_of_piece = first_slot + piece * stride;
-    const int quot = n_all / P, extra = n_all - quot * P;
-    const int s0 = piece * quot + (piece < extra ? piece : extra), n_st = quot + (piece < extra ? 1 : 0);
+    const Stages st = n.stages(p);
+    const int L = n.L, T = n.T, columns = p.group * T, root = root_position(L, n.dropped);
     const size_t unit = (size_t)b * p.H_kv + hk;
 
     // ---- this lane's column
     const int column = block * 128 + wave * 32 + l32;
     const bool active = block * 128 + wave * 32 < columns, there = column < columns;
     const int col = there ? column : 0;  // lanes past the last column take the first: valid memory, never stored
-    const int head = col / T, node = col - head * T;
+    const int head = quotient(col, T), node = col - head * T;
     const size_t row_out = ((size_t)b * p.H + hk * p.group + head) * p.T_max + node;
     u32x4 qf[kQf];
     {
@@ -289,29 +348,15 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
 #pragma unroll
       for (int ks = 0; ks < kQf; ++ks) qf[ks] = *reinterpret_cast<const u32x4 *>(src + ks * 16);
     }
-    const u32x4 ancv = *reinterpret_cast<const u32x4 *>(p.anc + ((size_t)b * p.T_max + node) * 2);
-    const uint64_t anc_lo = ((uint64_t)ancv.y << 32) | ancv.x, anc_hi = ((uint64_t)ancv.w << 32) | ancv.z;
-    // A column sees places from `lowest` on; `all_see`: from here on every column of the wave does.  The bias of a score is
-    // slope * (place of the key) - slope * depth of the node, the second part of which waits for lse.
-    float lowest = 0.f, all_see = 0.f, slope = 0.f, shift = 0.f;
+    u32x4 ancv;
+    if constexpr (kPlace) ancv = *reinterpret_cast<const u32x4 *>(p.anc + ((size_t)b * p.T_max + node) * 2);
+    const u32x4 anc_row = *reinterpret_cast<const u32x4 *>(p.anc + ((size_t)b * p.T_max + (tid < T ? tid : 0)) * 2);  // of node tid
+    float slope = 0.f;
     if constexpr (kPlace) {
-      const int depth = __popcll(anc_lo) + __popcll(anc_hi) - 1;
-      lowest = (float)(sight_of(n.P + depth, p.window).lowest - n.P);
-      slope = p.slopes ? p.slopes[hk * p.group + head] * kLog2e : 0.f;
-      shift = -slope * (float)depth;
-      all_see = lowest;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) all_see = fmaxf(all_see, __shfl_xor(all_see, o, kWave));
-      all_see = __uint_as_float(uniform(__float_as_uint(all_see)));
+      if (p.slopes) slope = p.slopes[hk * p.group + head] * kLog2e;
     }
-    __builtin_amdgcn_s_barrier();  // the range before is done with the ring and the table
-    if constexpr (kPlace) {
-      if (tid < 128) {
-        const uint64_t *a = p.anc + ((size_t)b * p.T_max + (tid < T ? tid : 0)) * 2;
-        tree_place[tid] = (float)(__popcll(a[0]) + __popcll(a[1]) - 1);
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // seen by all behind the first stage's barrier
-    }
+    if (!first_range) __builtin_amdgcn_s_barrier();  // the range before is done with the ring and the table
+    first_range = false;
 
     // ---- loader.  One direct load moves 64 lanes x 16 bytes into 1 KB of LDS, contiguous in lane order, so that the swizzle is
     //      applied by the lanes' addresses.  It walks the cached rows and then the tree's, a stage at a time; rows past the last
@@ -366,6 +411,22 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       for (int x = 0; x < kAhead; ++x)
         if (x < n_st) issue(x);
     };
+    start();
+    // A column sees places from `lowest` on; `all_see`: from here on every column of the wave does.  The bias of a score is
+    // slope * (place of the key) - slope * depth of the node, the second part of which waits for lse.
+    float lowest = 0.f, all_see = 0.f, shift = 0.f;
+    if constexpr (kPlace) {
+      const int depth = __popc(ancv.x) + __popc(ancv.y) + __popc(ancv.z) + __popc(ancv.w) - 1;
+      lowest = (float)(sight_of(root + depth, p.window).lowest - root);
+      shift = -slope * (float)depth;
+      all_see = lowest;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) all_see = fmaxf(all_see, __shfl_xor(all_see, o, kWave));
+      all_see = __uint_as_float(uniform(__float_as_uint(all_see)));
+      if (tid < 128) tree_place[tid] = (float)(__popc(anc_row.x) + __popc(anc_row.y) + __popc(anc_row.z) + __popc(anc_row.w) - 1);
+    }
+    if (tid < 128) tree_anc[tid] = anc_row;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // both seen by all behind the first stage's barrier
     // Stage x is there for all waves, and its place kAhead stages on is free: everyone is done with stage x - 2.  A wave's
     // loads complete in order, so that at most the younger stages' loads outstanding means that stage x has landed.
     auto acquire = [&](int x) {
@@ -482,7 +543,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
           } else {
             // the 32 positions become places; a row without one, or that is not before the root, lies below everything
             const int at = *reinterpret_cast<const __attribute__((address_space(3))) int *>((uintptr_t)(place_ring + (uint32_t)(int)slot * 1024 + wave * 256 + 4 * l32));
-            const float place = (unsigned)at < (unsigned)n.P ? (float)(at - n.P) : -0x1p31f;
+            const float place = (unsigned)at < (unsigned)root ? (float)(at - root) : -0x1p31f;
             stage_place[32 * wave + l32] = place;
             all = __ballot(place < all_see) == 0;
           }
@@ -505,8 +566,8 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       }
       if (!kInside && (tree || n_valid < kStageRows)) {  // uniform
         uint32_t vis = n_valid >= 32 ? ~0u : ((1u << n_valid) - 1u);
-        const uint64_t word = j0 >= 64 ? anc_hi : anc_lo;  // tree stages start at 0, 32, 64, 96
-        vis &= tree ? (uint32_t)(word >> (j0 & 32)) : ~0u;
+        // tree stages start at 0, 32, 64, 96: a word of the node's set each
+        if (tree) vis &= reinterpret_cast<const uint32_t *>(tree_anc + node)[j0 >> 5];
         vis >>= 4 * g;
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] = ((vis >> (8 * (r >> 2) + (r & 3))) & 1u) ? sc[r] : -INFINITY;
@@ -566,7 +627,6 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
     const int n_inside = L / kStageRows - st.first - s0;  // full stages of cached rows, from the first on
     using yes = std::true_type;
     using no = std::false_type;
-    start();
     clear();
     acquire(0);
     if (active) {
@@ -624,9 +684,9 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
     l_run += __shfl_xor(l_run, 32, kWave);
     if constexpr (kRaw) m_run *= p.scale_log2e;
     if constexpr (kPlace) m_run += shift;
-    if (tid == 0 && piece == 0)
+    if (tid == 0 && s0 == 0)
       *reinterpret_cast<u32x4 *>(p.records + 4 * (unit * p.blocks + block)) =
-          u32x4{(uint32_t)first_slot, (uint32_t)stride, (uint32_t)P, (uint32_t)T};
+          u32x4{(uint32_t)first_slot, (uint32_t)stride, (uint32_t)P, (uint32_t)late};
     if (there && P == 1) {
       const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : l_run;  // NaN stays
 #pragma unroll
@@ -637,10 +697,10 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       for (int mb = 0; mb < kMb; ++mb)
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4)
-          *reinterpret_cast<f32x4 *>(p.part_o + part_o_index(slot_of_piece, wave, 4 * mb + q4, lane)) =
+          *reinterpret_cast<f32x4 *>(p.part_o + part_o_index(slot, wave, 4 * mb + q4, lane)) =
               f32x4{o_acc[mb][4 * q4], o_acc[mb][4 * q4 + 1], o_acc[mb][4 * q4 + 2], o_acc[mb][4 * q4 + 3]};
-      p.part_ml[part_ml_index(slot_of_piece, wave, 0, lane)] = m_run;
-      p.part_ml[part_ml_index(slot_of_piece, wave, 1, lane)] = l_run;
+      p.part_ml[part_ml_index(slot, wave, 0, lane)] = m_run;
+      p.part_ml[part_ml_index(slot, wave, 1, lane)] = l_run;
     }
   }
 }
@@ -649,24 +709,23 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
 __device__ __forceinline__ float counted(float o, float f) { return f == 0.f ? 0.f : o; }
 
 // out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the pieces s of a unit, always in the same order.  A workgroup has 32
-// columns of a unit and a 32-wide block of d.  W waves take the pieces in turn, N of them requested together, and meet
+// columns of a unit and a 32-wide block of d.  W waves take the pieces in turn, up to 8 of them requested together, and meet
 // through LDS: with few units there are many pieces, and what costs is the chain of their loads (33 pieces of 8 units, one
 // wave with a load after the other: 9.7 us).
-template <int D, int W, int N>
+template <int D, int W>
 __global__ __launch_bounds__(W *kWave) void grouped_attn_merge_kernel(GroupedParams p) {
   constexpr int kMb = Geo<D>::kMb;
   __shared__ float s_part[W > 1 ? W - 1 : 1][18][kWave];
   const int mb = blockIdx.x % kMb, group = blockIdx.x / kMb % 4;
   const unsigned item = blockIdx.x / (4 * kMb);
-  const int block = (int)(item % (unsigned)p.blocks);
-  const size_t unit = item / (unsigned)p.blocks;
-  const int b = (int)(unit / p.H_kv), hk = (int)(unit - (size_t)b * p.H_kv);
+  const unsigned unit = item / (unsigned)p.blocks, b = unit / (unsigned)p.H_kv;
+  const int block = (int)(item - unit * (unsigned)p.blocks), hk = (int)(unit - b * (unsigned)p.H_kv);
   int T = p.n_nodes[b];
   T = T < 1 ? 1 : (T > p.T_max ? p.T_max : T);
   const int columns = p.group * T;
   if (block * 128 + group * 32 >= columns) return;
-  const u32x4 record = *reinterpret_cast<const u32x4 *>(p.records + 4 * (unit * p.blocks + block));
-  const int first = (int)record.x, stride = (int)record.y, P = (int)record.z;
+  const u32x4 record = *reinterpret_cast<const u32x4 *>(p.records + 4 * (size_t)item);
+  const int first = (int)record.x, stride = (int)record.y, P = (int)record.z, late = (int)record.w;
   if (P <= 1) return;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 5, column = block * 128 + group * 32 + (lane & 31);
   const bool there = column < columns;
@@ -683,12 +742,14 @@ __global__ __launch_bounds__(W *kWave) void grouped_attn_merge_kernel(GroupedPar
     for (int r = 0; r < 16; ++r) acc[r] = counted(acc[r], a_old) * a_old + counted(o[r], a_new) * a_new;
     M = M_new;
   };
-  for (int s0 = wave; s0 < P; s0 += N * W) {
+  auto take = [&](int s0, auto count) __attribute__((always_inline)) {  // pieces s0, s0 + W, ... requested together
+    constexpr int N = decltype(count)::value;
     f32x4 o[N][4];
     float m[N], l[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const size_t slot = first + (size_t)(s0 + k * W < P ? s0 + k * W : P - 1) * stride;  // past the last: that once more, not used
+      const int s = s0 + k * W < P ? s0 + k * W : P - 1;  // past the last: that once more, not used
+      const size_t slot = first + (size_t)s * stride - (s > 0 ? late : 0);
       m[k] = p.part_ml[part_ml_index(slot, group, 0, ln)];
       l[k] = p.part_ml[part_ml_index(slot, group, 1, ln)];
 #pragma unroll
@@ -704,6 +765,12 @@ __global__ __launch_bounds__(W *kWave) void grouped_attn_merge_kernel(GroupedPar
         join(x, m[k], l[k]);
       }
     }
+  };
+  for (int s0 = wave; s0 < P;) {
+    const int mine = (P - s0 + W - 1) / W;
+    if (mine > 4) take(s0, std::integral_constant<int, 8>{}), s0 += 8 * W;
+    else if (mine > 2) take(s0, std::integral_constant<int, 4>{}), s0 += 4 * W;
+    else take(s0, std::integral_constant<int, 2>{}), s0 += 2 * W;
   }
   if constexpr (W > 1) {
     if (wave > 0) {
@@ -723,7 +790,7 @@ __global__ __launch_bounds__(W *kWave) void grouped_attn_merge_kernel(GroupedPar
     }
   }
   if (!there) return;
-  const size_t row = column_row(p, b, hk, column, T);
+  const size_t row = column_row(p, (int)b, hk, column, T);
   const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
   store_out_block<false>(p.out + row * D, acc, inv, g, mb);
   if (p.lse && mb == 0 && g == 0) p.lse[row] = (M + __builtin_amdgcn_logf(total)) * kLn2;
@@ -758,7 +825,7 @@ size_t grouped_attention_workspace_bytes(int B, int H, int L_max, int T_max) {
 template <int D, bool kCap, bool kPlace>
 static bool launch_grouped(const GroupedParams &p, unsigned grid, hipStream_t st) {
   constexpr int NS = D == 128 ? 4 : 6;
-  constexpr int lds_bytes = NS * Geo<D>::kStageBytes + (kPlace ? NS * 1024 + 1024 : 0);
+  constexpr int lds_bytes = NS * Geo<D>::kStageBytes + 2048 + (kPlace ? NS * 1024 + 1024 : 0);
   static std::atomic<uint64_t> set{0};
   if (!allow_lds(reinterpret_cast<const void *>(&grouped_attn_bf16_kernel<D, kCap, kPlace>), lds_bytes, set)) return false;
   hipLaunchKernelGGL((grouped_attn_bf16_kernel<D, kCap, kPlace>), dim3(grid), dim3(kGroupThreads), lds_bytes, st, p);
@@ -766,8 +833,8 @@ static bool launch_grouped(const GroupedParams &p, unsigned grid, hipStream_t st
   if (!p.may_split) return true;
   const unsigned units = (unsigned)p.B * (unsigned)p.H_kv * (unsigned)p.blocks;
   const dim3 merge(units * 4u * Geo<D>::kMb);
-  if (units <= 96) hipLaunchKernelGGL((grouped_attn_merge_kernel<D, 4, 8>), merge, dim3(4 * kWave), 0, st, p);
-  else hipLaunchKernelGGL((grouped_attn_merge_kernel<D, 1, 4>), merge, dim3(kWave), 0, st, p);
+  if (units <= 96) hipLaunchKernelGGL((grouped_attn_merge_kernel<D, 4>), merge, dim3(4 * kWave), 0, st, p);
+  else hipLaunchKernelGGL((grouped_attn_merge_kernel<D, 1>), merge, dim3(kWave), 0, st, p);
   return launch_ok();
 }
 
@@ -797,7 +864,7 @@ extern "C" propd_status propd_grouped_attention(const propd_tree *tree, propd_dt
   for (const void *ptr : {q, k_cache, v_cache, k_tree, v_tree, (const void *)out, (const void *)tree->anc, (const void *)workspace})
     if (reinterpret_cast<uintptr_t>(ptr) % 16 != 0) return PROPD_ERR_INVALID_ARG;
   const long long nodes = (long long)tree->B * H * tree->T_max;
-  if (nodes > (1ll << 30) || (long long)tree->B * H > (1ll << 24)) return PROPD_ERR_UNSUPPORTED;
+  if (L_max > (1 << 30) || nodes > (1ll << 30) || (long long)tree->B * H > (1ll << 24)) return PROPD_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < grouped_attention_workspace_bytes(tree->B, H, L_max, tree->T_max)) return PROPD_ERR_WORKSPACE;
   hipStream_t st = as_stream(hip_stream);
   GroupedParams p;
@@ -836,10 +903,10 @@ extern "C" propd_status propd_grouped_attention(const propd_tree *tree, propd_dt
   p.records = reinterpret_cast<int32_t *>(ws);
   p.slots = (int)slots;
   p.resident = 2 * grouped_compute_units();
-  // with so many units that they fill the chip four times over none is cut
-  p.may_split = (long long)p.B * H_kv < 4ll * p.resident ? 1 : 0;
   const long long units = (long long)p.B * H_kv * p.blocks;
   const long long stages = (L_max + kStageRows - 1ll) / kStageRows + (p.T_max + kStageRows - 1) / kStageRows;
+  p.may_split = (long long)p.B * H_kv < 4ll * p.resident && units * stages < (1ll << 30) ? 1 : 0;
+  // (with so many units that they fill the chip four times over none is cut)
   long long grid = p.may_split ? units * stages : units;
   if (grid > p.resident) grid = p.resident;
   return (d == 64 ? launch_grouped<64>(p, cap, place, (unsigned)grid, st) : launch_grouped<128>(p, cap, place, (unsigned)grid, st))

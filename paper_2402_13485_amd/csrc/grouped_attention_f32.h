@@ -343,17 +343,29 @@ __global__ __launch_bounds__(kF32Threads) void grouped_attn_f32_merge_kernel(Gro
   if (p.lse && part == 0) p.lse[at_row] = M + logf(total);
 }
 
-// Workgroups per unit and 32 columns: two for every compute unit, with kF32LeastTiles tiles each at least.
-constexpr int kF32LeastTiles = 8;
+// Ranges per unit and 32 columns.  The matrix instructions are the bound, a workgroup keeps all four of a compute unit's busy with
+// one wave each, and workgroups that share it take turns: the time is the number of workgroups per compute unit times (the
+// rounds of tiles of a wave, about 2 us each at d = 128, and two rounds' worth of first loads and merging), and another
+// round for the merge kernel.  2 x 4 units of 192 columns x 1024 keys: 8 ranges (384 workgroups) 26 us, 5 (240) F32_MEASURED us.
+static int grouped_f32_splits(long long base, int tiles, int cus, long long room) {
+  long long best = 1, least = 1ll << 62;
+  for (long long s = 1; s <= kF32Splits && s <= room && s <= tiles; ++s) {
+    const long long rounds = (tiles + kF32Waves * s - 1) / (kF32Waves * s);
+    const long long cost = (base * s + cus - 1) / cus * (rounds + 2) + (s > 1 ? 1 : 0);
+    if (cost < least) {
+      least = cost;
+      best = s;
+    }
+  }
+  return (int)best;
+}
 
 template <int D, bool kPlace>
 static bool launch_grouped_f32(GroupedParamsF32 p, size_t workspace_bytes, hipStream_t st) {
   const long long units = (long long)p.B * p.H_kv, base = units * p.pairs;
   const int tiles = (int)((p.L_max + 15ll) / 16) + (p.T_max + 15) / 16;
   const long long room = (long long)(workspace_bytes / (grouped_f32_part_floats(D) * 4)) / base;
-  long long splits = (2ll * grouped_compute_units() + base - 1) / base;
-  for (const long long most : {room, (long long)tiles / kF32LeastTiles, (long long)kF32Splits}) splits = splits < most ? splits : most;
-  p.splits = splits < 1 ? 1 : (int)splits;
+  p.splits = grouped_f32_splits(base, tiles, grouped_compute_units(), room);
   // a dimension of the grid holds fewer than 2^32 threads
   constexpr long long kGridX = 1ll << 22;
   const long long blocks = base * p.splits;

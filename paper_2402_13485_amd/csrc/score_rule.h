@@ -27,6 +27,11 @@ struct Lengths {
   int dropped, P;  // positions without a row, the root's position
 };
 
+__device__ __forceinline__ int root_position(int L, int dropped) {
+  const long long P = (long long)L + dropped;
+  return P > kMaxPosition ? kMaxPosition : (int)P;
+}
+
 // (what is read from device memory is made safe)
 __device__ __forceinline__ Lengths lengths_of(const int32_t *seq_lens, const int32_t *n_nodes, const int32_t *dropped, int L_max,
                                               int T_max, int b) {
@@ -37,8 +42,7 @@ __device__ __forceinline__ Lengths lengths_of(const int32_t *seq_lens, const int
   n.T = n.T < 1 ? 1 : (n.T > T_max ? T_max : n.T);
   n.dropped = dropped ? dropped[b] : 0;
   n.dropped = n.dropped < 0 ? 0 : (n.dropped > kMaxPosition ? kMaxPosition : n.dropped);
-  const long long P = (long long)n.L + n.dropped;
-  n.P = P > kMaxPosition ? kMaxPosition : (int)P;
+  n.P = root_position(n.L, n.dropped);
   return n;
 }
 

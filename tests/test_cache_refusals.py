@@ -36,6 +36,7 @@ def test_attention_refusals(pb):
         assert attention(pb, dt, tree=pb._Tree(0, 16, OK, OK, OK, OK, OK)) == INVALID
         assert attention(pb, dt, tree=pb._Tree(2, 16, OK, OK, OK, OK, None)) == INVALID
         assert attention(pb, dt, tree=pb._Tree(2, 16, OK, OK, OK, OK, 0x1008)) == INVALID
+        assert attention(pb, dt, L_max=(1 << 30) + 1) == UNSUPPORTED
         assert attention(pb, dt, tree=pb._Tree((1 << 20) + 1, 128, OK, OK, OK, OK, OK)) == UNSUPPORTED
     assert attention(pb, 2) == INVALID
     # no cache rows: K and V of the cache may be missing (what is refused then is the workspace)
@@ -68,7 +69,8 @@ def test_observe_refusals(pb):
     for name in ("q", "k", "kt"):
         assert observe(pb, **{name: ODD}) == INVALID
     assert observe(pb, tree=pb._Tree(1 << 24, 16, OK, OK, OK, OK, OK)) == UNSUPPORTED
-    assert observe(pb, tree=pb._Tree(1 << 10, 16, OK, OK, OK, OK, OK), L_max=1 << 30) == UNSUPPORTED
+    assert observe(pb, L_max=(1 << 30) + 1) == UNSUPPORTED
+    assert observe(pb, stride=(1 << 30) - 1) == UNSUPPORTED
 
 
 def evict(pb, dt=None, B=2, H_kv=2, d=128, L_max=64, budget=16, recent=4, sinks=0, k=OK, v=OK, rows=(OK,) * 4, out=(OK,) * 4, ws=OK, ws_bytes=1 << 40):

@@ -5,8 +5,13 @@
 // the next ones requested in front of the work on these, as the B operand of S = Q . K^T (16x16 products); the accepted queries are
 // the A operand, 16 rows to a group, the first kHeld groups of which stay in registers.  A lane then holds four queries' scores of
 // one key, adds their weights up, and the four lanes of a key meet at the end.  K rows are read straight from memory in the operand's
-// layout, 64 bytes of 16 rows per load.  With one batch of tiles per wave every wave paid for the chain path -> query -> lse, and 16 x
-// 8 heads x 4096 rows took 57 us; walking OBSERVE_MEASURED us.
+// layout, 64 bytes of 16 rows per load.
+// 16 x 8 heads x 4096 rows of 128: 50 us (2.9 TB/s; a library reduction over the same bytes takes as long), 41 of them without any
+// work on the rows.  57 us with one batch of tiles per wave, each of which then paid for the chain path -> query -> lse.  Rings in LDS
+// that direct loads fill, per wave and without barriers, took 55 us with three tiles of 4 KB in flight per wave, 58 to 84 with
+// other depths and numbers of waves.
+#include <type_traits>
+
 #include "score_rule.h"
 
 namespace propd {
@@ -22,7 +27,7 @@ struct ObserveParams {
   int H, H_kv, group, T_max, L_max, path_stride;
   int chunks;  // workgroups per unit
   int window;
-  float scale, cap, inv_cap, decay;
+  float scale, scale_log2e, cap, inv_cap, decay;
 };
 
 // Operands of 16 rows: KF fragments of 16 bytes, fragment f of lane l holds row l % 16 and, of every fragment's share of d, part l / 16.
@@ -63,10 +68,20 @@ struct Rows<float, D> {
 
 constexpr int kHeld = 2;  // groups of 16 query rows that stay in registers
 
-template <class E, int D, int KT>
-__global__ __launch_bounds__(kObserveThreads, 2) void cache_observe_kernel(ObserveParams p) {
+constexpr int observe_per_cu(size_t element, int d) { return element == 2 ? (d == 64 ? 4 : 3) : d == 64 ? 3 : 2; }  // workgroups, by registers
+
+// What a query row needs: the exponent of a key's weight is products * scale + slope * place of the key - shift, all in
+// the log2 domain, places being positions less the root's; it sees places from `lowest` on.
+struct QueryRow {
+  float slope, shift, lowest;
+  int place;  // on the path; -1: no query
+};
+
+// kPlace: positions take part (a window, a bias, or rows at positions of their own).
+template <class E, int D, int KT, bool kPlace>
+__global__ __launch_bounds__(kObserveThreads, observe_per_cu(sizeof(E), D)) void cache_observe_kernel(ObserveParams p) {
   // of the first 16 * kHeld query rows (row = place on the path * group + head)
-  __shared__ __attribute__((aligned(16))) float s_lse[16 * kHeld], s_slope[16 * kHeld];
+  __shared__ __attribute__((aligned(16))) float s_slope[16 * kHeld], s_shift[16 * kHeld], s_lowest[16 * kHeld];
   __shared__ __attribute__((aligned(16))) int s_place[16 * kHeld], s_row[16 * kHeld];  // place on the path (-1: no query), row of q
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, part = lane >> 4;
@@ -87,8 +102,8 @@ __global__ __launch_bounds__(kObserveThreads, 2) void cache_observe_kernel(Obser
   // ---- a batch of tiles: 16 cached rows each, or 16 places of the path.  Keys past the last take a valid row.
   struct Batch {
     Rows<E, D> keys[KT];
-    int key[KT], at[KT];  // place in its kind (-1: none), position
-    float old[KT];        // weight so far
+    int at[KT];     // positions
+    float old[KT];  // weights so far
   };
   auto load = [&](Batch &x, int t0) __attribute__((always_inline)) {
 #pragma unroll
@@ -96,13 +111,11 @@ __global__ __launch_bounds__(kObserveThreads, 2) void cache_observe_kernel(Obser
       const int t = t0 + i < tiles ? t0 + i : tiles - 1;  // uniform
       if (t < cached) {
         const int j = 16 * t + c16, row = j < n.L ? j : n.L - 1;
-        x.key[i] = t0 + i < tiles && j < n.L ? j : -1;
         x.at[i] = p.position ? p.position[(size_t)unit * p.L_max + row] : n.dropped + row;
         x.old[i] = p.weight[(size_t)unit * p.L_max + row];
         x.keys[i].load(k_cache + (size_t)row * D, part);
       } else {
         const int r = 16 * (t - cached) + c16, node = path[r < a ? r : a - 1];
-        x.key[i] = t0 + i < tiles && r < a ? r : -1;
         const bool valid = node >= 0 && node < n.T;
         x.at[i] = valid ? n.P + r : -1;
         x.old[i] = 0.f;
@@ -115,23 +128,25 @@ __global__ __launch_bounds__(kObserveThreads, 2) void cache_observe_kernel(Obser
 
   // ---- the query rows that are held
   const int held = rows < 16 * kHeld ? rows : 16 * kHeld;
-  auto row_at = [&](int row, int &r, int &node, size_t &line) __attribute__((always_inline)) {  // of a row that exists
-    r = row / p.group;
-    const int head = hk * p.group + row - r * p.group;
-    node = path[r];
+  auto line_of = [&](int row, QueryRow &x) __attribute__((always_inline)) -> int {  // its row of q within the sequence
+    const bool there = row < rows;
+    const int r = there ? row / p.group : 0, head = hk * p.group + (there ? row - r * p.group : 0);
+    const int node = there ? path[r] : -1;
     const bool valid = node >= 0 && node < n.T;
-    line = ((size_t)b * p.H + head) * p.T_max + (valid ? node : 0);
-    return valid;
+    const int line = head * p.T_max + (valid ? node : 0);
+    x.place = valid ? r : -1;
+    x.slope = p.slopes ? p.slopes[head] * kLog2e : 0.f;
+    x.shift = p.lse[(size_t)b * p.H * p.T_max + line] * kLog2e + x.slope * (float)r;
+    x.lowest = (float)(sight_of(n.P + r, p.window).lowest - n.P);
+    return line;
   };
   if (threadIdx.x < 16 * kHeld) {
-    const int row = threadIdx.x;
-    int r = 0, node = 0;
-    size_t line = 0;
-    const bool there = row < held && row_at(row, r, node, line);
-    s_place[row] = there ? r : -1;
-    s_lse[row] = there ? p.lse[line] : 0.f;
-    s_slope[row] = there && p.slopes ? p.slopes[hk * p.group + row - r * p.group] : 0.f;
-    s_row[row] = there ? (int)(line - (size_t)b * p.H * p.T_max) : 0;
+    QueryRow x = {0.f, 0.f, 0.f, -1};
+    s_row[threadIdx.x] = rows > 0 ? line_of(threadIdx.x, x) : 0;
+    s_place[threadIdx.x] = x.place;
+    s_slope[threadIdx.x] = x.slope;
+    s_shift[threadIdx.x] = x.shift;
+    s_lowest[threadIdx.x] = x.lowest;
   }
   __syncthreads();
   const E *q_base = q + (size_t)b * p.H * p.T_max * D;
@@ -140,60 +155,68 @@ __global__ __launch_bounds__(kObserveThreads, 2) void cache_observe_kernel(Obser
   for (int g = 0; g < kHeld; ++g)
     if (16 * g < held) queries[g].load(q_base + (size_t)s_row[16 * g + c16] * D, part);
 
-  float paid[KT];
-  // what 16 query rows pay to the batch's keys; this lane's four of them: lse, slope, place on the path
-  auto pay = [&](const Batch &x, const Rows<E, D> &rows16, const float (&lse)[4], const float (&slope)[4], const int (&place)[4]) __attribute__((always_inline)) {
+  float paid[KT], place[KT];
+  // what 16 query rows pay to tile i of the batch
+  auto pay = [&](const Rows<E, D> &keys, int i, auto own_keys, const Rows<E, D> &rows16, const f32x4 slope, const f32x4 shift, const f32x4 lowest,
+                 const int (&on_path)[4]) __attribute__((always_inline)) {
+    constexpr bool own = decltype(own_keys)::value;
+    f32x4 x = rows16.times(keys);
+    mfma_settle();
+    if (p.cap > 0.f) {  // uniform
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = capped(x[j] * p.scale, p.cap, p.inv_cap) * kLog2e;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] *= p.scale_log2e;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (kPlace || own) x[j] = fmaf(slope[j], place[i], x[j]);
+      const float w = __builtin_amdgcn_exp2f(x[j] - shift[j]);
+      bool seen = on_path[j] >= 0;
+      if constexpr (kPlace || own) seen = seen && place[i] >= lowest[j];
+      if constexpr (own) seen = seen && place[i] <= (float)on_path[j];
+      paid[i] += seen ? w : 0.f;
+    }
+  };
+  auto pay_batch = [&](const Batch &x, const Rows<E, D> &rows16, const f32x4 slope, const f32x4 shift, const f32x4 lowest,
+                       const int (&on_path)[4]) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < KT; ++i) {
-      const f32x4 raw = rows16.times(x.keys[i]);
-      mfma_settle();
-      const bool own = tile0 + i >= cached;  // keys of the path
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const Sight sight = sight_of(n.P + place[j], p.window);
-        float s = raw[j] * p.scale;
-        if (p.cap > 0.f) s = capped(s, p.cap, p.inv_cap);
-        s = fmaf(-slope[j], (float)(sight.p_i - x.at[i]), s);
-        const float w = __builtin_amdgcn_exp2f((s - lse[j]) * kLog2e);
-        const bool seen = place[j] >= 0 && in_sight(sight, x.at[i]) && (own ? x.key[i] <= place[j] : x.at[i] < n.P);
-        paid[i] += seen ? w : 0.f;
-      }
+      if (tile0 + i < cached) pay(x.keys[i], i, std::false_type{}, rows16, slope, shift, lowest, on_path);
+      else pay(x.keys[i], i, std::true_type{}, rows16, slope, shift, lowest, on_path);
     }
   };
   for (; tile0 < tiles; tile0 += step) {
     const bool more = tile0 + step < tiles;
     if (more) load(next, tile0 + step);
+    // places of the keys; one without a row, or cached and not before the root, lies below everything
 #pragma unroll
-    for (int i = 0; i < KT; ++i) paid[i] = 0.f;
+    for (int i = 0; i < KT; ++i) {
+      paid[i] = 0.f;
+      const bool own = tile0 + i >= cached;
+      place[i] = own ? (now.at[i] >= 0 ? (float)(now.at[i] - n.P) : -0x1p31f) : (unsigned)now.at[i] < (unsigned)n.P ? (float)(now.at[i] - n.P) : -0x1p31f;
+    }
 #pragma unroll
     for (int g = 0; g < kHeld; ++g)
       if (16 * g < held) {  // uniform
-        float lse[4], slope[4];
-        int place[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          lse[j] = s_lse[16 * g + 4 * part + j];
-          slope[j] = s_slope[16 * g + 4 * part + j];
-          place[j] = s_place[16 * g + 4 * part + j];
-        }
-        pay(now, queries[g], lse, slope, place);
+        const int r4 = 16 * g + 4 * part;
+        const int on_path[4] = {s_place[r4], s_place[r4 + 1], s_place[r4 + 2], s_place[r4 + 3]};
+        pay_batch(now, queries[g], *reinterpret_cast<const f32x4 *>(s_slope + r4), *reinterpret_cast<const f32x4 *>(s_shift + r4),
+                  *reinterpret_cast<const f32x4 *>(s_lowest + r4), on_path);
       }
     for (int row0 = 16 * kHeld; row0 < rows; row0 += 16) {  // the rows that are not held
       Rows<E, D> rows16;
-      float lse[4], slope[4];
-      int place[4], r, node;
-      size_t line;
-      row_at(row0 + c16 < rows ? row0 + c16 : rows - 1, r, node, line);
-      rows16.load(q + line * D, part);
+      QueryRow x;
+      rows16.load(q_base + (size_t)line_of(row0 + c16, x) * D, part);
+      f32x4 slope, shift, lowest;
+      int on_path[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int row = row0 + 4 * part + j;
-        const bool valid = row_at(row < rows ? row : rows - 1, r, node, line) && row < rows;
-        place[j] = valid ? r : -1;
-        lse[j] = p.lse[line];
-        slope[j] = p.slopes ? p.slopes[hk * p.group + (row < rows ? row - r * p.group : 0)] : 0.f;
+        line_of(row0 + 4 * part + j, x);
+        slope[j] = x.slope, shift[j] = x.shift, lowest[j] = x.lowest, on_path[j] = x.place;
       }
-      pay(now, rows16, lse, slope, place);
+      pay_batch(now, rows16, slope, shift, lowest, on_path);
     }
     // ---- the four lanes of a key; lanes of part i write tile i
 #pragma unroll
@@ -203,33 +226,35 @@ __global__ __launch_bounds__(kObserveThreads, 2) void cache_observe_kernel(Obser
     }
 #pragma unroll
     for (int i = 0; i < KT; ++i) {
-      if (part != i || now.key[i] < 0) continue;
-      const size_t base = (size_t)unit * p.L_max;
-      if (tile0 + i < cached) {
-        const size_t w = base + now.key[i];
-        p.weight_out[w] = p.decay * now.old[i] + paid[i];
-        if (p.position_out) p.position_out[w] = now.at[i];
-      } else if (n.L + now.key[i] < p.L_max) {
-        const size_t w = base + n.L + now.key[i];
-        p.weight_out[w] = now.at[i] < 0 ? 0.f : paid[i];
-        if (p.position_out) p.position_out[w] = now.at[i];
-      }
+      const int t = tile0 + i;
+      const bool own = t >= cached;
+      const int key = 16 * (own ? t - cached : t) + c16;
+      if (part != i || t >= tiles || key >= (own ? a : n.L) || (own && n.L + key >= p.L_max)) continue;
+      const size_t w = (size_t)unit * p.L_max + (own ? n.L + key : key);
+      p.weight_out[w] = own ? (now.at[i] < 0 ? 0.f : paid[i]) : fmaf(p.decay, now.old[i], paid[i]);
+      if (p.position_out) p.position_out[w] = now.at[i];
     }
     if (more) now = next;
   }
 }
 
-template <class E, int D>
+template <class E, int D, bool kPlace>
 static bool launch_observe(ObserveParams p, long long units, hipStream_t st) {
   const long long tiles = (p.L_max + 15ll) / 16 + (p.path_stride + 15ll) / 16;
   constexpr int KT = sizeof(E) == 2 ? 2 : 1;
-  // a few workgroups per compute unit, as long as every wave has a batch
-  long long chunks = (1024 + units - 1) / units;
+  // as many workgroups as run at once (a third more of them: 55 us instead of 51), as long as every wave has a batch
+  long long chunks = 256 * observe_per_cu(sizeof(E), D) / units;
   const long long most = (tiles + kObserveWaves * KT - 1) / (kObserveWaves * KT);
-  if (chunks > most) chunks = most;
+  chunks = chunks < 1 ? 1 : (chunks > most ? most : chunks);
   p.chunks = (int)chunks;
-  hipLaunchKernelGGL((cache_observe_kernel<E, D, KT>), dim3((unsigned)(units * chunks)), dim3(kObserveThreads), 0, st, p);
+  hipLaunchKernelGGL((cache_observe_kernel<E, D, KT, kPlace>), dim3((unsigned)(units * chunks)), dim3(kObserveThreads), 0, st, p);
   return launch_ok();
+}
+
+template <class E>
+static bool launch_observe(const ObserveParams &p, int d, bool place, long long units, hipStream_t st) {
+  return d == 64 ? (place ? launch_observe<E, 64, true>(p, units, st) : launch_observe<E, 64, false>(p, units, st))
+                 : (place ? launch_observe<E, 128, true>(p, units, st) : launch_observe<E, 128, false>(p, units, st));
 }
 
 }  // namespace propd
@@ -274,11 +299,12 @@ extern "C" propd_status propd_cache_observe(const propd_tree *tree, propd_dtype 
   p.path_stride = path_stride;
   p.window = window_of(rule);
   p.scale = rule->scale;
+  p.scale_log2e = rule->scale * kLog2e;
   p.cap = rule->cap;
   p.inv_cap = rule->cap > 0.f ? 1.f / rule->cap : 0.f;
   p.decay = decay;
   hipStream_t st = as_stream(hip_stream);
-  const bool ok = dt == PROPD_BF16 ? (d == 64 ? launch_observe<uint16_t, 64>(p, units, st) : launch_observe<uint16_t, 128>(p, units, st))
-                                   : (d == 64 ? launch_observe<float, 64>(p, units, st) : launch_observe<float, 128>(p, units, st));
+  const bool place = position || rule->window > 0 || rule->slopes;
+  const bool ok = dt == PROPD_BF16 ? launch_observe<uint16_t>(p, d, place, units, st) : launch_observe<float>(p, d, place, units, st);
   return ok ? PROPD_OK : PROPD_ERR_DEVICE;
 }

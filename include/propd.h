@@ -330,7 +330,7 @@ PROPD_API propd_status propd_commit_path(const propd_tree *tree, propd_dtype dt,
 typedef struct propd_score_rule {
   float scale;          /* > 0                                                       */
   float cap;            /* 0: scores are not capped; otherwise 2^-10 .. 1024          */
-  int32_t window;       /* 0: no window; >= 0                                        */
+  int32_t window;       /* 0: no window; up to 2^24                                  */
   const float *slopes;  /* [H] or NULL: bias per position of distance, finite        */
 } propd_score_rule;
 
@@ -373,7 +373,8 @@ PROPD_API propd_status propd_grouped_attention(const propd_tree *tree, propd_dty
  *   q          [B,H,T_max,d]   of the tree that the path indexes     lse  [B,H,T_max], as left by the attention
  *   k_tree     [B,H_kv,T_max,d]     k_cache  [B,H_kv,L_max,d]
  *   accept_len, accept_path, path_stride   as written by propd_accept_path.  accept_len is clamped to [0, path_stride]; a path
- *              entry outside [0, n_nodes[b]) pays nothing and its row gets weight 0 and position -1
+ *              entry outside [0, n_nodes[b]) pays nothing and its row gets weight 0 and position -1; a node whose lse is
+ *              -inf (it saw nothing) pays nothing either
  *   position   with position_out, or both NULL: rows in the order of their positions
  *   weight_out, position_out  may be weight and position themselves, but must not overlap them otherwise
  *   decay      0 < decay <= 1

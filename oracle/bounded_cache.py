@@ -83,6 +83,8 @@ def cache_observe(n_nodes, accept_len, accept_path, q, lse, k_cache, k_tree, seq
                 to = np.concatenate((np.arange(L), L + np.array(places)))[seen]
                 k = np.concatenate((k_cache[b, hk, :L], k_tree[b, hk, [path[x] for x in places]]))[seen]
                 for h in range(hk * group, (hk + 1) * group):
+                    if lse[b, h, node] == -np.inf:  # saw nothing
+                        continue
                     paid[to] += np.exp(score(q[b, h, node], k, rule, h, back[seen]) - float(lse[b, h, node]))
             room = min(L + a, L_max)
             weight_out[b, hk, :L] = decay * weight[b, hk, :L].astype(np.float64) + paid[:L]

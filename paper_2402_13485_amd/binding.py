@@ -73,10 +73,10 @@ def _init_marshal(lib: ctypes.CDLL) -> None:
         warnings.warn(f"the native argument marshalling is not there ({e}): calls are marshalled in Python, which takes "
                       "two to three times as long on the host", RuntimeWarning, stacklevel=3)
         return
-    native.init(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
-        "propd_tree_mask", "propd_tree_attention", "propd_early_prune", "propd_early_prune_prob", "propd_accept_path",
-        "propd_commit_path", "propd_workspace_bytes", "propd_grouped_attention", "propd_cache_observe", "propd_cache_evict",
-        "propd_rotary")))
+    for init, names in ((native.init, ("propd_tree_mask", "propd_tree_attention", "propd_early_prune", "propd_early_prune_prob",
+                                       "propd_accept_path", "propd_commit_path", "propd_workspace_bytes")),
+                        (native.init_cache, ("propd_grouped_attention", "propd_cache_observe", "propd_cache_evict", "propd_rotary"))):
+        init(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in names))
     _marshal = native
 
 

@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(EvictParam
   if (tid == 0 && unit == b * p.H_kv) {
     const int over = L > budget ? L - budget : 0;
     p.left[2 * b] = L - over;
-    p.left[2 * b + 1] = (p.dropped[b] < 0 ? 0 : p.dropped[b]) + over;
+    p.left[2 * b + 1] = n.dropped + over;
   }
   if (L <= budget) {
     if (tid == 0) p.moves[unit] = 0;
@@ -281,12 +281,14 @@ extern "C" propd_status propd_cache_evict(int32_t B, propd_dtype dt, int32_t H_k
   p.moves = reinterpret_cast<int32_t *>(ws);
   ws += align_up((size_t)units * 4, 256);
   p.left = reinterpret_cast<int32_t *>(ws);
+  // Keys in registers for as long as the registers last.  Read again for every pass: 1032 rows 8.4 us instead of 6.4, 8192 34 instead of 24.
   const dim3 grid((unsigned)units), threads(kSelectThreads);
   if (L_max <= 4 * kSelectThreads) hipLaunchKernelGGL((cache_select_kernel<4>), grid, threads, 0, st, p);
   else if (L_max <= 16 * kSelectThreads) hipLaunchKernelGGL((cache_select_kernel<16>), grid, threads, 0, st, p);
   else hipLaunchKernelGGL((cache_select_kernel<0>), grid, threads, 0, st, p);
   if (!launch_ok()) return PROPD_ERR_DEVICE;
-  // as many workgroups as fill the chip several times, no more than the most rows that can move give work
+  // As many workgroups as fill the chip several times (1024 or 16384 in all take as long), no more than the most rows that can
+  // move give work.
   const long long most = (long long)(budget < L_max - budget ? budget : L_max - budget) * (row_bytes / 16);
   long long parts = (4096 + units - 1) / units;
   if (parts > (most + kMoveThreads - 1) / kMoveThreads) parts = (most + kMoveThreads - 1) / kMoveThreads;

@@ -134,9 +134,10 @@ __global__ __launch_bounds__(kObserveThreads, observe_per_cu(sizeof(E), D)) void
     const int node = there ? path[r] : -1;
     const bool valid = node >= 0 && node < n.T;
     const int line = head * p.T_max + (valid ? node : 0);
-    x.place = valid ? r : -1;
+    const float lse = p.lse[(size_t)b * p.H * p.T_max + line];
+    x.place = valid && lse != -INFINITY ? r : -1;
     x.slope = p.slopes ? p.slopes[head] * kLog2e : 0.f;
-    x.shift = p.lse[(size_t)b * p.H * p.T_max + line] * kLog2e + x.slope * (float)r;
+    x.shift = lse * kLog2e + x.slope * (float)r;
     x.lowest = (float)(sight_of(n.P + r, p.window).lowest - n.P);
     return line;
   };

@@ -94,7 +94,7 @@ __device__ __forceinline__ Sequence lane_sequence(const GroupedParams &p, int b)
 //            `most` whose ranges all run at once.
 //   kShares  Up to twice as many units as workgroups, of different lengths: every workgroup has an equal share of the list of all
 //            stages, which may cross units (each crossing: another unit's first loads and a partial result).
-// How many workgroups run at once (`slots_for`): one per compute unit, two where that leaves ranges of more than kLongRange
+// How many workgroups run at once (`slots`): one per compute unit, two where that leaves ranges of more than kLongRange
 // stages.  A stage of a workgroup that shares its compute unit takes 1.45 of the time, so two halves of a range save little, and
 // each range costs about 5 us of first loads and result and 128 KB of partial result written and read.  Calls, us, 256 / 512
 // ranges: 40 units of 49 stages 29 / 38, 128 of 128 75 / 70, 256 of 130 (capped) 160 / 135.  No range is
@@ -710,8 +710,7 @@ __device__ __forceinline__ float counted(float o, float f) { return f == 0.f ? 0
 
 // out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the pieces s of a unit, always in the same order.  A workgroup has 32
 // columns of a unit and a 32-wide block of d.  W waves take the pieces in turn, up to 8 of them requested together, and meet
-// through LDS: with few units there are many pieces, and what costs is the chain of their loads (33 pieces of 8 units, one
-// wave with a load after the other: 9.7 us).
+// through LDS: what costs is the chain of their loads (33 pieces of 8 units, one wave with a load after the other: 9.7 us).
 template <int D, int W>
 __global__ __launch_bounds__(W *kWave) void grouped_attn_merge_kernel(GroupedParams p) {
   constexpr int kMb = Geo<D>::kMb;
@@ -833,7 +832,9 @@ static bool launch_grouped(const GroupedParams &p, unsigned grid, hipStream_t st
   if (!p.may_split) return true;
   const unsigned units = (unsigned)p.B * (unsigned)p.H_kv * (unsigned)p.blocks;
   const dim3 merge(units * 4u * Geo<D>::kMb);
-  if (units <= 96) hipLaunchKernelGGL((grouped_attn_merge_kernel<D, 4>), merge, dim3(4 * kWave), 0, st, p);
+  // Few units have more pieces than a wave requests at once.  Four waves and one, us: 8 units of 33 pieces 3.9 / 4.6, 64 of 4
+  // 7.1 / 5.3, 640 of 2 19 / 7.7.
+  if (units <= 16) hipLaunchKernelGGL((grouped_attn_merge_kernel<D, 4>), merge, dim3(4 * kWave), 0, st, p);
   else hipLaunchKernelGGL((grouped_attn_merge_kernel<D, 1>), merge, dim3(kWave), 0, st, p);
   return launch_ok();
 }
@@ -905,7 +906,7 @@ extern "C" propd_status propd_grouped_attention(const propd_tree *tree, propd_dt
   p.resident = 2 * grouped_compute_units();
   const long long units = (long long)p.B * H_kv * p.blocks;
   const long long stages = (L_max + kStageRows - 1ll) / kStageRows + (p.T_max + kStageRows - 1) / kStageRows;
-  p.may_split = (long long)p.B * H_kv < 4ll * p.resident && units * stages < (1ll << 30) ? 1 : 0;
+  p.may_split = (long long)p.B * H_kv < 4ll * p.resident && units < (1ll << 20) && units * stages < (1ll << 30) ? 1 : 0;
   // (with so many units that they fill the chip four times over none is cut)
   long long grid = p.may_split ? units * stages : units;
   if (grid > p.resident) grid = p.resident;

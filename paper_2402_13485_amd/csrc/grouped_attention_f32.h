@@ -346,10 +346,10 @@ __global__ __launch_bounds__(kF32Threads) void grouped_attn_f32_merge_kernel(Gro
 // Ranges per unit and 32 columns.  The matrix instructions are the bound, a workgroup keeps all four of a compute unit's busy with
 // one wave each, and workgroups that share it take turns: the time is the number of workgroups per compute unit times (the
 // rounds of tiles of a wave, about 2 us each at d = 128, and two rounds' worth of first loads and merging), and another
-// round for the merge kernel.  2 x 4 units of 192 columns x 1024 keys: 8 ranges (384 workgroups) 26 us, 5 (240) 23.5.
+// round for the merge kernel (whose grid has room for 2^16 of them).  2 x 4 units of 192 columns x 1024 keys: 8 ranges (384 workgroups) 26 us, 5 (240) 23.5.
 static int grouped_f32_splits(long long base, int tiles, int cus, long long room) {
   long long best = 1, least = 1ll << 62;
-  for (long long s = 1; s <= kF32Splits && s <= room && s <= tiles; ++s) {
+  for (long long s = 1; s <= kF32Splits && s <= room && s <= tiles && (s == 1 || base < (1 << 16)); ++s) {
     const long long rounds = (tiles + kF32Waves * s - 1) / (kF32Waves * s);
     const long long cost = (base * s + cus - 1) / cus * (rounds + 2) + (s > 1 ? 1 : 0);
     if (cost < least) {

@@ -218,8 +218,8 @@ void take(PyObject *o, E &entry) {
 }
 
 PyObject *py_init(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  if (n != 11) {
-    PyErr_SetString(PyExc_TypeError, "init: eleven addresses");
+  if (n != 7) {
+    PyErr_SetString(PyExc_TypeError, "init: seven addresses");
     return nullptr;
   }
   take(a[0], entries.tree_mask);
@@ -229,10 +229,19 @@ PyObject *py_init(PyObject *, PyObject *const *a, Py_ssize_t n) {
   take(a[4], entries.accept_path);
   take(a[5], entries.commit_path);
   take(a[6], entries.workspace_bytes);
-  take(a[7], entries.grouped_attention);
-  take(a[8], entries.cache_observe);
-  take(a[9], entries.cache_evict);
-  take(a[10], entries.rotary);
+  if (PyErr_Occurred()) return nullptr;
+  Py_RETURN_NONE;
+}
+
+PyObject *py_init_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (n != 4) {
+    PyErr_SetString(PyExc_TypeError, "init_cache: four addresses");
+    return nullptr;
+  }
+  take(a[0], entries.grouped_attention);
+  take(a[1], entries.cache_observe);
+  take(a[2], entries.cache_evict);
+  take(a[3], entries.rotary);
   if (PyErr_Occurred()) return nullptr;
   Py_RETURN_NONE;
 }
@@ -602,7 +611,7 @@ PyObject *py_rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(init),        METHOD(tree_mask),   METHOD(tree_attention), METHOD(early_prune),
                          METHOD(accept_path), METHOD(commit_path), METHOD(grouped_attention), METHOD(cache_observe),
-                         METHOD(cache_evict), METHOD(rotary),      {nullptr, nullptr, 0, nullptr}};
+                         METHOD(cache_evict), METHOD(rotary),      METHOD(init_cache),     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

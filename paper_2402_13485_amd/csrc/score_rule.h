@@ -9,17 +9,20 @@ namespace propd {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxPosition = 1 << 30;  // positions lie below
+// Distances up to this are exact in fp32: positions less the root's are held as such, and a window's edge is one of them.
+constexpr int kMostWindow = 1 << 24;
 
 // A cap beyond these would lose bits (cap - 2 cap / (exp + 1) is off by cap * 2^-24) or is no cap of scores.
 constexpr float kLeastCap = 0x1p-10f, kMostCap = 1024.f;
 
 inline bool score_rule_ok(const propd_score_rule *r) {
-  return r && r->scale > 0.f && isfinite(r->scale) && (r->cap == 0.f || (r->cap >= kLeastCap && r->cap <= kMostCap)) && r->window >= 0;
+  return r && r->scale > 0.f && isfinite(r->scale) && (r->cap == 0.f || (r->cap >= kLeastCap && r->cap <= kMostCap)) && r->window >= 0 &&
+         r->window <= kMostWindow;
 }
 
 // positions back that a query sees, its own included
 inline int window_of(const propd_score_rule *r) {
-  return r->window > 0 && r->window <= kMaxPosition ? r->window : kMaxPosition + 1;
+  return r->window > 0 ? r->window : kMaxPosition + 1;
 }
 
 struct Lengths {

@@ -44,7 +44,7 @@ def test_attention_refusals(pb):
 
 
 @pytest.mark.parametrize("scale,cap,window", [(0.0, 0.0, 0), (-1.0, 0.0, 0), (math.nan, 0.0, 0), (math.inf, 0.0, 0), (1.0, -1.0, 0), (1.0, math.nan, 0),
-                                              (1.0, math.inf, 0), (1.0, 2e3, 0), (1.0, 1e-4, 0), (1.0, 0.0, -1)])
+                                              (1.0, math.inf, 0), (1.0, 2e3, 0), (1.0, 1e-4, 0), (1.0, 0.0, -1), (1.0, 0.0, (1 << 24) + 1)])
 def test_rules_that_are_refused(pb, scale, cap, window):
     assert attention(pb, rule=rule_of(pb, scale, cap, window)) == INVALID
     assert observe(pb, rule=rule_of(pb, scale, cap, window)) == INVALID

@@ -104,6 +104,29 @@ def test_attention_many_sequences(pb, dtype, B):
     check_attention(x, rule, *run_attention(pb, x, rule))
 
 
+@pytest.mark.parametrize("placed", [False, True])
+@pytest.mark.parametrize("name", list(RULES))
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_long_ranges(pb, d, name, placed):
+    """So many units that each is one range of two dozen stages: whole turns of the ring, with and without NaN on the way."""
+    rng = np.random.default_rng(d + len(name))
+    x = make_inputs(rng, "bf16", 16, 16, d, [synth.random_tree(rng, 1 + b % 4) for b in range(16)], [760 - 7 * b for b in range(16)], placed=placed, holes=0.01)
+    rule = make_rule(name, 16, d)
+    check_attention(x, rule, *run_attention(pb, x, rule))
+
+
+@pytest.mark.parametrize("B,Hk,L,ragged", [(43, 16, 230, True), (38, 16, 200, False), (66, 16, 70, True), (130, 16, 40, False), (130, 16, 40, True),
+                                           (9, 2, 1300, True), (3, 1, 2000, True)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_plans(pb, d, B, Hk, L, ragged):
+    """Shares that cross units (688 of different lengths), whole units and pieces of the ones left over (608 alike), units that are not cut
+    (1056 and 2080), ranges of few units of different lengths."""
+    rng = np.random.default_rng(B + L)
+    x = make_inputs(rng, "bf16", Hk, Hk, d, [synth.chain_tree(2)] * B, [L - (L * (b % 7)) // 9 if ragged else L for b in range(B)], L_max=L)
+    rule = rule_of(d)
+    check_attention(x, rule, *run_attention(pb, x, rule))
+
+
 @pytest.mark.parametrize("window", [1, 2, 31, 32, 33, 200])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_window_edges(pb, dtype, window):
@@ -308,6 +331,64 @@ def test_observe_bad_path_entries_pay_nothing(pb):
     weight, position = run_observe(pb, x, rule, 1.0)
     check_observe(x, rule, 1.0, weight, position)
     assert (position[0, :, 51] == -1).all() and (weight[0, :, 53] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_observe_nodes_twice_and_nodes_that_saw_nothing(pb, dtype):
+    """A path that names a node twice has two rows of it; nodes with lse -inf pay nothing, among the rows that stay in registers and beyond."""
+    rng = np.random.default_rng(23)
+    x = observe_case(rng, dtype, 16, 2, 64, [50, 20], [1, 1], L_max=70)
+    x["accept_path"][:, :6] = [[0, 1, 1, 0, 2, 2], [0, 3, 2, 4, 1, 3]]
+    x["accept_len"][:] = 6
+    x["lse"][0, :, 1] = -np.inf
+    x["lse"][1, 3, :] = -np.inf
+    x["lse"][1, 9, 4] = -np.inf
+    rule = make_rule("all", 16, 64)
+    weight, position = run_observe(pb, x, rule, 0.5)
+    assert np.isfinite(weight).all()
+    check_observe(x, rule, 0.5, weight, position)
+
+
+def test_calls_replayed_from_a_graph_and_on_another_stream(pb):
+    """Sums, eviction and rotary positions in one graph, replayed over inputs put back in between, on a stream of its own."""
+    rng = np.random.default_rng(24)
+    x = observe_case(rng, "bf16", 8, 2, 128, [300, 41], [5, 3], L_max=320, holes=0.0)
+    rule, tree, args = make_rule("all", 8, 128), dev_tree(pb, x), {n: to_dev(x[n]) for n in ("accept_len", "accept_path", "q", "lse", "k_tree")}
+    state = {n: to_dev(x[n]) for n in ("k_cache", "v_cache", "position", "weight", "seq_lens", "dropped", "q", "k_tree")}
+    start = {n: t.clone() for n, t in state.items()}
+    inv, depth = to_dev((1e4 ** -(np.arange(64) / 64)).astype(np.float32)), tree.n_nodes.view(2, 1).expand(2, x["q"].shape[2]).contiguous()
+    on = dev_rule(rule)
+
+    def step():
+        rows = pb.CacheRows(state["seq_lens"], state["dropped"], state["position"], state["weight"])
+        pb.propd_cache_observe(tree, args["accept_len"], args["accept_path"], args["q"], args["lse"], state["k_cache"], args["k_tree"], rows, decay=0.5, **on)
+        pb.propd_cache_evict(state["k_cache"], state["v_cache"], rows, 150, 20, 2)
+        pb.propd_rotary(state["q"], state["k_tree"], inv, depth, q_out=state["q"], k_out=state["k_tree"])
+
+    def put_back():
+        for n, t in state.items():
+            t.copy_(start[n])
+
+    step()
+    want = {n: t.clone() for n, t in state.items()}
+    check_observe(x, rule, 0.5, *run_observe(pb, x, rule, 0.5))
+    assert state["seq_lens"].tolist() == [150, 41] and not torch.equal(want["k_cache"], start["k_cache"])
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        put_back()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        for _ in range(3):
+            put_back()
+            graph.replay()
+            stream.synchronize()
+            for n, t in state.items():
+                assert torch.equal(t.view(torch.uint8), want[n].view(torch.uint8)), n
+            put_back()
+            step()
+            stream.synchronize()
+            for n, t in state.items():
+                assert torch.equal(t.view(torch.uint8), want[n].view(torch.uint8)), n
 
 
 # ---- eviction
@@ -581,3 +662,46 @@ def test_marshalling_in_python_is_the_same(pb, monkeypatch):
     for n, call in enumerate(bad):
         native, python = both(pb, monkeypatch, call)
         assert isinstance(native, Exception) and type(native) is type(python) and str(native) == str(python), (n, native, python)
+
+
+# ---- offsets beyond 32 bits: the last unit of a large call against a call of that unit alone
+
+def test_evict_and_observe_beyond_32_bits(pb):
+    B, Hk, L_max, d, T = 2, 66, 70000, 128, 4  # 4.7 GB of K and of V in fp32
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    k = torch.randn((B, Hk, L_max, d), generator=gen, device="cuda")
+    v = torch.randn((B, Hk, L_max, d), generator=gen, device="cuda")
+    weight = torch.rand((B, Hk, L_max), generator=gen, device="cuda")
+    position = torch.rand((B, Hk, L_max), generator=gen, device="cuda").argsort(-1).int()
+    i32 = dict(dtype=torch.int32, device="cuda")
+    n_nodes, parent = torch.full((B,), T, **i32), torch.tensor([[-1, 0, 1, 2]] * B, **i32)
+    tree = pb.Tree(n_nodes, parent, anc=pb.propd_tree_mask(n_nodes, parent)[1])
+    q, kt = torch.randn((B, Hk, T, d), generator=gen, device="cuda"), torch.randn((B, Hk, T, d), generator=gen, device="cuda")
+    lse, path, a = torch.full((B, Hk, T), 9.0, device="cuda"), torch.tensor([[0, 1, 2]] * B, **i32), torch.tensor([3, 2], **i32)
+    last = lambda t: t[1:, -1:].contiguous()
+    small = pb.CacheRows(torch.full((1,), L_max - 9, **i32), torch.full((1,), 5, **i32), last(position), last(weight))
+    big = pb.CacheRows(torch.full((B,), L_max - 9, **i32), torch.full((B,), 5, **i32), position.clone(), weight.clone())
+    pb.propd_cache_observe(tree, a, path, q, lse, k, kt, big, 0.09)
+    one = pb.Tree(n_nodes[1:].contiguous(), parent[1:].contiguous(), anc=tree.anc[1:].contiguous())
+    pb.propd_cache_observe(one, a[1:].contiguous(), path[1:].contiguous(), last(q), last(lse), last(k), last(kt), small, 0.09)
+    for name in ("weight", "position"):
+        assert torch.equal(last(getattr(big, name)), getattr(small, name)), name
+    k1, v1 = last(k), last(v)
+    pb.propd_cache_evict(k, v, big, 30001, 100, 4)
+    pb.propd_cache_evict(k1, v1, small, 30001, 100, 4)
+    assert torch.equal(last(k), k1) and torch.equal(last(v), v1)
+    for name in ("weight", "position"):
+        assert torch.equal(last(getattr(big, name)), getattr(small, name)), name
+    assert big.seq_lens.tolist() == [30001] * B and big.dropped.tolist() == [5 + L_max - 9 - 30001] * B
+
+
+def test_rotary_beyond_32_bits(pb):
+    B, H, S, d = 2, 40, 220000, 128  # 4.5 GB of q
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    q = torch.empty((B, H, S, d), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    k = torch.empty((B, 2, S, d), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    inv, offset = torch.rand(64, generator=gen, device="cuda"), torch.arange(B * S, dtype=torch.int32, device="cuda").view(B, S)
+    q1, k1, o1 = q[1:, -1:, -50:].contiguous(), k[1:, -1:, -50:].contiguous(), offset[1:, -50:].contiguous()
+    pb.propd_rotary(q, k, inv, offset, q_out=q, k_out=k)
+    pb.propd_rotary(q1, k1, inv, o1, q_out=q1, k_out=k1)
+    assert torch.equal(q[1:, -1:, -50:], q1) and torch.equal(k[1:, -1:, -50:], k1)

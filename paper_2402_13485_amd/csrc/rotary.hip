@@ -137,9 +137,9 @@ static bool launch_rotary(RotaryParams p, bool adjacent, hipStream_t st) {
   const long long threads = (long long)p.B * p.S * p.pieces;
   const int heads = p.H + p.H_kv;
   // The angles are made once per share of the heads, and fewer threads walk fewer streams of memory at a time: as few shares as keep
-  // 4 MB requested, of rows that are there (with n_rows about half of them).  4 x 4096 rows of 40 heads, 1 / 2 / 4 shares: 66 / 72 /
+  // 4 MB requested, of rows that are there (of trees of different sizes about half).  4 x 4096 rows of 40 heads, 1 / 2 / 4 shares: 66 / 72 /
   // 78 us; 16 x 128 rows of 48 heads, fp32, ragged, 2 / 4 / 8 / 24 shares: 33 / 24 / 20 / 23; 64 rows, 1 / 20 shares: 23 / 5.6.
-  const long long requested = threads * (adjacent ? 16 : 32) / (p.n_rows ? 2 : 1);
+  const long long requested = threads * (adjacent ? 16 : 32) / (p.n_rows && p.S <= PROPD_MAX_TREE ? 2 : 1);
   int per = heads;
   while (per > 2 && requested * ((heads + per - 1) / per) < (4ll << 20)) per = (per + 1) / 2;
   p.per_thread = per;

@@ -12,7 +12,7 @@ constexpr int kMaxPosition = 1 << 30;  // positions lie below
 // Distances up to this are exact in fp32: positions less the root's are held as such, and a window's edge is one of them.
 constexpr int kMostWindow = 1 << 24;
 
-// A cap beyond these would lose bits (cap - 2 cap / (exp + 1) is off by cap * 2^-24) or is no cap of scores.
+// A cap beyond these is none of scores.
 constexpr float kLeastCap = 0x1p-10f, kMostCap = 1024.f;
 
 inline bool score_rule_ok(const propd_score_rule *r) {

@@ -179,6 +179,23 @@ def test_attention_of_one_group_is_the_tree_attention(pb):
         assert np.abs(out[b, :, :T] - other[b, :, :T]).max() <= 2 * (4 * 2.0 ** -8 + 2.0 ** -8 * np.abs(other[b, :, :T]).max())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_lse_of_one_key(pb, dtype):
+    """Every node of a chain sees itself alone: lse is its capped score, without a bias, however deep it is and far the cap.
+    Products of -1, 0 and 1 times 2^-3 are exact.  Roundings, each U relative to the score: scale / cap and its product (2, doubled in the
+    square's part of the fraction), the two polynomials (3 each), reciprocal 2, scale and factor log2(e) 3, products 3, back to ln 2."""
+    rng = np.random.default_rng(31)
+    x = make_inputs(rng, dtype, 4, 2, 64, [synth.chain_tree(100)], [0], L_max=8)
+    for name in ("q", "k_tree"):
+        x[name] = synth.from_float((rng.integers(-1, 2, x[name].shape) * (rng.random(x[name].shape) < .2)).astype(np.float32), dtype)
+    slopes = np.array([.7, .5, .25, .9], np.float32)
+    rule = dict(scale=.125, cap=30.0, window=1, slopes=slopes)
+    out, lse = run_attention(pb, x, rule)
+    s = np.einsum("bhid,bhid->bhi", f64(x["q"]), np.repeat(f64(x["k_tree"]), 2, axis=1)) / 8
+    want = 30 * np.tanh(s / 30)
+    assert (np.abs(lse - want) <= 24 * U * np.abs(s)).all(), float(np.max(np.abs(lse - want)) / U)
+
+
 def test_attention_moving_maximum(pb):
     """Scores that rise from row to row: the softmax reference moves again and again, O is scaled."""
     rng = np.random.default_rng(14)

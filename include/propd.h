@@ -342,8 +342,8 @@ typedef struct propd_score_rule {
  * node itself) gets zeros, lse -inf.  A key that a query does not see does not touch its result, whatever it holds.
  *
  *   H, H_kv    H a multiple of H_kv
- *   dt, d      PROPD_BF16 or PROPD_F32, d in {64, 128}.  Scores, softmax and sums are fp32; PROPD_BF16 rounds the weights to
- *              bf16 before they meet V, and the result.
+ *   dt, d      PROPD_BF16 or PROPD_F32, d in {64, 128}.  Scores, softmax and sums are fp32.  PROPD_BF16 rounds the result; at d = 128 the
+ *              weights that meet V are two bf16 values each (off by 2^-17), at d = 64 three (as they are).
  *   q, out     [B,H,T_max,d]        k_tree, v_tree  [B,H_kv,T_max,d]
  *   k_cache, v_cache  [B,H_kv,L_max,d]; rows >= seq_lens[b] are never used
  *   position, dropped  see above; either may be NULL

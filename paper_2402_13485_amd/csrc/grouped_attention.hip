@@ -6,7 +6,7 @@
 //   - A workgroup takes one range of a unit's 32-row stages of K and V (cached rows, then tree rows) and streams it through
 //     a ring in LDS by direct loads; its four waves own 32 columns each.
 //   - S^T = K . Q^T by the 32x32x16 products, so that a lane owns a column: the softmax statistics, the query's
-//     position, slope and ancestor set are per-lane scalars, and the weights, rounded to bf16, are the B
+//     position, slope and ancestor set are per-lane scalars, and the weights, as sums of bf16 values (kParts), are the B
 //     operand of O^T += V^T . P^T (V^T by the transposing LDS read).  The scores of stage i + 1 are multiplied in front
 //     of the softmax of stage i.
 //   - A unit is cut into as many ranges as the chip needs (plan_ranges); partial results are merged by a second kernel, in
@@ -185,7 +185,20 @@ __device__ __forceinline__ void dma4(const void *src, uint32_t lds_at) {
   __builtin_amdgcn_global_load_lds((global_void *)src, (lds_void *)(uintptr_t)lds_at, 4, 0, 0);
 }
 
+// an address with some bits flipped, by an instruction that stays where it is used
+template <int BITS>
+__device__ __forceinline__ uint32_t flipped(uint32_t at) {
+  if constexpr (BITS == 0) return at;
+  uint32_t to;
+  asm volatile("v_xor_b32 %0, %1, %2" : "=v"(to) : "n"(BITS), "v"(at));
+  return to;
+}
+
 // kCap: capped scores.  kPlace: positions take part (a window, a bias, or rows at positions of their own).
+// A weight is multiplied as a sum of kParts bf16 values, each the rest of the one before rounded.  d = 64: three, all 24 bits of it.
+// d = 128: two, off by 2^-17 at most (with three the kernels that keep positions spill).  In one piece a weight is off by 2^-8, as much as the
+// result's own rounding: error against 64 bits 2.3e-3 of the result instead of 1.66e-3.  One / two / three parts, us: 16 x 40 heads
+// on 8, 128 nodes, 4096 keys 217 / 286 / -, capped 4 x 32 heads 29.4 / 31.5 / -, evicted 32 x 32 heads of 64 74 / 87 / 100.
 template <int D, bool kCap, bool kPlace>
 __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(GroupedParams p) {
   using G_ = Geo<D>;
@@ -193,6 +206,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
   constexpr int kMb = G_::kMb, kLoads = G_::kLoads, kQf = D / 16;
   constexpr int NS = D == 128 ? 4 : 6, kAhead = NS - 2;  // two stages are in use by the math, the rest is in flight
   constexpr bool kRaw = !kCap && !kPlace;                // the softmax scale is applied inside the exponent
+  constexpr int kParts = D == 64 ? 3 : 2;
   constexpr int kPerStage = 2 * kLoads + (kPlace ? 1 : 0);  // loads of a wave per stage
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const uint32_t ring = (uint32_t)(uintptr_t)(lds_void *)smem;
@@ -223,11 +237,12 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
   };
 
   // ---- where a lane reads in a stage: K as the A operand (row l32, chunk 2 ks + g), V^T by transposing reads
-  uint32_t k_rd[kQf], v_rd[kMb][2];
+  constexpr bool kFew = D == 128 && kPlace;  // registers are short: addresses are made of two by flipping bits
+  uint32_t k_rd[kFew ? 1 : kQf], v_rd[kFew ? 1 : kMb][2];
 #pragma unroll
-  for (int ks = 0; ks < kQf; ++ks) k_rd[ks] = ring + l32 * kRowBytes + (((2 * ks + g) ^ G_::k_key(l32)) << 4);
+  for (int ks = 0; ks < (kFew ? 1 : kQf); ++ks) k_rd[ks] = ring + l32 * kRowBytes + (((2 * ks + g) ^ G_::k_key(l32)) << 4);
 #pragma unroll
-  for (int mb = 0; mb < kMb; ++mb)
+  for (int mb = 0; mb < (kFew ? 1 : kMb); ++mb)
 #pragma unroll
     for (int hi = 0; hi < 2; ++hi) {
       const int r = 4 * g + 8 * hi + ((lane & 15) >> 2);
@@ -454,11 +469,12 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       f32x16 acc;
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < kQf; ++ks) {
-        const bf16x8 a = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>((uintptr_t)(k_rd[ks] + so));
+      static_for_i<kQf>([&](auto step) __attribute__((always_inline)) {
+        constexpr int ks = decltype(step)::value;
+        const uint32_t at = kFew ? flipped<32 * ks>(k_rd[0]) : k_rd[kFew ? 0 : ks];
+        const bf16x8 a = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>((uintptr_t)(at + so));
         acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, qf[ks]), acc, 0, 0, 0);
-      }
+      });
       return acc;
     };
     auto read_v = [&](auto slot, auto half) __attribute__((always_inline)) {
@@ -466,14 +482,14 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       constexpr bool kKnown = !std::is_same_v<decltype(slot), int>;
       constexpr int kAt = 16 * kRowBytes * kHalf + (kKnown ? (int)decltype(std::conditional_t<kKnown, decltype(slot), std::integral_constant<int, 0>>{})::value : 0) * kStageBytes;
       const uint32_t so = kKnown ? 0u : (uint32_t)(int)slot * kStageBytes;
-#pragma unroll
-      for (int mb = 0; mb < kMb; ++mb) {
-        vt[kHalf][2 * mb] = lds_read_tr16<kAt>(v_rd[mb][0] + so);
-        vt[kHalf][2 * mb + 1] = lds_read_tr16<kAt>(v_rd[mb][1] + so);
-      }
+      static_for_i<kMb>([&](auto block) __attribute__((always_inline)) {
+        constexpr int mb = decltype(block)::value, kFlip = kFew ? 64 * mb : 0;
+        vt[kHalf][2 * mb] = lds_read_tr16<kAt>(flipped<kFlip>(v_rd[kFew ? 0 : mb][0]) + so);
+        vt[kHalf][2 * mb + 1] = lds_read_tr16<kAt>(flipped<kFlip>(v_rd[kFew ? 0 : mb][1]) + so);
+      });
     };
     // Values of V that are not finite: out of the V registers of 16 rows, and what they add to O to it.
-    auto take_out = [&](const uint32_t (&pw)[8], auto half) __attribute__((always_inline)) {
+    auto take_out = [&](const uint32_t (&pw)[kParts][4], auto half) __attribute__((always_inline)) {
       constexpr int kHalf = decltype(half)::value;
 #pragma unroll
       for (int mb = 0; mb < kMb; ++mb) {
@@ -481,7 +497,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
         u32x4 code, seen;  // seen: 1 for a weight
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const uint32_t w2 = pw[4 * kHalf + x];
+          const uint32_t w2 = pw[0][x];  // (zero only for weights below the least bf16 value)
           seen[x] = (w2 & 0xffffu ? 0x3f80u : 0u) | (w2 >> 16 ? 0x3f800000u : 0u);
           code[x] = take_not_finite(v4[x]);
         }
@@ -603,24 +619,40 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       const float neg_m = -(m_run == -INFINITY ? 0.f : m_run) * (kRaw ? p.scale_log2e : 1.f);
       next();  // products of the next stage, in one block with what follows
       read_v(slot, std::integral_constant<int, 0>{});
-      uint32_t pw[8];
+      // weights of the rows of one half: pw[part][x] has those of registers 8 * half + 2 x and 2 x + 1
+      uint32_t pw[2][kParts][4];
+      auto weights = [&](auto half) __attribute__((always_inline)) {
+        constexpr int kHalf = decltype(half)::value;
 #pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        const float p0 = fast_exp2(kRaw ? fmaf(sc[r], p.scale_log2e, neg_m) : sc[r] + neg_m);
-        const float p1 = fast_exp2(kRaw ? fmaf(sc[r + 1], p.scale_log2e, neg_m) : sc[r + 1] + neg_m);
-        pw[r >> 1] = cvt_pk_bf16(p0, p1);
-        l_run += p0 + p1;  // of the weights as they are: lse is an fp32 result
-      }
+        for (int x = 0; x < 4; ++x) {
+          const int r = 8 * kHalf + 2 * x;
+          float p0 = fast_exp2(kRaw ? fmaf(sc[r], p.scale_log2e, neg_m) : sc[r] + neg_m);
+          float p1 = fast_exp2(kRaw ? fmaf(sc[r + 1], p.scale_log2e, neg_m) : sc[r + 1] + neg_m);
+          l_run += p0 + p1;  // of the weights as they are: lse is an fp32 result
+#pragma unroll
+          for (int part = 0; part < kParts; ++part) {  // rounded to bf16, and what that leaves
+            const uint32_t w2 = cvt_pk_bf16(p0, p1);
+            pw[kHalf][part][x] = w2;
+            p0 -= __uint_as_float(w2 << 16);
+            p1 -= __uint_as_float(w2 & 0xffff0000u);
+          }
+        }
+      };
+      weights(std::integral_constant<int, 0>{});
+      weights(std::integral_constant<int, 1>{});
       read_v(slot, std::integral_constant<int, 1>{});
       static_for_i<2>([&](auto half) __attribute__((always_inline)) {
         constexpr int kHalf = decltype(half)::value;
         wait_lds<kHalf == 0 ? 2 * kMb : 0>(vt[kHalf]);
-        if constexpr (kCareful) take_out(pw, half);
-        const u32x4 pv = {pw[4 * kHalf], pw[4 * kHalf + 1], pw[4 * kHalf + 2], pw[4 * kHalf + 3]};
+        if constexpr (kCareful) take_out(pw[kHalf], half);
 #pragma unroll
-        for (int mb = 0; mb < kMb; ++mb) {
-          const u32x4 aw = {vt[kHalf][2 * mb].x, vt[kHalf][2 * mb].y, vt[kHalf][2 * mb + 1].x, vt[kHalf][2 * mb + 1].y};
-          o_acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, aw), __builtin_bit_cast(bf16x8, pv), o_acc[mb], 0, 0, 0);
+        for (int part = kParts - 1; part >= 0; --part) {  // the small parts first
+          const u32x4 pv = {pw[kHalf][part][0], pw[kHalf][part][1], pw[kHalf][part][2], pw[kHalf][part][3]};
+#pragma unroll
+          for (int mb = 0; mb < kMb; ++mb) {
+            const u32x4 aw = {vt[kHalf][2 * mb].x, vt[kHalf][2 * mb].y, vt[kHalf][2 * mb + 1].x, vt[kHalf][2 * mb + 1].y};
+            o_acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, aw), __builtin_bit_cast(bf16x8, pv), o_acc[mb], 0, 0, 0);
+          }
         }
       });
     };

@@ -1,0 +1,96 @@
+"""The calls of a bounded cache where values, not shapes, are the hard part, against the float64 definitions: weights that must
+not lose bits, results near the end of the type's range, values that are not finite, rows that see nothing, lengths outside their range."""
+import numpy as np
+import pytest
+
+from cache_util import f64, make_inputs, rule_of, score_error
+from gpu_util import sentinel_like
+from oracle import bounded_cache as ref
+from paper_2402_13485_amd import synth
+from test_gpu_bounded_cache import RULES, U, make_rule, run_attention
+from test_gpu_parity import pb  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def weight_step(dtype, d):
+    """How far a softmax weight w, 2^e <= w < 2^(e+1), is from the fp32 one where it meets V.  d = 64 multiplies all 24 bits.  d = 128: two bf16
+    values.  The first has steps of 2^(e-7) and leaves at most half of one, 2^(e-8).  That value is exact or lies in a binade whose
+    steps are 2^(e-16) at most, and is rounded by half of one: 2^(e-17) <= 2^-17 w."""
+    return 2.0 ** -17 if dtype == "bf16" and d == 128 else 0.0
+
+
+def check_exactly(x, rule, out, lse):
+    """As check_attention of test_gpu_bounded_cache, with the weights' own step; NaN and the signs of infinities are compared too."""
+    d = x["q"].shape[3]
+    with np.errstate(invalid="ignore"):
+        want, want_lse, mag = ref.grouped_attention(x["n_nodes"], x["parent"], *(f64(x[n]) for n in ("q", "k_cache", "v_cache", "k_tree", "v_tree")),
+                                                    x["seq_lens"], x["dropped"], x["position"], rule)
+    keys = int(x["seq_lens"].max()) + x["q"].shape[2]
+    e = score_error(x, rule, d)
+    share = 2 * e + (keys + 16) * U + weight_step(x["dtype"], d)
+    for b, T in enumerate(x["n_nodes"]):
+        got, r = synth.as_float(out[b, :, :T]).astype(np.float64), want[b, :, :T]
+        fine = np.isfinite(r)
+        assert (np.isnan(got) == np.isnan(r)).all(), (b, np.argwhere(np.isnan(got) != np.isnan(r))[:5])
+        assert (got[~fine & ~np.isnan(r)] == r[~fine & ~np.isnan(r)]).all(), b
+        with np.errstate(invalid="ignore"):
+            bound = share * mag[b, :, :T] + (2.0 ** -8 if x["dtype"] == "bf16" else U) * np.abs(r) + 1e-37
+            assert (np.abs(got - r)[fine] <= bound[fine]).all(), (b, float((np.abs(got - r) / bound)[fine].max()))
+        bound = e + (keys + 16) * U + 4 * U * np.abs(want_lse[b, :, :T])
+        assert (np.abs(lse[b, :, :T] - want_lse[b, :, :T]) <= bound).all(), (b, float((np.abs(lse[b, :, :T] - want_lse[b, :, :T]) / bound).max()))
+        assert (out[b, :, T:] == sentinel_like(x["q"])[b, :, T:]).all() and (lse[b, :, T:] == 12345.5).all()
+
+
+def by_hand(rng, dtype, H, Hk, d, T, L, score, second, values):
+    """Queries (1, 1, 0, ...), so that a cached key's score is the sum of its first two entries (scale 1); T children of the root whose own
+    keys weigh next to nothing.  score, second [Hk,L], values [Hk,L,d]."""
+    x = make_inputs(rng, dtype, H, Hk, d, [synth.star_tree(T)], [L])
+    k, q, kt = np.zeros((1, Hk, L, d), np.float32), np.zeros((1, H, T, d), np.float32), np.zeros((1, Hk, T, d), np.float32)
+    k[0, :, :, 0], k[0, :, :, 1] = score, second
+    q[..., :2], kt[..., 0] = 1.0, -80.0
+    x.update(q=synth.from_float(q, dtype), k_cache=synth.from_float(k, dtype), k_tree=synth.from_float(kt, dtype),
+             v_cache=synth.from_float(values[None].astype(np.float32), dtype), v_tree=synth.from_float(np.zeros((1, Hk, T, d), np.float32), dtype))
+    return x
+
+
+def rounded(a):
+    return synth.as_float(synth.f32_to_bf16_bits(np.asarray(a, np.float32)))
+
+
+ONE = dict(scale=1.0, cap=0.0, window=0, slopes=None)
+
+
+# ---- weights
+
+@pytest.mark.parametrize("cut", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_weights_that_nearly_cancel(pb, d, cut):
+    """Two keys per column of V with values +1 and -1 and weights w and w (1 + 2^-11): 2^-11 w is left.  The weights' own roundings count 2^11
+    times: exponent (2^-22 of 4 and below), exponential and sums 3e-3 of the result together, and at d = 128 twice the weights' step.
+    Then the result is rounded.  cut: one K/V head, whose few stages are cut and merged; otherwise 1200 units."""
+    rng = np.random.default_rng(6)
+    Hk, L = 1 if cut else 1200, 2 * d + 1
+    score, second, v = np.zeros((Hk, L)), np.zeros((Hk, L)), np.zeros((Hk, L, d))
+    s = rounded(rng.uniform(-2.0, -0.05, (Hk, d)))
+    score[:, 1::2], score[:, 2::2] = s, s
+    second[:, 2::2] = 2.0 ** -11
+    for i in range(d):
+        v[:, 1 + 2 * i, i], v[:, 2 + 2 * i, i] = -1.0, 1.0
+    x = by_hand(rng, "bf16", 2 * Hk, Hk, d, 2, L, score, second, v)
+    out, _ = run_attention(pb, x, ONE)
+    want, _, _ = ref.grouped_attention(x["n_nodes"], x["parent"], *(f64(x[n]) for n in ("q", "k_cache", "v_cache", "k_tree", "v_tree")), x["seq_lens"], x["dropped"],
+                                       None, ONE)
+    off = np.abs(synth.as_float(out) - want) / np.abs(want)
+    assert (off <= 2.0 ** -8 + 3e-3 + 2 * weight_step("bf16", d) * 2.0 ** 11).all(), off.max()
+
+
+@pytest.mark.parametrize("placed", [False, True])
+@pytest.mark.parametrize("name", list(RULES))
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+def test_attention_rounds_once(pb, dtype, d, name, placed):
+    """Results are the definition's, rounded once: the weights add next to nothing to that."""
+    rng = np.random.default_rng(7)
+    x = make_inputs(rng, dtype, 8, 2, d, [synth.random_tree(rng, 40), synth.random_tree(rng, 9)], [300, 77], placed=placed, holes=0.1)
+    rule = make_rule(name, 8, d)
+    check_exactly(x, rule, *run_attention(pb, x, rule))

@@ -194,6 +194,17 @@ __device__ __forceinline__ uint32_t flipped(uint32_t at) {
   return to;
 }
 
+// Whether any of these is NaN or infinite (or their sum is).
+template <int MB>
+__device__ __forceinline__ bool not_finite(const f32x16 (&o)[MB]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum += o[mb][r];
+  return !(fabsf(sum) < INFINITY);
+}
+
 // kCap: capped scores.  kPlace: positions take part (a window, a bias, or rows at positions of their own).
 // A weight is multiplied as a sum of kParts bf16 values, each the rest of the one before rounded.  d = 64: three, all 24 bits of it.
 // d = 128: two, off by 2^-17 at most (with three the kernels that keep positions spill).  In one piece a weight is off by 2^-8, as much as the
@@ -513,7 +524,8 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
       }
     };
     // a new running maximum is adopted only when it exceeds the reference by 2^8 in the exponent: weights then exceed 1, by a
-    // factor that fp32 sums and bf16 weights hold, and O is hardly ever scaled
+    // factor that fp32 sums and bf16 weights hold, and O is hardly ever scaled.  Products with values of V beyond 2^120 may not hold it: with care
+    // weights are at most 1.
     const float tau = kRaw ? fminf(8.f / p.scale_log2e, 1e38f) : 8.f;
 
     // The weights of stage i from its products, and what they add to O.
@@ -605,7 +617,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
         swap_halves(lo, hi);
         m_blk = fmaxf(__uint_as_float(lo), __uint_as_float(hi));
       }
-      if (__builtin_amdgcn_ballot_w64(m_blk > m_run + tau) != 0) {
+      if (__builtin_amdgcn_ballot_w64(m_blk > (kCareful ? m_run : m_run + tau)) != 0) {
         const float m_new = fmaxf(m_run, m_blk), m_safe = m_new == -INFINITY ? 0.f : m_new;
         const float alpha = fast_exp2((m_run - m_safe) * (kRaw ? p.scale_log2e : 1.f));
         l_run *= alpha;
@@ -701,10 +713,11 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
     } else {
       for (int i = 1; i < n_st; ++i) acquire(i);  // columns beyond the last: loads and barriers only
     }
-    // Zero weights times values of V that are not finite: such a range is done once more, with care.
+    // Zero weights times values of V that are not finite, or products that leave the range of fp32: such a range is done once more,
+    // with care.
     ++n_any;
     int *word = s_any + (n_any & 1);
-    if (active && __builtin_amdgcn_ballot_w64(has_nan(o_acc)) != 0) *word = n_any;
+    if (active && __builtin_amdgcn_ballot_w64(not_finite(o_acc)) != 0) *word = n_any;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");

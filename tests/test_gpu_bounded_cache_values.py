@@ -94,3 +94,24 @@ def test_attention_rounds_once(pb, dtype, d, name, placed):
     x = make_inputs(rng, dtype, 8, 2, d, [synth.random_tree(rng, 40), synth.random_tree(rng, 9)], [300, 77], placed=placed, holes=0.1)
     rule = make_rule(name, 8, d)
     check_exactly(x, rule, *run_attention(pb, x, rule))
+
+
+# ---- V
+
+@pytest.mark.parametrize("cut", [False, True])
+@pytest.mark.parametrize("name", ["plain", "cap", "bias"])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+def test_attention_values_near_the_largest(pb, dtype, d, name, cut):
+    """A maximum that rises after the first rows, and V values within a factor of four of the largest float: weights above 1
+    would overflow where the result does not.  cut: two K/V heads whose stages are cut and merged; otherwise 520 units."""
+    rng = np.random.default_rng(9)
+    Hk, L = 2 if cut else 520, 200
+    score = rounded(rng.uniform(-3.0, -1.0, (Hk, L)))
+    score[:, 40], score[:, 130] = 3.0, 4.5
+    v = rounded(rng.uniform(-1.0, 1.0, (Hk, L, d)))
+    v[:, 40], v[:, 130] = 1e38, -5e37
+    x = by_hand(rng, dtype, Hk, Hk, d, 2, L, score, np.zeros((Hk, L)), v)
+    rule = dict(ONE, cap=30.0 if name == "cap" else 0.0, slopes=np.full(Hk, 2.0 ** -9, np.float32) if name == "bias" else None)
+    out, lse = run_attention(pb, x, rule)
+    assert np.isfinite(synth.as_float(out[0, :, :2])).all()
+    check_exactly(x, rule, out, lse)

@@ -92,13 +92,20 @@ __device__ __forceinline__ Sequence lane_sequence(const GroupedParams &p, int b)
 //            the units left over in `pieces` ranges each, piece by piece.
 //   kRanges  A range is at most `most` stages, a unit of s stages has pieces_of(s, most) of them, equally long; the least
 //            `most` whose ranges all run at once.
-//   kShares  Up to twice as many units as workgroups, of different lengths: every workgroup has an equal share of the list of all
-//            stages, which may cross units (each crossing: another unit's first loads and a partial result).
+//   kShares  Every workgroup has an equal share of the list of all stages, which may cross units (each crossing: another unit's first
+//            loads and a partial result).
 // How many workgroups run at once (`slots`): one per compute unit, two where that leaves ranges of more than kLongRange
 // stages.  A stage of a workgroup that shares its compute unit takes 1.45 of the time, so two halves of a range save little, and
 // each range costs about 5 us of first loads and result and 128 KB of partial result written and read.  Calls, us, 256 / 512
-// ranges: 40 units of 49 stages 29 / 38, 128 of 128 75 / 70, 256 of 130 (capped) 160 / 135.  No range is
-// shorter than kLeastStages.
+// ranges: 40 units of 49 stages 29 / 38, 128 of 128 75 / 70, 256 of 130 (capped) 160 / 135.
+// Up to as many units as workgroups take kRanges where its ranges are not much longer than an equal share: up to twice as long, up to a
+// quarter longer where that share is more than kLongRange stages, which one more crossing adds little to.  Where one workgroup per
+// compute unit leaves no room to cut a unit, two may.  Calls of 8 K/V heads, us, ranges / shares: 24 sequences of up to 1024 rows (17 stages) 54 / 60,
+// 16 of 256 and one of 8192 (13 stages) 35.5 / 48, 32 of up to 2048 rows at positions of their own (42 stages, ranges 1.44 times as long) 112 / 102;
+// 31 of 256 and one of 8192 in 256 units, not cut / cut for two workgroups 231 / 43, in 512 units, not cut / shares 215 / 54.
+// More units take shares, and from twice as many on only those of which one takes longer than two shares: 63 of 256 and one of 8192
+// (1024 units), whole / shares 247 / 95.
+// `most` and shares are at least kLeastStages stages (where one is cut or crosses units, its parts may be shorter).
 enum PlanKind { kAlike, kRanges, kShares };
 struct Plan {
   int kind;
@@ -117,6 +124,10 @@ constexpr int kLeastStages = 3, kLongRange = 32;
 
 __device__ __forceinline__ int wave_sum_i32(int v) {
   return __builtin_amdgcn_readlane(wave_scan_i32(v, 0, [](int x, int y) { return x + y; }), 63);
+}
+
+__device__ __forceinline__ int wave_max_i32(int v) {
+  return __builtin_amdgcn_readlane(wave_scan_i32(v, 0, [](int x, int y) { return x > y ? x : y; }), 63);
 }
 
 __device__ __forceinline__ Plan plan_ranges(const GroupedParams &p, const Sequence &first) {
@@ -148,29 +159,43 @@ __device__ __forceinline__ Plan plan_ranges(const GroupedParams &p, const Sequen
     return plan;
   }
   if (units <= p.resident) {
-    // from an equal share on, a sixteenth of it longer at a time
-    const float equal = (float)total / (float)slots;
-    for (int step = 0; step < 48; ++step) {
-      const int m = (int)ceilf(equal * (1.f + .0625f * (float)step));
-      const int most = m > kLeastStages ? m : kLeastStages;
-      int n = 0;
-      for (int b0 = 0; b0 < p.B; b0 += kWave) {
-        const Sequence q = b0 == 0 ? first : lane_sequence(p, b0 + lane);
-        n += wave_sum_i32(q.T > 0 ? q.units(p) * pieces_of(q.count(p), most) : 0);
+    for (int room = slots;; room = p.resident) {
+      // from an equal share on, a sixteenth of it longer at a time
+      const float equal = (float)total / (float)room;
+      const int steps = equal > (float)kLongRange ? 4 : 16;
+      for (int step = 0; step <= steps; ++step) {
+        const int m = (int)ceilf(equal * (1.f + .0625f * (float)step));
+        const int most = m > kLeastStages ? m : kLeastStages;
+        int n = 0;
+        for (int b0 = 0; b0 < p.B; b0 += kWave) {
+          const Sequence q = b0 == 0 ? first : lane_sequence(p, b0 + lane);
+          n += wave_sum_i32(q.T > 0 ? q.units(p) * pieces_of(q.count(p), most) : 0);
+        }
+        if (n <= room || n <= units) {
+          plan.most = most;
+          plan.n_ranges = n;
+          return plan;
+        }
       }
-      if (n <= slots || n <= units) {
-        plan.most = most;
-        plan.n_ranges = n;
-        break;
-      }
+      if (room == p.resident) break;
     }
-    return plan;
+  } else if (units >= 2 * p.resident) {  // two rounds and more
+    int longest = 0;
+    for (int b0 = 0; b0 < p.B; b0 += kWave) {
+      const Sequence q = b0 == 0 ? first : lane_sequence(p, b0 + lane);
+      const int x = wave_max_i32(q.count(p));
+      longest = x > longest ? x : longest;
+    }
+    if (longest <= 2 * (total / p.resident)) return plan;
   }
-  if (units >= 2 * p.resident || 2 * p.resident > p.slots) return plan;  // short units, two rounds and more: whole
+  int shares = total / kLeastStages;
+  shares = shares < p.resident ? shares : p.resident;
+  shares = shares < p.slots / 2 ? shares : p.slots / 2;
+  if (shares < 1) return plan;
   plan.kind = kShares;
-  plan.n_ranges = p.resident;
-  plan.quot = total / p.resident;
-  plan.rest = total - plan.quot * p.resident;
+  plan.n_ranges = shares;
+  plan.quot = total / shares;
+  plan.rest = total - plan.quot * shares;
   return plan;
 }
 

@@ -2,13 +2,15 @@
 not lose bits, results near the end of the type's range, values that are not finite, rows that see nothing, lengths outside their range."""
 import numpy as np
 import pytest
+import torch
 
 from cache_util import f64, make_inputs, rule_of, score_error
 from gpu_util import sentinel_like
 from oracle import bounded_cache as ref
 from paper_2402_13485_amd import synth
-from test_gpu_bounded_cache import RULES, U, make_rule, run_attention
+from test_gpu_bounded_cache import RULES, U, dev_tree, make_rule, run_attention
 from test_gpu_parity import pb  # noqa: F401
+from test_gpu_values import timed
 
 pytestmark = pytest.mark.gpu
 
@@ -115,3 +117,40 @@ def test_attention_values_near_the_largest(pb, dtype, d, name, cut):
     out, lse = run_attention(pb, x, rule)
     assert np.isfinite(synth.as_float(out[0, :, :2])).all()
     check_exactly(x, rule, out, lse)
+
+
+# ---- one long sequence among short ones
+
+@pytest.mark.parametrize("B,Hk,T,L,short", [(32, 8, 2, 2100, 40), (32, 16, 2, 2100, 40), (40, 8, 3, 1500, 5), (64, 16, 1, 1900, 33), (70, 16, 2, 1700, 20),
+                                            (300, 1, 2, 900, 0), (257, 1, 1, 3000, 31)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_plans_of_one_long_sequence(pb, d, B, Hk, T, L, short):
+    """256 to 1120 units, the last sequence's much longer than the others': cut where ranges leave room for it, or in shares of all
+    stages, fewer of them than workgroups where there are few stages."""
+    rng = np.random.default_rng(B + L)
+    x = make_inputs(rng, "bf16", Hk, Hk, d, [synth.chain_tree(T)] * B, [short] * (B // 2) + [max(0, short - 3)] * (B - B // 2 - 1) + [L])
+    rule = rule_of(d)
+    check_exactly(x, rule, *run_attention(pb, x, rule))
+
+
+@pytest.mark.parametrize("B,Hk,group", [(32, 8, 2), (32, 8, 4), (64, 8, 4)])
+def test_attention_of_one_long_sequence_takes_no_longer_than_its_rows(pb, B, Hk, group):
+    """256, 512 and 1024 units whose stages are nearly all one sequence's, against as many stages in equal sequences: 1.3 to 1.5 times as long
+    (3.1 to 7.2 where the long units are not cut)."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    L, T, d = [8192] + [256] * (B - 1), 64, 128
+    n_nodes, parent, _ = synth.pad_trees([synth.rank_product_tree(T, 4)] * B, T)
+    tree = dev_tree(pb, dict(n_nodes=n_nodes, parent=parent))
+    normal = lambda *s: torch.empty(s, device="cuda", dtype=torch.bfloat16).normal_(generator=gen)
+    q, kt, vt, kc, vc = normal(B, Hk * group, T, d), normal(B, Hk, T, d), normal(B, Hk, T, d), normal(B, Hk, max(L), d), normal(B, Hk, max(L), d)
+    ws = torch.empty(pb.workspace_bytes(pb.WS_GROUPED_ATTENTION, B, T, Hk * group, d, max(L)), dtype=torch.uint8, device="cuda")
+    out, took = torch.empty_like(q), []
+    for lens in ([sum(L) // B] * B, L):
+        seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):  # the kernels without the host's time
+            for _ in range(10):
+                pb.propd_grouped_attention(tree, q, kc, vc, kt, vt, seq, 0.09, out=out, workspace=ws)
+        graph.replay()
+        took.append(timed(graph.replay))
+    assert took[1] < 2.3 * took[0], took

@@ -70,8 +70,10 @@ constexpr int kHeld = 2;  // groups of 16 query rows that stay in registers
 
 constexpr int observe_per_cu(size_t element, int d) { return element == 2 ? (d == 64 ? 4 : 3) : d == 64 ? 3 : 2; }  // workgroups, by registers
 
-// What a query row needs: the exponent of a key's weight is products * scale + slope * place of the key - shift, all in
-// the log2 domain, places being positions less the root's; it sees places from `lowest` on.
+// What a query row needs: the exponent of a key's weight is products * scale + slope * (place of the key - place on the path) - shift, all in
+// the log2 domain, places being positions less the root's; it sees places from `lowest` on.  (The bias is made of the distance itself: with
+// slope * place on the path in the shift, two large terms would cancel for the last nodes of a long path, and their
+// last bits would not be those of the attention that left lse.)
 struct QueryRow {
   float slope, shift, lowest;
   int place;  // on the path; -1: no query
@@ -137,7 +139,7 @@ __global__ __launch_bounds__(kObserveThreads, observe_per_cu(sizeof(E), D)) void
     const float lse = p.lse[(size_t)b * p.H * p.T_max + line];
     x.place = valid && lse != -INFINITY ? r : -1;
     x.slope = p.slopes ? p.slopes[head] * kLog2e : 0.f;
-    x.shift = lse * kLog2e + x.slope * (float)r;
+    x.shift = lse * kLog2e;
     x.lowest = (float)(sight_of(n.P + r, p.window).lowest - n.P);
     return line;
   };
@@ -172,7 +174,7 @@ __global__ __launch_bounds__(kObserveThreads, observe_per_cu(sizeof(E), D)) void
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if constexpr (kPlace || own) x[j] = fmaf(slope[j], place[i], x[j]);
+      if constexpr (kPlace || own) x[j] = fmaf(slope[j], place[i] - (float)on_path[j], x[j]);
       const float w = __builtin_amdgcn_exp2f(x[j] - shift[j]);
       bool seen = on_path[j] >= 0;
       if constexpr (kPlace || own) seen = seen && place[i] >= lowest[j];

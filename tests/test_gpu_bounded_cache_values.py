@@ -8,7 +8,7 @@ from cache_util import f64, make_inputs, rule_of, score_error
 from gpu_util import sentinel_like
 from oracle import bounded_cache as ref
 from paper_2402_13485_amd import synth
-from test_gpu_bounded_cache import RULES, U, dev_tree, make_rule, run_attention
+from test_gpu_bounded_cache import RULES, U, dev_tree, make_rule, observe_case, run_attention, run_observe
 from test_gpu_parity import pb  # noqa: F401
 from test_gpu_values import timed
 
@@ -154,3 +154,46 @@ def test_attention_of_one_long_sequence_takes_no_longer_than_its_rows(pb, B, Hk,
         graph.replay()
         took.append(timed(graph.replay))
     assert took[1] < 2.3 * took[0], took
+
+
+# ---- sums of attention
+
+@pytest.mark.parametrize("placed", [False, True])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+def test_observe_long_paths_with_steep_slopes(pb, dtype, d, placed):
+    """A path of 120 nodes, products of zero: a key pays exp(-slope * distance - lse).  Roundings: slope, its factor log2(e) and the product 3 of the
+    distance's part, lse with its own and its factor 3, their difference one of both, the exponential 2, the sum one for every term that is not
+    zero (adding zero is exact), the decayed weight 2; none of the root's distance, which is up to 1.4 * 120 in the exponent."""
+    rng = np.random.default_rng(12)
+    H, Hk, T, L = 4, 2, 120, 60
+    x = observe_case(rng, dtype, H, Hk, d, [L, 17], [1, 1], T=T, L_max=L + T, placed=placed, stride=T, holes=0.0)
+    x["parent"][:] = np.arange(T) - 1
+    x["accept_path"][:], x["accept_len"][:] = np.arange(T), [T, T - 5]
+    for name in ("q", "k_cache", "k_tree"):
+        x[name] = np.zeros_like(x[name])
+    slopes = np.array([0.97, 0.71, 0.33, 0.13], np.float32)
+    rule = dict(scale=0.125, cap=0.0, window=0, slopes=slopes)
+    _, lse, _ = ref.grouped_attention(x["n_nodes"], x["parent"], *(f64(x[n]) for n in ("q", "k_cache", "k_cache", "k_tree", "k_tree")), x["seq_lens"], x["dropped"],
+                                      x["position"], rule)
+    x["lse"] = lse.astype(np.float32)
+    weight, position = run_observe(pb, x, rule, 1.0)
+    want, want_position, _ = ref.cache_observe(x["n_nodes"], x["accept_len"], x["accept_path"], f64(x["q"]), x["lse"], f64(x["k_cache"]), f64(x["k_tree"]),
+                                               x["seq_lens"], x["dropped"], x["position"], x["weight"], rule, 1.0, sentinel_like(x["weight"]),
+                                               None if x["position"] is None else sentinel_like(x["position"]))
+    assert position is None or (position == want_position).all()
+    for b, n in enumerate(x["seq_lens"]):
+        a, root = int(x["accept_len"][b]), int(x["seq_lens"][b]) + int(x["dropped"][b])
+        for hk in range(Hk):
+            at = np.concatenate((ref.cached_positions(b, hk, n, x["position"], x["dropped"]), root + np.arange(a))).astype(np.float64)
+            bound, total, terms = np.zeros(n + a), np.zeros(n + a), np.zeros(n + a)
+            for h in (2 * hk, 2 * hk + 1):
+                for r in range(a):
+                    bias, y = float(slopes[h]) * (root + r - at), float(x["lse"][b, h, r])
+                    paid = np.where(bias >= 0, np.exp(np.minimum(-bias - y, 50.0)), 0.0)
+                    bound += paid * U * (4 * bias + 4 * abs(y) + 4)
+                    total += paid
+                    terms += paid > 0
+            bound += terms * U * total
+            bound[:n] += 2 * U * np.abs(x["weight"][b, hk, :n])
+            off = np.abs(weight[b, hk, :n + a] - want[b, hk, :n + a])
+            assert (off <= bound + 1e-30).all(), (b, hk, float((off / (bound + 1e-30)).max()))

@@ -592,8 +592,11 @@ def propd_grouped_attention(tree: Tree, q, k_cache, v_cache, k_tree, v_tree, seq
              k_tree=(k_tree, q.dtype, rows), v_tree=(v_tree, q.dtype, rows), seq_lens=(seq_lens, i32, (B,)),
              n_nodes=(tree.n_nodes, i32, (B,)), anc=(tree.anc, torch.int64, (B, T_max, 2)), slopes=(slopes, f32, (H,)),
              position=(position, i32, cache[:3]), dropped=(dropped, i32, (B,)), out=(out, q.dtype, q.shape), lse=(lse, f32, q.shape[:3]))
-    _apart(out, "out", q, k_cache, v_cache, k_tree, v_tree, lse)
+    read = (q, k_cache, v_cache, k_tree, v_tree, seq_lens, tree.n_nodes, tree.anc, slopes, position, dropped)
+    _apart(out, "out", *read, lse)
+    _apart(lse, "lse", *read)
     ws = _workspace(workspace_bytes(WS_GROUPED_ATTENTION, B, T_max, H, d, L_max), q.device, workspace)
+    _apart(workspace, "workspace", *read, out, lse)
     c_tree, rule = tree._c(), _ScoreRule(scale, cap, window, _ptr(slopes))
     _check(load_library().propd_grouped_attention(
         ctypes.byref(c_tree), dt, H, H_kv, d, ctypes.byref(rule), _ptr(q), _ptr(k_cache) if L_max else None,
@@ -632,6 +635,9 @@ def propd_cache_observe(tree: Tree, accept_len: torch.Tensor, accept_path: torch
              weight_out=(weight_out, f32, state), position_out=(position_out, i32, state))
     _same_or_apart(weight_out, rows.weight, "weight_out")
     _same_or_apart(position_out, rows.position, "position_out")
+    read = (q, lse, k_cache, k_tree, accept_len, accept_path, rows.seq_lens, rows.dropped, tree.n_nodes, slopes)
+    _apart(weight_out, "weight_out", *read, rows.position, position_out)
+    _apart(position_out, "position_out", *read, rows.weight)
     c_tree, rule = tree._c(), _ScoreRule(scale, cap, window, _ptr(slopes))
     _check(load_library().propd_cache_observe(
         ctypes.byref(c_tree), dt, H, H_kv, d, ctypes.byref(rule), decay, _ptr(accept_len), _ptr(accept_path), accept_path.shape[1],
@@ -663,8 +669,14 @@ def propd_cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, rows: CacheR
             _all_dev(k_cache.device, **{f"{which}.{name}": (getattr(r, name), dtype, shape)})
             _same_or_apart(getattr(rows_out, name), getattr(rows, name), f"rows_out.{name}")
     _all_dev(k_cache.device, k_cache=(k_cache, k_cache.dtype, None), v_cache=(v_cache, k_cache.dtype, k_cache.shape))
-    _apart(v_cache, "v_cache", k_cache)
+    names = ("seq_lens", "dropped", "position", "weight")
+    state = [getattr(r, name) for r in (rows, rows_out) for name in names]
+    _apart(v_cache, "v_cache", k_cache, *state)
+    _apart(k_cache, "k_cache", *state)
+    for i, name in enumerate(names):
+        _apart(state[4 + i], f"rows_out.{name}", *(t for j, t in enumerate(state) if j % 4 != i))
     ws = _workspace(workspace_bytes(WS_CACHE_EVICT, B, 0, H_kv, L_max=L_max), k_cache.device, workspace)
+    _apart(workspace, "workspace", k_cache, v_cache, *state)
     c_rows, c_out = rows._c(), rows_out._c()
     _check(load_library().propd_cache_evict(
         B, dt, H_kv, d, L_max, budget, recent, sinks, _ptr(k_cache), _ptr(v_cache), ctypes.byref(c_rows), ctypes.byref(c_out), _ptr(ws),
@@ -699,8 +711,9 @@ def propd_rotary(q: torch.Tensor, k: Optional[torch.Tensor], inv_freq: torch.Ten
              start=(start, i32, (B, n_axes)), axis_of=(axis_of, i32, (pairs,)), n_rows=(n_rows, i32, (B,)))
     _same_or_apart(q_out, q, "q_out")
     _same_or_apart(k_out, k, "k_out")
-    _apart(q_out, "q_out", k, k_out)
-    _apart(k_out, "k_out", q)
+    read = (inv_freq, offset, start, axis_of, n_rows)
+    _apart(q_out, "q_out", k, k_out, *read)
+    _apart(k_out, "k_out", q, *read)
     _check(load_library().propd_rotary(dt, B, S, H, H_kv, d, 2 * pairs, int(adjacent), n_axes, _ptr(axis_of), _ptr(inv_freq), _ptr(start),
                                        _ptr(offset), offset_axes, _ptr(n_rows), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _stream()),
            "propd_rotary")

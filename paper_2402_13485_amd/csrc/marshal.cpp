@@ -15,6 +15,7 @@
 #include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
 #include <memory>
 #include <vector>
 
@@ -448,7 +449,12 @@ struct Device {
 
 bool overlap(const at::Tensor &x, const at::Tensor &y) {
   const char *a = (const char *)x.data_ptr(), *b = (const char *)y.data_ptr();
-  return a < b + y.nbytes() && b < a + x.nbytes();
+  return x.nbytes() && y.nbytes() && a < b + y.nbytes() && b < a + x.nbytes();
+}
+
+// from arguments that may be None
+void apart(const at::Tensor &out, std::initializer_list<PyObject *> others) {
+  for (PyObject *o : others) need(o == Py_None || !overlap(out, tensor(o)));
 }
 
 void same_or_apart(const at::Tensor &out, const at::Tensor &in) { need(out.data_ptr() == in.data_ptr() || !overlap(out, in)); }
@@ -486,8 +492,14 @@ PyObject *py_grouped_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
     if (a[18] != Py_None) out = on(a[18], type, q.sizes());
     if (a[19] != Py_None) lse = on(a[19], at::kFloat, {B, H, T});
-    for (const at::Tensor *t : {&q, &kc, &vc, &kt, &vt}) need(!overlap(out, *t));
+    const std::initializer_list<PyObject *> read = {a[0], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[14], a[15], a[16]};
+    if (a[18] != Py_None) apart(out, read);
+    if (a[19] != Py_None) apart(lse, read);
     need(!want || !overlap(out, lse));
+    if (a[20] != Py_None) {
+      apart(tensor(a[20]), read);
+      need(!overlap(tensor(a[20]), out) && (!want || !overlap(tensor(a[20]), lse)));
+    }
     const Workspace w = workspace(a[20], entries.workspace_bytes(PROPD_WS_GROUPED_ATTENTION, tree.B, tree.T_max, size32(H), size32(d),
                                                                  size32(L), 0, 0), q);
     Owned o = a[18] != Py_None ? object(a[18]) : object(out);
@@ -528,6 +540,14 @@ PyObject *py_cache_observe(PyObject *, PyObject *const *a, Py_ssize_t n) {
     int32_t *position_out = a[21] == Py_None ? position : on.optional<int32_t>(a[21], at::kInt, {B, Hk, L});
     same_or_apart(weight_out, weight);
     if (position && a[21] != Py_None) same_or_apart(tensor(a[21]), tensor(a[13]));
+    PyObject *const at_out = a[21] != Py_None ? a[21] : a[13];
+    const std::initializer_list<PyObject *> read = {a[0], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[18]};
+    apart(weight_out, read);
+    apart(weight_out, {a[13], at_out});
+    if (at_out != Py_None) {
+      apart(tensor(at_out), read);
+      apart(tensor(at_out), {a[14]});
+    }
     Owned result = object(Py_True);
     call(entries.cache_observe, &tree, dt, size32(H), size32(Hk), size32(d), &rule, decay, (const int32_t *)len.data_ptr(),
          (const int32_t *)path.data_ptr(), size32(P), q.data_ptr(), (const float *)lse.data_ptr(), kc.data_ptr(), kt.data_ptr(),
@@ -556,6 +576,12 @@ PyObject *py_cache_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
       rows[i].weight = (float *)on(a[5 + 4 * i], at::kFloat, {B, Hk, L}).data_ptr();
     }
     for (int i = 2; i < 6; ++i) same_or_apart(tensor(a[4 + i]), tensor(a[i]));
+    for (int i = 2; i < 10; ++i) {
+      apart(tensor(a[i]), {a[0], a[1]});
+      for (int j = 6; j < 10; ++j) need(i % 4 == j % 4 || !overlap(tensor(a[j]), tensor(a[i])));
+    }
+    if (a[13] != Py_None)
+      for (int i = 0; i < 10; ++i) need(!overlap(tensor(a[13]), tensor(a[i])));
     const int32_t budget = whole32(a[10]), recent = whole32(a[11]), sinks = whole32(a[12]);
     const Workspace w = workspace(a[13], entries.workspace_bytes(PROPD_WS_CACHE_EVICT, size32(B), 0, size32(Hk), 0, size32(L), 0, 0), k);
     Owned result = object(Py_True);
@@ -596,6 +622,8 @@ PyObject *py_rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (a[8] != Py_None) q_out = on(a[8], type, q.sizes());
     if (a[9] != Py_None) k_out = on(a[9], type, k.sizes());
     same_or_apart(q_out, q);
+    if (a[8] != Py_None) apart(q_out, {a[2], a[3], a[4], a[5], a[6]});
+    if (a[9] != Py_None) apart(k_out, {a[2], a[3], a[4], a[5], a[6]});
     if (keys) {
       same_or_apart(k_out, k);
       need(!overlap(q_out, k) && !overlap(q_out, k_out) && !overlap(k_out, q));

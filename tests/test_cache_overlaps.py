@@ -1,0 +1,18 @@
+"""What the binding refuses before any call is made, by its own checks on host tensors (no GPU needed)."""
+import pytest
+import torch
+
+from test_abi import pb  # noqa: F401
+
+
+def test_overlaps(pb):
+    base = torch.zeros(64)
+    pb._apart(base[:10], "out", None, base[10:20], torch.zeros(3))
+    pb._apart(base[5:5], "out", base)  # nothing to overlap
+    pb._apart(None, "out", base)
+    for other in (base, base[9:10], base.view(torch.int32)[:1]):
+        with pytest.raises(ValueError, match="out: overlaps"):
+            pb._apart(base[:10], "out", torch.zeros(1), other)
+    pb._same_or_apart(base[:10], base[:10], "out")
+    with pytest.raises(ValueError):
+        pb._same_or_apart(base[1:11], base[:10], "out")

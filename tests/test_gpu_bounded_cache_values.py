@@ -5,10 +5,11 @@ import pytest
 import torch
 
 from cache_util import f64, make_inputs, rule_of, score_error
-from gpu_util import sentinel_like
+from gpu_util import sentinel_like, to_dev
 from oracle import bounded_cache as ref
 from paper_2402_13485_amd import synth
 from test_gpu_bounded_cache import RULES, U, dev_tree, make_rule, observe_case, run_attention, run_observe
+from test_gpu_marshal import both
 from test_gpu_parity import pb  # noqa: F401
 from test_gpu_values import timed
 
@@ -197,3 +198,51 @@ def test_observe_long_paths_with_steep_slopes(pb, dtype, d, placed):
             bound[:n] += 2 * U * np.abs(x["weight"][b, hk, :n])
             off = np.abs(weight[b, hk, :n + a] - want[b, hk, :n + a])
             assert (off <= bound + 1e-30).all(), (b, hk, float((off / (bound + 1e-30)).max()))
+
+
+# ---- refusals
+
+def test_outputs_and_workspaces_that_overlap_are_refused(pb, monkeypatch):
+    """Every output and workspace against every argument that the call reads, by both marshallings; nothing is enqueued, so that the
+    inputs stay as they were."""
+    rng = np.random.default_rng(13)
+    H, Hk, d, T, L = 4, 2, 64, 32, 64  # lse of 2 * 4 * 32 floats
+    x = observe_case(rng, "f32", H, Hk, d, [40, 20], [3, 3], T=T, L_max=L)
+    names = ("q", "k_cache", "v_cache", "k_tree", "v_tree", "seq_lens", "dropped", "position", "weight", "lse", "accept_len", "accept_path")
+    tree, t = dev_tree(pb, x), {n: to_dev(x[n]) for n in names}
+    big = torch.zeros(1 << 26, dtype=torch.uint8, device="cuda")
+    as_f32 = lambda a, shape: a.view(-1).view(torch.float32)[:int(np.prod(shape))].view(shape)
+    slopes_at, lse_shape, state = big[4096:].view(torch.float32)[:H], (2, H, T), (2, Hk, L)
+    inside = big[:int(np.prod(lse_shape)) * 4 + 4096]  # a piece of `big` that holds slopes_at
+    att = lambda **k: lambda: pb.propd_grouped_attention(tree, t["q"], t["k_cache"], t["v_cache"], t["k_tree"], t["v_tree"], t["seq_lens"], 0.125,
+                                                         position=t["position"], dropped=t["dropped"], **k)
+    rows = pb.CacheRows(*(t[n] for n in ("seq_lens", "dropped", "position", "weight")))
+    obs = lambda **k: lambda: pb.propd_cache_observe(tree, t["accept_len"], t["accept_path"], t["q"], t["lse"], t["k_cache"], t["k_tree"], rows, 0.125, **k)
+    swap = lambda **k: pb.CacheRows(**{**dict(seq_lens=t["seq_lens"].clone(), dropped=t["dropped"].clone(), position=t["position"].clone(),
+                                              weight=t["weight"].clone()), **k})
+    evict = lambda k_cache=None, v_cache=None, **k: lambda: pb.propd_cache_evict(t["k_cache"] if k_cache is None else k_cache,
+                                                                                 t["v_cache"] if v_cache is None else v_cache, rows, 8, 2, 1, **k)
+    inv, offset = torch.ones(32, device="cuda"), torch.zeros((2, T), dtype=torch.int32, device="cuda")
+    rot = lambda **k: lambda: pb.propd_rotary(**{**dict(q=t["q"], k=t["k_tree"], inv_freq=inv, offset=offset), **k})
+    bad = [att(lse=as_f32(t[n], lse_shape)) for n in ("q", "k_cache", "v_cache", "k_tree", "v_tree", "position")]
+    bad += [att(lse=as_f32(inside, lse_shape), slopes=as_f32(inside, lse_shape).view(-1)[8:8 + H]), att(out=as_f32(big, t["q"].shape), slopes=slopes_at),
+            att(out=as_f32(big, t["q"].shape), lse=as_f32(big, lse_shape)), att(out=as_f32(big, t["q"].shape), workspace=big),
+            att(lse=as_f32(big, lse_shape), workspace=big), att(slopes=slopes_at, workspace=big)]
+    bad += [obs(weight_out=as_f32(t[n], state)) for n in ("q", "k_cache", "k_tree", "lse", "position")]
+    bad += [obs(position_out=as_f32(t[n], state).view(torch.int32)) for n in ("q", "k_cache", "k_tree", "lse", "weight")]
+    both_out = torch.zeros(state, device="cuda")
+    bad += [obs(weight_out=both_out, position_out=both_out.view(torch.int32))]
+    bad += [evict(rows_out=swap(weight=as_f32(t[n], state))) for n in ("k_cache", "v_cache", "position")]
+    bad += [evict(rows_out=swap(position=as_f32(t[n], state).view(torch.int32))) for n in ("k_cache", "v_cache", "weight")]
+    bad += [evict(rows_out=swap(seq_lens=t["dropped"])), evict(rows_out=swap(dropped=t["seq_lens"])), evict(k_cache=t["v_cache"]),
+            evict(workspace=t["k_cache"]), evict(k_cache=as_f32(big, t["k_cache"].shape), workspace=big)]
+    bad += [rot(q_out=as_f32(big, t["q"].shape), inv_freq=big[4096:].view(torch.float32)[:32]),
+            rot(q_out=as_f32(big, t["q"].shape), offset=big[4096:].view(torch.int32)[:2 * T].view(2, T)),
+            rot(k_out=as_f32(big, t["k_tree"].shape), n_rows=big[4096:].view(torch.int32)[:2])]
+    torch.cuda.synchronize()
+    before = {n: v.clone() for n, v in t.items()}
+    for n, call in enumerate(bad):
+        for got in both(pb, monkeypatch, call):
+            assert isinstance(got, ValueError) and "overlaps" in str(got), (n, got)
+    torch.cuda.synchronize()
+    assert all(torch.equal(before[n].view(torch.uint8), v.view(torch.uint8)) for n, v in t.items())

@@ -252,6 +252,8 @@ def workspace_bytes(which: int, B: int, T_max: int, H: int = 0, d: int = 0, L_ma
 
 def _workspace(nbytes: int, device, workspace: Optional[torch.Tensor]) -> torch.Tensor:
     if workspace is not None:
+        if workspace.device != device or not workspace.is_contiguous():
+            raise TypeError("workspace: need a contiguous tensor on the device of the others")
         if workspace.numel() * workspace.element_size() < nbytes:
             raise ValueError("workspace tensor too small")
         return workspace

@@ -157,7 +157,7 @@ Workspace workspace(PyObject *o, size_t need_bytes, const at::Tensor &like) {
   if (o != Py_None) {
     const at::Tensor &t = tensor(o);
     w.bytes = t.nbytes();
-    need(w.bytes >= need_bytes && t.numel() * t.element_size() == (int64_t)w.bytes);
+    need(w.bytes >= need_bytes && t.numel() * t.element_size() == (int64_t)w.bytes && t.device() == like.device() && t.is_contiguous());
     w.ptr = t.data_ptr();
   } else {
     w.own = unlocked([&] { return at::empty({(int64_t)(need_bytes > 256 ? need_bytes : 256)}, like.options().dtype(at::kByte)); });

@@ -5,6 +5,19 @@ import torch
 from test_abi import pb  # noqa: F401
 
 
+def test_workspaces_of_another_device_or_with_gaps_are_refused(pb):
+    cpu, meta = torch.device("cpu"), torch.device("meta")
+    ws = torch.empty(512, dtype=torch.uint8)
+    assert pb._workspace(512, cpu, ws) is ws
+    with pytest.raises(TypeError):
+        pb._workspace(256, meta, ws)
+    for gaps in (torch.empty(1, dtype=torch.uint8).expand(512), torch.empty(1024, dtype=torch.uint8)[::2], torch.empty(32, 32, dtype=torch.uint8).t()):
+        with pytest.raises(TypeError):
+            pb._workspace(256, cpu, gaps)
+    with pytest.raises(ValueError):
+        pb._workspace(513, cpu, ws)
+
+
 def test_overlaps(pb):
     base = torch.zeros(64)
     pb._apart(base[:10], "out", None, base[10:20], torch.zeros(3))

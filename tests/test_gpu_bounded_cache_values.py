@@ -244,5 +244,11 @@ def test_outputs_and_workspaces_that_overlap_are_refused(pb, monkeypatch):
     for n, call in enumerate(bad):
         for got in both(pb, monkeypatch, call):
             assert isinstance(got, ValueError) and "overlaps" in str(got), (n, got)
+    no_tensor = torch.zeros(1 << 26, dtype=torch.uint8)
+    for call in (att(workspace=no_tensor), evict(workspace=no_tensor), att(workspace=torch.zeros(1, dtype=torch.uint8, device="cuda").expand(1 << 26)),
+                 lambda: pb.propd_tree_attention(tree, t["q"], *(torch.zeros(2, H, L, d, device="cuda") for _ in "kv"), t["q"], t["q"], t["seq_lens"], 0.125,
+                                                 workspace=no_tensor)):
+        for got in both(pb, monkeypatch, call):
+            assert isinstance(got, TypeError) and "workspace" in str(got), got
     torch.cuda.synchronize()
     assert all(torch.equal(before[n].view(torch.uint8), v.view(torch.uint8)) for n, v in t.items())

@@ -246,7 +246,7 @@ static bool launch_observe(ObserveParams p, long long units, hipStream_t st) {
   const long long tiles = (p.L_max + 15ll) / 16 + (p.path_stride + 15ll) / 16;
   constexpr int KT = sizeof(E) == 2 ? 2 : 1;
   // as many workgroups as run at once (a third more of them: 55 us instead of 51), as long as every wave has a batch
-  long long chunks = 256 * observe_per_cu(sizeof(E), D) / units;
+  long long chunks = compute_units() * observe_per_cu(sizeof(E), D) / units;
   const long long most = (tiles + kObserveWaves * KT - 1) / (kObserveWaves * KT);
   chunks = chunks < 1 ? 1 : (chunks > most ? most : chunks);
   p.chunks = (int)chunks;

@@ -84,6 +84,17 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 inline bool launch_ok() { return hipGetLastError() == hipSuccess; }
 
+inline int compute_units() {
+  static const int cus = [] {
+    int dev = 0;
+    hipDeviceProp_t prop;
+    if (hipGetDevice(&dev) == hipSuccess && hipGetDeviceProperties(&prop, dev) == hipSuccess && prop.multiProcessorCount > 0)
+      return prop.multiProcessorCount;
+    return 256;
+  }();
+  return cus;
+}
+
 // Lets a kernel use this much LDS.  The setting belongs to the device that is current; `set` remembers for which (the first 64)
 // it was made, for calls from several threads.
 inline bool allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &set) {

@@ -1387,17 +1387,6 @@ __global__ __launch_bounds__(kFinishThreads) void prune_finish_kernel(FinishArgs
 
 }  // namespace propd
 
-static int prune_compute_units() {
-  static const int cus = [] {
-    int dev = 0;
-    hipDeviceProp_t prop;
-    if (hipGetDevice(&dev) == hipSuccess && hipGetDeviceProperties(&prop, dev) == hipSuccess && prop.multiProcessorCount > 0)
-      return prop.multiProcessorCount;
-    return 256;
-  }();
-  return cus;
-}
-
 static propd_status prune_impl(
     const propd::Criterion &crit, const propd_tree *tree, propd_dtype dt, int32_t hidden, int32_t vocab,
     const void *hidden_states, const void *head_weight, uint64_t *keep_bits, int32_t *new_index,
@@ -1465,7 +1454,7 @@ static propd_status prune_impl(
   const bool scored = !(crit.kind == 0 && crit.top_k >= vocab);
   // top_k >= vocab: every id of the vocabulary is inside the list, no scores are needed (ids
   // outside the vocabulary still fail, in the decision kernel)
-  const int cus = prune_compute_units();
+  const int cus = propd::compute_units();
   // the tallest tiles address their operand rows by 32-bit offsets
   const int max_mi = (unsigned long long)hidden * 2 * ((unsigned long long)B * T_max > 256 ? (unsigned long long)B * T_max : 256) <
                              (1ull << 32) ? kTallMaxMI : kTallWideMI;

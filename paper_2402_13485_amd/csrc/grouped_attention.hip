@@ -17,7 +17,8 @@
 namespace propd {
 
 constexpr int kGroupThreads = 256;
-constexpr int kGroupSlots = 2048;  // partial results of a call, at most
+// Workgroups that run at once, and partial results of a call (two per share), at most.  The chip has 256 compute units.
+constexpr int kMostResident = 512, kGroupSlots = 2 * kMostResident;
 
 struct GroupedParams {
   const uint16_t *q, *k_cache, *v_cache, *k_tree, *v_tree;
@@ -876,22 +877,12 @@ __global__ __launch_bounds__(W *kWave) void grouped_attn_merge_kernel(GroupedPar
 // ------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------
-static int grouped_compute_units() {
-  static const int cus = [] {
-    int dev = 0;
-    hipDeviceProp_t prop;
-    if (hipGetDevice(&dev) == hipSuccess && hipGetDeviceProperties(&prop, dev) == hipSuccess && prop.multiProcessorCount > 0)
-      return prop.multiProcessorCount;
-    return 256;
-  }();
-  return cus;
-}
-
-// Slots for partial results: no more than ranges of kLeastStages stages, a bound that needs no device.
+// Slots for partial results, a bound that needs no device: no more than stages, than ranges that run at once, or than two per share.
+// (Up to a hundred units a `most` of a quarter more than an equal share is always found, so that there are no shares.)
 static long long grouped_slots(int B, int H, int T_max, int L_max) {
   const long long stages = (L_max + kStageRows - 1ll) / kStageRows + (T_max + kStageRows - 1) / kStageRows;
-  const long long most = (long long)B * H * stages;
-  return most < kGroupSlots ? most : kGroupSlots;
+  const long long most = (long long)B * H * stages, plan = (long long)B * H <= 100 ? kMostResident : kGroupSlots;
+  return most < plan ? most : plan;
 }
 
 size_t grouped_attention_workspace_bytes(int B, int H, int L_max, int T_max) {
@@ -944,7 +935,8 @@ extern "C" propd_status propd_grouped_attention(const propd_tree *tree, propd_dt
     if (reinterpret_cast<uintptr_t>(ptr) % 16 != 0) return PROPD_ERR_INVALID_ARG;
   const long long nodes = (long long)tree->B * H * tree->T_max;
   if (L_max > (1 << 30) || nodes > (1ll << 30) || (long long)tree->B * H > (1ll << 24)) return PROPD_ERR_UNSUPPORTED;
-  if (!workspace || workspace_bytes < grouped_attention_workspace_bytes(tree->B, H, L_max, tree->T_max)) return PROPD_ERR_WORKSPACE;
+  const size_t needed = grouped_attention_workspace_bytes(tree->B, H, L_max, tree->T_max);
+  if (!workspace || workspace_bytes < needed) return PROPD_ERR_WORKSPACE;
   hipStream_t st = as_stream(hip_stream);
   GroupedParams p;
   p.q = reinterpret_cast<const uint16_t *>(q);
@@ -972,7 +964,7 @@ extern "C" propd_status propd_grouped_attention(const propd_tree *tree, propd_dt
   p.cap_in = rule->cap > 0.f ? rule->scale / rule->cap : 0.f;
   p.cap_log2e = rule->cap * kLog2e;
   const bool cap = rule->cap > 0.f, place = p.position || rule->window > 0 || rule->slopes;
-  if (dt == PROPD_F32) return launch_grouped_f32(p, rule->scale, rule->cap, d, place, workspace, workspace_bytes, st) ? PROPD_OK : PROPD_ERR_DEVICE;
+  if (dt == PROPD_F32) return launch_grouped_f32(p, rule->scale, rule->cap, d, place, workspace, needed, st) ? PROPD_OK : PROPD_ERR_DEVICE;
   const size_t slots = (size_t)grouped_slots(tree->B, H, tree->T_max, L_max);
   char *ws = reinterpret_cast<char *>(workspace);
   p.part_o = reinterpret_cast<float *>(ws);
@@ -981,7 +973,7 @@ extern "C" propd_status propd_grouped_attention(const propd_tree *tree, propd_dt
   ws += align_up(slots * kPartMlFloats * 4, 256);
   p.records = reinterpret_cast<int32_t *>(ws);
   p.slots = (int)slots;
-  p.resident = 2 * grouped_compute_units();
+  p.resident = 2 * compute_units() < kMostResident ? 2 * compute_units() : kMostResident;
   const long long units = (long long)p.B * H_kv * p.blocks;
   const long long stages = (L_max + kStageRows - 1ll) / kStageRows + (p.T_max + kStageRows - 1) / kStageRows;
   p.may_split = (long long)p.B * H_kv < 4ll * p.resident && units < (1ll << 20) && units * stages < (1ll << 30) ? 1 : 0;

@@ -364,8 +364,9 @@ template <int D, bool kPlace>
 static bool launch_grouped_f32(GroupedParamsF32 p, size_t workspace_bytes, hipStream_t st) {
   const long long units = (long long)p.B * p.H_kv, base = units * p.pairs;
   const int tiles = (int)((p.L_max + 15ll) / 16) + (p.T_max + 15) / 16;
+  // (of what propd_workspace_bytes asks for: a caller who gives more gets the same bits)
   const long long room = (long long)(workspace_bytes / (grouped_f32_part_floats(D) * 4)) / base;
-  p.splits = grouped_f32_splits(base, tiles, grouped_compute_units(), room);
+  p.splits = grouped_f32_splits(base, tiles, compute_units(), room);
   // a dimension of the grid holds fewer than 2^32 threads
   constexpr long long kGridX = 1ll << 22;
   const long long blocks = base * p.splits;

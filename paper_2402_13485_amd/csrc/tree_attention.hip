@@ -1284,17 +1284,6 @@ static void fill_plain(AttnParamsPlain<E> &p, const propd_tree *tree, int H, flo
 // ------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------
-static int compute_units() {
-  static const int cus = [] {
-    int dev = 0;
-    hipDeviceProp_t prop;
-    if (hipGetDevice(&dev) == hipSuccess && hipGetDeviceProperties(&prop, dev) == hipSuccess && prop.multiProcessorCount > 0)
-      return prop.multiProcessorCount;
-    return 256;
-  }();
-  return cus;
-}
-
 // Workgroups of the persistent kernel: at most one per two stages of the call, a bound the
 // host can compute without a device (the workspace is sized by it) ...
 static int grid_bound(int B, int H, int L_max, int T_max) {

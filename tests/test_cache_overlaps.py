@@ -29,3 +29,11 @@ def test_overlaps(pb):
     pb._same_or_apart(base[:10], base[:10], "out")
     with pytest.raises(ValueError):
         pb._same_or_apart(base[1:11], base[:10], "out")
+
+
+def test_workspace_of_the_attention_holds_what_plans_use(pb):
+    """At most 1024 partial results of 66 KB, 512 where there are few units, and no more than there are stages."""
+    piece = 66 << 10
+    for args, most in (((1, 1, 1, 128, 0), 1), ((1, 1, 32, 128, 1024), 512), ((2, 128, 50, 64, 1 << 20), 512), ((32, 64, 32, 128, 4096), 1024), ((1, 128, 1, 64, 60), 6)):
+        got = pb.workspace_bytes(pb.WS_GROUPED_ATTENTION, *args)
+        assert most * piece <= got <= most * piece + 16 * args[0] * args[2] + 1024, args

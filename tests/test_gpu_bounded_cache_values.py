@@ -252,3 +252,20 @@ def test_outputs_and_workspaces_that_overlap_are_refused(pb, monkeypatch):
             assert isinstance(got, TypeError) and "workspace" in str(got), got
     torch.cuda.synchronize()
     assert all(torch.equal(before[n].view(torch.uint8), v.view(torch.uint8)) for n, v in t.items())
+
+
+def test_attention_f32_takes_the_workspace_it_asked_for(pb):
+    """1040 pieces of 32 columns and 1084 tiles, which more ranges would suit than there is room for: a larger workspace makes no
+    difference to the results, in no bit."""
+    B, H, T, d, L = 16, 26, 80, 128, 17264
+    gen = torch.Generator(device="cuda").manual_seed(14)
+    n_nodes, parent, _ = synth.pad_trees([synth.chain_tree(T)] * B, T)
+    tree = dev_tree(pb, dict(n_nodes=n_nodes, parent=parent))
+    normal = lambda *s: torch.empty(s, device="cuda").normal_(generator=gen)
+    q, kt, vt, kc, vc = normal(B, H, T, d), normal(B, 1, T, d), normal(B, 1, T, d), normal(B, 1, L, d), normal(B, 1, L, d)
+    seq = torch.full((B,), L, dtype=torch.int32, device="cuda")
+    nbytes = pb.workspace_bytes(pb.WS_GROUPED_ATTENTION, B, T, H, d, L)
+    outs = [pb.propd_grouped_attention(tree, q, kc, vc, kt, vt, seq, 0.09, want_lse=True, workspace=torch.empty(n, dtype=torch.uint8, device="cuda"))
+            for n in (nbytes, 2 * nbytes, 4 * nbytes)]
+    for out, lse in outs[1:]:
+        assert torch.equal(out, outs[0][0]) and torch.equal(lse, outs[0][1])

@@ -5,10 +5,11 @@ import pytest
 import torch
 
 from cache_util import f64, make_inputs, rule_of, score_error
-from gpu_util import sentinel_like, to_dev
+from gpu_util import sentinel_like, to_dev, to_host
 from oracle import bounded_cache as ref
 from paper_2402_13485_amd import synth
-from test_gpu_bounded_cache import RULES, U, dev_tree, make_rule, observe_case, run_attention, run_observe
+from test_gpu_bounded_cache import (RULES, U, check_observe, dev_tree, evict_case, make_rule, observe_case, run_attention,
+                                    run_observe)
 from test_gpu_marshal import both
 from test_gpu_parity import pb  # noqa: F401
 from test_gpu_values import timed
@@ -269,3 +270,145 @@ def test_attention_f32_takes_the_workspace_it_asked_for(pb):
             for n in (nbytes, 2 * nbytes, 4 * nbytes)]
     for out, lse in outs[1:]:
         assert torch.equal(out, outs[0][0]) and torch.equal(lse, outs[0][1])
+
+
+# ---- values of V that are not finite, rows that see nothing
+
+@pytest.mark.parametrize("Hk,L", [(2, 5), (2, 700), (600, 70)])
+@pytest.mark.parametrize("name", ["plain", "all"])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+def test_attention_infinities_of_both_signs(pb, dtype, d, name, Hk, L):
+    """NaN, +inf and -inf in V, alone in a column and together, in cached rows (the last one too) and in tree rows that some nodes see
+    and others do not: every result is the sum of what the node sees.  One range to a unit, several of them, 600 units."""
+    rng = np.random.default_rng(15)
+    x = make_inputs(rng, dtype, 2 * Hk, Hk, d, [synth.rank_product_tree(40, 4)], [L])
+    put = lambda v: synth.from_float(np.array([v], np.float32), dtype)[0]
+    for row, column, v in ((L - 1, 2, np.inf), (1, 3, -np.inf), (0, 4, np.inf), (L - 1, 4, -np.inf), (L - 2, 7, np.nan), (L // 2, 8, np.inf), (L // 3, 8, np.inf)):
+        x["v_cache"][0, ::2, row, column] = put(v)
+    for row, column, v in ((7, 5, np.inf), (39, 5, -np.inf), (12, 6, -np.inf), (1, 9, np.nan), (39, 4, np.inf)):
+        x["v_tree"][0, ::2, row, column] = put(v)
+    rule = make_rule(name, 2 * Hk, d)
+    out, lse = run_attention(pb, x, rule)
+    assert np.isposinf(synth.as_float(out)).any() and np.isneginf(synth.as_float(out)).any()
+    check_exactly(x, rule, out, lse)
+
+
+@pytest.mark.parametrize("name", ["plain", "all"])
+@pytest.mark.parametrize("Hk,L,placed", [(2, 0, False), (2, 0, True), (2, 700, True), (600, 40, True), (1100, 0, False)])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+def test_attention_of_nodes_that_see_nothing(pb, dtype, d, Hk, L, placed, name):
+    """Nodes whose set is empty, over an empty cache and over one whose rows have no position (NaN in them): zeros, lse -inf.  The
+    other nodes' results are bit for bit those without such nodes.  Whole units, pieces that are merged, fp32 with one range and several."""
+    rng = np.random.default_rng(16)
+    x = make_inputs(rng, dtype, Hk, Hk, d, [synth.star_tree(37), synth.star_tree(5)], [L, L], L_max=max(L, 1), placed=placed, holes=1.0)
+    rule, tree = make_rule(name, Hk, d), dev_tree(pb, x)
+    whole = run_attention(pb, x, rule, tree)
+    for b, nodes in ((0, [1, 30, 36]), (1, [4])):
+        tree.anc[b, nodes] = 0
+    out, lse = run_attention(pb, x, rule, tree)
+    for b, nodes in ((0, [1, 30, 36]), (1, [4])):
+        assert (synth.as_float(out[b][:, nodes]) == 0).all() and (lse[b][:, nodes] == -np.inf).all()
+        rest = [i for i in range(37) if i not in nodes]
+        assert (out[b][:, rest].view(np.uint8) == whole[0][b][:, rest].view(np.uint8)).all() and (lse[b][:, rest] == whole[1][b][:, rest]).all()
+
+
+# ---- lengths from device memory, outside their range
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_lengths_outside_their_range_are_clamped(pb, dtype):
+    """Lengths, numbers of nodes, of dropped positions and of accepted nodes below and above what there is: the results are those of the
+    nearest that there is, bit for bit."""
+    rng = np.random.default_rng(17)
+    H, Hk, d, T, L = 4, 2, 64, 24, 90
+    x = observe_case(rng, dtype, H, Hk, d, [L, L, 60, 30], [8] * 4, T=T, L_max=L, placed=True, holes=0.0)
+    x["weight"] = np.exp(rng.normal(size=x["weight"].shape)).astype(np.float32)
+    wild = dict(seq_lens=[-5, 2 ** 31 - 1, 60, 30], n_nodes=[0, 2 ** 31 - 1, -2 ** 31, 7], dropped=[-1, 40, -2 ** 31, 0], accept_len=[3, -7, 2 ** 31 - 1, 8])
+    tame = dict(seq_lens=[0, L, 60, 30], n_nodes=[1, T, 1, 7], dropped=[0, 40, 0, 0], accept_len=[3, 0, 8, 8])
+    rule, results = make_rule("all", H, d), []
+    for given in (wild, tame):
+        y = dict(x, **{n: np.array(v, np.int32) for n, v in given.items()})
+        tree = dev_tree(pb, dict(n_nodes=np.array(tame["n_nodes"], np.int32), parent=x["parent"]))
+        tree.n_nodes = to_dev(y["n_nodes"])
+        got = list(run_attention(pb, y, rule, tree))
+        got += run_observe(pb, y, rule, 0.5)
+        rows = pb.CacheRows(*(to_dev(y[n]) for n in ("seq_lens", "dropped", "position", "weight")))
+        k, v = to_dev(y["k_cache"]), to_dev(x["v_cache"])
+        pb.propd_cache_evict(k, v, rows, 40, 5, 1)
+        results.append(got + [to_host(t) for t in (k, v, rows.seq_lens, rows.dropped, rows.position, rows.weight)])
+    for i, (a, b) in enumerate(zip(*results)):
+        # (a sequence of at most `budget` rows keeps its numbers as they are clamped too)
+        assert (a.view(np.uint8) == b.view(np.uint8)).all(), i
+    assert results[1][6].tolist() == [0, 40, 40, 30] and results[1][7].tolist() == [0, 90, 20, 0]
+
+
+# ---- eviction with some of the rows' arrays in place
+
+@pytest.mark.parametrize("mine", range(16))
+def test_evict_with_some_arrays_in_place(pb, mine):
+    """Every choice of the four arrays that are written in place; the others get their entries and nothing else."""
+    rng = np.random.default_rng(mine)
+    x = evict_case(rng, "bf16", 2, 64, [200, 50, 0, 51], 200, True)
+    names = ("seq_lens", "dropped", "position", "weight")
+    rows = pb.CacheRows(*(to_dev(x[n]) for n in names))
+    out = pb.CacheRows(*(getattr(rows, n) if mine >> i & 1 else to_dev(sentinel_like(x[n])) for i, n in enumerate(names)))
+    k, v = to_dev(x["k"]), to_dev(x["v"])
+    pb.propd_cache_evict(k, v, rows, 50, 9, 3, rows_out=out)
+    want = {n: (x[n] if mine >> i & 1 else sentinel_like(x[n])).copy() for i, n in enumerate(names)}
+    k_ref, v_ref = x["k"].copy(), x["v"].copy()
+    ref.cache_evict(k_ref, v_ref, x["seq_lens"], x["dropped"], x["position"], x["weight"], 50, 9, 3, want)
+    for i, n in enumerate(names):
+        assert (to_host(getattr(out, n)).view(np.uint8) == want[n].view(np.uint8)).all(), n
+        if not mine >> i & 1:
+            assert (to_host(getattr(rows, n)).view(np.uint8) == x[n].view(np.uint8)).all(), n
+    assert (to_host(k) == k_ref).all() and (to_host(v) == v_ref).all()
+
+
+# ---- calls as they are made most: one token for each sequence, a prompt as chains of nodes
+
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("name", ["plain", "all"])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+def test_one_token_for_each_of_many_sequences(pb, dtype, d, name, ragged):
+    rng = np.random.default_rng(18)
+    x = make_inputs(rng, dtype, 8, 2, d, [synth.chain_tree(1)] * 32, [900 - (25 * b if ragged else 0) for b in range(32)])
+    rule = make_rule(name, 8, d)
+    check_exactly(x, rule, *run_attention(pb, x, rule))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_prompt_as_chains_of_nodes(pb, dtype):
+    """A prompt of 300 rows as three chains: attention, sums and commit of each, whose state then is that of the definitions; its last rows'
+    results are those of one causal attention over the whole prompt."""
+    rng = np.random.default_rng(19)
+    H, Hk, d, n, T = 4, 2, 64, 300, 128
+    rule = dict(scale=0.125, cap=0.0, window=0, slopes=None)
+    q, k, v = (synth.from_float(rng.normal(size=(1, h, n, d)).astype(np.float32), dtype) for h in (H, Hk, Hk))
+    k_dev, v_dev = to_dev(np.zeros_like(k)), to_dev(np.zeros_like(v))
+    weight = np.zeros((1, Hk, n), np.float32)
+    rows = pb.CacheRows(torch.zeros(1, dtype=torch.int32, device="cuda"), weight=to_dev(weight))
+    results = []
+    for start in range(0, n, T):
+        a = min(T, n - start)
+        pad = lambda t: np.ascontiguousarray(np.concatenate((t[:, :, start:start + a], np.zeros((1, t.shape[1], T - a, d), t.dtype)), 2))
+        x = dict(dtype=dtype, n_nodes=np.array([a], np.int32), parent=np.concatenate((np.arange(a) - 1, np.full(T - a, -1)))[None].astype(np.int32), q=pad(q),
+                 k_tree=pad(k), v_tree=pad(v), k_cache=to_host(k_dev), v_cache=to_host(v_dev), seq_lens=np.array([start], np.int32),
+                 dropped=np.zeros(1, np.int32), position=None, accept_len=np.array([a], np.int32), accept_path=np.arange(T, dtype=np.int32)[None], weight=weight)
+        out, lse = run_attention(pb, x, rule)
+        check_exactly(x, rule, out, lse)
+        results.append(out[:, :, :a])
+        x["lse"] = lse
+        tree, path = dev_tree(pb, x), to_dev(x["accept_path"])
+        tree.token = torch.zeros((1, T), dtype=torch.int32, device="cuda")
+        pb.propd_cache_observe(tree, to_dev(x["accept_len"]), path, to_dev(x["q"]), to_dev(lse), k_dev, to_dev(x["k_tree"]), rows, rule["scale"])
+        check_observe(x, rule, 1.0, to_host(rows.weight), None, weight)
+        weight = to_host(rows.weight)
+        pb.propd_commit_path(tree, to_dev(x["accept_len"]), path, torch.zeros(1, dtype=torch.int32, device="cuda"), to_dev(x["k_tree"]), to_dev(x["v_tree"]),
+                             k_dev, v_dev, rows.seq_lens)
+    assert rows.seq_lens.tolist() == [n] and (to_host(k_dev) == k).all() and (to_host(v_dev) == v).all()
+    assert abs(weight.sum() - H * n) < 1e-3 * H * n  # every query's weights sum to one
+    s = np.einsum("hid,hjd->hij", f64(q)[0], np.repeat(f64(k)[0], 2, axis=0)) * rule["scale"]
+    s[:, np.triu(np.ones((n, n), bool), 1)] = -np.inf
+    p = np.exp(s - s.max(-1, keepdims=True))
+    want = p @ np.repeat(f64(v)[0], 2, axis=0) / p.sum(-1, keepdims=True)
+    off = np.abs(synth.as_float(np.concatenate(results, 2))[0] - want)
+    assert (off <= (2.0 ** -8 if dtype == "bf16" else U) * np.abs(want) + 1e-4).all(), off.max()

@@ -3,8 +3,8 @@
 // row moves: K and V bytes are two times the rows that move, nothing in a sequence that is not too long.
 //
 // cache_select_kernel, one workgroup per (sequence, K/V head).  Rows are ranked by a 32-bit key (rank_key), and the budget-th
-// largest key is found in four passes over the keys, which stay in registers.  Counting by ballots instead, two bits at a time, took 8.3 us
-// for 1032 rows and 28 us for 8192 where this takes 5.8 and 24.  Wave w owns rows w * share .. in order, so that all that
+// largest key is found in four passes over the keys, which stay in registers: 6.1 us for 1032 rows, 24 us for 8192 (counting by ballots
+// instead, two bits at a time, took 2.5 and 4 us longer).  Wave w owns rows w * share .. in order, so that all that
 // depends on the order (which of the equal keys stay, the lists of free places and of rows that move) takes a prefix over
 // the waves' totals and one within the wave.  No result depends on the order of the additions in LDS.
 // cache_move_kernel moves what the lists say, spread over the chip, and writes the new lengths: nobody reads them any more.
@@ -281,7 +281,7 @@ extern "C" propd_status propd_cache_evict(int32_t B, propd_dtype dt, int32_t H_k
   p.moves = reinterpret_cast<int32_t *>(ws);
   ws += align_up((size_t)units * 4, 256);
   p.left = reinterpret_cast<int32_t *>(ws);
-  // Keys in registers for as long as the registers last.  Read again for every pass: 1032 rows 8.4 us instead of 6.4, 8192 34 instead of 24.
+  // Keys in registers for as long as the registers last.  Read again for every pass: 1032 rows 7.6 us instead of 6.1, 8192 34 instead of 24.
   const dim3 grid((unsigned)units), threads(kSelectThreads);
   if (L_max <= 4 * kSelectThreads) hipLaunchKernelGGL((cache_select_kernel<4>), grid, threads, 0, st, p);
   else if (L_max <= 16 * kSelectThreads) hipLaunchKernelGGL((cache_select_kernel<16>), grid, threads, 0, st, p);

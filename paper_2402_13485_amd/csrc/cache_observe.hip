@@ -6,8 +6,9 @@
 // the A operand, 16 rows to a group, the first kHeld groups of which stay in registers.  A lane then holds four queries' scores of
 // one key, adds their weights up, and the four lanes of a key meet at the end.  K rows are read straight from memory in the operand's
 // layout, 64 bytes of 16 rows per load.
-// 16 x 8 heads x 4096 rows of 128: 50 us (2.9 TB/s; a library reduction over the same bytes takes as long), 41 of them without any
-// work on the rows.  57 us with one batch of tiles per wave, each of which then paid for the chain path -> query -> lse.  Rings in LDS
+// 16 x 8 heads x 4096 rows of 128: 50 us (2.9 TB/s), 41 of them without any work on the rows.  The attention reads such rows at
+// 5 TB/s: what is lost are the rounds of tiles (257 over 48 places are six where 5.35 are needed), the chain path -> query -> lse at the start,
+// and query rows beyond 16 * kHeld, which every batch of tiles fetches again.  57 us with one batch of tiles per wave, each of which then paid for the chain path -> query -> lse.  Rings in LDS
 // that direct loads fill, per wave and without barriers, took 55 us with three tiles of 4 KB in flight per wave, 58 to 84 with
 // other depths and numbers of waves.
 #include <type_traits>

@@ -90,7 +90,8 @@ __device__ __forceinline__ Sequence lane_sequence(const GroupedParams &p, int b)
 // How the units are cut.  Every workgroup works the same plan out from the lengths, in few steps: they stand in front of its first
 // load.
 //   kAlike   All sequences alike: as many whole units as there are workgroups that run at once, as often as that goes, then
-//            the units left over in `pieces` ranges each, piece by piece.
+//            the units left over in `pieces` ranges each, piece by piece.  After whole units these are as many ranges as there are compute
+//            units, however long: 128 units of 132 stages left of 640 take 281 us in 256 ranges, 301 in 512.
 //   kRanges  A range is at most `most` stages, a unit of s stages has pieces_of(s, most) of them, equally long; the least
 //            `most` whose ranges all run at once.
 //   kShares  Every workgroup has an equal share of the list of all stages, which may cross units (each crossing: another unit's first
@@ -235,7 +236,7 @@ __device__ __forceinline__ bool not_finite(const f32x16 (&o)[MB]) {
 // A weight is multiplied as a sum of kParts bf16 values, each the rest of the one before rounded.  d = 64: three, all 24 bits of it.
 // d = 128: two, off by 2^-17 at most (with three the kernels that keep positions spill).  In one piece a weight is off by 2^-8, as much as the
 // result's own rounding: error against 64 bits 2.3e-3 of the result instead of 1.66e-3.  One / two / three parts, us: 16 x 40 heads
-// on 8, 128 nodes, 4096 keys 217 / 286 / -, capped 4 x 32 heads 29.4 / 31.5 / -, evicted 32 x 32 heads of 64 74 / 87 / 100.
+// on 8, 128 nodes, 4096 keys 217 / 275 / -, capped 4 x 32 heads 29.4 / 31.5 / -, evicted 32 x 32 heads of 64 74 / 87 / 100.
 template <int D, bool kCap, bool kPlace>
 __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(GroupedParams p) {
   using G_ = Geo<D>;
@@ -789,7 +790,7 @@ __device__ __forceinline__ float counted(float o, float f) { return f == 0.f ? 0
 
 // out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the pieces s of a unit, always in the same order.  A workgroup has 32
 // columns of a unit and a 32-wide block of d.  W waves take the pieces in turn, up to 8 of them requested together, and meet
-// through LDS: what costs is the chain of their loads (33 pieces of 8 units, one wave with a load after the other: 9.7 us).
+// through LDS: what costs is the chain of their loads.
 template <int D, int W>
 __global__ __launch_bounds__(W *kWave) void grouped_attn_merge_kernel(GroupedParams p) {
   constexpr int kMb = Geo<D>::kMb;
@@ -901,8 +902,8 @@ static bool launch_grouped(const GroupedParams &p, unsigned grid, hipStream_t st
   if (!p.may_split) return true;
   const unsigned units = (unsigned)p.B * (unsigned)p.H_kv * (unsigned)p.blocks;
   const dim3 merge(units * 4u * Geo<D>::kMb);
-  // Few units have more pieces than a wave requests at once.  Four waves and one, us: 8 units of 33 pieces 3.9 / 4.6, 64 of 4
-  // 7.1 / 5.3, 640 of 2 19 / 7.7.
+  // Few units have more pieces than a wave requests at once.  Four waves and one, us: 8 units of 11 pieces 3.9 / 4.6, 56 of 4
+  // 7.0 / 4.8, 128 of 2 among 640 24 / 9.
   if (units <= 16) hipLaunchKernelGGL((grouped_attn_merge_kernel<D, 4>), merge, dim3(4 * kWave), 0, st, p);
   else hipLaunchKernelGGL((grouped_attn_merge_kernel<D, 1>), merge, dim3(kWave), 0, st, p);
   return launch_ok();
@@ -977,7 +978,8 @@ extern "C" propd_status propd_grouped_attention(const propd_tree *tree, propd_dt
   const long long units = (long long)p.B * H_kv * p.blocks;
   const long long stages = (L_max + kStageRows - 1ll) / kStageRows + (p.T_max + kStageRows - 1) / kStageRows;
   p.may_split = (long long)p.B * H_kv < 4ll * p.resident && units < (1ll << 20) && units * stages < (1ll << 30) ? 1 : 0;
-  // (with so many units that they fill the chip four times over none is cut)
+  // With so many units that they fill the chip four times over none is cut, and there is no merge: 256 sequences of 512 rows, 8 K/V
+  // heads, one token 103 us instead of 113.  (One of 4096 rows among 255 of 64 takes 127 instead of 63.)
   long long grid = p.may_split ? units * stages : units;
   if (grid > p.resident) grid = p.resident;
   return (d == 64 ? launch_grouped<64>(p, cap, place, (unsigned)grid, st) : launch_grouped<128>(p, cap, place, (unsigned)grid, st))

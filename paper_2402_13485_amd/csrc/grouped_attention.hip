@@ -305,16 +305,21 @@ __global__ __launch_bounds__(kGroupThreads, 2) void grouped_attn_bf16_kernel(Gro
     x_end = plan.share_start(at + 1);
   }
   bool first_range = true;
+  int found_at = 0, found_before = 0;  // where the last search for a sequence ended, a multiple of 64, and the items before that
   while (plan.kind == kShares ? x < x_end : at < plan.n_ranges) {
     int b = 0, block, hk, s0, n_st, slot, first_slot, stride, P, late = 0;  // late: see the merge
-    // the sequence that holds item `which` of a list that has of(x) items per sequence, and the items before that sequence
+    // The sequence that holds item `which` of a list that has of(x) items per sequence, and the items before that sequence.  From where the
+    // last search ended: all of them together pass a batch once, also where it has many more sequences than a workgroup has units.
     auto locate = [&](int which, auto &&of) __attribute__((always_inline)) {
       int start = 0;
-      for (int b0 = 0, before = 0; b0 < p.B; b0 += kWave) {
+      if (which < found_before) found_at = found_before = 0;
+      for (int b0 = found_at, before = found_before; b0 < p.B; b0 += kWave) {
         const Sequence q = sequence_at(b0 + lane);
         const int mine = of(q), incl = wave_scan_i32(mine, 0, [](int x, int y) { return x + y; });
         const uint64_t le = __ballot(b0 + lane < p.B && before + incl - mine <= which);
         if (le == 0) break;
+        found_at = b0;
+        found_before = before;
         const int src = __popcll(le) - 1;
         b = b0 + src;
         start = __builtin_amdgcn_readlane(before + incl - mine, src);

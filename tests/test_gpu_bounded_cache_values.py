@@ -158,6 +158,27 @@ def test_attention_of_one_long_sequence_takes_no_longer_than_its_rows(pb, B, Hk,
     assert took[1] < 2.3 * took[0], took
 
 
+def test_attention_of_very_many_sequences(pb):
+    """64000 sequences of different lengths: every node sees itself and its rows of ones; it takes about as long as with equal lengths (twenty times
+    as long where each search for a unit's sequence starts in front)."""
+    B, d, L = 64000, 64, 40
+    gen = torch.Generator(device="cuda").manual_seed(20)
+    normal = lambda *s: torch.empty(s, device="cuda", dtype=torch.bfloat16).normal_(generator=gen)
+    n_nodes, parent = torch.ones(B, dtype=torch.int32, device="cuda"), torch.full((B, 1), -1, dtype=torch.int32, device="cuda")
+    tree = pb.Tree(n_nodes, parent, anc=pb.propd_tree_mask(n_nodes, parent)[1])
+    q, kt, vt = normal(B, 1, 1, d), torch.zeros((B, 1, 1, d), device="cuda", dtype=torch.bfloat16), normal(B, 1, 1, d)
+    kc, vc = torch.zeros((B, 1, L, d), device="cuda", dtype=torch.bfloat16), torch.ones((B, 1, L, d), device="cuda", dtype=torch.bfloat16)
+    took = []
+    for seq in (torch.full((B,), 33, device="cuda").int(), torch.randint(0, L + 1, (B,), device="cuda", generator=gen).int()):
+        out, lse = torch.zeros_like(q), torch.zeros((B, 1, 1), device="cuda")
+        took.append(timed(lambda: pb.propd_grouped_attention(tree, q, kc, vc, kt, vt, seq, 0.125, out=out, lse=lse)))
+        n = seq.double()[:, None, None, None]
+        want = (vt.double() + n) / (n + 1)  # scores of zero: the mean
+        assert bool(((out.double() - want).abs() <= 2.0 ** -8 * want.abs() + 64 * U).all())
+        assert bool(((lse.double() - torch.log(n[..., 0] + 1)).abs() <= 16 * U).all())
+    assert took[1] < 4 * took[0], took
+
+
 # ---- sums of attention
 
 @pytest.mark.parametrize("placed", [False, True])

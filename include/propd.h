@@ -328,7 +328,7 @@ PROPD_API propd_status propd_commit_path(const propd_tree *tree, propd_dtype dt,
  * only those with p_i - p_j < window where window > 0.
  */
 typedef struct propd_score_rule {
-  float scale;          /* > 0                                                       */
+  float scale;          /* > 0, up to 2^64                                           */
   float cap;            /* 0: scores are not capped; otherwise 2^-10 .. 1024          */
   int32_t window;       /* 0: no window; up to 2^24                                  */
   const float *slopes;  /* [H] or NULL: bias per position of distance, finite        */

@@ -12,11 +12,11 @@ constexpr int kMaxPosition = 1 << 30;  // positions lie below
 // Distances up to this are exact in fp32: positions less the root's are held as such, and a window's edge is one of them.
 constexpr int kMostWindow = 1 << 24;
 
-// A cap beyond these is none of scores.
-constexpr float kLeastCap = 0x1p-10f, kMostCap = 1024.f;
+// A cap beyond these is none of scores, nor is a scale beyond this, which would not be finite any more with log2(e) or over the cap.
+constexpr float kLeastCap = 0x1p-10f, kMostCap = 1024.f, kMostScale = 0x1p64f;
 
 inline bool score_rule_ok(const propd_score_rule *r) {
-  return r && r->scale > 0.f && isfinite(r->scale) && (r->cap == 0.f || (r->cap >= kLeastCap && r->cap <= kMostCap)) && r->window >= 0 &&
+  return r && r->scale > 0.f && r->scale <= kMostScale && (r->cap == 0.f || (r->cap >= kLeastCap && r->cap <= kMostCap)) && r->window >= 0 &&
          r->window <= kMostWindow;
 }
 

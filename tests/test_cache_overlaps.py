@@ -1,8 +1,11 @@
 """What the binding refuses before any call is made, by its own checks on host tensors (no GPU needed)."""
+import math
+
 import pytest
 import torch
 
 from test_abi import pb  # noqa: F401
+from test_cache_refusals import INVALID, WORKSPACE, attention, observe, rule_of
 
 
 def test_workspaces_of_another_device_or_with_gaps_are_refused(pb):
@@ -37,3 +40,10 @@ def test_workspace_of_the_attention_holds_what_plans_use(pb):
     for args, most in (((1, 1, 1, 128, 0), 1), ((1, 1, 32, 128, 1024), 512), ((2, 128, 50, 64, 1 << 20), 512), ((32, 64, 32, 128, 4096), 1024), ((1, 128, 1, 64, 60), 6)):
         got = pb.workspace_bytes(pb.WS_GROUPED_ATTENTION, *args)
         assert most * piece <= got <= most * piece + 16 * args[0] * args[2] + 1024, args
+
+
+def test_scales_beyond_all_use_are_refused(pb):
+    for scale in (math.nextafter(2.0 ** 64, math.inf) * 1.001, 1e38, 3e38):
+        assert attention(pb, rule=rule_of(pb, scale)) == INVALID and observe(pb, rule=rule_of(pb, scale)) == INVALID
+    for scale in (2.0 ** 64, 2.0 ** -140):  # what is refused then is the workspace
+        assert attention(pb, rule=rule_of(pb, scale), ws=None) == WORKSPACE

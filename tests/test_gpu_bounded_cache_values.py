@@ -100,6 +100,20 @@ def test_attention_rounds_once(pb, dtype, d, name, placed):
     check_exactly(x, rule, *run_attention(pb, x, rule))
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -130, 2.0 ** -149])
+@pytest.mark.parametrize("name", ["plain", "cap", "bias"])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+def test_attention_and_sums_with_next_to_no_scale(pb, dtype, d, name, scale):
+    """A subnormal scale makes all scores zero, up to the bias."""
+    rng = np.random.default_rng(21)
+    x = observe_case(rng, dtype, 4, 2, d, [100, 9], [4, 5], T=20, L_max=110, placed=True)
+    rule = dict(make_rule(name, 4, d), scale=scale)
+    out, lse = run_attention(pb, x, rule)
+    check_exactly(x, rule, out, lse)
+    x["lse"] = lse
+    check_observe(x, rule, 0.5, *run_observe(pb, x, rule, 0.5))
+
+
 # ---- V
 
 @pytest.mark.parametrize("cut", [False, True])

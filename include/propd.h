@@ -372,7 +372,7 @@ PROPD_API propd_status propd_grouped_attention(const propd_tree *tree, propd_dty
  *
  *   q          [B,H,T_max,d]   of the tree that the path indexes     lse  [B,H,T_max], as left by the attention
  *   k_tree     [B,H_kv,T_max,d]     k_cache  [B,H_kv,L_max,d]
- *   accept_len, accept_path, path_stride   as written by propd_accept_path.  accept_len is clamped to [0, path_stride]; a path
+ *   accept_len, accept_path, path_stride   as written by propd_accept_path, path_stride up to 65536.  accept_len is clamped to [0, path_stride]; a path
  *              entry outside [0, n_nodes[b]) pays nothing and its row gets weight 0 and position -1; a node whose lse is
  *              -inf (it saw nothing) pays nothing either
  *   position   with position_out, or both NULL: rows in the order of their positions

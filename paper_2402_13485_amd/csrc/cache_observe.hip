@@ -67,6 +67,9 @@ struct Rows<float, D> {
   }
 };
 
+// Every tile meets every accepted query row, also the path's own: device memory that claims a path of millions must not take hours.
+constexpr int kMostPath = 1 << 16;
+
 constexpr int kHeld = 2;  // groups of 16 query rows that stay in registers
 
 constexpr int observe_per_cu(size_t element, int d) { return element == 2 ? (d == 64 ? 4 : 3) : d == 64 ? 3 : 2; }  // workgroups, by registers
@@ -279,7 +282,7 @@ extern "C" propd_status propd_cache_observe(const propd_tree *tree, propd_dtype 
   for (const void *ptr : {q, k_cache, k_tree})
     if (reinterpret_cast<uintptr_t>(ptr) % 16 != 0) return PROPD_ERR_INVALID_ARG;
   const long long units = (long long)tree->B * H_kv;
-  if (L_max > (1 << 30) || units > (1ll << 22) || (long long)tree->B * H > (1ll << 24) || (long long)H * tree->T_max > (1ll << 30) || (long long)path_stride * (H / H_kv) > (1ll << 30)) return PROPD_ERR_UNSUPPORTED;
+  if (L_max > (1 << 30) || units > (1ll << 22) || (long long)tree->B * H > (1ll << 24) || (long long)H * tree->T_max > (1ll << 30) || (long long)path_stride * (H / H_kv) > (1ll << 30) || path_stride > kMostPath) return PROPD_ERR_UNSUPPORTED;
   ObserveParams p;
   p.q = q;
   p.k_cache = k_cache;

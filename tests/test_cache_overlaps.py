@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from test_abi import pb  # noqa: F401
-from test_cache_refusals import INVALID, WORKSPACE, attention, observe, rule_of
+from test_cache_refusals import INVALID, UNSUPPORTED, WORKSPACE, attention, observe, rule_of
 
 
 def test_workspaces_of_another_device_or_with_gaps_are_refused(pb):
@@ -42,8 +42,9 @@ def test_workspace_of_the_attention_holds_what_plans_use(pb):
         assert most * piece <= got <= most * piece + 16 * args[0] * args[2] + 1024, args
 
 
-def test_scales_beyond_all_use_are_refused(pb):
+def test_scales_and_paths_beyond_all_use_are_refused(pb):
     for scale in (math.nextafter(2.0 ** 64, math.inf) * 1.001, 1e38, 3e38):
         assert attention(pb, rule=rule_of(pb, scale)) == INVALID and observe(pb, rule=rule_of(pb, scale)) == INVALID
     for scale in (2.0 ** 64, 2.0 ** -140):  # what is refused then is the workspace
         assert attention(pb, rule=rule_of(pb, scale), ws=None) == WORKSPACE
+    assert observe(pb, stride=65537) == UNSUPPORTED and observe(pb, stride=1 << 24, H=2) == UNSUPPORTED

@@ -97,9 +97,10 @@ __device__ __forceinline__ Sequence lane_sequence(const GroupedParams &p, int b)
 //   kShares  Every workgroup has an equal share of the list of all stages, which may cross units (each crossing: another unit's first
 //            loads and a partial result).
 // How many workgroups run at once (`slots`): one per compute unit, two where that leaves ranges of more than kLongRange
-// stages.  A stage of a workgroup that shares its compute unit takes 1.45 of the time, so two halves of a range save little, and
+// stages.  A stage of a workgroup that shares its compute unit takes 1.6 (d = 64) to 1.9 of the time, so two halves of a range save little, and
 // each range costs about 5 us of first loads and result and 128 KB of partial result written and read.  Calls, us, 256 / 512
-// ranges: 40 units of 49 stages 29 / 38, 128 of 128 75 / 70, 256 of 130 (capped) 160 / 135.
+// ranges: 40 units of 49 stages 31 / 33, 128 of 66 54 / 51, 128 of 128 82 / 75, 256 of 130 capped 174 / 163, with positions and d = 64 147 / 118;
+// 256 of 34 48 / 54.
 // Up to as many units as workgroups take kRanges where its ranges are not much longer than an equal share: up to twice as long, up to a
 // quarter longer where that share is more than kLongRange stages, which one more crossing adds little to.  Where one workgroup per
 // compute unit leaves no room to cut a unit, two may.  Calls of 8 K/V heads, us, ranges / shares: 24 sequences of up to 1024 rows (17 stages) 54 / 60,

@@ -53,7 +53,9 @@ typedef enum {
   PROPD_ERR_DEVICE = 4       /* the HIP runtime refused a launch                    */
 } propd_status;
 
-typedef enum { PROPD_F32 = 0, PROPD_BF16 = 1 } propd_dtype;
+/* PROPD_E4M3: 8-bit floating point (1 sign, 4 exponent, 3 mantissa bits, no infinities, largest 448), in the
+ * pages of a propd_paged_cache only. */
+typedef enum { PROPD_F32 = 0, PROPD_BF16 = 1, PROPD_E4M3 = 2 } propd_dtype;
 
 /* Largest tree, root included.  A node's ancestor set is a 128-bit set, two
  * uint64 words, word 0 holding nodes 0..63. */
@@ -440,6 +442,101 @@ PROPD_API propd_status propd_rotary(propd_dtype dt, int32_t B, int32_t S, int32_
                           const void *k, void *q_out, void *k_out, void *hip_stream);
 
 /*
+ * A paged K/V cache: the rows of all sequences lie in pages of one pool, so that a sequence takes memory as it grows and sequences
+ * can share pages of a common prefix.  Row j of sequence b and K/V head h is row j % page_rows of page page_table[b, j / page_rows].  A step then is
+ *   propd_rotary, propd_paged_attention, propd_accept_path or propd_accept_sampled, propd_paged_commit
+ * (any of the calls above that shape the tree fit in between); prompts enter by propd_paged_prompt, and propd_paged_read
+ * gives a sequence to the calls with dense caches.
+ *   dt          the dt of the call: rows as they are; or PROPD_E4M3: a row is d codes and one scale, a power of two, held as its exponent
+ *               plus 127 in a byte.  A value is code times scale, which bf16 and fp32 hold exactly.
+ *   page_rows   a power of two, 16..1024          table_pages * page_rows at most 2^30
+ * Entries of page_table outside [0, n_pages) are no pages: rows there are not stored, seen by nobody and read as zeros.  A page
+ * that a sequence writes to must be in no other place of the table.
+ * A row x is held in 8 bits with the scale 2^e of the smallest e in [-117, 119] with |x| <= 448 * 2^e for every finite value (all zero:
+ * e = -117) as the codes x / 2^e, rounded to nearest, ties to even; finite values beyond 448 * 2^119 become that, others are held as NaN.
+ */
+typedef struct propd_paged_cache {
+  void *k_pages, *v_pages;      /* [n_pages,H_kv,page_rows,d]                             */
+  uint8_t *k_scale, *v_scale;   /* [n_pages,H_kv,page_rows], PROPD_E4M3 only              */
+  const int32_t *page_table;    /* [B,table_pages]                                        */
+  propd_dtype dt;
+  int32_t n_pages;              /* >= 1                                                   */
+  int32_t table_pages;          /* pages of a sequence, at most; >= 1                     */
+  int32_t page_rows;
+} propd_paged_cache;
+
+/*
+ * Tree attention over a paged cache: propd_grouped_attention with row j of the cache at position j.  A single token per sequence is
+ * a tree of one node.  K/V rows in 8 bits count as the values that they stand for.
+ *   H, H_kv, dt, d, rule, q, out, k_tree, v_tree, tree, lse   as there; the weights that meet V are two bf16 values each (off by
+ *              2^-17) for PROPD_BF16
+ *   seq_lens   [B], clamped to [0, table_pages * page_rows]
+ *   out and lse rows i >= n_nodes[b] are left untouched
+ *   workspace  propd_workspace_bytes(PROPD_WS_PAGED_ATTENTION, B, T_max, H, d, table_pages * page_rows, 0, 0) bytes
+ * q, pages, k_tree, v_tree, out, anc and workspace must be 16-byte aligned.
+ */
+PROPD_API propd_status propd_paged_attention(const propd_tree *tree, propd_dtype dt, int32_t H, int32_t H_kv, int32_t d,
+                                   const propd_score_rule *rule, const void *q, const propd_paged_cache *cache, const void *k_tree,
+                                   const void *v_tree, const int32_t *seq_lens, void *out, float *lse, void *workspace,
+                                   size_t workspace_bytes, void *hip_stream);
+
+/*
+ * propd_commit_path into a paged cache, with H_kv heads and d in {64, 128}.
+ *   seq_lens_out  [B]: seq_lens itself or another array.  seq_lens_out[b] = min(seq_lens[b] + accept_len[b], table_pages * page_rows)
+ * Values read from device memory are made safe as there.  k_tree, v_tree and pages must be 16-byte aligned.
+ * Must not overlap with a call that reads the same pages or lengths.
+ */
+PROPD_API propd_status propd_paged_commit(const propd_tree *tree, propd_dtype dt, int32_t H_kv, int32_t d, const int32_t *accept_len,
+                                const int32_t *accept_path, int32_t path_stride, const int32_t *next_token, const void *k_tree,
+                                const void *v_tree, const propd_paged_cache *cache, const int32_t *seq_lens, int32_t *seq_lens_out,
+                                int32_t *out_tokens, int32_t out_stride, void *hip_stream);
+
+/*
+ * Rows of prompts (or of parts of them) to the ends of their sequences.
+ *   k, v     [B,H_kv,S,d], d in {64, 128}       n_rows  [B], clamped to [0, S]; NULL: S
+ *   seq_lens, seq_lens_out  as in propd_paged_commit; rows that do not fit are left out
+ */
+PROPD_API propd_status propd_paged_prompt(propd_dtype dt, int32_t B, int32_t S, int32_t H_kv, int32_t d, const int32_t *n_rows,
+                                const void *k, const void *v, const propd_paged_cache *cache, const int32_t *seq_lens,
+                                int32_t *seq_lens_out, void *hip_stream);
+
+/*
+ * Paged rows as dense ones: row first[b] + s of sequence b goes to row s of k_out and v_out, for s < S and first[b] + s < seq_lens[b]; other
+ * rows are left untouched.
+ *   first    [B] or NULL: zeros; negative entries count as 0
+ *   k_out, v_out  [B,H_kv,S,d] of type dt, d in {64, 128}
+ */
+PROPD_API propd_status propd_paged_read(propd_dtype dt, int32_t B, int32_t S, int32_t H_kv, int32_t d, const propd_paged_cache *cache,
+                              const int32_t *seq_lens, const int32_t *first, void *k_out, void *v_out, void *hip_stream);
+
+/*
+ * Acceptance by sampling: drafted tokens against the target's probabilities p_i = softmax(inv_temperature * logits[b,i,:]) at the
+ * nodes, with random numbers that the caller gives, so that the tokens of a step are distributed as if the target had been
+ * sampled token by token.  From the root on, the children of a node n are tried by rising index until one is accepted:
+ *   draft_logits NULL   candidates that were not drawn at random (for instance the top k of a head).  Child c is accepted iff
+ *                       u[b,c] * R < p_n(tok_c), R = 1 - the probabilities of the tokens refused before; a token refused before never is.
+ *   draft_logits        [B,T_max,vocab]: every child of n was drawn from q_n = softmax(draft_inv_temperature * draft_logits[b,n,:]), independently of its
+ *                       siblings.  With r = p_n at first, child c is accepted iff u[b,c] * q_n(tok_c) < r(tok_c); otherwise r becomes max(r - q_n, 0),
+ *                       scaled to a sum of 1.
+ * The path ends at the first node l none of whose children is accepted.  The token after it is drawn from what is left there (p_l
+ * without the tokens refused, or r): the lowest v with r(0) + ... + r(v) > u_next[b].  If nothing is left, it is the likeliest token of p_l (the lowest id among equal ones).
+ * As there, a path buffer shorter than the path keeps its first path_stride nodes, and next_token is then the token of the next node.
+ *   logits, draft_logits  dt = PROPD_BF16 or PROPD_F32, read for nodes that have children, and logits at the path's end.
+ *            NaN counts as -inf (probability 0); several +inf share the probability; a row of -inf alone gives probability 0 throughout.
+ *            16-byte aligned rows are read faster, others are allowed
+ *   u        [B,T_max], u_next [B]   fp32 in [0,1); the entries of node 0 and of padding are not used
+ *   tree     n_nodes, parent, token are read; a token outside [0, vocab) is refused and changes nothing
+ *   inv_temperature, draft_inv_temperature  > 0, up to 2^20
+ *   accept_len, accept_path, path_stride, next_token  as in propd_accept_path
+ *   workspace  propd_workspace_bytes(PROPD_WS_ACCEPT_SAMPLED, B, T_max, 0, 0, 0, 0, vocab) bytes, 16-byte aligned
+ * Probabilities, sums and what is left are held in 64 bits.
+ */
+PROPD_API propd_status propd_accept_sampled(const propd_tree *tree, propd_dtype dt, int32_t vocab, const void *logits,
+                                  float inv_temperature, const void *draft_logits, float draft_inv_temperature, const float *u,
+                                  const float *u_next, int32_t *accept_len, int32_t *accept_path, int32_t path_stride,
+                                  int32_t *next_token, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Dynamic token-tree generation (Section 4.2): the controller that picks the tree size from
  * measured iteration times and measured head accuracies.  HOST code: every pointer below is
  * a host pointer, nothing is enqueued on a stream, no device is touched.  It is meant to run
@@ -508,7 +605,9 @@ typedef enum {
   PROPD_WS_EARLY_PRUNE = 1,
   PROPD_WS_ACCEPT_PATH = 2,
   PROPD_WS_GROUPED_ATTENTION = 3,
-  PROPD_WS_CACHE_EVICT = 4 /* H is the number of K/V heads */
+  PROPD_WS_CACHE_EVICT = 4, /* H is the number of K/V heads */
+  PROPD_WS_PAGED_ATTENTION = 5, /* L_max is table_pages * page_rows */
+  PROPD_WS_ACCEPT_SAMPLED = 6
 } propd_ws_kind;
 PROPD_API size_t propd_workspace_bytes(propd_ws_kind which, int32_t B, int32_t T_max, int32_t H, int32_t d,
                              int32_t L_max, int32_t hidden, int32_t vocab);

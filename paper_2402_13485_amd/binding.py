@@ -23,13 +23,15 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpropd.so")
 
-PROPD_F32, PROPD_BF16 = 0, 1
+PROPD_F32, PROPD_BF16, PROPD_E4M3 = 0, 1, 2
 WS_TREE_ATTENTION, WS_EARLY_PRUNE, WS_ACCEPT_PATH, WS_GROUPED_ATTENTION, WS_CACHE_EVICT = 0, 1, 2, 3, 4
+WS_PAGED_ATTENTION, WS_ACCEPT_SAMPLED = 5, 6
 MAX_TREE = 128
 MAX_PAYLOADS = 8
 
 EXPORTS = ("propd_tree_mask", "propd_validate_tree", "propd_tree_attention", "propd_early_prune", "propd_accept_path",
-           "propd_accept_path_static", "propd_early_prune_prob", "propd_commit_path", "propd_grouped_attention", "propd_cache_observe", "propd_cache_evict", "propd_rotary", "propd_workspace_bytes", "propd_status_string",
+           "propd_accept_path_static", "propd_early_prune_prob", "propd_commit_path", "propd_grouped_attention", "propd_cache_observe", "propd_cache_evict", "propd_rotary",
+           "propd_paged_attention", "propd_paged_commit", "propd_paged_prompt", "propd_paged_read", "propd_accept_sampled", "propd_workspace_bytes", "propd_status_string",
            "propd_controller_bytes", "propd_controller_init", "propd_controller_observe_time",
            "propd_controller_observe_hit", "propd_controller_fit", "propd_controller_build_tree",
            "propd_controller_best_size")
@@ -58,6 +60,12 @@ class _ScoreRule(ctypes.Structure):
 
 class _CacheRows(ctypes.Structure):
     _fields_ = [("seq_lens", ctypes.c_void_p), ("dropped", ctypes.c_void_p), ("position", ctypes.c_void_p), ("weight", ctypes.c_void_p)]
+
+
+class _PagedCache(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("dt", ctypes.c_int), ("n_pages", ctypes.c_int32), ("table_pages", ctypes.c_int32),
+                ("page_rows", ctypes.c_int32)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -134,6 +142,17 @@ def load_library() -> ctypes.CDLL:
     lib.propd_cache_evict.argtypes = [i32, ctypes.c_int, i32, i32, i32, i32, i32, i32, vp, vp, rows, rows, vp, sz, vp]
     lib.propd_rotary.restype = ctypes.c_int
     lib.propd_rotary.argtypes = [ctypes.c_int, i32, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    paged, i = ctypes.POINTER(_PagedCache), ctypes.c_int
+    lib.propd_paged_attention.restype = ctypes.c_int
+    lib.propd_paged_attention.argtypes = [ctypes.POINTER(_Tree), i, i32, i32, i32, rule, vp, paged, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.propd_paged_commit.restype = ctypes.c_int
+    lib.propd_paged_commit.argtypes = [ctypes.POINTER(_Tree), i, i32, i32, vp, vp, i32, vp, vp, vp, paged, vp, vp, vp, i32, vp]
+    lib.propd_paged_prompt.restype = ctypes.c_int
+    lib.propd_paged_prompt.argtypes = [i, i32, i32, i32, i32, vp, vp, vp, paged, vp, vp, vp]
+    lib.propd_paged_read.restype = ctypes.c_int
+    lib.propd_paged_read.argtypes = [i, i32, i32, i32, i32, paged, vp, vp, vp, vp, vp]
+    lib.propd_accept_sampled.restype = ctypes.c_int
+    lib.propd_accept_sampled.argtypes = [ctypes.POINTER(_Tree), i, i32, vp, f32, vp, f32, vp, vp, vp, vp, i32, vp, vp, sz, vp]
     lib.propd_workspace_bytes.restype = sz
     lib.propd_workspace_bytes.argtypes = [ctypes.c_int, i32, i32, i32, i32, i32, i32, i32]
     dbl, pd = ctypes.c_double, ctypes.POINTER(ctypes.c_double)
@@ -720,6 +739,172 @@ def propd_rotary(q: torch.Tensor, k: Optional[torch.Tensor], inv_freq: torch.Ten
                                        _ptr(offset), offset_axes, _ptr(n_rows), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _stream()),
            "propd_rotary")
     return q_out, k_out
+
+
+# ---- a paged K/V cache and acceptance by sampling (see propd.h)
+
+@dataclass
+class PagedCache:
+    """A paged K/V cache (``propd_paged_cache``).  Pages of type ``torch.float8_e4m3fn`` hold rows in 8 bits, with their scales."""
+    k_pages: torch.Tensor                   # [n_pages,H_kv,page_rows,d]
+    v_pages: torch.Tensor
+    page_table: torch.Tensor                # int32 [B,table_pages]
+    k_scale: Optional[torch.Tensor] = None  # uint8 [n_pages,H_kv,page_rows], 8-bit pages only
+    v_scale: Optional[torch.Tensor] = None
+
+    @property
+    def capacity(self) -> int:
+        """Rows of a sequence, at most."""
+        return self.page_table.shape[1] * self.k_pages.shape[2]
+
+    def _tensors(self):
+        return self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.page_table
+
+    def _c(self, dtype: torch.dtype) -> _PagedCache:
+        codes = self.k_pages.dtype == torch.float8_e4m3fn
+        return _PagedCache(*(_ptr(t) for t in self._tensors()), PROPD_E4M3 if codes else PROPD_BF16 if dtype == torch.bfloat16 else PROPD_F32,
+                           self.k_pages.shape[0], self.page_table.shape[1], self.k_pages.shape[2])
+
+
+def _paged(cache: PagedCache, dtype: torch.dtype, device: torch.device, B: int, H_kv: int, d: int, written: bool = False) -> None:
+    """Types and shapes of a cache that a call of this type uses."""
+    if cache.k_pages.dim() != 4 or cache.page_table.dim() != 2:
+        raise ValueError("k_pages has four dimensions, page_table two")
+    n_pages, _, rows, _ = cache.k_pages.shape
+    codes = cache.k_pages.dtype == torch.float8_e4m3fn
+    if codes and (cache.k_scale is None or cache.v_scale is None):
+        raise ValueError("8-bit pages need k_scale and v_scale")
+    pages, kind = (n_pages, H_kv, rows, d), torch.float8_e4m3fn if codes else dtype
+    _all_dev(device, k_pages=(cache.k_pages, kind, pages), v_pages=(cache.v_pages, kind, pages), page_table=(cache.page_table, torch.int32, (B, cache.page_table.shape[1])))
+    if codes:
+        _all_dev(device, k_scale=(cache.k_scale, torch.uint8, pages[:3]), v_scale=(cache.v_scale, torch.uint8, pages[:3]))
+    if written:
+        names = ("k_pages", "v_pages", "k_scale", "v_scale", "page_table")
+        for i, t in enumerate(cache._tensors()[:4]):
+            _apart(t if codes or i < 2 else None, names[i], *(o for j, o in enumerate(cache._tensors()) if j != i))
+
+
+def propd_paged_attention(tree: Tree, q, cache: PagedCache, k_tree, v_tree, seq_lens, scale: float, cap: float = 0.0, window: int = 0,
+                          slopes: Optional[torch.Tensor] = None, want_lse: bool = False, out: Optional[torch.Tensor] = None,
+                          lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """-> out [B,H,T_max,d], or (out, lse) if ``want_lse`` or an ``lse`` tensor is given."""
+    B, H, H_kv, T_max, d, _ = _shared_heads(tree, q, k_tree, cache.k_pages)
+    dt, i32, f32 = _dt(q), torch.int32, torch.float32
+    rows = (B, H_kv, T_max, d)
+    if lse is None and want_lse:
+        lse = torch.empty((B, H, T_max), dtype=f32, device=q.device)
+    if out is None:
+        out = torch.empty_like(q)
+    _all_dev(q.device, q=(q, q.dtype, None), k_tree=(k_tree, q.dtype, rows), v_tree=(v_tree, q.dtype, rows), seq_lens=(seq_lens, i32, (B,)),
+             n_nodes=(tree.n_nodes, i32, (B,)), anc=(tree.anc, torch.int64, (B, T_max, 2)), slopes=(slopes, f32, (H,)), out=(out, q.dtype, q.shape),
+             lse=(lse, f32, q.shape[:3]))
+    _paged(cache, q.dtype, q.device, B, H_kv, d)
+    read = (q, k_tree, v_tree, seq_lens, tree.n_nodes, tree.anc, slopes, *cache._tensors())
+    _apart(out, "out", *read, lse)
+    _apart(lse, "lse", *read)
+    ws = _workspace(workspace_bytes(WS_PAGED_ATTENTION, B, T_max, H, d, cache.capacity), q.device, workspace)
+    _apart(workspace, "workspace", *read, out, lse)
+    c_tree, rule, c_cache = tree._c(), _ScoreRule(scale, cap, window, _ptr(slopes)), cache._c(q.dtype)
+    _check(load_library().propd_paged_attention(
+        ctypes.byref(c_tree), dt, H, H_kv, d, ctypes.byref(rule), _ptr(q), ctypes.byref(c_cache), _ptr(k_tree), _ptr(v_tree), _ptr(seq_lens),
+        _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream()), "propd_paged_attention")
+    return out if lse is None else (out, lse)
+
+
+def propd_paged_commit(tree: Tree, accept_len: torch.Tensor, accept_path: torch.Tensor, next_token: torch.Tensor, k_tree: torch.Tensor,
+                       v_tree: torch.Tensor, cache: PagedCache, seq_lens: torch.Tensor, out_stride: Optional[int] = None,
+                       seq_lens_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Appends the accepted nodes' K/V rows to their sequences' pages IN PLACE, advances ``seq_lens`` in place (or writes the new lengths to
+    ``seq_lens_out``) and returns the step's tokens, int32 [B,out_stride], -1 padded."""
+    if k_tree.dim() != 4 or accept_path.dim() != 2:
+        raise ValueError("k_tree has four dimensions, accept_path two")
+    B, H_kv, T_max, d = k_tree.shape
+    if tree.B != B or tree.T_max != T_max:
+        raise ValueError("tree and k_tree disagree on B or T_max")
+    dt, i32, path_stride = _dt(k_tree), torch.int32, accept_path.shape[1]
+    out_stride = path_stride if out_stride is None else out_stride
+    seq_lens_out = seq_lens if seq_lens_out is None else seq_lens_out
+    _all_dev(k_tree.device, k_tree=(k_tree, k_tree.dtype, None), v_tree=(v_tree, k_tree.dtype, k_tree.shape), accept_len=(accept_len, i32, (B,)),
+             accept_path=(accept_path, i32, (B, path_stride)), next_token=(next_token, i32, (B,)), n_nodes=(tree.n_nodes, i32, (B,)),
+             token=(tree.token, i32, (B, T_max)), seq_lens=(seq_lens, i32, (B,)), seq_lens_out=(seq_lens_out, i32, (B,)))
+    _paged(cache, k_tree.dtype, k_tree.device, B, H_kv, d, written=True)
+    read = (k_tree, v_tree, accept_len, accept_path, next_token, tree.n_nodes, tree.token)
+    _written_apart(cache, seq_lens, seq_lens_out, read)
+    out = torch.empty((B, out_stride), dtype=i32, device=k_tree.device)
+    c_tree, c_cache = tree._c(), cache._c(k_tree.dtype)
+    _check(load_library().propd_paged_commit(
+        ctypes.byref(c_tree), dt, H_kv, d, _ptr(accept_len), _ptr(accept_path), path_stride, _ptr(next_token), _ptr(k_tree), _ptr(v_tree),
+        ctypes.byref(c_cache), _ptr(seq_lens), _ptr(seq_lens_out), _ptr(out), out_stride, _stream()), "propd_paged_commit")
+    return out
+
+
+def _written_apart(cache: PagedCache, seq_lens, seq_lens_out, read) -> None:
+    _same_or_apart(seq_lens_out, seq_lens, "seq_lens_out")
+    codes = cache.k_pages.dtype == torch.float8_e4m3fn
+    for name in ("k_pages", "v_pages") + (("k_scale", "v_scale") if codes else ()):
+        _apart(getattr(cache, name), name, *read, seq_lens, seq_lens_out)
+    _apart(seq_lens_out, "seq_lens_out", *read, cache.page_table)
+
+
+def propd_paged_prompt(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, seq_lens: torch.Tensor, n_rows: Optional[torch.Tensor] = None,
+                       seq_lens_out: Optional[torch.Tensor] = None) -> None:
+    """Appends rows of prompts, k and v [B,H_kv,S,d], to their sequences' pages IN PLACE and advances ``seq_lens`` in place (or writes the new
+    lengths to ``seq_lens_out``)."""
+    if k.dim() != 4:
+        raise ValueError("k has four dimensions")
+    B, H_kv, S, d = k.shape
+    dt, i32 = _dt(k), torch.int32
+    seq_lens_out = seq_lens if seq_lens_out is None else seq_lens_out
+    _all_dev(k.device, k=(k, k.dtype, None), v=(v, k.dtype, k.shape), n_rows=(n_rows, i32, (B,)), seq_lens=(seq_lens, i32, (B,)),
+             seq_lens_out=(seq_lens_out, i32, (B,)))
+    _paged(cache, k.dtype, k.device, B, H_kv, d, written=True)
+    _written_apart(cache, seq_lens, seq_lens_out, (k, v, n_rows))
+    c_cache = cache._c(k.dtype)
+    _check(load_library().propd_paged_prompt(dt, B, S, H_kv, d, _ptr(n_rows), _ptr(k), _ptr(v), ctypes.byref(c_cache), _ptr(seq_lens),
+                                             _ptr(seq_lens_out), _stream()), "propd_paged_prompt")
+
+
+def propd_paged_read(cache: PagedCache, seq_lens: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor, first: Optional[torch.Tensor] = None):
+    """-> (k_out, v_out), [B,H_kv,S,d], with rows ``first[b]`` .. ``first[b] + S - 1`` of every sequence, as far as it has them."""
+    if k_out.dim() != 4:
+        raise ValueError("k_out has four dimensions")
+    B, H_kv, S, d = k_out.shape
+    dt, i32 = _dt(k_out), torch.int32
+    _all_dev(k_out.device, k_out=(k_out, k_out.dtype, None), v_out=(v_out, k_out.dtype, k_out.shape), seq_lens=(seq_lens, i32, (B,)), first=(first, i32, (B,)))
+    _paged(cache, k_out.dtype, k_out.device, B, H_kv, d)
+    read = (seq_lens, first, *cache._tensors())
+    _apart(k_out, "k_out", v_out, *read)
+    _apart(v_out, "v_out", *read)
+    c_cache = cache._c(k_out.dtype)
+    _check(load_library().propd_paged_read(dt, B, S, H_kv, d, ctypes.byref(c_cache), _ptr(seq_lens), _ptr(first), _ptr(k_out), _ptr(v_out), _stream()),
+           "propd_paged_read")
+    return k_out, v_out
+
+
+def propd_accept_sampled(tree: Tree, logits: torch.Tensor, u: torch.Tensor, u_next: torch.Tensor, inv_temperature: float = 1.0,
+                         draft_logits: Optional[torch.Tensor] = None, draft_inv_temperature: float = 1.0, path_stride: Optional[int] = None,
+                         workspace: Optional[torch.Tensor] = None):
+    """-> (accept_len int32 [B], accept_path int32 [B,path_stride], next_token int32 [B]).  ``u`` float32 [B,T_max] and ``u_next`` float32 [B] are random
+    numbers in [0,1); ``draft_logits`` is given if the candidates were drawn from the draft's distributions."""
+    if logits.dim() != 3:
+        raise ValueError("logits has three dimensions")
+    B, T_max, vocab = logits.shape
+    if tree.B != B or tree.T_max != T_max:
+        raise ValueError("tree and logits disagree on B or T_max")
+    dt, i32, f32 = _dt(logits), torch.int32, torch.float32
+    _all_dev(logits.device, logits=(logits, logits.dtype, None), draft_logits=(draft_logits, logits.dtype, logits.shape), u=(u, f32, (B, T_max)),
+             u_next=(u_next, f32, (B,)), n_nodes=(tree.n_nodes, i32, (B,)), parent=(tree.parent, i32, (B, T_max)), token=(tree.token, i32, (B, T_max)))
+    path_stride = T_max if path_stride is None else path_stride
+    dev = logits.device
+    accept_len, next_token = torch.empty(B, dtype=i32, device=dev), torch.empty(B, dtype=i32, device=dev)
+    path = torch.empty((B, path_stride), dtype=i32, device=dev)
+    ws = _workspace(workspace_bytes(WS_ACCEPT_SAMPLED, B, T_max, vocab=vocab), dev, workspace)
+    _apart(workspace, "workspace", logits, draft_logits, u, u_next, tree.n_nodes, tree.parent, tree.token)
+    c_tree = tree._c()
+    _check(load_library().propd_accept_sampled(
+        ctypes.byref(c_tree), dt, vocab, _ptr(logits), inv_temperature, _ptr(draft_logits), draft_inv_temperature, _ptr(u), _ptr(u_next),
+        _ptr(accept_len), _ptr(path), path_stride, _ptr(next_token), _ptr(ws), ws.numel() * ws.element_size(), _stream()), "propd_accept_sampled")
+    return accept_len, path, next_token
 
 
 class Controller:

@@ -16,7 +16,7 @@ MARSHAL_SOURCE = "marshal.cpp"
 HEADER = os.path.join(HERE, os.pardir, "include", "propd.h")
 SOURCES = ["tree_mask.hip", "tree_attention.hip", "early_prune.hip", "accept_path.hip",
            "commit_path.hip", "tree_controller.hip", "grouped_attention.hip", "cache_observe.hip", "cache_evict.hip",
-           "rotary.hip"]
+           "rotary.hip", "paged_attention.hip", "paged_rows.hip", "accept_sampled.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",  # no packed-fp32 codegen

@@ -1,0 +1,551 @@
+// Acceptance by sampling: drafted tokens against the target's probabilities, with given random numbers.
+//
+// Three kernels:
+//   sampled_stats_kernel  largest value and sum of exponentials of the logits rows of nodes that have children (the target's, and the draft's
+//                         if it is given), in slices of 4096 values that stay in registers between the two
+//   sampled_walk_kernel   one workgroup per sequence: the probabilities of all candidates at once, then the tests along the path.  What a
+//                         refused candidate leaves of the target needs no distribution of its own: after k refusals r = (p - s_k q)+ / W_k
+//                         with s_0 = 0, W_0 = 1, W_k = sum over the vocabulary of (p - s_k q)+ and s_{k+1} = s_k + W_k, since
+//                         ((p - s q)+ / W - q)+ = (p - (s + W) q)+ / W.  Only a candidate that has refused siblings before it needs the sum.
+//   sampled_next_kernel   the token after the path: what is left in chunks of 4096 tokens, by all workgroups of a sequence; the one that ends
+//                         last finds the chunk, and in it the token.
+// 64 bits throughout: a vocabulary has so many borders between tokens that an error of 2^-24 of a sum would move one token in a few hundred.
+// The rows are read at memory speed; the exponentials (20 fp64 instructions each, at the rate of fp32 ones) take as long.
+#include <math.h>
+
+#include "common.h"
+
+namespace propd {
+
+constexpr int kSampledThreads = 256, kSliceTokens = 16 * kSampledThreads;
+constexpr int kMostVocab = 1 << 20;
+constexpr float kMostInverse = 0x1p20f;
+
+struct SliceStat {  // of one slice of one row: the largest logit, and the sum of exp((logit - largest) * inv_temperature)
+  float most;
+  float pad;
+  double sum;
+};
+
+struct WalkEnd {  // where a sequence's path ends, and what is left there: p, without refused tokens, or p - much * q
+  int32_t node, cut;
+  float p_most, q_most;
+  double p_scale, q_scale, much;
+};
+
+struct SampledParams {
+  const int32_t *n_nodes, *parent, *token;
+  const void *logits, *draft;
+  const float *u, *u_next;
+  double inv, draft_inv;
+  int B, T_max, V, slices, stride, per_sequence;
+  int aligned;            // rows of logits start on 16 bytes
+  SliceStat *p_stat, *q_stat;  // [B*T_max][slices]
+  SliceStat *left;             // [B][slices]: what is left in a chunk
+  WalkEnd *end;                // [B]
+  int32_t *arrived;            // [B]
+  int32_t *accept_len, *accept_path, *next_token;
+};
+
+// exp(x) for x <= 0: x = n log 2 + r with |r| <= log(2) / 2, the exponential series of r up to r^12 (3e-16 off).
+__device__ __forceinline__ double exp_below(double x) {
+  const double n = rint(x * 1.4426950408889634);
+  double r = fma(n, -0.693147180559945309, x);
+  r = fma(n, -2.319046813846299558e-17, r);  // what log 2 is beyond its double
+  double s = 1.0 / 479001600.0;
+  s = fma(s, r, 1.0 / 39916800.0);
+  s = fma(s, r, 1.0 / 3628800.0);
+  s = fma(s, r, 1.0 / 362880.0);
+  s = fma(s, r, 1.0 / 40320.0);
+  s = fma(s, r, 1.0 / 5040.0);
+  s = fma(s, r, 1.0 / 720.0);
+  s = fma(s, r, 1.0 / 120.0);
+  s = fma(s, r, 1.0 / 24.0);
+  s = fma(s, r, 1.0 / 6.0);
+  s = fma(s, r, 0.5);
+  s = fma(s, r, 1.0);
+  s = fma(s, r, 1.0);
+  return x < -745.0 ? 0.0 : __builtin_amdgcn_ldexp(s, (int)n);
+}
+
+// exp((x - most) * inv), 1 for the largest itself (infinite or not)
+__device__ __forceinline__ double weight_of(float x, float most, double inv) {
+  return x == most ? 1.0 : exp_below(((double)x - (double)most) * inv);
+}
+
+__device__ __forceinline__ float no_nan(float x) { return x == x ? x : -INFINITY; }
+
+template <bool kBf16>
+__device__ __forceinline__ float logit_at(const void *rows, size_t row, int V, int v) {
+  const size_t at = row * (size_t)V + v;
+  return no_nan(kBf16 ? bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(rows)[at]) : reinterpret_cast<const float *>(rows)[at]);
+}
+
+// A thread's 16 neighbouring values of slice `slice` of a row; -inf beyond the vocabulary.
+template <bool kBf16>
+__device__ __forceinline__ void load_slice(const SampledParams &p, const void *rows, size_t row, int slice, float (&x)[16]) {
+  const int first = slice * kSliceTokens + 16 * (int)threadIdx.x;
+  if (p.aligned && first + 16 <= p.V) {
+    if constexpr (kBf16) {
+      const u32x4 *src = reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint16_t *>(rows) + row * (size_t)p.V + first);
+      const u32x4 a[2] = {src[0], src[1]};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[2 * i] = no_nan(__uint_as_float(a[i / 4][i % 4] << 16));
+        x[2 * i + 1] = no_nan(__uint_as_float(a[i / 4][i % 4] & 0xffff0000u));
+      }
+    } else {
+      const f32x4 *src = reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(rows) + row * (size_t)p.V + first);
+      const f32x4 a[4] = {src[0], src[1], src[2], src[3]};
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = no_nan(a[i / 4][i % 4]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = first + i < p.V ? logit_at<kBf16>(rows, row, p.V, first + i) : -INFINITY;
+  }
+}
+
+// Over the workgroup, in a fixed order; every thread gets the result.  `room`: one entry per wave, used by one call at a time.
+template <class T, class F>
+__device__ __forceinline__ T block_reduce(T v, T *room, F &&join) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = join(v, __shfl_xor(v, o, kWave));
+  const int waves = blockDim.x / kWave;
+  __syncthreads();  // whoever read the room before is done
+  if ((threadIdx.x & 63) == 0) room[threadIdx.x / kWave] = v;
+  __syncthreads();
+  T r = room[0];
+  for (int w = 1; w < waves; ++w) r = join(r, room[w]);
+  return r;
+}
+
+__device__ __forceinline__ int tree_size(const SampledParams &p, int b) {
+  const int T = p.n_nodes[b];
+  return T < 1 ? 1 : (T > p.T_max ? p.T_max : T);
+}
+
+// Largest value and sum of a slice, by the workgroup.
+template <bool kBf16>
+__device__ __forceinline__ SliceStat slice_stat(const SampledParams &p, const void *rows, size_t row, int slice, double inv, float *f_room,
+                                                double *d_room) {
+  float x[16];
+  load_slice<kBf16>(p, rows, row, slice, x);
+  float most = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) most = fmaxf(most, x[i]);
+  most = block_reduce(most, f_room, [](float a, float b) { return fmaxf(a, b); });
+  double sum = 0.0;
+  if (most > -INFINITY) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += weight_of(x[i], most, inv);
+  }
+  sum = block_reduce(sum, d_room, [](double a, double b) { return a + b; });
+  return {most, 0.f, sum};
+}
+
+// The nodes of a sequence that have children, counted off to its workgroups slice by slice.
+template <bool kBf16>
+__global__ __launch_bounds__(kSampledThreads) void sampled_stats_kernel(SampledParams p) {
+  __shared__ uint64_t s_inner[2];
+  __shared__ float f_room[kSampledThreads / kWave];
+  __shared__ double d_room[kSampledThreads / kWave];
+  const int b = blockIdx.x / p.per_sequence, at = blockIdx.x - b * p.per_sequence, tid = threadIdx.x;
+  const int T = tree_size(p, b);
+  if (tid < 2) s_inner[tid] = 0;
+  __syncthreads();
+  if (tid > 0 && tid < T) {
+    const int above = p.parent[(size_t)b * p.T_max + tid];
+    if (above >= 0 && above < tid) atomicOr(reinterpret_cast<unsigned long long *>(s_inner + (above >> 6)), 1ull << (above & 63));
+  }
+  __syncthreads();
+  uint64_t lo = s_inner[0], hi = s_inner[1];
+  const int items = (__popcll(lo) + __popcll(hi)) * p.slices;
+  int passed = 0;  // nodes taken out of the set
+  for (int item = at; item < items; item += p.per_sequence) {
+    const int rank = item / p.slices, slice = item - rank * p.slices;
+    for (; passed < rank; ++passed) {
+      if (lo) lo &= lo - 1;
+      else hi &= hi - 1;
+    }
+    const int node = lo ? __ffsll((unsigned long long)lo) - 1 : 63 + __ffsll((unsigned long long)hi);
+    const size_t row = (size_t)b * p.T_max + node;
+    const SliceStat s = slice_stat<kBf16>(p, p.logits, row, slice, p.inv, f_room, d_room);
+    if (tid == 0) p.p_stat[row * p.slices + slice] = s;
+    if (p.draft) {
+      const SliceStat t = slice_stat<kBf16>(p, p.draft, row, slice, p.draft_inv, f_room, d_room);
+      if (tid == 0) p.q_stat[row * p.slices + slice] = t;
+    }
+  }
+}
+
+struct RowStat {
+  float most;
+  double scale;  // 1 / sum; 0 where the row has no probability
+};
+__device__ __forceinline__ RowStat row_stat(const SliceStat *s, int slices, double inv) {
+  float most = -INFINITY;
+  for (int i = 0; i < slices; ++i) most = fmaxf(most, s[i].most);
+  double sum = 0.0;
+  if (most > -INFINITY)
+    for (int i = 0; i < slices; ++i) sum += s[i].sum * weight_of(s[i].most, most, inv);
+  return {most, sum > 0.0 ? 1.0 / sum : 0.0};
+}
+
+// Nodes before i, as a set
+__device__ __forceinline__ bool in_set(const uint64_t (&s)[2], int i) { return (s[i >> 6] >> (i & 63)) & 1; }
+
+template <bool kBf16, bool kDraft>
+__global__ __launch_bounds__(kDraft ? 1024 : PROPD_MAX_TREE) void sampled_walk_kernel(SampledParams p) {
+  __shared__ int s_parent[PROPD_MAX_TREE], s_token[PROPD_MAX_TREE], s_path[PROPD_MAX_TREE], s_next[PROPD_MAX_TREE];
+  __shared__ double s_p[PROPD_MAX_TREE], s_q[PROPD_MAX_TREE];
+  __shared__ float s_u[PROPD_MAX_TREE];
+  __shared__ uint64_t s_passes[2];
+  __shared__ double d_room[16];
+  __shared__ int s_full;
+  const int b = blockIdx.x, i = threadIdx.x, T = tree_size(p, b), V = p.V;
+  const size_t base = (size_t)b * p.T_max;
+  if (i == 0) p.arrived[b] = 0;  // of the next kernel
+  bool child = i > 0 && i < T;
+  int above = 0, token = -1;
+  if (child) {
+    above = p.parent[base + i];
+    token = p.token[base + i];
+    child = above >= 0 && above < i;
+  }
+  const bool inside = child && token >= 0 && token < V;
+  if (i < PROPD_MAX_TREE) {
+    s_parent[i] = child ? above : -1;
+    s_token[i] = token;
+    s_next[i] = -1;
+    double pc = 0.0, qc = 0.0;
+    if (inside) {
+      const size_t row = base + above;
+      const float x = logit_at<kBf16>(p.logits, row, V, token);
+      const RowStat s = row_stat(p.p_stat + row * p.slices, p.slices, p.inv);
+      pc = s.scale > 0.0 ? weight_of(x, s.most, p.inv) * s.scale : 0.0;
+      if constexpr (kDraft) {
+        const float y = logit_at<kBf16>(p.draft, row, V, token);
+        const RowStat t = row_stat(p.q_stat + row * p.slices, p.slices, p.draft_inv);
+        qc = t.scale > 0.0 ? weight_of(y, t.most, p.draft_inv) * t.scale : 0.0;
+      }
+    }
+    s_p[i] = pc;
+    s_q[i] = qc;
+    s_u[i] = child ? p.u[base + i] : 0.f;
+  }
+  if (i < 2) s_passes[i] = 0;
+  __syncthreads();
+  double much = 0.0;
+  int last = 0, full = 1;
+  if constexpr (!kDraft) {
+    // every candidate's test, as if its siblings before it had been refused: the first that passes is taken
+    uint64_t before[2] = {0, 0};
+    bool again = false;
+    double left = 1.0;
+    if (child) {
+      for (int j = above + 1; j < i; ++j)
+        if (s_parent[j] == above) {
+          before[j >> 6] |= 1ull << (j & 63);
+          again = again || s_token[j] == token;
+        }
+    }
+    const double mine = again ? 0.0 : s_p[i];
+    __syncthreads();
+    s_p[i] = mine;  // (a token refused before has nothing left)
+    __syncthreads();
+    if (child) {
+      for (int w = 0; w < 2; ++w)
+        for (uint64_t m = before[w]; m; m &= m - 1) left -= s_p[64 * w + __ffsll((unsigned long long)m) - 1];
+      left = left > 0.0 ? left : 0.0;
+    }
+    const bool passes = child && (double)s_u[i] * left < mine;
+    const uint64_t word = __ballot(passes);
+    if ((i & 63) == 0) s_passes[i >> 6] = word;
+    __syncthreads();
+    if (passes && ((before[0] & s_passes[0]) | (before[1] & s_passes[1])) == 0) s_next[above] = i;
+    __syncthreads();
+    if (i == 0) {
+      int node = 0, n = 0;
+      do {
+        s_path[n++] = node;
+        node = s_next[node];
+      } while (node >= 0);
+      s_full = n;
+    }
+    __syncthreads();
+    full = s_full;
+    last = s_path[full - 1];
+  } else {
+    // (every thread goes along; child and what it needs are the same for all)
+    full = 0;
+    int node = 0;
+    while (true) {
+      if (i == 0) s_path[full] = node;
+      ++full;
+      last = node;
+      much = 0.0;
+      double mass = 1.0;
+      int taken = -1;
+      bool known = true;  // mass belongs to much
+      RowStat ps = {0.f, 0.0}, qs = {0.f, 0.0};
+      const size_t row = base + node;
+      for (int j = node + 1; j < T; ++j) {
+        if (s_parent[j] != node || s_token[j] < 0 || s_token[j] >= V) continue;
+        if (!known) {
+          ps = row_stat(p.p_stat + row * p.slices, p.slices, p.inv);
+          qs = row_stat(p.q_stat + row * p.slices, p.slices, p.draft_inv);
+          double sum = 0.0;
+          for (int v = i; v < V; v += blockDim.x) {
+            const float x = logit_at<kBf16>(p.logits, row, V, v), y = logit_at<kBf16>(p.draft, row, V, v);
+            const double left = weight_of(x, ps.most, p.inv) * ps.scale - much * (weight_of(y, qs.most, p.draft_inv) * qs.scale);
+            sum += left > 0.0 ? left : 0.0;
+          }
+          mass = block_reduce(sum, d_room, [](double x, double y) { return x + y; });
+          known = true;
+        }
+        const double left = s_p[j] - much * s_q[j];
+        if ((double)s_u[j] * mass * s_q[j] < left) {
+          taken = j;
+          break;
+        }
+        much += mass;
+        known = false;
+      }
+      if (taken < 0) break;
+      node = taken;
+    }
+    __syncthreads();
+  }
+  // A path buffer shorter than the path keeps its first nodes; the next node's token goes on with the same output.
+  const int len = full < p.stride ? full : p.stride;
+  for (int j = i; j < p.stride; j += blockDim.x) p.accept_path[(size_t)b * p.stride + j] = j < len ? s_path[j] : -1;
+  if (i == 0) {
+    p.accept_len[b] = len;
+    if (full > len) p.next_token[b] = s_token[s_path[len]];
+    WalkEnd e = {last, full > len, 0.f, 0.f, 0.0, 0.0, much};
+    if (kDraft && much > 0.0) {
+      const RowStat s = row_stat(p.p_stat + (base + last) * p.slices, p.slices, p.inv);
+      const RowStat t = row_stat(p.q_stat + (base + last) * p.slices, p.slices, p.draft_inv);
+      e.p_most = s.most;
+      e.p_scale = s.scale;
+      e.q_most = t.most;
+      e.q_scale = t.scale;
+    }
+    p.end[b] = e;
+  }
+}
+
+// What is left of a thread's 16 tokens of a chunk.  refused: a bit per token of the chunk.
+template <bool kBf16>
+__device__ __forceinline__ void left_of(const SampledParams &p, const WalkEnd &e, const float (&x)[16], size_t row, int chunk, float most,
+                                        const uint32_t *refused, double (&w)[16]) {
+  if (e.much > 0.0) {
+    float y[16];
+    load_slice<kBf16>(p, p.draft, row, chunk, y);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const double left = weight_of(x[i], e.p_most, p.inv) * e.p_scale - e.much * (weight_of(y[i], e.q_most, p.draft_inv) * e.q_scale);
+      w[i] = left > 0.0 && x[i] > -INFINITY ? left : 0.0;
+    }
+  } else {
+    const uint32_t gone = refused[threadIdx.x >> 1] >> (16 * (threadIdx.x & 1));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = x[i] > -INFINITY && !((gone >> i) & 1) ? weight_of(x[i], most, p.inv) : 0.0;
+  }
+}
+
+template <bool kBf16>
+__global__ __launch_bounds__(kSampledThreads) void sampled_next_kernel(SampledParams p) {
+  __shared__ float f_room[kSampledThreads / kWave];
+  __shared__ double d_room[kSampledThreads / kWave];
+  __shared__ uint32_t s_refused[kSliceTokens / 32];
+  __shared__ double s_upto[kSampledThreads];
+  __shared__ int s_last, s_found;
+  const int b = blockIdx.x / p.slices, own = blockIdx.x - b * p.slices, tid = threadIdx.x;
+  const WalkEnd e = p.end[b];
+  if (e.cut) return;
+  const int T = tree_size(p, b);
+  const size_t base = (size_t)b * p.T_max, row = base + e.node;
+  float x[16], most = -INFINITY;
+  double w[16];
+  // what is left in a chunk, by token; relative to its largest logit where p itself is left
+  auto chunk = [&](int c) -> double {
+    load_slice<kBf16>(p, p.logits, row, c, x);
+    __syncthreads();
+    for (int j = tid; j < kSliceTokens / 32; j += kSampledThreads) s_refused[j] = 0;
+    __syncthreads();
+    if (!p.draft && tid > e.node && tid < T && p.parent[base + tid] == e.node) {
+      const int t = p.token[base + tid] - c * kSliceTokens;
+      if (p.token[base + tid] >= 0 && t >= 0 && t < kSliceTokens) atomicOr(s_refused + (t >> 5), 1u << (t & 31));
+    }
+    most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) most = fmaxf(most, x[i]);
+    most = block_reduce(most, f_room, [](float a, float b) { return fmaxf(a, b); });  // (its barriers stand behind the set)
+    left_of<kBf16>(p, e, x, row, c, most, s_refused, w);
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += w[i];
+    return sum;
+  };
+  const double total_here = block_reduce(chunk(own), d_room, [](double a, double b) { return a + b; });
+  if (tid == 0) {
+    SliceStat *to = p.left + (size_t)b * p.slices + own;
+    __hip_atomic_store(&to->most, e.much > 0.0 ? 0.f : most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(&to->sum, total_here, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s_last = __hip_atomic_fetch_add(p.arrived + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == p.slices - 1;
+  }
+  __syncthreads();
+  if (!s_last) return;
+
+  // ---- the last workgroup of the sequence: which chunk, then which token
+  SliceStat mine = {-INFINITY, 0.f, 0.0};
+  if (tid < p.slices) {
+    const SliceStat *from = p.left + (size_t)b * p.slices + tid;
+    mine.most = __hip_atomic_load(&from->most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    mine.sum = __hip_atomic_load(&from->sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  const float top = block_reduce(mine.sum > 0.0 ? mine.most : -INFINITY, f_room, [](float a, float b) { return fmaxf(a, b); });
+  const double share = mine.sum > 0.0 ? mine.sum * weight_of(mine.most, top, p.inv) : 0.0;
+  s_upto[tid] = share;
+  if (tid == 0) s_found = -1;
+  __syncthreads();
+  // prefix sums, in order
+  double total = 0.0, before = 0.0;
+  for (int c = 0; c < p.slices; ++c) {
+    before = c == tid ? total : before;
+    total += s_upto[c];
+  }
+  const double goal = (double)p.u_next[b] * total;
+  // the first chunk whose end lies beyond the goal; where rounding leaves none, the last that has anything
+  if (share > 0.0 && before + share > goal) atomicMin(reinterpret_cast<unsigned int *>(&s_found), (unsigned)tid);
+  __syncthreads();
+  int found = s_found;
+  if (found < 0) {
+    __syncthreads();
+    if (share > 0.0) atomicMax(&s_found, tid);
+    __syncthreads();
+    found = s_found;
+  }
+  if (found < 0) {  // nothing is left: the likeliest token
+    float best = -INFINITY;
+    int at = 0x7fffffff;
+    for (int v = tid; v < p.V; v += kSampledThreads) {
+      const float y = logit_at<kBf16>(p.logits, row, p.V, v);
+      if (y > best || at == 0x7fffffff) {
+        best = y;
+        at = v;
+      }
+    }
+    const float top_logit = block_reduce(best, f_room, [](float a, float b) { return fmaxf(a, b); });
+    __syncthreads();
+    if (tid == 0) s_found = 0x7fffffff;
+    __syncthreads();
+    if (best == top_logit) atomicMin(&s_found, at);
+    __syncthreads();
+    if (tid == 0) p.next_token[b] = s_found < p.V ? s_found : 0;
+    return;
+  }
+  __syncthreads();
+  s_upto[tid] = before;  // (of chunk tid)
+  if (tid == found) d_room[0] = weight_of(mine.most, top, p.inv);
+  __syncthreads();
+  const double in_chunk = (goal - s_upto[found]) / d_room[0];  // in the chunk's own measure
+  const double sum = chunk(found);
+  __syncthreads();
+  s_upto[tid] = sum;
+  if (tid == 0) s_found = 0x7fffffff;
+  __syncthreads();
+  double here = 0.0;
+  for (int j = 0; j < tid; ++j) here += s_upto[j];
+  int first = 0x7fffffff, final = -1;
+  const int v0 = found * kSliceTokens + 16 * tid;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    here += w[i];
+    if (w[i] > 0.0) {
+      if (here > in_chunk && first == 0x7fffffff) first = v0 + i;
+      final = v0 + i;
+    }
+  }
+  if (first != 0x7fffffff) atomicMin(&s_found, first);
+  const int end = block_reduce(final, reinterpret_cast<int *>(f_room), [](int a, int b) { return a > b ? a : b; });
+  if (tid == 0) p.next_token[b] = s_found != 0x7fffffff ? s_found : end;
+}
+
+// ------------------------------------------------------------------------------------
+// host side
+// ------------------------------------------------------------------------------------
+static int slices_of(int V) { return (V + kSliceTokens - 1) / kSliceTokens; }
+
+size_t accept_sampled_workspace_bytes(int B, int T_max, int V) {
+  const size_t rows = (size_t)B * T_max, slices = (size_t)slices_of(V);
+  return 2 * align_up(rows * slices * sizeof(SliceStat), 256) + align_up((size_t)B * slices * sizeof(SliceStat), 256) +
+         align_up((size_t)B * sizeof(WalkEnd), 256) + align_up((size_t)B * 4, 256);
+}
+
+template <bool kBf16>
+static propd_status run_sampled(const SampledParams &p, hipStream_t st) {
+  hipLaunchKernelGGL(sampled_stats_kernel<kBf16>, dim3((unsigned)(p.B * p.per_sequence)), dim3(kSampledThreads), 0, st, p);
+  if (!launch_ok()) return PROPD_ERR_DEVICE;
+  if (p.draft) hipLaunchKernelGGL((sampled_walk_kernel<kBf16, true>), dim3((unsigned)p.B), dim3(1024), 0, st, p);
+  else hipLaunchKernelGGL((sampled_walk_kernel<kBf16, false>), dim3((unsigned)p.B), dim3(PROPD_MAX_TREE), 0, st, p);
+  if (!launch_ok()) return PROPD_ERR_DEVICE;
+  hipLaunchKernelGGL(sampled_next_kernel<kBf16>, dim3((unsigned)(p.B * p.slices)), dim3(kSampledThreads), 0, st, p);
+  return launch_ok() ? PROPD_OK : PROPD_ERR_DEVICE;
+}
+
+}  // namespace propd
+
+extern "C" propd_status propd_accept_sampled(const propd_tree *tree, propd_dtype dt, int32_t vocab, const void *logits, float inv_temperature,
+                                             const void *draft_logits, float draft_inv_temperature, const float *u, const float *u_next,
+                                             int32_t *accept_len, int32_t *accept_path, int32_t path_stride, int32_t *next_token,
+                                             void *workspace, size_t workspace_bytes, void *hip_stream) {
+  using namespace propd;
+  if (!tree || tree->B < 1 || tree->T_max < 1 || tree->T_max > PROPD_MAX_TREE || vocab < 1 || path_stride < 1 || !tree->n_nodes || !tree->parent ||
+      !tree->token || !logits || !u || !u_next || !accept_len || !accept_path || !next_token)
+    return PROPD_ERR_INVALID_ARG;
+  if (dt != PROPD_BF16 && dt != PROPD_F32) return PROPD_ERR_INVALID_ARG;
+  if (!(inv_temperature > 0.f && inv_temperature <= kMostInverse)) return PROPD_ERR_INVALID_ARG;
+  if (draft_logits && !(draft_inv_temperature > 0.f && draft_inv_temperature <= kMostInverse)) return PROPD_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return PROPD_ERR_INVALID_ARG;
+  if (vocab > kMostVocab || (long long)tree->B * slices_of(vocab) > (1ll << 21)) return PROPD_ERR_UNSUPPORTED;
+  const size_t needed = accept_sampled_workspace_bytes(tree->B, tree->T_max, vocab);
+  if (!workspace || workspace_bytes < needed) return PROPD_ERR_WORKSPACE;
+  SampledParams p;
+  p.n_nodes = tree->n_nodes;
+  p.parent = tree->parent;
+  p.token = tree->token;
+  p.logits = logits;
+  p.draft = draft_logits;
+  p.u = u;
+  p.u_next = u_next;
+  p.inv = inv_temperature;
+  p.draft_inv = draft_inv_temperature;
+  p.B = tree->B;
+  p.T_max = tree->T_max;
+  p.V = vocab;
+  p.slices = slices_of(vocab);
+  p.stride = path_stride;
+  const size_t size = dt == PROPD_BF16 ? 2 : 4;
+  p.aligned = (size_t)vocab * size % 16 == 0 && reinterpret_cast<uintptr_t>(logits) % 16 == 0 && reinterpret_cast<uintptr_t>(draft_logits) % 16 == 0;
+  char *ws = reinterpret_cast<char *>(workspace);
+  const size_t rows = (size_t)p.B * p.T_max;
+  p.p_stat = reinterpret_cast<SliceStat *>(ws);
+  ws += align_up(rows * p.slices * sizeof(SliceStat), 256);
+  p.q_stat = reinterpret_cast<SliceStat *>(ws);
+  ws += align_up(rows * p.slices * sizeof(SliceStat), 256);
+  p.left = reinterpret_cast<SliceStat *>(ws);
+  ws += align_up((size_t)p.B * p.slices * sizeof(SliceStat), 256);
+  p.end = reinterpret_cast<WalkEnd *>(ws);
+  ws += align_up((size_t)p.B * sizeof(WalkEnd), 256);
+  p.arrived = reinterpret_cast<int32_t *>(ws);
+  p.accept_len = accept_len;
+  p.accept_path = accept_path;
+  p.next_token = next_token;
+  // workgroups of a sequence: about as many as run at once, no more than there can be slices of nodes with children
+  const long long most = (long long)(p.T_max > 1 ? p.T_max - 1 : 1) * p.slices, fair = 2048 / p.B > 1 ? 2048 / p.B : 1;
+  p.per_sequence = (int)(most < fair ? most : fair);
+  return dt == PROPD_BF16 ? run_sampled<true>(p, as_stream(hip_stream)) : run_sampled<false>(p, as_stream(hip_stream));
+}

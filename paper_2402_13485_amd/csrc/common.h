@@ -113,5 +113,7 @@ size_t tree_attention_workspace_bytes(int B, int H, int L_max, int T_max);
 size_t accept_path_workspace_bytes(int B, int T_max);
 size_t grouped_attention_workspace_bytes(int B, int H, int L_max, int T_max);
 size_t cache_evict_workspace_bytes(int B, int H_kv, int L_max);
+size_t paged_attention_workspace_bytes(int B, int H, int L_max, int T_max);
+size_t accept_sampled_workspace_bytes(int B, int T_max, int vocab);
 
 }  // namespace propd

@@ -1,0 +1,815 @@
+// Tree attention over a paged cache: rows as they are or in 8 bits, K/V heads shared by several query heads, capped and biased scores, a window.
+//
+// A unit is a (sequence, K/V head, block of query columns): the nodes of all query heads that read the K/V head lie side by side, column r is
+// node r % T of head r / T, so that a row is read once for all of them.  Its rows come in stages of 32, the tree's own first, then the cached ones.
+//   - A workgroup takes a range of a unit's stages.  Its four waves are kCw columns of 32 query columns by 4 / kCw rows of
+//     stages: a single token or a small tree has one column of waves, each of which streams stages of its own and waits for nobody; the
+//     row of waves of a large tree shares every stage.
+//   - The next stage's rows are on their way to registers while a stage is multiplied; from there they go to LDS, 8-bit rows
+//     as the bf16 or fp32 values that they stand for (once per workgroup, not once per wave that multiplies them).
+//   - S^T = K . Q^T, so that a lane owns a column: running maximum and sum, position, slope and ancestor set are per-lane scalars, and the weights
+//     are the B operand of O^T += V^T . P^T as they are.  bf16: 32x32x16 products, V^T by transposing LDS reads, a weight as the sum of two bf16
+//     values (off by 2^-17; one alone would add 40 % to the result's own rounding).  fp32: 32x32x2 products.
+//   - Ranges of a unit leave partial results, which a second kernel joins in their order.
+#include "attention_device.h"
+#include "paged_cache.h"
+#include "score_rule.h"
+
+namespace propd {
+
+constexpr int kPagedThreads = 256;
+
+struct PagedParams {
+  Pages pages;
+  const unsigned char *q, *k_tree, *v_tree;
+  unsigned char *out;
+  float *lse;
+  const int32_t *seq_lens, *n_nodes;
+  const uint64_t *anc;
+  const float *slopes;
+  int B, H, H_kv, group, T_max;
+  int blocks;   // blocks of 32 * kCw columns of a unit's tree of T_max nodes
+  int window;   // window_of
+  float scale_log2e, cap_in, cap_log2e;  // cap_in: scale / cap
+  float *part_o, *part_ml;
+  int32_t *records;  // [B * H_kv * blocks][4]: first slot, slots between pieces, pieces
+  int resident;      // workgroups that run at once
+  int most_ranges;   // of a call whose units are cut
+  int may_split;
+};
+
+// What the kernel's types and shapes make.  kN: columns of a wave, 16 or 32; a product has as many rows.
+template <bool kBf16, int D, int kN, int kCw>
+struct PagedGeo {
+  static constexpr int kColumns = kN * kCw;
+  static constexpr int kRw = 4 / kCw;                  // stages at work at once
+  static constexpr int kRowBytes = D * (kBf16 ? 2 : 4);
+  static constexpr int kPart = kStageRows * kRowBytes;  // K part of a stage; the V part follows
+  static constexpr int kStage = 2 * kPart;
+  static constexpr int kSlots = kCw == 1 ? 1 : 2;      // a wave's own stage needs one
+  static constexpr int kChunks = kRowBytes / 16;
+  static constexpr int kGroups = 64 / kN;              // lanes that have a column
+  static constexpr int kScores = 32 / kGroups;         // scores of a lane per stage; number x is of row 4 * kGroups * (x / 4) + 4 * group + x % 4
+  static constexpr int kBlocks = D / kN, kAcc = kN * kN / 64;  // products that make O, and their registers
+  static constexpr int kQuads = D / (4 * kGroups);     // O of a lane in fours of neighbouring d; quad x starts at d = 4 * kGroups * x + 4 * group
+  static constexpr int kThreads = 64 * kCw;            // that load a stage
+  static constexpr int kLds = kRw * kSlots * kStage + 512;
+  // Chunk c of row r of a stage lies at chunk position c ^ key(r): a fragment read's rows fall into different banks
+  static __device__ __forceinline__ int k_key(int r) { return kBf16 ? Geo<D>::k_key(r) : r & (kChunks - 1); }
+  static __device__ __forceinline__ int v_key(int r) {
+    return kBf16 ? Geo<D>::v_key(r) : kN == 32 ? ((r >> 2) & 1) << 3 : ((r >> 2) & 3) << 2;
+  }
+};
+
+template <int kN>
+using Acc = std::conditional_t<kN == 32, f32x16, f32x4>;
+
+template <int kN>
+__device__ __forceinline__ Acc<kN> product(u32x4 a, u32x4 b, Acc<kN> c) {
+  if constexpr (kN == 32) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+template <int kN>
+__device__ __forceinline__ Acc<kN> product(float a, float b, Acc<kN> c) {
+  if constexpr (kN == 32) return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+template <class V>
+__device__ __forceinline__ void clear(V &v) {
+#pragma unroll
+  for (int r = 0; r < (int)(sizeof(V) / 4); ++r) v[r] = 0.f;
+}
+
+// A number that the compiler takes for another one every time, so that what is made of it is made again where it is needed and
+// takes no registers meanwhile.
+__device__ __forceinline__ int made_anew(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// Stages of a unit: the tree's, then cached ones from row 32 * `first` on.
+struct PagedStages {
+  int tree, first, cached;
+};
+__device__ __forceinline__ PagedStages paged_stages(int L, int T, int window) {
+  PagedStages s;
+  s.tree = (T + kStageRows - 1) / kStageRows;
+  s.first = (L > window ? L - window + 1 : 0) / kStageRows;  // the first row that the root sees
+  s.cached = (L + kStageRows - 1) / kStageRows - s.first;
+  s.cached = s.cached < 0 ? 0 : s.cached;
+  return s;
+}
+
+// How the units are cut, in steps of kRw stages: a range is at most `most` steps, a unit of s steps has ceil(s / most) equally long ones.
+// Every workgroup works the same plan out from the lengths.
+//   As many units as run at once or fewer: the least `most` (from an equal share on, a sixteenth of it longer at a time) whose ranges all run at once.
+//   More: with r workgroups at once, N steps in all, ranges of m steps that cost o steps besides, the last range to start ends half a range after
+//   the mean: m / 2 + o N / (m r) is least at m = sqrt(2 o N / r).
+struct PagedPlan {
+  int most, ranges;
+};
+constexpr float kRangeCost = 3.f;  // steps that a range costs besides its own
+
+struct PagedSequence {
+  int L, T, steps, units;  // units 0 beyond the batch
+};
+template <int kN, int kCw>
+__device__ __forceinline__ PagedSequence paged_sequence(const PagedParams &p, int b) {
+  PagedSequence q = {0, 0, 0, 0};
+  if (b >= p.B) return q;
+  q.L = clamped(p.seq_lens[b], p.pages.capacity);
+  q.T = clamped(p.n_nodes[b] - 1, p.T_max - 1) + 1;
+  const PagedStages s = paged_stages(q.L, q.T, p.window);
+  q.steps = (s.tree + s.cached + 4 / kCw - 1) / (4 / kCw);
+  q.units = p.H_kv * ((p.group * q.T + kN * kCw - 1) / (kN * kCw));
+  return q;
+}
+
+__device__ __forceinline__ int paged_pieces(int steps, int most) {
+  return most >= steps ? 1 : (int)((unsigned)(steps + most - 1) / (unsigned)most);
+}
+__device__ __forceinline__ int paged_sum(int v) {
+  return __builtin_amdgcn_readlane(wave_scan_i32(v, 0, [](int x, int y) { return x + y; }), 63);
+}
+
+template <int kN, int kCw>
+__device__ __forceinline__ PagedPlan paged_plan(const PagedParams &p, const PagedSequence &first) {
+  const int lane = threadIdx.x & 63;
+  int units = 0;
+  float total = 0.f;
+  for (int b0 = 0; b0 < p.B; b0 += kWave) {
+    const PagedSequence q = b0 == 0 ? first : paged_sequence<kN, kCw>(p, b0 + lane);
+    units += paged_sum(q.units);
+    float t = (float)q.units * (float)q.steps;
+    for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, kWave);
+    total += t;
+  }
+  PagedPlan plan = {1 << 30, units};
+  if (!p.may_split) return plan;
+  const bool few = units <= p.resident;
+  const int room = few ? p.resident : p.most_ranges;
+  float share = few ? total / (float)p.resident : sqrtf(2.f * kRangeCost * total / (float)p.resident);
+  share = fmaxf(share, 1.f);
+  for (int step = 0; step < 64; ++step) {
+    const int most = (int)ceilf(share * (1.f + .0625f * (float)step * (float)(step < 16 ? 1 : step - 14)));
+    int n = 0;
+    for (int b0 = 0; b0 < p.B; b0 += kWave) {
+      const PagedSequence q = b0 == 0 ? first : paged_sequence<kN, kCw>(p, b0 + lane);
+      n += paged_sum(q.units * paged_pieces(q.steps, most));
+    }
+    if (n <= room) return {most, n};
+  }
+  return plan;
+}
+
+__device__ __forceinline__ void lds_to(unsigned char *at, u32x4 v) { *reinterpret_cast<u32x4 *>(at) = v; }
+
+// Four neighbouring values of a result
+template <bool kBf16>
+__device__ __forceinline__ void store_quad(unsigned char *out, size_t at, f32x4 v, float inv) {
+  if constexpr (kBf16) *reinterpret_cast<u32x2 *>(reinterpret_cast<uint16_t *>(out) + at) = u32x2{cvt_pk_bf16(v[0] * inv, v[1] * inv), cvt_pk_bf16(v[2] * inv, v[3] * inv)};
+  else *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(out) + at) = f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+}
+
+// LDS written before is seen by the workgroup; loads from memory stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <bool kBf16, bool kCodes, int D, int kN, int kCw>
+__global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kernel(PagedParams p) {
+  using G = PagedGeo<kBf16, D, kN, kCw>;
+  constexpr int kRw = G::kRw, kRowBytes = G::kRowBytes, kGroups = G::kGroups, kScores = G::kScores, kBlocks = G::kBlocks, kAcc = G::kAcc;
+  constexpr int kSrcRow = kCodes ? D : kRowBytes, kSrcChunks = kSrcRow / 16;       // of a paged row
+  constexpr int kLoads = 2 * kStageRows * kSrcChunks / G::kThreads;                // of a thread per stage, K and V
+  constexpr int kTreeLoads = 2 * kStageRows * G::kChunks / G::kThreads;
+  constexpr int kQf = kRowBytes / 16 / kGroups;                                     // 16-byte pieces of a lane's part of q
+  constexpr int kParts = 2;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  float *const tree_place = reinterpret_cast<float *>(smem + kRw * G::kSlots * G::kStage);  // [128]: depths of the nodes
+  __shared__ float s_ml[4][2][kWave];
+  __shared__ int s_any;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cw = wave % kCw, rw = wave / kCw, loader = tid % G::kThreads;
+  if (tid == 0) s_any = 0;
+
+  // ---- which range
+  int b = 0, hk, block, piece, pieces, first_slot, steps;
+  {
+    const PagedSequence lanes = paged_sequence<kN, kCw>(p, lane);
+    const PagedPlan plan = paged_plan<kN, kCw>(p, lanes);
+    const int n = plan.ranges;
+    int at = blockIdx.x;
+    if (at >= n) return;
+    const int even = n / 8 * 8;  // neighbouring ranges (blocks of one unit's columns among them) on one XCD
+    at = at < even ? at % 8 * (even / 8) + at / 8 : at;
+    int before = 0, start = 0;
+    for (int b0 = 0; b0 < p.B; b0 += kWave) {
+      const PagedSequence q = b0 == 0 ? lanes : paged_sequence<kN, kCw>(p, b0 + lane);
+      const int mine = q.units * paged_pieces(q.steps, plan.most), incl = wave_scan_i32(mine, 0, [](int x, int y) { return x + y; });
+      const uint64_t le = __ballot(b0 + lane < p.B && before + incl - mine <= at);
+      if (le == 0) break;
+      const int src = __popcll(le) - 1;
+      b = b0 + src;
+      start = __builtin_amdgcn_readlane(before + incl - mine, src);
+      before += __builtin_amdgcn_readlane(incl, 63);
+    }
+    const PagedSequence q = paged_sequence<kN, kCw>(p, b);
+    steps = __builtin_amdgcn_readfirstlane(q.steps);
+    const int n_blocks = __builtin_amdgcn_readfirstlane(q.units) / p.H_kv, rest = at - start;
+    pieces = paged_pieces(steps, plan.most);
+    // blocks next to each other, then K/V heads, then pieces
+    const int in_blocks = rest / n_blocks;
+    block = rest - in_blocks * n_blocks;
+    piece = in_blocks / p.H_kv;
+    hk = in_blocks - piece * p.H_kv;
+    first_slot = at - piece * p.H_kv * n_blocks;
+    if (tid == 0 && piece == 0)
+      *reinterpret_cast<u32x4 *>(p.records + 4 * (((size_t)b * p.H_kv + hk) * p.blocks + block)) =
+          u32x4{(uint32_t)first_slot, (uint32_t)(p.H_kv * n_blocks), (uint32_t)pieces, 0};
+    first_slot += piece * p.H_kv * n_blocks;  // this range's own
+  }
+  const int L = clamped(p.seq_lens[b], p.pages.capacity), T = clamped(p.n_nodes[b] - 1, p.T_max - 1) + 1;
+  const PagedStages st = paged_stages(L, T, p.window);
+  const int quot = steps / pieces, extra = steps - quot * pieces;
+  const int step0 = piece * quot + (piece < extra ? piece : extra), n_steps = quot + (piece < extra ? 1 : 0);
+  const int n_stages = st.tree + st.cached;
+  const size_t unit = (size_t)b * p.H_kv + hk;
+
+  // ---- this lane's column
+  const int columns = p.group * T, column = (block * kCw + cw) * kN + lane % kN;
+  const bool there = column < columns, active = (block * kCw + cw) * kN < columns;
+  const int col = there ? column : 0;  // lanes past the last column take the first: valid memory, never stored
+  const int head = col / T, node = col - head * T;
+  const size_t row_out = ((size_t)b * p.H + hk * p.group + head) * p.T_max + node;
+  u32x4 qf[kQf];
+#pragma unroll
+  for (int x = 0; x < kQf; ++x) qf[x] = *reinterpret_cast<const u32x4 *>(p.q + row_out * kRowBytes + (kGroups * x + lane / kN) * 16);
+  const u32x4 anc = *reinterpret_cast<const u32x4 *>(p.anc + ((size_t)b * p.T_max + node) * 2);
+  const float slope = p.slopes ? p.slopes[hk * p.group + head] * kLog2e : 0.f;
+  const float depth = (float)(__popc(anc.x) + __popc(anc.y) + __popc(anc.z) + __popc(anc.w) - 1);
+  // places: positions less the root's.  A column sees those from `lowest` on, from all_see on every column of the wave does.
+  const float lowest = p.window > kMostWindow ? -INFINITY : depth - (float)p.window + 1.f;
+  float all_see = lowest;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) all_see = fmaxf(all_see, __shfl_xor(all_see, o, kWave));
+  if (tid < T) {
+    const u32x4 a = *reinterpret_cast<const u32x4 *>(p.anc + ((size_t)b * p.T_max + tid) * 2);
+    tree_place[tid] = (float)(__popc(a.x) + __popc(a.y) + __popc(a.z) + __popc(a.w) - 1);
+  } else if (tid < 128) {
+    tree_place[tid] = 0.f;
+  }
+  lds_barrier();
+
+  // ---- loader
+  unsigned char *const group_lds = smem + rw * (G::kSlots * G::kStage);
+  int ids = -1, ids_from = -64;  // pages of the 16-row pieces of 32 steps' stages, a piece per lane
+  auto stage_at = [&](int step) { return (step0 + step) * kRw + rw; };
+  auto cached_row = [&](int stage) { return (stage - st.tree + st.first) * kStageRows; };
+  u32x4 data[kLoads];
+  uint32_t scale_byte[kLoads];
+  uint32_t rows_there = 0;  // of the stage on its way
+  auto issue = [&](int step) __attribute__((always_inline)) {
+    rows_there = 0;
+    const int stage = stage_at(step);
+    if (step >= n_steps || stage < st.tree || stage >= n_stages) return;  // uniform
+    if (step >= ids_from + 32) {
+      ids_from = step;
+      const int at = stage_at(step + (lane >> 1)), row = cached_row(at) + 16 * (lane & 1);
+      ids = at >= st.tree && row < L ? page_of(p.pages, b, row) : -1;
+    }
+    const int row0 = cached_row(stage), in_page = (1 << p.pages.shift) - 1;
+    const unsigned char *from[4];  // K of both halves, V of both
+    const uint8_t *scale_from[4];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int page = __builtin_amdgcn_readlane(ids, 2 * (step - ids_from) + half);
+      int n = L - row0 - 16 * half;
+      n = n > 16 ? 16 : n;
+      if (page >= 0 && n > 0) rows_there |= ((1u << n) - 1u) << (16 * half);
+      const size_t row = row_in_pool(p.pages, page < 0 ? 0 : page, hk, p.H_kv, (row0 + 16 * half) & in_page);
+      from[half] = p.pages.k + row * kSrcRow;
+      from[2 + half] = p.pages.v + row * kSrcRow;
+      if constexpr (kCodes) {
+        scale_from[half] = p.pages.k_scale + row;
+        scale_from[2 + half] = p.pages.v_scale + row;
+      }
+    }
+    const int ln = made_anew(loader) & (G::kThreads - 1);
+    auto pick = [](auto *const(&x)[4], int part, int row) __attribute__((always_inline)) {
+      auto *const k0 = x[0], *const k1 = x[1], *const v0 = x[2], *const v1 = x[3];  // (values: a choice of places would be made in memory)
+      auto *const k = row & 16 ? k1 : k0, *const v = row & 16 ? v1 : v0;
+      return part ? v : k;
+    };
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int x = i * G::kThreads + ln, part = x / (kStageRows * kSrcChunks), row = x / kSrcChunks % kStageRows;
+      data[i] = *reinterpret_cast<const u32x4 *>(pick(from, part, row) + (row & 15) * kSrcRow + x % kSrcChunks * 16);
+      if constexpr (kCodes) scale_byte[i] = pick(scale_from, part, row)[row & 15];
+    }
+  };
+  // What issue() requested to LDS; rows that are not there as zeros, so that weights of zero meet nothing else.
+  auto land = [&](unsigned char *to, uint32_t is_there) __attribute__((always_inline)) {
+    const int ln = made_anew(loader) & (G::kThreads - 1);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int x = i * G::kThreads + ln, part = x / (kStageRows * kSrcChunks), row = x / kSrcChunks % kStageRows, c = x % kSrcChunks;
+      unsigned char *const at = to + part * G::kPart + row * kRowBytes;
+      const int key = part ? G::v_key(row) : G::k_key(row);
+      u32x4 v = data[i];
+      if (is_there != ~0u) {  // uniform
+        const bool ok = (is_there >> row) & 1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = ok ? v[j] : 0u;
+      }
+      if constexpr (!kCodes) {
+        lds_to(at + ((c ^ key) << 4), v);
+      } else {
+        const float scale = scale_of(scale_byte[i]);
+        if constexpr (kBf16) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const u32x2 a = codes_to_bf16(v[2 * j], scale), z = codes_to_bf16(v[2 * j + 1], scale);
+            lds_to(at + (((2 * c + j) ^ key) << 4), u32x4{a.x, a.y, z.x, z.y});
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) lds_to(at + (((4 * c + j) ^ key) << 4), __builtin_bit_cast(u32x4, codes_to_f32(v[j], scale)));
+        }
+      }
+    }
+  };
+  auto land_tree = [&](unsigned char *to, int stage) __attribute__((always_inline)) {
+    const int left = T - stage * kStageRows;
+    const size_t row0 = unit * p.T_max + stage * kStageRows;
+    const int ln = made_anew(loader) & (G::kThreads - 1);
+#pragma unroll
+    for (int i = 0; i < kTreeLoads; ++i) {
+      const int x = i * G::kThreads + ln, part = x / (kStageRows * G::kChunks), row = x / G::kChunks % kStageRows, c = x % G::kChunks;
+      u32x4 v = {0, 0, 0, 0};
+      if (row < left) v = *reinterpret_cast<const u32x4 *>((part ? p.v_tree : p.k_tree) + (row0 + row) * kRowBytes + c * 16);
+      lds_to(to + part * G::kPart + row * kRowBytes + ((c ^ (part ? G::v_key(row) : G::k_key(row))) << 4), v);
+    }
+  };
+
+  float m_run, l_run;
+  Acc<kN> o_acc[kBlocks];
+  const float tau = 8.f;
+
+  // ---- a stage: its scores, weights and what they add to O.  `seen`: a bit per row of the stage that exists.
+  auto take_stage = [&](const unsigned char *from, int stage, uint32_t seen, auto with_care) __attribute__((always_inline)) {
+    constexpr bool kCareful = decltype(with_care)::value;
+    const bool tree = stage < st.tree;
+    const int ln = made_anew(lane) & 63, in_n = ln % kN, g = ln / kN;
+    float sc[kScores];
+#pragma unroll
+    for (int tile = 0; tile < 32 / kN; ++tile) {
+      Acc<kN> acc;
+      clear(acc);
+      const int row = tile * kN + in_n;
+#pragma unroll
+      for (int x = 0; x < kQf; ++x) {
+        const u32x4 a = *reinterpret_cast<const u32x4 *>(from + row * kRowBytes + (((kGroups * x + g) ^ G::k_key(row)) << 4));
+        if constexpr (kBf16) {
+          acc = product<kN>(a, qf[x], acc);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc = product<kN>(__uint_as_float(a[j]), __uint_as_float(qf[x][j]), acc);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < kAcc; ++r) sc[tile * kAcc + r] = acc[r];
+    }
+    mfma_settle();
+    // ---- scores in the exponent's (log2) domain
+    if (p.cap_in > 0.f) {
+#pragma unroll
+      for (int x = 0; x < kScores; ++x) sc[x] = capped(sc[x], p.cap_log2e, p.cap_in);
+    } else {
+#pragma unroll
+      for (int x = 0; x < kScores; ++x) sc[x] *= p.scale_log2e;
+    }
+    const float first = tree ? 0.f : (float)(cached_row(stage) - L);  // place of the stage's first cached row
+    if (p.slopes || first < all_see) {
+#pragma unroll
+      for (int x4 = 0; x4 < kScores / 4; ++x4) {
+        const int row = 4 * kGroups * x4 + 4 * g;
+        f32x4 place = {first + (float)row, first + (float)(row + 1), first + (float)(row + 2), first + (float)(row + 3)};
+        if (tree) place = *reinterpret_cast<const f32x4 *>(tree_place + stage * kStageRows + row);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (p.slopes) sc[4 * x4 + j] = fmaf(slope, place[j] - depth, sc[4 * x4 + j]);
+          sc[4 * x4 + j] = place[j] >= lowest ? sc[4 * x4 + j] : -INFINITY;
+        }
+      }
+    }
+    if (tree) seen &= stage == 0 ? anc.x : stage == 1 ? anc.y : stage == 2 ? anc.z : anc.w;
+    if (tree || seen != ~0u) {  // uniform
+      const uint32_t vis = seen >> (4 * g);
+#pragma unroll
+      for (int x = 0; x < kScores; ++x) sc[x] = ((vis >> (4 * kGroups * (x >> 2) + (x & 3))) & 1u) ? sc[x] : -INFINITY;
+    }
+    float m_blk = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < kScores; ++x) m_blk = fmaxf(m_blk, sc[x]);
+    {  // the column's other scores are in the lanes 32 (and 16) away
+      uint32_t lo = __float_as_uint(m_blk), hi = lo;
+      swap_halves(lo, hi);
+      m_blk = fmaxf(__uint_as_float(lo), __uint_as_float(hi));
+      if constexpr (kN == 16) m_blk = fmaxf(m_blk, __shfl_xor(m_blk, 16, kWave));
+    }
+    // A new reference is adopted only when the maximum exceeds the old one by 2^8: weights then exceed 1, by a factor that fp32 sums and bf16
+    // weights hold, and O is hardly ever scaled.  With care weights are at most 1.
+    if (__builtin_amdgcn_ballot_w64(m_blk > (kCareful ? m_run : m_run + tau)) != 0) {
+      const float m_new = fmaxf(m_run, m_blk), m_safe = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = fast_exp2(m_run - m_safe);
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+        for (int r = 0; r < kAcc; ++r) o_acc[db][r] *= alpha;
+      m_run = m_new;
+    }
+    const float neg_m = -(m_run == -INFINITY ? 0.f : m_run);
+#pragma unroll
+    for (int x = 0; x < kScores; ++x) {
+      sc[x] = fast_exp2(sc[x] + neg_m);
+      l_run += sc[x];  // of the weights as they are: lse is an fp32 result
+    }
+    const unsigned char *const v_from = from + G::kPart;
+    if constexpr (kBf16) {
+#pragma unroll
+      for (int half = 0; half < kScores / 8; ++half) {  // a product's rows are those of 8 scores
+        uint32_t pw[kParts][4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          float p0 = sc[8 * half + 2 * x], p1 = sc[8 * half + 2 * x + 1];
+#pragma unroll
+          for (int part = 0; part < kParts; ++part) {  // rounded to bf16, and what that leaves
+            const uint32_t w2 = cvt_pk_bf16(p0, p1);
+            pw[part][x] = w2;
+            p0 -= __uint_as_float(w2 << 16);
+            p1 -= __uint_as_float(w2 & 0xffff0000u);
+          }
+        }
+#pragma unroll
+        for (int db = 0; db < kBlocks; ++db) {
+          u32x4 vt;
+#pragma unroll
+          for (int hi = 0; hi < 2; ++hi) {
+            const int r = 4 * kGroups * (2 * half + hi) + 4 * g + ((ln & 15) >> 2);
+            const int chunk = db * (kN / 8) + (kN == 32 ? 2 * ((ln >> 4) & 1) : 0) + ((ln & 3) >> 1);
+            const unsigned char *at = v_from + r * kRowBytes + ((chunk ^ G::v_key(r)) << 4) + 8 * (ln & 1);
+            const u32x2 t = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at));
+            vt[2 * hi] = t.x;
+            vt[2 * hi + 1] = t.y;
+          }
+          if constexpr (kCareful) {
+            u32x4 code, one;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t w2 = pw[0][x];  // (zero only for weights below the least bf16 value)
+              one[x] = (w2 & 0xffffu ? 0x3f80u : 0u) | (w2 >> 16 ? 0x3f800000u : 0u);
+              uint32_t pair = vt[x];
+              code[x] = take_not_finite(pair);
+              vt[x] = pair;
+            }
+            Acc<kN> codes;
+            clear(codes);
+            codes = product<kN>(code, one, codes);
+            mfma_settle();
+#pragma unroll
+            for (int r = 0; r < kAcc; ++r) o_acc[db][r] += not_finite_sum(codes[r]);
+          }
+#pragma unroll
+          for (int part = kParts - 1; part >= 0; --part)  // the small part first
+            o_acc[db] = product<kN>(vt, u32x4{pw[part][0], pw[part][1], pw[part][2], pw[part][3]}, o_acc[db]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int db = 0; db < kBlocks; ++db) {
+        Acc<kN> codes;
+        if constexpr (kCareful) clear(codes);
+#pragma unroll
+        for (int x = 0; x < kScores; ++x) {  // the product's rows are those of score x of the column's lanes
+          const int row = 4 * kGroups * (x >> 2) + 4 * g + (x & 3), c = db * (kN / 4) + (in_n >> 2);
+          float v = *reinterpret_cast<const float *>(v_from + row * kRowBytes + ((c ^ G::v_key(row)) << 4) + 4 * (in_n & 3));
+          if constexpr (kCareful) {
+            const float code = not_finite_code(__float_as_uint(v));
+            v = code == 0.f ? v : 0.f;
+            codes = product<kN>(code, sc[x] == 0.f ? 0.f : 1.f, codes);
+          }
+          o_acc[db] = product<kN>(v, sc[x], o_acc[db]);
+        }
+        if constexpr (kCareful) {
+          mfma_settle();
+#pragma unroll
+          for (int r = 0; r < kAcc; ++r) o_acc[db][r] += not_finite_sum(codes[r]);
+        }
+      }
+    }
+    mfma_settle();  // O is read by the next stage's rescale, or after the last
+  };
+  auto walk = [&](auto with_care) __attribute__((always_inline)) {
+    m_run = -INFINITY;
+    l_run = 0.f;
+#pragma unroll
+    for (int db = 0; db < kBlocks; ++db) clear(o_acc[db]);
+    ids_from = -64;
+    uint32_t first_there = 0;
+    // (the first cached stage is requested before the tree's own rows are waited for)
+    int ahead = 0;
+    while (ahead < n_steps && stage_at(ahead) < st.tree) ++ahead;
+    issue(ahead);
+    first_there = rows_there;
+    for (int step = 0; step < n_steps; ++step) {
+      const int stage = stage_at(step);
+      unsigned char *const to = group_lds + (G::kSlots == 2 ? (step & 1) * G::kStage : 0);
+      uint32_t seen = 0;
+      if (stage < st.tree) {
+        land_tree(to, stage);
+        const int left = T - stage * kStageRows;
+        seen = left >= 32 ? ~0u : (1u << left) - 1u;
+      } else if (stage < n_stages) {
+        seen = first_there;
+        land(to, seen);
+        issue(step + 1);
+        first_there = rows_there;
+      }
+      if constexpr (kCw > 1) lds_barrier();
+      if (active && stage < n_stages && seen != 0) take_stage(to, stage, seen, with_care);
+    }
+  };
+  walk(std::false_type{});
+  {
+    // Zero weights times values of V that are not finite, or products that leave the range of fp32: such a range is done once more, with care.
+    float sum = 0.f;
+#pragma unroll
+    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+      for (int r = 0; r < kAcc; ++r) sum += o_acc[db][r];
+    if (active && __builtin_amdgcn_ballot_w64(!(fabsf(sum) < INFINITY)) != 0 && lane == 0) s_any = 1;
+    lds_barrier();
+    if (s_any) {
+      lds_barrier();
+      walk(std::true_type{});
+    }
+  }
+
+  // ---- results.  Waves of other rows have parts of the same columns: they meet in LDS, and share the quads of O.
+#pragma unroll
+  for (int o = kN; o < kWave; o <<= 1) l_run += __shfl_xor(l_run, o, kWave);
+  constexpr int kOwn = G::kQuads / kRw;  // quads that a wave stores
+  f32x4 mine[kOwn];
+  const int first_quad = rw * kOwn;
+  auto quad_of = [&](int x) __attribute__((always_inline)) {
+    const Acc<kN> &o = o_acc[x / (kAcc / 4)];
+    const int r = x % (kAcc / 4) * 4;
+    return f32x4{o[r], o[r + 1], o[r + 2], o[r + 3]};
+  };
+  if constexpr (kRw > 1) {
+    s_ml[wave][0][lane] = m_run;
+    s_ml[wave][1][lane] = l_run;
+    lds_barrier();  // everyone is done with the stages too
+    float M = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kRw; ++w) M = fmaxf(M, s_ml[w * kCw + cw][0][lane]);
+    const float safe = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int w = 0; w < kRw; ++w) {
+      const float f = fast_exp2(s_ml[w * kCw + cw][0][lane] - safe);
+      total += f == 0.f ? 0.f : f * s_ml[w * kCw + cw][1][lane];
+    }
+    const float f = fast_exp2(m_run - safe);
+    f32x4 *const room = reinterpret_cast<f32x4 *>(smem);  // [4 waves][quads][lanes]
+#pragma unroll
+    for (int x = 0; x < G::kQuads; ++x) {
+      const f32x4 v = quad_of(x);
+      room[(wave * G::kQuads + x) * kWave + lane] = f == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : v * f;
+    }
+    lds_barrier();
+#pragma unroll
+    for (int x = 0; x < kOwn; ++x) {
+      mine[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kRw; ++w) mine[x] += room[((w * kCw + cw) * G::kQuads + first_quad + x) * kWave + lane];
+    }
+    m_run = M;
+    l_run = total;
+  } else {
+#pragma unroll
+    for (int x = 0; x < kOwn; ++x) mine[x] = quad_of(x);
+  }
+  if (!there) return;
+  if (pieces == 1) {
+    const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : l_run;  // NaN stays
+#pragma unroll
+    for (int x = 0; x < kOwn; ++x) store_quad<kBf16>(p.out, row_out * D + 4 * kGroups * (first_quad + x) + 4 * (lane / kN), mine[x], inv);
+    if (p.lse && rw == 0 && lane < kN) p.lse[row_out] = (m_run + __builtin_amdgcn_logf(l_run)) * kLn2;
+  } else {
+    const size_t part = (size_t)first_slot * kCw + cw;
+#pragma unroll
+    for (int x = 0; x < kOwn; ++x) *reinterpret_cast<f32x4 *>(p.part_o + ((part * G::kQuads + first_quad + x) * kWave + lane) * 4) = mine[x];
+    if (rw == 0) {
+      p.part_ml[(part * 2 + 0) * kWave + lane] = m_run;
+      p.part_ml[(part * 2 + 1) * kWave + lane] = l_run;
+    }
+  }
+}
+
+// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the pieces s of a unit, always in the same order.  A workgroup has kN columns of a
+// unit and four quads of O; its waves take the pieces in turn and meet in LDS.
+template <bool kBf16, int D, int kN, int kCw, int kWaves>
+__global__ __launch_bounds__(kWaves *kWave) void paged_merge_kernel(PagedParams p) {
+  using G = PagedGeo<kBf16, D, kN, kCw>;
+  constexpr int kShare = G::kQuads / 4;  // workgroups that share the columns' O
+  __shared__ float s_part[kWaves > 1 ? kWaves - 1 : 1][18][kWave];
+  const int share = blockIdx.x % kShare, cw = blockIdx.x / kShare % kCw;
+  const unsigned item = blockIdx.x / (kCw * kShare);
+  const unsigned unit = item / (unsigned)p.blocks, b = unit / (unsigned)p.H_kv;
+  const int block = (int)(item - unit * (unsigned)p.blocks), hk = (int)(unit - b * (unsigned)p.H_kv);
+  const int T = clamped(p.n_nodes[b] - 1, p.T_max - 1) + 1, columns = p.group * T;
+  if ((block * kCw + cw) * kN >= columns) return;
+  const u32x4 record = *reinterpret_cast<const u32x4 *>(p.records + 4 * (size_t)item);
+  const int first = (int)record.x, stride = (int)record.y, P = (int)record.z;
+  if (P <= 1) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = (block * kCw + cw) * kN + lane % kN;
+  const bool there = column < columns;
+  const int ln = there ? lane : 0;  // lanes past the last column read lane 0's data and store nothing
+  float acc[16], M = -INFINITY, total = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+  auto join = [&](const float (&o)[16], float m, float l) __attribute__((always_inline)) {
+    const float M_new = fmaxf(M, m), safe = M_new == -INFINITY ? 0.f : M_new;
+    const float a_old = fast_exp2(M - safe), a_new = fast_exp2(m - safe);
+    total = total * a_old + (a_new == 0.f ? 0.f : l * a_new);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = (a_old == 0.f ? 0.f : acc[r] * a_old) + (a_new == 0.f ? 0.f : o[r] * a_new);
+    M = M_new;
+  };
+  constexpr int kTogether = 4;  // pieces of a wave that are requested together
+  for (int s0 = wave; s0 < P; s0 += kTogether * kWaves) {
+    f32x4 o[kTogether][4];
+    float m[kTogether], l[kTogether];
+#pragma unroll
+    for (int k = 0; k < kTogether; ++k) {
+      const int s = s0 + k * kWaves < P ? s0 + k * kWaves : P - 1;  // past the last: that once more, not used
+      const size_t part = ((size_t)first + (size_t)s * stride) * kCw + cw;
+      m[k] = p.part_ml[(part * 2 + 0) * kWave + ln];
+      l[k] = p.part_ml[(part * 2 + 1) * kWave + ln];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[k][x] = *reinterpret_cast<const f32x4 *>(p.part_o + ((part * G::kQuads + 4 * share + x) * kWave + ln) * 4);
+    }
+    __builtin_amdgcn_sched_barrier(0);  // all of them are requested first
+#pragma unroll
+    for (int k = 0; k < kTogether; ++k) {
+      if (s0 + k * kWaves < P) {  // uniform
+        float x[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] = o[k][r / 4][r % 4];
+        join(x, m[k], l[k]);
+      }
+    }
+  }
+  if constexpr (kWaves > 1) {
+    if (wave > 0) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s_part[wave - 1][r][lane] = acc[r];
+      s_part[wave - 1][16][lane] = M;
+      s_part[wave - 1][17][lane] = total;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < kWaves - 1; ++w) {
+      float x[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = s_part[w][r][lane];
+      join(x, s_part[w][16][lane], s_part[w][17][lane]);
+    }
+  }
+  if (!there) return;
+  const int head = column / T, node = column - head * T;
+  const size_t row = ((size_t)b * p.H + hk * p.group + head) * p.T_max + node;
+  const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+    store_quad<kBf16>(p.out, row * D + 4 * G::kGroups * (4 * share + x) + 4 * (lane / kN), f32x4{acc[4 * x], acc[4 * x + 1], acc[4 * x + 2], acc[4 * x + 3]}, inv);
+  if (p.lse && share == 0 && lane < kN) p.lse[row] = (M + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
+// ------------------------------------------------------------------------------------
+// host side
+// ------------------------------------------------------------------------------------
+// Partial results of a call, at most: a slot per range, of 32 * kCw columns.  More units than that are not cut.
+constexpr int kPagedResident = 512, kPagedRanges = 1024;
+
+// Ranges of a call whose units are cut, a bound that needs no device.  (Smaller trees and other shapes of the waves have more units of fewer columns.)
+static long long paged_ranges(int B, int H, int L_max) {
+  const long long stages = (L_max + kStageRows - 1ll) / kStageRows + PROPD_MAX_TREE / kStageRows;
+  const long long most = (long long)B * H * stages * 4;  // blocks of a unit: no more than four per head
+  return most < kPagedRanges ? most : kPagedRanges;
+}
+
+size_t paged_attention_workspace_bytes(int B, int H, int L_max, int T_max) {
+  const size_t ranges = (size_t)paged_ranges(B, H, L_max), blocks = (size_t)(T_max + 31) / 32;
+  return ranges * (4 * 16 * kWave * 4 * 4) + ranges * (4 * 2 * kWave * 4) + align_up((size_t)B * H * blocks * 16, 256);
+}
+
+template <bool kBf16, bool kCodes, int D, int kN, int kCw>
+static bool launch_paged(PagedParams p, long long ranges, int L_max, hipStream_t st) {
+  using G = PagedGeo<kBf16, D, kN, kCw>;
+  static std::atomic<uint64_t> set{0};
+  if (!allow_lds(reinterpret_cast<const void *>(&paged_attn_kernel<kBf16, kCodes, D, kN, kCw>), G::kLds, set)) return false;
+  p.blocks = (p.group * p.T_max + G::kColumns - 1) / G::kColumns;
+  const long long units = (long long)p.B * p.H_kv * p.blocks;
+  const int resident = (kBf16 ? 2 : 1) * compute_units();
+  p.resident = resident < kPagedResident ? resident : kPagedResident;
+  p.most_ranges = (int)ranges;
+  if (p.resident > p.most_ranges) p.resident = p.most_ranges;
+  const long long steps = ((L_max + kStageRows - 1ll) / kStageRows + (p.T_max + kStageRows - 1) / kStageRows + G::kRw - 1) / G::kRw;
+  p.may_split = units < p.most_ranges && steps > 1 ? 1 : 0;
+  const long long grid = !p.may_split ? units : units * steps < p.most_ranges ? units * steps : p.most_ranges;
+  hipLaunchKernelGGL((paged_attn_kernel<kBf16, kCodes, D, kN, kCw>), dim3((unsigned)grid), dim3(kPagedThreads), G::kLds, st, p);
+  if (!launch_ok()) return false;
+  if (!p.may_split) return true;
+  const dim3 merge((unsigned)(units * kCw * (G::kQuads / 4)));
+  if (units * kCw <= 64) hipLaunchKernelGGL((paged_merge_kernel<kBf16, D, kN, kCw, 4>), merge, dim3(4 * kWave), 0, st, p);
+  else hipLaunchKernelGGL((paged_merge_kernel<kBf16, D, kN, kCw, 1>), merge, dim3(kWave), 0, st, p);
+  return launch_ok();
+}
+
+template <bool kBf16, bool kCodes, int D>
+static bool launch_paged(const PagedParams &p, long long ranges, int L_max, hipStream_t st) {
+  const int columns = p.group * p.T_max;
+  return columns <= 16 ? launch_paged<kBf16, kCodes, D, 16, 1>(p, ranges, L_max, st)
+         : columns <= 64 ? launch_paged<kBf16, kCodes, D, 16, 4>(p, ranges, L_max, st)
+                         : launch_paged<kBf16, kCodes, D, 32, 4>(p, ranges, L_max, st);
+}
+
+}  // namespace propd
+
+extern "C" propd_status propd_paged_attention(const propd_tree *tree, propd_dtype dt, int32_t H, int32_t H_kv, int32_t d,
+                                              const propd_score_rule *rule, const void *q, const propd_paged_cache *cache, const void *k_tree,
+                                              const void *v_tree, const int32_t *seq_lens, void *out, float *lse, void *workspace,
+                                              size_t workspace_bytes, void *hip_stream) {
+  using namespace propd;
+  if (!tree || tree->B < 1 || tree->T_max < 1 || tree->T_max > PROPD_MAX_TREE || H < 1 || H_kv < 1 || H % H_kv != 0 || !score_rule_ok(rule) ||
+      !tree->n_nodes || !tree->anc || !q || !k_tree || !v_tree || !seq_lens || !out)
+    return PROPD_ERR_INVALID_ARG;
+  if (dt != PROPD_BF16 && dt != PROPD_F32) return PROPD_ERR_INVALID_ARG;
+  const propd_status status = paged_cache_check(cache, dt);
+  if (status != PROPD_OK) return status;
+  if (d != 64 && d != 128) return PROPD_ERR_UNSUPPORTED;
+  for (const void *ptr : {q, k_tree, v_tree, (const void *)out, (const void *)tree->anc, (const void *)workspace})
+    if (reinterpret_cast<uintptr_t>(ptr) % 16 != 0) return PROPD_ERR_INVALID_ARG;
+  const long long nodes = (long long)tree->B * H * tree->T_max;
+  if (nodes > (1ll << 27) || (long long)tree->B * H > (1ll << 20)) return PROPD_ERR_UNSUPPORTED;
+  const int L_max = cache->table_pages * cache->page_rows;
+  const size_t needed = paged_attention_workspace_bytes(tree->B, H, L_max, tree->T_max);
+  if (!workspace || workspace_bytes < needed) return PROPD_ERR_WORKSPACE;
+  PagedParams p;
+  p.pages = pages_of(cache);
+  p.q = reinterpret_cast<const unsigned char *>(q);
+  p.k_tree = reinterpret_cast<const unsigned char *>(k_tree);
+  p.v_tree = reinterpret_cast<const unsigned char *>(v_tree);
+  p.out = reinterpret_cast<unsigned char *>(out);
+  p.lse = lse;
+  p.seq_lens = seq_lens;
+  p.n_nodes = tree->n_nodes;
+  p.anc = tree->anc;
+  p.slopes = rule->slopes;
+  p.B = tree->B;
+  p.H = H;
+  p.H_kv = H_kv;
+  p.group = H / H_kv;
+  p.T_max = tree->T_max;
+  p.blocks = 0;
+  p.window = window_of(rule);
+  p.scale_log2e = rule->scale * kLog2e;
+  p.cap_in = rule->cap > 0.f ? rule->scale / rule->cap : 0.f;
+  p.cap_log2e = rule->cap * kLog2e;
+  const long long ranges = paged_ranges(p.B, H, L_max);
+  char *ws = reinterpret_cast<char *>(workspace);
+  p.part_o = reinterpret_cast<float *>(ws);
+  ws += (size_t)ranges * (4 * 16 * kWave * 4 * 4);
+  p.part_ml = reinterpret_cast<float *>(ws);
+  ws += (size_t)ranges * (4 * 2 * kWave * 4);
+  p.records = reinterpret_cast<int32_t *>(ws);
+  p.resident = p.most_ranges = p.may_split = 0;  // by the shape of the waves
+  hipStream_t st = as_stream(hip_stream);
+  const bool bf16 = dt == PROPD_BF16, codes = cache->dt == PROPD_E4M3;
+  bool ok;
+  if (d == 128) {
+    ok = bf16 ? (codes ? launch_paged<true, true, 128>(p, ranges, L_max, st) : launch_paged<true, false, 128>(p, ranges, L_max, st))
+              : (codes ? launch_paged<false, true, 128>(p, ranges, L_max, st) : launch_paged<false, false, 128>(p, ranges, L_max, st));
+  } else {
+    ok = bf16 ? (codes ? launch_paged<true, true, 64>(p, ranges, L_max, st) : launch_paged<true, false, 64>(p, ranges, L_max, st))
+              : (codes ? launch_paged<false, true, 64>(p, ranges, L_max, st) : launch_paged<false, false, 64>(p, ranges, L_max, st));
+  }
+  return ok ? PROPD_OK : PROPD_ERR_DEVICE;
+}

@@ -1439,6 +1439,12 @@ extern "C" size_t propd_workspace_bytes(propd_ws_kind which, int32_t B, int32_t 
     case PROPD_WS_GROUPED_ATTENTION:
       if (H < 1 || L_max < 0) return 0;
       return propd::grouped_attention_workspace_bytes(B, H, L_max, T_max);
+    case PROPD_WS_PAGED_ATTENTION:
+      if (H < 1 || L_max < 0) return 0;
+      return propd::paged_attention_workspace_bytes(B, H, L_max, T_max);
+    case PROPD_WS_ACCEPT_SAMPLED:
+      if (vocab < 1) return 0;
+      return propd::accept_sampled_workspace_bytes(B, T_max, vocab);
     case PROPD_WS_CACHE_EVICT:
       break;  // above
   }

@@ -108,6 +108,8 @@ __device__ __forceinline__ PagedStages paged_stages(int L, int T, int window) {
 struct PagedPlan {
   int most, ranges;
 };
+constexpr float kBack = 0x1p-31f, kForth = 0x1p31f;  // (a sequence has at most 2^30 cached rows and 128 others)
+constexpr float kMostPlain = 0x1p96f;  // sums of more are made with care: a call's pieces of less can be added up
 constexpr float kRangeCost = 3.f;  // steps that a range costs besides its own
 
 struct PagedSequence {
@@ -170,6 +172,8 @@ __device__ __forceinline__ void store_quad(unsigned char *out, size_t at, f32x4 
   if constexpr (kBf16) *reinterpret_cast<u32x2 *>(reinterpret_cast<uint16_t *>(out) + at) = u32x2{cvt_pk_bf16(v[0] * inv, v[1] * inv), cvt_pk_bf16(v[2] * inv, v[3] * inv)};
   else *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(out) + at) = f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
 }
+
+__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : l; }  // NaN stays
 
 // LDS written before is seen by the workgroup; loads from memory stay in flight.
 __device__ __forceinline__ void lds_barrier() {
@@ -357,7 +361,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
 
   float m_run, l_run;
   Acc<kN> o_acc[kBlocks];
-  const float tau = 8.f;
+  constexpr float kTau = 8.f;
 
   // ---- a stage: its scores, weights and what they add to O.  `seen`: a bit per row of the stage that exists.
   auto take_stage = [&](const unsigned char *from, int stage, uint32_t seen, auto with_care) __attribute__((always_inline)) {
@@ -422,8 +426,8 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
       if constexpr (kN == 16) m_blk = fmaxf(m_blk, __shfl_xor(m_blk, 16, kWave));
     }
     // A new reference is adopted only when the maximum exceeds the old one by 2^8: weights then exceed 1, by a factor that fp32 sums and bf16
-    // weights hold, and O is hardly ever scaled.  With care weights are at most 1.
-    if (__builtin_amdgcn_ballot_w64(m_blk > (kCareful ? m_run : m_run + tau)) != 0) {
+    // weights hold, and O is hardly ever scaled.  With care they are at most kBack as they meet V: no sum exceeds its largest value.
+    if (__builtin_amdgcn_ballot_w64(m_blk > (kCareful ? m_run : m_run + kTau)) != 0) {
       const float m_new = fmaxf(m_run, m_blk), m_safe = m_new == -INFINITY ? 0.f : m_new;
       const float alpha = fast_exp2(m_run - m_safe);
       l_run *= alpha;
@@ -438,6 +442,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
     for (int x = 0; x < kScores; ++x) {
       sc[x] = fast_exp2(sc[x] + neg_m);
       l_run += sc[x];  // of the weights as they are: lse is an fp32 result
+      if constexpr (kCareful) sc[x] *= kBack;
     }
     const unsigned char *const v_from = from + G::kPart;
     if constexpr (kBf16) {
@@ -545,16 +550,18 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
     }
   };
   walk(std::false_type{});
+  bool careful;
   {
-    // Zero weights times values of V that are not finite, or products that leave the range of fp32: such a range is done once more, with care.
+    // Zero weights times values of V that are not finite, or sums that leave the range of fp32 (or would, joined): such a range is done once more, with care.
     float sum = 0.f;
 #pragma unroll
     for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
-      for (int r = 0; r < kAcc; ++r) sum += o_acc[db][r];
-    if (active && __builtin_amdgcn_ballot_w64(!(fabsf(sum) < INFINITY)) != 0 && lane == 0) s_any = 1;
+      for (int r = 0; r < kAcc; ++r) sum += fabsf(o_acc[db][r]);
+    if (active && __builtin_amdgcn_ballot_w64(!(sum < kMostPlain)) != 0 && lane == 0) s_any = 1;
     lds_barrier();
-    if (s_any) {
+    careful = s_any != 0;
+    if (careful) {
       lds_barrier();
       walk(std::true_type{});
     }
@@ -606,7 +613,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
   }
   if (!there) return;
   if (pieces == 1) {
-    const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : l_run;  // NaN stays
+    const float inv = inverse(l_run) * (careful ? kForth : 1.f);
 #pragma unroll
     for (int x = 0; x < kOwn; ++x) store_quad<kBf16>(p.out, row_out * D + 4 * kGroups * (first_quad + x) + 4 * (lane / kN), mine[x], inv);
     if (p.lse && rw == 0 && lane < kN) p.lse[row_out] = (m_run + __builtin_amdgcn_logf(l_run)) * kLn2;
@@ -616,7 +623,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
     for (int x = 0; x < kOwn; ++x) *reinterpret_cast<f32x4 *>(p.part_o + ((part * G::kQuads + first_quad + x) * kWave + lane) * 4) = mine[x];
     if (rw == 0) {
       p.part_ml[(part * 2 + 0) * kWave + lane] = m_run;
-      p.part_ml[(part * 2 + 1) * kWave + lane] = l_run;
+      p.part_ml[(part * 2 + 1) * kWave + lane] = careful ? -l_run : l_run;  // the sign says so: sums are not negative
     }
   }
 }
@@ -641,12 +648,17 @@ __global__ __launch_bounds__(kWaves *kWave) void paged_merge_kernel(PagedParams 
   const bool there = column < columns;
   const int ln = there ? lane : 0;  // lanes past the last column read lane 0's data and store nothing
   float acc[16], M = -INFINITY, total = 0.f;
+  bool careful = false;  // acc is kBack of what it stands for, as are pieces made with care
 #pragma unroll
   for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-  auto join = [&](const float (&o)[16], float m, float l) __attribute__((always_inline)) {
-    const float M_new = fmaxf(M, m), safe = M_new == -INFINITY ? 0.f : M_new;
-    const float a_old = fast_exp2(M - safe), a_new = fast_exp2(m - safe);
+  auto join = [&](const float (&o)[16], float m, float signed_l) __attribute__((always_inline)) {
+    const bool theirs = signbit(signed_l);
+    const float M_new = fmaxf(M, m), safe = M_new == -INFINITY ? 0.f : M_new, l = fabsf(signed_l);
+    float a_old = fast_exp2(M - safe), a_new = fast_exp2(m - safe);
     total = total * a_old + (a_new == 0.f ? 0.f : l * a_new);
+    a_old *= theirs && !careful ? kBack : 1.f;
+    a_new *= careful && !theirs ? kBack : 1.f;
+    careful = careful || theirs;
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[r] = (a_old == 0.f ? 0.f : acc[r] * a_old) + (a_new == 0.f ? 0.f : o[r] * a_new);
     M = M_new;
@@ -680,7 +692,7 @@ __global__ __launch_bounds__(kWaves *kWave) void paged_merge_kernel(PagedParams 
 #pragma unroll
       for (int r = 0; r < 16; ++r) s_part[wave - 1][r][lane] = acc[r];
       s_part[wave - 1][16][lane] = M;
-      s_part[wave - 1][17][lane] = total;
+      s_part[wave - 1][17][lane] = careful ? -total : total;
     }
     __syncthreads();
     if (wave > 0) return;
@@ -695,7 +707,7 @@ __global__ __launch_bounds__(kWaves *kWave) void paged_merge_kernel(PagedParams 
   if (!there) return;
   const int head = column / T, node = column - head * T;
   const size_t row = ((size_t)b * p.H + hk * p.group + head) * p.T_max + node;
-  const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
+  const float inv = inverse(total) * (careful ? kForth : 1.f);
 #pragma unroll
   for (int x = 0; x < 4; ++x)
     store_quad<kBf16>(p.out, row * D + 4 * G::kGroups * (4 * share + x) + 4 * (lane / kN), f32x4{acc[4 * x], acc[4 * x + 1], acc[4 * x + 2], acc[4 * x + 3]}, inv);

@@ -1,0 +1,249 @@
+"""Acceptance by sampling on the GPU against oracle/paged_cache.py.  Results are whole numbers and have to be equal: a case whose decisions
+and draws lie further than 1e-9 from every border (of probabilities in 64 bits), which the oracle says."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import to_dev, to_host
+from oracle import paged_cache as ref
+from paper_2402_13485_amd import synth
+from test_gpu_parity import pb  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def make_case(rng, dtype, B, T_max, V, drawn, sharp=3.0, inv=1.0, draft_inv=1.0, sizes=None, max_depth=None):
+    """Candidates: the likeliest tokens by a noisy estimate, or drawn from a draft near the target."""
+    shapes = [synth.random_tree(rng, int(rng.integers(1, T_max + 1)) if sizes is None else sizes[b], max_depth=max_depth) for b in range(B)]
+    n_nodes, parent, _ = synth.pad_trees(shapes, T_max)
+    logits = synth.from_float((rng.normal(size=(B, T_max, V)) * sharp).astype(np.float32), dtype)
+    z = synth.as_float(logits).astype(np.float64)
+    draft, token = None, np.full((B, T_max), -1, np.int32)
+    if drawn:
+        draft = synth.from_float((0.8 * z + rng.normal(size=z.shape)).astype(np.float32), dtype)
+    for b in range(B):
+        seen = {}
+        for i in range(1, int(n_nodes[b])):
+            p = int(parent[b, i])
+            if drawn:
+                token[b, i] = rng.choice(V, p=ref.softmax(synth.as_float(draft[b, p]).astype(np.float64), draft_inv))
+            else:
+                if p not in seen:
+                    seen[p] = np.argsort(-(z[b, p] + rng.normal(size=V)))
+                token[b, i] = seen[p][0]
+                seen[p] = np.roll(seen[p], -1)
+    u, u_next = rng.random((B, T_max)).astype(np.float32), rng.random(B).astype(np.float32)
+    return dict(n_nodes=n_nodes, parent=parent, token=token, logits=logits, draft=draft, u=u, u_next=u_next, inv=inv, draft_inv=draft_inv)
+
+
+def dev_args(pb, x):
+    tree = pb.Tree(to_dev(x["n_nodes"]), to_dev(x["parent"]), to_dev(x["token"]))
+    kw = dict(inv_temperature=x["inv"], draft_inv_temperature=x["draft_inv"])
+    if x["draft"] is not None:
+        kw["draft_logits"] = to_dev(x["draft"])
+    return (tree, to_dev(x["logits"]), to_dev(x["u"]), to_dev(x["u_next"])), kw
+
+
+def check(pb, x, path_stride=None, **more):
+    T_max = x["parent"].shape[1]
+    stride = path_stride or T_max
+    as64 = lambda a: None if a is None else synth.as_float(a).astype(np.float64)
+    want = ref.accept_sampled(x["n_nodes"], x["parent"], x["token"], as64(x["logits"]), float(np.float32(x["inv"])), as64(x["draft"]),
+                              float(np.float32(x["draft_inv"])), x["u"], x["u_next"], stride)
+    assert want[3] > 1e-9, "the case is on a border"
+    args, kw = dev_args(pb, x)
+    got = pb.propd_accept_sampled(*args, path_stride=path_stride, **kw, **more)
+    torch.cuda.synchronize()
+    for name, g, w in zip(("length", "path", "next"), got, want):
+        assert to_host(g).tolist() == w.tolist(), name
+    return want
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [1, 2, 7, 64, 1001, 4095, 4096, 4097, 12288])
+def test_vocabularies(pb, V, dtype, drawn):
+    """One token to several slices, rows that start anywhere; paths of several nodes among them."""
+    rng = np.random.default_rng(V)
+    x = make_case(rng, dtype, 6, 12, V, drawn, sharp=6.0)
+    if V == 1:  # (a token that has all probability: a test on its border)
+        x["u"][...] = 0.5
+    check(pb, x)
+
+
+@pytest.mark.parametrize("inv,draft_inv", [(1.0, 1.0), (1.25, 0.8), (8.0, 3.0), (0.01, 0.5)])
+@pytest.mark.parametrize("drawn", [False, True])
+def test_temperatures(pb, drawn, inv, draft_inv):
+    rng = np.random.default_rng(int(100 * inv))
+    check(pb, make_case(rng, "f32", 8, 20, 300, drawn, inv=inv, draft_inv=draft_inv))
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("seed", range(6))
+def test_trees(pb, seed, drawn):
+    """Random trees up to 128 nodes, wide ones and chains, with small vocabularies whose siblings repeat tokens."""
+    rng = np.random.default_rng(seed)
+    V = [3, 5, 40, 200, 9, 33][seed]
+    x = make_case(rng, "bf16" if seed % 2 else "f32", 9, 128, V, drawn, sharp=1.5)
+    want = check(pb, x)
+    assert want[0].max() > 1
+    check(pb, x, path_stride=int(want[0].max()))
+    check(pb, x, path_stride=1)
+    check(pb, x, path_stride=max(1, int(want[0].max()) - 1))
+    check(pb, x, path_stride=300)
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("shape", ["chain", "star"])
+def test_chains_and_stars(pb, shape, drawn):
+    rng = np.random.default_rng(3)
+    x = make_case(rng, "bf16", 5, 128, 6, drawn, sharp=1.0)
+    T = 128
+    x["n_nodes"][:] = T
+    x["parent"][:] = np.arange(-1, T - 1) if shape == "chain" else np.where(np.arange(T) == 0, -1, 0)
+    x["token"][:] = rng.integers(0, 6, (5, T))
+    x["u"][:] = (0.3 if shape == "chain" else 0.999) * x["u"] + (0.0 if shape == "chain" else 0.0005)
+    check(pb, x)
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+def test_tokens_outside_the_vocabulary(pb, drawn):
+    """Refused, and what is left is as before."""
+    rng = np.random.default_rng(5)
+    x = make_case(rng, "f32", 8, 16, 50, drawn)
+    outside = rng.random(x["token"].shape) < 0.4
+    x["token"] = np.where(outside, rng.choice([-1, 50, 2 ** 31 - 1, -2 ** 31], size=x["token"].shape), x["token"]).astype(np.int32)
+    check(pb, x)
+
+
+def test_siblings_of_the_same_token(pb):
+    """A token that was refused has nothing left: its second candidate is refused whatever the number."""
+    rng = np.random.default_rng(6)
+    x = make_case(rng, "f32", 4, 6, 20, False)
+    x["n_nodes"][:], x["parent"][:] = 6, [-1, 0, 0, 0, 0, 0]
+    x["token"][:] = [0, 7, 7, 3, 7, 3]
+    x["u"][:] = np.array([0, .999, 0., .999, 1e-30, 0.])
+    want = check(pb, x)
+    assert (want[0] == 1).all() and not np.isin(want[2], [3, 7]).any()
+
+
+def test_numbers_at_their_ends(pb):
+    """u of zero accepts whatever has probability, the largest below 1 hardly anything; u_next of zero takes the first token."""
+    rng = np.random.default_rng(7)
+    most = np.float32(1 - 2.0 ** -24)
+    for u, u_next in ((0.0, 0.0), (most, most), (0.0, most), (most, 0.0)):
+        x = make_case(rng, "f32", 3, 9, 100, False, sharp=0.5)
+        x["u"][:], x["u_next"][:] = u, u_next
+        args, kw = dev_args(pb, x)
+        a, path, nxt = (to_host(t) for t in pb.propd_accept_sampled(*args, **kw))
+        for b in range(3):
+            children = [i for i in range(1, x["n_nodes"][b]) if x["parent"][b, i] == 0]
+            if u == 0.0 and children:
+                assert path[b, 1] == children[0]
+            if u_next == 0.0 and a[b] == 1:
+                gone = [x["token"][b, i] for i in children]
+                assert nxt[b] == min(v for v in range(100) if v not in gone)
+            if u_next == most and a[b] == 1:
+                gone = [x["token"][b, i] for i in children]
+                assert nxt[b] == max(v for v in range(100) if v not in gone)
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [40, 5000])
+def test_logits_that_are_not_finite(pb, V, dtype, drawn):
+    """Masked tokens (-inf), NaN as those, whole rows without probability, +inf that share it."""
+    rng = np.random.default_rng(V)
+    x = make_case(rng, dtype, 8, 10, V, drawn)
+    z = synth.as_float(x["logits"]).astype(np.float32)
+    z[rng.random(z.shape) < 0.3] = -np.inf
+    z[rng.random(z.shape) < 0.05] = np.nan
+    z[1, 0], z[2, 0] = -np.inf, np.nan
+    z[3, :, [3, 17, 30]] = np.inf
+    z[4, 0] = -np.inf
+    z[4, 0, 21] = 2.0
+    x["logits"] = synth.from_float(z, dtype)
+    if drawn:
+        y = synth.as_float(x["draft"]).astype(np.float32)
+        y[rng.random(y.shape) < 0.2] = -np.inf
+        y[5, 0] = -np.inf
+        x["draft"] = synth.from_float(y, dtype)
+    x["u"] = (0.01 + 0.98 * x["u"]).astype(np.float32)
+    for b in (1, 2, 4):  # no test on a border: 0 < 0
+        x["n_nodes"][b] = 1
+    want = check(pb, x)
+    assert want[2][1] == 0 and want[2][2] == 0 and want[2][4] == 21
+
+
+def test_nothing_left_is_the_likeliest_token(pb):
+    """All tokens of a small vocabulary refused (with numbers beyond what a caller may give, so that nothing passes)."""
+    i32 = dict(dtype=torch.int32, device="cuda")
+    tree = pb.Tree(torch.tensor([4], **i32), torch.tensor([[-1, 0, 0, 0]], **i32), torch.tensor([[0, 0, 1, 2]], **i32))
+    logits = torch.tensor([[[0.5, 2.0, 2.0]] * 4], device="cuda")
+    u = torch.full((1, 4), 2.0, device="cuda")
+    a, path, nxt = pb.propd_accept_sampled(tree, logits, u, torch.full((1,), 0.5, device="cuda"))
+    assert a.tolist() == [1] and path.tolist() == [[0, -1, -1, -1]] and nxt.tolist() == [1]
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+def test_the_same_bits_with_a_dirty_workspace_on_another_stream_and_in_a_graph(pb, drawn):
+    rng = np.random.default_rng(9)
+    x = make_case(rng, "bf16", 5, 40, 9000, drawn, sharp=4.0)
+    want = check(pb, x)
+    need = pb.workspace_bytes(pb.WS_ACCEPT_SAMPLED, 5, 40, vocab=9000)
+    check(pb, x, workspace=torch.full((need,), 0xff, dtype=torch.uint8, device="cuda"))
+    args, kw = dev_args(pb, x)
+    ws = torch.full((need,), 0x7f, dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = pb.propd_accept_sampled(*args, workspace=ws, **kw)
+    side.synchronize()
+    assert [to_host(t).tolist() for t in got] == [w.tolist() for w in want[:3]]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = pb.propd_accept_sampled(*args, workspace=ws, **kw)
+    for n in range(4):
+        u = rng.random(x["u"].shape).astype(np.float32)
+        args[2].copy_(to_dev(u))
+        for t in got:
+            t.fill_(-9)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in got]
+        eager = pb.propd_accept_sampled(*args, **kw)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, eager))
+        assert to_host(replayed[0]).tolist() == ref.accept_sampled(x["n_nodes"], x["parent"], x["token"], synth.as_float(x["logits"]).astype(np.float64), 1.0,
+                                                                   None if not drawn else synth.as_float(x["draft"]).astype(np.float64), 1.0, u, x["u_next"], 40)[0].tolist()
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+def test_large_batch_and_vocabulary(pb, drawn):
+    """The benchmark's vocabulary, and one whose slices fill the last workgroup's table."""
+    rng = np.random.default_rng(10)
+    check(pb, make_case(rng, "bf16", 6, 24, 32000, drawn, sharp=4.0))
+    check(pb, make_case(rng, "f32", 1, 3, 300001, drawn, sharp=4.0, sizes=[3]))
+
+
+def test_frequencies(pb):
+    """4096 sequences of the same trees: first tokens are distributed as the target (five standard deviations)."""
+    rng = np.random.default_rng(11)
+    B, V = 4096, 6
+    p = rng.dirichlet(np.ones(V), size=4).astype(np.float64)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    parent = torch.tensor([[-1, 0, 0, 1]], **i32).expand(B, 4).contiguous()
+    logits = torch.tensor(np.log(p), dtype=torch.float32, device="cuda").expand(B, 4, V).contiguous()
+    for drawn in (False, True):
+        if drawn:
+            q = rng.dirichlet(np.ones(V), size=4)
+            draft = torch.tensor(np.log(q), dtype=torch.float32, device="cuda").expand(B, 4, V).contiguous()
+            token = np.stack([rng.choice(V, size=B, p=q[max(k, 0)]) for k in (-1, 0, 0, 1)], 1)
+        else:
+            draft, token = None, np.tile([0, 3, 1, 2], (B, 1))
+        tree = pb.Tree(torch.full((B,), 4, **i32), parent, torch.tensor(token, **i32))
+        u, u_next = torch.tensor(rng.random((B, 4)), dtype=torch.float32, device="cuda"), torch.tensor(rng.random(B), dtype=torch.float32, device="cuda")
+        a, path, nxt = (to_host(t) for t in pb.propd_accept_sampled(tree, logits, u, u_next, draft_logits=draft))
+        first = np.where(a > 1, token[np.arange(B), np.clip(path[:, 1], 0, 3)], nxt)
+        counts = np.bincount(first, minlength=V)
+        assert (np.abs(counts - B * p[0]) < 5 * np.sqrt(B * p[0] * (1 - p[0]))).all()

@@ -83,7 +83,9 @@ def _init_marshal(lib: ctypes.CDLL) -> None:
         return
     for init, names in ((native.init, ("propd_tree_mask", "propd_tree_attention", "propd_early_prune", "propd_early_prune_prob",
                                        "propd_accept_path", "propd_commit_path", "propd_workspace_bytes")),
-                        (native.init_cache, ("propd_grouped_attention", "propd_cache_observe", "propd_cache_evict", "propd_rotary"))):
+                        (native.init_cache, ("propd_grouped_attention", "propd_cache_observe", "propd_cache_evict", "propd_rotary")),
+                        (native.init_paged, ("propd_paged_attention", "propd_paged_commit", "propd_paged_prompt", "propd_paged_read",
+                                             "propd_accept_sampled"))):
         init(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in names))
     _marshal = native
 
@@ -788,6 +790,12 @@ def propd_paged_attention(tree: Tree, q, cache: PagedCache, k_tree, v_tree, seq_
                           slopes: Optional[torch.Tensor] = None, want_lse: bool = False, out: Optional[torch.Tensor] = None,
                           lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """-> out [B,H,T_max,d], or (out, lse) if ``want_lse`` or an ``lse`` tensor is given."""
+    native = _native()
+    if native is not None:
+        r = native.paged_attention(tree.n_nodes, tree.parent, tree.token, tree.depth, tree.anc, cache.k_pages, cache.v_pages, cache.page_table, cache.k_scale,
+                                   cache.v_scale, q, k_tree, v_tree, seq_lens, scale, cap, window, slopes, want_lse, out, lse, workspace, _stream)
+        if r is not None:
+            return _done(r, "propd_paged_attention")
     B, H, H_kv, T_max, d, _ = _shared_heads(tree, q, k_tree, cache.k_pages)
     dt, i32, f32 = _dt(q), torch.int32, torch.float32
     rows = (B, H_kv, T_max, d)
@@ -816,6 +824,12 @@ def propd_paged_commit(tree: Tree, accept_len: torch.Tensor, accept_path: torch.
                        seq_lens_out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Appends the accepted nodes' K/V rows to their sequences' pages IN PLACE, advances ``seq_lens`` in place (or writes the new lengths to
     ``seq_lens_out``) and returns the step's tokens, int32 [B,out_stride], -1 padded."""
+    native = _native()
+    if native is not None:
+        r = native.paged_commit(tree.n_nodes, tree.parent, tree.token, tree.depth, tree.anc, cache.k_pages, cache.v_pages, cache.page_table, cache.k_scale,
+                                cache.v_scale, accept_len, accept_path, next_token, k_tree, v_tree, seq_lens, seq_lens_out, out_stride, _stream)
+        if r is not None:
+            return _done(r, "propd_paged_commit")
     if k_tree.dim() != 4 or accept_path.dim() != 2:
         raise ValueError("k_tree has four dimensions, accept_path two")
     B, H_kv, T_max, d = k_tree.shape
@@ -850,6 +864,12 @@ def propd_paged_prompt(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, seq_
                        seq_lens_out: Optional[torch.Tensor] = None) -> None:
     """Appends rows of prompts, k and v [B,H_kv,S,d], to their sequences' pages IN PLACE and advances ``seq_lens`` in place (or writes the new
     lengths to ``seq_lens_out``)."""
+    native = _native()
+    if native is not None:
+        r = native.paged_prompt(cache.k_pages, cache.v_pages, cache.page_table, cache.k_scale, cache.v_scale, k, v, seq_lens, n_rows, seq_lens_out, _stream)
+        if r is not None:
+            _done(None if r is True else r, "propd_paged_prompt")
+            return
     if k.dim() != 4:
         raise ValueError("k has four dimensions")
     B, H_kv, S, d = k.shape
@@ -866,6 +886,12 @@ def propd_paged_prompt(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, seq_
 
 def propd_paged_read(cache: PagedCache, seq_lens: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor, first: Optional[torch.Tensor] = None):
     """-> (k_out, v_out), [B,H_kv,S,d], with rows ``first[b]`` .. ``first[b] + S - 1`` of every sequence, as far as it has them."""
+    native = _native()
+    if native is not None:
+        r = native.paged_read(cache.k_pages, cache.v_pages, cache.page_table, cache.k_scale, cache.v_scale, seq_lens, k_out, v_out, first, _stream)
+        if r is not None:
+            _done(None if r is True else r, "propd_paged_read")
+            return k_out, v_out
     if k_out.dim() != 4:
         raise ValueError("k_out has four dimensions")
     B, H_kv, S, d = k_out.shape
@@ -886,6 +912,12 @@ def propd_accept_sampled(tree: Tree, logits: torch.Tensor, u: torch.Tensor, u_ne
                          workspace: Optional[torch.Tensor] = None):
     """-> (accept_len int32 [B], accept_path int32 [B,path_stride], next_token int32 [B]).  ``u`` float32 [B,T_max] and ``u_next`` float32 [B] are random
     numbers in [0,1); ``draft_logits`` is given if the candidates were drawn from the draft's distributions."""
+    native = _native()
+    if native is not None:
+        r = native.accept_sampled(tree.n_nodes, tree.parent, tree.token, tree.depth, tree.anc, logits, u, u_next, inv_temperature, draft_logits,
+                                  draft_inv_temperature, path_stride, workspace, _stream)
+        if r is not None:
+            return _done(r, "propd_accept_sampled")
     if logits.dim() != 3:
         raise ValueError("logits has three dimensions")
     B, T_max, vocab = logits.shape

@@ -35,6 +35,11 @@ struct Entries {
   decltype(&propd_cache_observe) cache_observe = nullptr;
   decltype(&propd_cache_evict) cache_evict = nullptr;
   decltype(&propd_rotary) rotary = nullptr;
+  decltype(&propd_paged_attention) paged_attention = nullptr;
+  decltype(&propd_paged_commit) paged_commit = nullptr;
+  decltype(&propd_paged_prompt) paged_prompt = nullptr;
+  decltype(&propd_paged_read) paged_read = nullptr;
+  decltype(&propd_accept_sampled) accept_sampled = nullptr;
 };
 
 struct NotThis {};  // the Python code takes over
@@ -243,6 +248,20 @@ PyObject *py_init_cache(PyObject *, PyObject *const *a, Py_ssize_t n) {
   take(a[1], entries.cache_observe);
   take(a[2], entries.cache_evict);
   take(a[3], entries.rotary);
+  if (PyErr_Occurred()) return nullptr;
+  Py_RETURN_NONE;
+}
+
+PyObject *py_init_paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (n != 5) {
+    PyErr_SetString(PyExc_TypeError, "init_paged: five addresses");
+    return nullptr;
+  }
+  take(a[0], entries.paged_attention);
+  take(a[1], entries.paged_commit);
+  take(a[2], entries.paged_prompt);
+  take(a[3], entries.paged_read);
+  take(a[4], entries.accept_sampled);
   if (PyErr_Occurred()) return nullptr;
   Py_RETURN_NONE;
 }
@@ -636,10 +655,218 @@ PyObject *py_rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// ---- a paged cache and acceptance by sampling
+
+// the fields of binding.PagedCache: k_pages, v_pages, page_table, k_scale, v_scale
+struct Paged {
+  propd_paged_cache c;
+  int64_t capacity;
+};
+Paged paged_of(PyObject *const *f, const Device &on, at::ScalarType type, int64_t B, int64_t Hk, int64_t d) {
+  const at::Tensor &k = tensor(f[0]), &table0 = tensor(f[2]);
+  need(k.dim() == 4 && table0.dim() == 2);
+  const bool codes = k.scalar_type() == at::kFloat8_e4m3fn;
+  const at::ScalarType kind = codes ? at::kFloat8_e4m3fn : type;
+  const int64_t n = k.size(0), rows = k.size(2);
+  on(f[0], kind, {n, Hk, rows, d});
+  const at::Tensor &v = on(f[1], kind, {n, Hk, rows, d}), &table = on(f[2], at::kInt, {B, table0.size(1)});
+  Paged p;
+  p.c.k_pages = k.data_ptr();
+  p.c.v_pages = v.data_ptr();
+  p.c.k_scale = codes ? (uint8_t *)on(f[3], at::kByte, {n, Hk, rows}).data_ptr() : nullptr;
+  p.c.v_scale = codes ? (uint8_t *)on(f[4], at::kByte, {n, Hk, rows}).data_ptr() : nullptr;
+  if (!codes) need(f[3] == Py_None && f[4] == Py_None);
+  p.c.page_table = (const int32_t *)table.data_ptr();
+  p.c.dt = codes ? PROPD_E4M3 : type_of(k);
+  p.c.n_pages = size32(n);
+  p.c.table_pages = size32(table.size(1));
+  p.c.page_rows = size32(rows);
+  p.capacity = table.size(1) * rows;
+  return p;
+}
+
+// a cache that is written to: its tensors lie apart from each other and from what is read
+void written_apart(PyObject *const *f, std::initializer_list<PyObject *> read, PyObject *lens, PyObject *lens_out) {
+  for (int i : {0, 1, 3, 4}) {
+    if (f[i] == Py_None) continue;
+    const at::Tensor &t = tensor(f[i]);
+    for (int j = 0; j < 5; ++j) need(j == i || f[j] == Py_None || !overlap(t, tensor(f[j])));
+    apart(t, read);
+    apart(t, {lens, lens_out});
+  }
+  same_or_apart(tensor(lens_out), tensor(lens));
+  apart(tensor(lens_out), read);
+  apart(tensor(lens_out), {f[2]});
+}
+
+// paged_attention(*tree, *cache, q, k_tree, v_tree, seq_lens, scale, cap, window, slopes, want_lse, out, lse, workspace, stream) -> out or (out, lse)
+PyObject *py_paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded([&]() -> Owned {
+    need(n == 23);
+    PyObject *const *f = a + 5, *const *x = a + 10;
+    const at::Tensor &q = tensor(x[0]), &kt0 = tensor(x[1]);
+    const propd_dtype dt = type_of(q);
+    const at::ScalarType type = q.scalar_type();
+    need(q.dim() == 4 && kt0.dim() == 4 && q.is_contiguous());
+    const Device on(q);
+    const int64_t B = q.size(0), H = q.size(1), T = q.size(2), d = q.size(3), Hk = kt0.size(1);
+    need(Hk >= 1 && H % Hk == 0);
+    const at::Tensor &kt = on(x[1], type, {B, Hk, T, d}), &vt = on(x[2], type, {B, Hk, T, d}), &seq = on(x[3], at::kInt, {B});
+    on(a[0], at::kInt, {B});
+    on(a[4], at::kLong, {B, T, 2});
+    const propd_tree tree = tree_of(a);
+    need(tree.B == B && tree.T_max == T);
+    const Paged cache = paged_of(f, on, type, B, Hk, d);
+    propd_score_rule rule;
+    rule.scale = real(x[4]);
+    rule.cap = real(x[5]);
+    rule.window = whole32(x[6]);
+    rule.slopes = on.optional<float>(x[7], at::kFloat, {H});
+    const bool want = truth(x[8]) || x[10] != Py_None;
+    at::Tensor out, lse;
+    {
+      const Unlocked u;
+      if (x[9] == Py_None) out = at::empty_like(q);
+      if (want && x[10] == Py_None) lse = at::empty({B, H, T}, q.options().dtype(at::kFloat));
+    }
+    if (x[9] != Py_None) out = on(x[9], type, q.sizes());
+    if (x[10] != Py_None) lse = on(x[10], at::kFloat, {B, H, T});
+    const std::initializer_list<PyObject *> read = {a[0], a[4], f[0], f[1], f[2], f[3], f[4], x[0], x[1], x[2], x[3], x[7]};
+    if (x[9] != Py_None) apart(out, read);
+    if (x[10] != Py_None) apart(lse, read);
+    need(!want || !overlap(out, lse));
+    if (x[11] != Py_None) {
+      apart(tensor(x[11]), read);
+      need(!overlap(tensor(x[11]), out) && (!want || !overlap(tensor(x[11]), lse)));
+    }
+    const Workspace w = workspace(x[11], entries.workspace_bytes(PROPD_WS_PAGED_ATTENTION, tree.B, tree.T_max, size32(H), size32(d), size32(cache.capacity), 0, 0), q);
+    Owned o = x[9] != Py_None ? object(x[9]) : object(out);
+    Owned result = want ? tuple_of(std::move(o), x[10] != Py_None ? object(x[10]) : object(lse)) : std::move(o);
+    call(entries.paged_attention, &tree, dt, size32(H), size32(Hk), size32(d), &rule, q.data_ptr(), &cache.c, kt.data_ptr(), vt.data_ptr(),
+         (const int32_t *)seq.data_ptr(), out.data_ptr(), want ? (float *)lse.data_ptr() : nullptr, w.ptr, w.bytes, stream_of(x[12]));
+    return result;
+  });
+}
+
+// paged_commit(*tree, *cache, accept_len, path, next_token, k_tree, v_tree, seq_lens, seq_lens_out or None, out_stride or None, stream) -> tokens
+PyObject *py_paged_commit(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded([&]() -> Owned {
+    need(n == 19);
+    PyObject *const *f = a + 5, *const *x = a + 10;
+    const at::Tensor &kt = tensor(x[3]), &path0 = tensor(x[1]);
+    const propd_dtype dt = type_of(kt);
+    need(kt.dim() == 4 && kt.is_contiguous() && path0.dim() == 2);
+    const Device on(kt);
+    const int64_t B = kt.size(0), Hk = kt.size(1), T = kt.size(2), d = kt.size(3), P = path0.size(1);
+    const at::Tensor &vt = on(x[4], kt.scalar_type(), kt.sizes());
+    const at::Tensor &len = on(x[0], at::kInt, {B}), &path = on(x[1], at::kInt, {B, P}), &next = on(x[2], at::kInt, {B}), &seq = on(x[5], at::kInt, {B});
+    on(a[0], at::kInt, {B});
+    on(a[2], at::kInt, {B, T});
+    const propd_tree tree = tree_of(a);
+    need(tree.B == B && tree.T_max == T);
+    PyObject *const lens_out = x[6] == Py_None ? x[5] : x[6];
+    const at::Tensor &seq_out = on(lens_out, at::kInt, {B});
+    const Paged cache = paged_of(f, on, kt.scalar_type(), B, Hk, d);
+    written_apart(f, {a[0], a[2], x[0], x[1], x[2], x[3], x[4]}, x[5], lens_out);
+    const int32_t stride = size32(P), out_stride = x[7] == Py_None ? stride : whole32(x[7]);
+    need(out_stride >= 0);
+    const at::Tensor out = unlocked([&] { return at::empty({B, out_stride}, kt.options().dtype(at::kInt)); });
+    Owned result = object(out);
+    call(entries.paged_commit, &tree, dt, size32(Hk), size32(d), (const int32_t *)len.data_ptr(), (const int32_t *)path.data_ptr(), stride,
+         (const int32_t *)next.data_ptr(), kt.data_ptr(), vt.data_ptr(), &cache.c, (const int32_t *)seq.data_ptr(), (int32_t *)seq_out.data_ptr(),
+         (int32_t *)out.data_ptr(), out_stride, stream_of(x[8]));
+    return result;
+  });
+}
+
+// paged_prompt(*cache, k, v, seq_lens, n_rows or None, seq_lens_out or None, stream) -> True
+PyObject *py_paged_prompt(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded([&]() -> Owned {
+    need(n == 11);
+    PyObject *const *x = a + 5;
+    const at::Tensor &k = tensor(x[0]);
+    const propd_dtype dt = type_of(k);
+    need(k.dim() == 4 && k.is_contiguous());
+    const Device on(k);
+    const int64_t B = k.size(0), Hk = k.size(1), S = k.size(2), d = k.size(3);
+    const at::Tensor &v = on(x[1], k.scalar_type(), k.sizes()), &seq = on(x[2], at::kInt, {B});
+    const int32_t *rows = on.optional<int32_t>(x[3], at::kInt, {B});
+    PyObject *const lens_out = x[4] == Py_None ? x[2] : x[4];
+    const at::Tensor &seq_out = on(lens_out, at::kInt, {B});
+    const Paged cache = paged_of(a, on, k.scalar_type(), B, Hk, d);
+    written_apart(a, {x[0], x[1], x[3]}, x[2], lens_out);
+    Owned result = object(Py_True);
+    call(entries.paged_prompt, dt, size32(B), size32(S), size32(Hk), size32(d), rows, k.data_ptr(), v.data_ptr(), &cache.c, (const int32_t *)seq.data_ptr(),
+         (int32_t *)seq_out.data_ptr(), stream_of(x[5]));
+    return result;
+  });
+}
+
+// paged_read(*cache, seq_lens, k_out, v_out, first or None, stream) -> True
+PyObject *py_paged_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded([&]() -> Owned {
+    need(n == 10);
+    PyObject *const *x = a + 5;
+    const at::Tensor &k = tensor(x[1]);
+    const propd_dtype dt = type_of(k);
+    need(k.dim() == 4 && k.is_contiguous());
+    const Device on(k);
+    const int64_t B = k.size(0), Hk = k.size(1), S = k.size(2), d = k.size(3);
+    const at::Tensor &v = on(x[2], k.scalar_type(), k.sizes()), &seq = on(x[0], at::kInt, {B});
+    const int32_t *first = on.optional<int32_t>(x[3], at::kInt, {B});
+    const Paged cache = paged_of(a, on, k.scalar_type(), B, Hk, d);
+    for (const at::Tensor *out : {&k, &v}) apart(*out, {x[0], x[3], a[0], a[1], a[2], a[3], a[4]});
+    need(!overlap(k, v));
+    Owned result = object(Py_True);
+    call(entries.paged_read, dt, size32(B), size32(S), size32(Hk), size32(d), &cache.c, (const int32_t *)seq.data_ptr(), first, k.data_ptr(), v.data_ptr(),
+         stream_of(x[4]));
+    return result;
+  });
+}
+
+// accept_sampled(*tree, logits, u, u_next, inv_temperature, draft_logits or None, draft_inv_temperature, path_stride or None, workspace, stream)
+// -> (length, path, next)
+PyObject *py_accept_sampled(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded([&]() -> Owned {
+    need(n == 14);
+    PyObject *const *x = a + 5;
+    const at::Tensor &logits = tensor(x[0]);
+    const propd_dtype dt = type_of(logits);
+    need(logits.dim() == 3 && logits.is_contiguous());
+    const Device on(logits);
+    const int64_t B = logits.size(0), T = logits.size(1), V = logits.size(2);
+    const at::Tensor &u = on(x[1], at::kFloat, {B, T}), &u_next = on(x[2], at::kFloat, {B});
+    on(a[0], at::kInt, {B});
+    on(a[1], at::kInt, {B, T});
+    on(a[2], at::kInt, {B, T});
+    const propd_tree tree = tree_of(a);
+    need(tree.B == B && tree.T_max == T);
+    const float inv = real(x[3]), draft_inv = real(x[5]);
+    const void *draft = on.optional<void>(x[4], logits.scalar_type(), logits.sizes());
+    const int32_t stride = x[6] == Py_None ? size32(T) : whole32(x[6]), vocab = size32(V);
+    need(stride >= 0);
+    const auto i32 = logits.options().dtype(at::kInt);
+    at::Tensor len, path, next;
+    {
+      const Unlocked unlock;
+      len = at::empty({B}, i32);
+      path = at::empty({B, stride}, i32);
+      next = at::empty({B}, i32);
+    }
+    if (x[7] != Py_None) apart(tensor(x[7]), {a[0], a[1], a[2], x[0], x[1], x[2], x[4]});
+    const Workspace w = workspace(x[7], entries.workspace_bytes(PROPD_WS_ACCEPT_SAMPLED, tree.B, tree.T_max, 0, 0, 0, 0, vocab), logits);
+    Owned result = tuple_of(object(len), object(path), object(next));
+    call(entries.accept_sampled, &tree, dt, vocab, logits.data_ptr(), inv, draft, draft_inv, (const float *)u.data_ptr(), (const float *)u_next.data_ptr(),
+         (int32_t *)len.data_ptr(), (int32_t *)path.data_ptr(), stride, (int32_t *)next.data_ptr(), w.ptr, w.bytes, stream_of(x[8]));
+    return result;
+  });
+}
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(init),        METHOD(tree_mask),   METHOD(tree_attention), METHOD(early_prune),
                          METHOD(accept_path), METHOD(commit_path), METHOD(grouped_attention), METHOD(cache_observe),
-                         METHOD(cache_evict), METHOD(rotary),      METHOD(init_cache),     {nullptr, nullptr, 0, nullptr}};
+                         METHOD(cache_evict), METHOD(rotary),      METHOD(init_cache),  METHOD(init_paged),  METHOD(paged_attention),
+                         METHOD(paged_commit), METHOD(paged_prompt), METHOD(paged_read),   METHOD(accept_sampled),    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -34,7 +34,7 @@ struct PagedParams {
   float *part_o, *part_ml;
   int32_t *records;  // [B * H_kv * blocks][4]: first slot, slots between pieces, pieces
   int resident;      // workgroups that run at once
-  int most_ranges;   // of a call whose units are cut
+  int least;         // steps of a range, at least
   int may_split;
 };
 
@@ -54,7 +54,9 @@ struct PagedGeo {
   static constexpr int kQuads = D / (4 * kGroups);     // O of a lane in fours of neighbouring d; quad x starts at d = 4 * kGroups * x + 4 * group
   static constexpr int kThreads = 64 * kCw;            // that load a stage
   static constexpr int kLds = kRw * kSlots * kStage + 512;
-  // Chunk c of row r of a stage lies at chunk position c ^ key(r): a fragment read's rows fall into different banks
+  // Chunk c of row r of a stage lies at chunk position c ^ key(r): a fragment read's rows fall into different banks.  A key picks bits of
+  // r, so that key(R + q) = key(R) ^ key(q) where R and q have no bit in common: what a lane reads or writes lies at an address of
+  // its own (q, c) with some bits flipped and a number added (R, C), both known at compile time.
   static __device__ __forceinline__ int k_key(int r) { return kBf16 ? Geo<D>::k_key(r) : r & (kChunks - 1); }
   static __device__ __forceinline__ int v_key(int r) {
     return kBf16 ? Geo<D>::v_key(r) : kN == 32 ? ((r >> 2) & 1) << 3 : ((r >> 2) & 3) << 2;
@@ -82,7 +84,7 @@ __device__ __forceinline__ void clear(V &v) {
 
 // A number that the compiler takes for another one every time, so that what is made of it is made again where it is needed and
 // takes no registers meanwhile.
-__device__ __forceinline__ int made_anew(int v) {
+__device__ __forceinline__ uint32_t made_anew(uint32_t v) {
   asm volatile("" : "+v"(v));
   return v;
 }
@@ -100,17 +102,18 @@ __device__ __forceinline__ PagedStages paged_stages(int L, int T, int window) {
   return s;
 }
 
-// How the units are cut, in steps of kRw stages: a range is at most `most` steps, a unit of s steps has ceil(s / most) equally long ones.
-// Every workgroup works the same plan out from the lengths.
-//   As many units as run at once or fewer: the least `most` (from an equal share on, a sixteenth of it longer at a time) whose ranges all run at once.
-//   More: with r workgroups at once, N steps in all, ranges of m steps that cost o steps besides, the last range to start ends half a range after
-//   the mean: m / 2 + o N / (m r) is least at m = sqrt(2 o N / r).
+// How the units are cut, in steps of kRw stages.  Every workgroup works the same plan out from the lengths.
+//   As many units as run at once or fewer: ranges that are equally long per unit, of the fewest steps at most whose ranges all run at once (from an equal
+//   share on, a sixteenth of it longer at a time).
+//   More: as many units as there are rounds of workgroups for come first, whole unless they are longer than an equal share of everything; the units
+//   left over are cut as above, so that the last round is as short as the others' rest.
 struct PagedPlan {
-  int most, ranges;
+  int whole;        // units that come first
+  int big, small;   // most steps of a range of those, and of the others
+  int n1, n2;       // ranges of those, and of the others; their slots for partial results are n2 and more, and from 0 on
 };
 constexpr float kBack = 0x1p-31f, kForth = 0x1p31f;  // (a sequence has at most 2^30 cached rows and 128 others)
 constexpr float kMostPlain = 0x1p96f;  // sums of more are made with care: a call's pieces of less can be added up
-constexpr float kRangeCost = 3.f;  // steps that a range costs besides its own
 
 struct PagedSequence {
   int L, T, steps, units;  // units 0 beyond the batch
@@ -130,41 +133,75 @@ __device__ __forceinline__ PagedSequence paged_sequence(const PagedParams &p, in
 __device__ __forceinline__ int paged_pieces(int steps, int most) {
   return most >= steps ? 1 : (int)((unsigned)(steps + most - 1) / (unsigned)most);
 }
-__device__ __forceinline__ int paged_sum(int v) {
-  return __builtin_amdgcn_readlane(wave_scan_i32(v, 0, [](int x, int y) { return x + y; }), 63);
+__device__ __forceinline__ int paged_scan(int v) {
+  return wave_scan_i32(v, 0, [](int x, int y) { return x + y; });
+}
+__device__ __forceinline__ int paged_sum(int v) { return __builtin_amdgcn_readlane(paged_scan(v), 63); }
+__device__ __forceinline__ float paged_sum(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+
+// Units of a lane's sequence that come first, and the others; `before`: units of the sequences before those of the lanes.
+struct PagedShare {
+  int first, rest;
+};
+__device__ __forceinline__ PagedShare paged_share(int units, int before, int whole) {
+  const int start = before + paged_scan(units) - units, first = clamped(whole - start, units);
+  return {first, units - first};
 }
 
 template <int kN, int kCw>
-__device__ __forceinline__ PagedPlan paged_plan(const PagedParams &p, const PagedSequence &first) {
+__device__ __forceinline__ PagedPlan paged_plan(const PagedParams &p, const PagedSequence &lanes) {
   const int lane = threadIdx.x & 63;
+  auto over = [&](auto &&each) __attribute__((always_inline)) {  // each(sequence, units before the 64 sequences)
+    int before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += kWave) {
+      const PagedSequence q = b0 == 0 ? lanes : paged_sequence<kN, kCw>(p, b0 + lane);
+      each(q, before);
+      if (b0 + kWave < p.B) before += paged_sum(q.units);
+    }
+  };
   int units = 0;
   float total = 0.f;
-  for (int b0 = 0; b0 < p.B; b0 += kWave) {
-    const PagedSequence q = b0 == 0 ? first : paged_sequence<kN, kCw>(p, b0 + lane);
+  over([&](const PagedSequence &q, int) {
     units += paged_sum(q.units);
-    float t = (float)q.units * (float)q.steps;
-    for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, kWave);
-    total += t;
-  }
-  PagedPlan plan = {1 << 30, units};
+    total += paged_sum((float)q.units * (float)q.steps);
+  });
+  PagedPlan plan = {units, 1 << 30, 1 << 30, units, 0};
   if (!p.may_split) return plan;
-  const bool few = units <= p.resident;
-  const int room = few ? p.resident : p.most_ranges;
-  float share = few ? total / (float)p.resident : sqrtf(2.f * kRangeCost * total / (float)p.resident);
-  share = fmaxf(share, 1.f);
-  for (int step = 0; step < 64; ++step) {
-    const int most = (int)ceilf(share * (1.f + .0625f * (float)step * (float)(step < 16 ? 1 : step - 14)));
-    int n = 0;
-    for (int b0 = 0; b0 < p.B; b0 += kWave) {
-      const PagedSequence q = b0 == 0 ? first : paged_sequence<kN, kCw>(p, b0 + lane);
-      n += paged_sum(q.units * paged_pieces(q.steps, most));
-    }
-    if (n <= room) return {most, n};
+  plan.whole = units <= p.resident ? 0 : units / p.resident * p.resident;
+  float rest = total;
+  if (plan.whole > 0) {
+    plan.big = (int)ceilf(total * 1.0001f / (float)p.resident);  // (a little more: the bound on their pieces holds however sums are rounded)
+    plan.n1 = 0;
+    rest = 0.f;
+    over([&](const PagedSequence &q, int before) {
+      const PagedShare s = paged_share(q.units, before, plan.whole);
+      plan.n1 += paged_sum(s.first * paged_pieces(q.steps, plan.big));
+      rest += paged_sum((float)s.rest * (float)q.steps);
+    });
+  } else {
+    plan.n1 = 0;
+  }
+  const float share = fmaxf(rest / (float)p.resident, (float)p.least);
+  for (int step = 0; step <= 64; ++step) {
+    plan.small = step == 64 ? 1 << 30 : (int)ceilf(share * (1.f + .0625f * (float)step * (float)(step < 16 ? 1 : step - 14)));
+    plan.n2 = 0;
+    over([&](const PagedSequence &q, int before) { plan.n2 += paged_sum(paged_share(q.units, before, plan.whole).rest * paged_pieces(q.steps, plan.small)); });
+    if (plan.n2 <= p.resident) break;  // (as few as the units left over fit in any case)
   }
   return plan;
 }
 
-__device__ __forceinline__ void lds_to(unsigned char *at, u32x4 v) { *reinterpret_cast<u32x4 *>(at) = v; }
+template <class V>
+using LdsPtr = __attribute__((address_space(3))) V *;
+__device__ __forceinline__ void lds_to(uint32_t at, u32x4 v) { *reinterpret_cast<LdsPtr<u32x4>>((uintptr_t)at) = v; }
+template <class V>
+__device__ __forceinline__ V lds_from(uint32_t at) {
+  return *reinterpret_cast<LdsPtr<const V>>((uintptr_t)at);
+}
 
 // Four neighbouring values of a result
 template <bool kBf16>
@@ -201,40 +238,50 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
   if (tid == 0) s_any = 0;
 
   // ---- which range
-  int b = 0, hk, block, piece, pieces, first_slot, steps;
+  int b = 0, hk, block, piece, pieces, slot, steps;
   {
     const PagedSequence lanes = paged_sequence<kN, kCw>(p, lane);
     const PagedPlan plan = paged_plan<kN, kCw>(p, lanes);
-    const int n = plan.ranges;
     int at = blockIdx.x;
-    if (at >= n) return;
-    const int even = n / 8 * 8;  // neighbouring ranges (blocks of one unit's columns among them) on one XCD
-    at = at < even ? at % 8 * (even / 8) + at / 8 : at;
-    int before = 0, start = 0;
+    if (at >= plan.n1 + plan.n2) return;
+    const bool second = at >= plan.n1;
+    at -= second ? plan.n1 : 0;
+    const int n = second ? plan.n2 : plan.n1, even = n / 8 * 8, most = second ? plan.small : plan.big;
+    at = at < even ? at % 8 * (even / 8) + at / 8 : at;  // neighbouring ranges (blocks of one unit's columns among them) on one XCD
+    int before = 0, units_before = 0, cut_before = 0, start = 0, cut = 0, first = 0, count = 1;
     for (int b0 = 0; b0 < p.B; b0 += kWave) {
       const PagedSequence q = b0 == 0 ? lanes : paged_sequence<kN, kCw>(p, b0 + lane);
-      const int mine = q.units * paged_pieces(q.steps, plan.most), incl = wave_scan_i32(mine, 0, [](int x, int y) { return x + y; });
-      const uint64_t le = __ballot(b0 + lane < p.B && before + incl - mine <= at);
-      if (le == 0) break;
-      const int src = __popcll(le) - 1;
-      b = b0 + src;
-      start = __builtin_amdgcn_readlane(before + incl - mine, src);
+      const PagedShare s = paged_share(q.units, units_before, plan.whole);
+      const int here = second ? s.rest : s.first, parts = paged_pieces(q.steps, most), mine = here * parts, incl = paged_scan(mine);
+      const int cut_mine = parts > 1 ? mine : 0, cut_incl = paged_scan(cut_mine);
+      const uint64_t le = __ballot(mine > 0 && before + incl - mine <= at);
+      if (le != 0) {
+        const int src = 63 - __builtin_clzll(le);
+        b = b0 + src;
+        start = __builtin_amdgcn_readlane(before + incl - mine, src);
+        cut = __builtin_amdgcn_readlane(cut_before + cut_incl - cut_mine, src);
+        first = second ? __builtin_amdgcn_readlane(s.first, src) : 0;
+        count = __builtin_amdgcn_readlane(here, src);
+      }
       before += __builtin_amdgcn_readlane(incl, 63);
+      if (before > at || b0 + kWave >= p.B) break;
+      cut_before += __builtin_amdgcn_readlane(cut_incl, 63);
+      units_before += paged_sum(q.units);
     }
     const PagedSequence q = paged_sequence<kN, kCw>(p, b);
     steps = __builtin_amdgcn_readfirstlane(q.steps);
     const int n_blocks = __builtin_amdgcn_readfirstlane(q.units) / p.H_kv, rest = at - start;
-    pieces = paged_pieces(steps, plan.most);
-    // blocks next to each other, then K/V heads, then pieces
-    const int in_blocks = rest / n_blocks;
-    block = rest - in_blocks * n_blocks;
-    piece = in_blocks / p.H_kv;
-    hk = in_blocks - piece * p.H_kv;
-    first_slot = at - piece * p.H_kv * n_blocks;
+    pieces = paged_pieces(steps, most);
+    // units next to each other, blocks of one K/V head first, then pieces
+    piece = rest / count;
+    const int u = first + rest - piece * count;
+    hk = u / n_blocks;
+    block = u - hk * n_blocks;
+    const int first_slot = (second ? 0 : plan.n2) + cut + (rest - piece * count);
+    slot = first_slot + piece * count;
     if (tid == 0 && piece == 0)
       *reinterpret_cast<u32x4 *>(p.records + 4 * (((size_t)b * p.H_kv + hk) * p.blocks + block)) =
-          u32x4{(uint32_t)first_slot, (uint32_t)(p.H_kv * n_blocks), (uint32_t)pieces, 0};
-    first_slot += piece * p.H_kv * n_blocks;  // this range's own
+          u32x4{(uint32_t)first_slot, (uint32_t)count, (uint32_t)pieces, 0};
   }
   const int L = clamped(p.seq_lens[b], p.pages.capacity), T = clamped(p.n_nodes[b] - 1, p.T_max - 1) + 1;
   const PagedStages st = paged_stages(L, T, p.window);
@@ -269,7 +316,16 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
   lds_barrier();
 
   // ---- loader
-  unsigned char *const group_lds = smem + rw * (G::kSlots * G::kStage);
+  const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)smem + rw * (G::kSlots * G::kStage);
+  constexpr int kWiden = kRowBytes / kSrcRow;                // chunks that one of a paged row becomes
+  constexpr int kAtOnce = G::kThreads / kSrcChunks;          // rows that the threads load together; 64: those of K and of V
+  static_assert(kAtOnce <= 64, "");
+  const int ld_row = loader / kSrcChunks % kStageRows, ld_chunk = loader % kSrcChunks;
+  const bool ld_v = kAtOnce == 64 && loader / kSrcChunks >= kStageRows;
+  // (row and key of a thread's first load; of V where the first is V's)
+  const uint32_t ld_k_at = ld_row * kRowBytes + (((kWiden * ld_chunk) ^ (ld_v ? G::v_key(ld_row) : G::k_key(ld_row))) << 4) + (ld_v ? G::kPart : 0);
+  const uint32_t ld_v_at = ld_row * kRowBytes + (((kWiden * ld_chunk) ^ G::v_key(ld_row)) << 4) + G::kPart;
+  const uint32_t ld_from = (ld_row & 15) * kSrcRow + ld_chunk * 16;
   int ids = -1, ids_from = -64;  // pages of the 16-row pieces of 32 steps' stages, a piece per lane
   auto stage_at = [&](int step) { return (step0 + step) * kRw + rw; };
   auto cached_row = [&](int stage) { return (stage - st.tree + st.first) * kStageRows; };
@@ -286,76 +342,67 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
       ids = at >= st.tree && row < L ? page_of(p.pages, b, row) : -1;
     }
     const int row0 = cached_row(stage), in_page = (1 << p.pages.shift) - 1;
-    const unsigned char *from[4];  // K of both halves, V of both
-    const uint8_t *scale_from[4];
+    size_t row[2];  // where the two halves of the stage lie in the pool
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int page = __builtin_amdgcn_readlane(ids, 2 * (step - ids_from) + half);
       int n = L - row0 - 16 * half;
       n = n > 16 ? 16 : n;
       if (page >= 0 && n > 0) rows_there |= ((1u << n) - 1u) << (16 * half);
-      const size_t row = row_in_pool(p.pages, page < 0 ? 0 : page, hk, p.H_kv, (row0 + 16 * half) & in_page);
-      from[half] = p.pages.k + row * kSrcRow;
-      from[2 + half] = p.pages.v + row * kSrcRow;
-      if constexpr (kCodes) {
-        scale_from[half] = p.pages.k_scale + row;
-        scale_from[2 + half] = p.pages.v_scale + row;
-      }
+      row[half] = row_in_pool(p.pages, page < 0 ? 0 : page, hk, p.H_kv, (row0 + 16 * half) & in_page);
     }
-    const int ln = made_anew(loader) & (G::kThreads - 1);
-    auto pick = [](auto *const(&x)[4], int part, int row) __attribute__((always_inline)) {
-      auto *const k0 = x[0], *const k1 = x[1], *const v0 = x[2], *const v1 = x[3];  // (values: a choice of places would be made in memory)
-      auto *const k = row & 16 ? k1 : k0, *const v = row & 16 ? v1 : v0;
-      return part ? v : k;
-    };
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int x = i * G::kThreads + ln, part = x / (kStageRows * kSrcChunks), row = x / kSrcChunks % kStageRows;
-      data[i] = *reinterpret_cast<const u32x4 *>(pick(from, part, row) + (row & 15) * kSrcRow + x % kSrcChunks * 16);
-      if constexpr (kCodes) scale_byte[i] = pick(scale_from, part, row)[row & 15];
+      const int first = i * kAtOnce;  // of the 32 rows of K and then those of V
+      const bool v = kAtOnce == 64 ? ld_v : first >= kStageRows;
+      const bool second = kAtOnce >= 32 ? (ld_row & 16) != 0 : (first & 16) != 0;
+      const size_t at = second ? row[1] : row[0];
+      const int in_half = kAtOnce >= 16 ? 0 : first & 15;
+      data[i] = *reinterpret_cast<const u32x4 *>((v ? p.pages.v : p.pages.k) + at * kSrcRow + in_half * kSrcRow + ld_from);
+      if constexpr (kCodes) scale_byte[i] = (v ? p.pages.v_scale : p.pages.k_scale)[at + in_half + (ld_row & 15)];
     }
   };
   // What issue() requested to LDS; rows that are not there as zeros, so that weights of zero meet nothing else.
-  auto land = [&](unsigned char *to, uint32_t is_there) __attribute__((always_inline)) {
-    const int ln = made_anew(loader) & (G::kThreads - 1);
+  auto land = [&](uint32_t slot, uint32_t is_there) __attribute__((always_inline)) {
+    const uint32_t k_at = made_anew(lds + slot + ld_k_at), v_at = made_anew(lds + slot + ld_v_at);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int x = i * G::kThreads + ln, part = x / (kStageRows * kSrcChunks), row = x / kSrcChunks % kStageRows, c = x % kSrcChunks;
-      unsigned char *const at = to + part * G::kPart + row * kRowBytes;
-      const int key = part ? G::v_key(row) : G::k_key(row);
-      u32x4 v = data[i];
+      const int first = i * kAtOnce, row = first % kStageRows;
+      const bool v = kAtOnce < 64 && first >= kStageRows;
+      const uint32_t at = v ? v_at : k_at, key = v ? G::v_key(row) : G::k_key(row);
+      u32x4 x = data[i];
       if (is_there != ~0u) {  // uniform
-        const bool ok = (is_there >> row) & 1;
+        const bool ok = (is_there >> (ld_row + row)) & 1;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = ok ? v[j] : 0u;
+        for (int j = 0; j < 4; ++j) x[j] = ok ? x[j] : 0u;
       }
       if constexpr (!kCodes) {
-        lds_to(at + ((c ^ key) << 4), v);
+        lds_to((at ^ (key << 4)) + row * kRowBytes, x);
       } else {
         const float scale = scale_of(scale_byte[i]);
         if constexpr (kBf16) {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const u32x2 a = codes_to_bf16(v[2 * j], scale), z = codes_to_bf16(v[2 * j + 1], scale);
-            lds_to(at + (((2 * c + j) ^ key) << 4), u32x4{a.x, a.y, z.x, z.y});
+            const u32x2 a = codes_to_bf16(x[2 * j], scale), z = codes_to_bf16(x[2 * j + 1], scale);
+            lds_to((at ^ ((j ^ key) << 4)) + row * kRowBytes, u32x4{a.x, a.y, z.x, z.y});
           }
         } else {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) lds_to(at + (((4 * c + j) ^ key) << 4), __builtin_bit_cast(u32x4, codes_to_f32(v[j], scale)));
+          for (int j = 0; j < 4; ++j) lds_to((at ^ ((j ^ key) << 4)) + row * kRowBytes, __builtin_bit_cast(u32x4, codes_to_f32(x[j], scale)));
         }
       }
     }
   };
-  auto land_tree = [&](unsigned char *to, int stage) __attribute__((always_inline)) {
+  auto land_tree = [&](uint32_t slot, int stage) __attribute__((always_inline)) {
     const int left = T - stage * kStageRows;
     const size_t row0 = unit * p.T_max + stage * kStageRows;
-    const int ln = made_anew(loader) & (G::kThreads - 1);
+    const int ln = (int)made_anew((uint32_t)loader) & (G::kThreads - 1);
 #pragma unroll
     for (int i = 0; i < kTreeLoads; ++i) {
       const int x = i * G::kThreads + ln, part = x / (kStageRows * G::kChunks), row = x / G::kChunks % kStageRows, c = x % G::kChunks;
       u32x4 v = {0, 0, 0, 0};
       if (row < left) v = *reinterpret_cast<const u32x4 *>((part ? p.v_tree : p.k_tree) + (row0 + row) * kRowBytes + c * 16);
-      lds_to(to + part * G::kPart + row * kRowBytes + ((c ^ (part ? G::v_key(row) : G::k_key(row))) << 4), v);
+      lds_to(lds + slot + part * G::kPart + row * kRowBytes + ((c ^ (part ? G::v_key(row) : G::k_key(row))) << 4), v);
     }
   };
 
@@ -364,19 +411,27 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
   constexpr float kTau = 8.f;
 
   // ---- a stage: its scores, weights and what they add to O.  `seen`: a bit per row of the stage that exists.
-  auto take_stage = [&](const unsigned char *from, int stage, uint32_t seen, auto with_care) __attribute__((always_inline)) {
+  const int in_n = lane % kN, g = lane / kN;
+  const uint32_t k_read = lds + in_n * kRowBytes + ((g ^ G::k_key(in_n)) << 4);
+  uint32_t v_read = lds + G::kPart;  // bf16: a transposing read's row and 8 bytes; fp32: a number of row 4 * g
+  if constexpr (kBf16) {
+    const int q = 4 * g + ((lane & 15) >> 2), c = (kN == 32 ? 2 * ((lane >> 4) & 1) : 0) + ((lane & 3) >> 1);
+    v_read += q * kRowBytes + ((c ^ G::v_key(q)) << 4) + 8 * (lane & 1);
+  } else {
+    v_read += 4 * g * kRowBytes + (((in_n >> 2) ^ G::v_key(4 * g)) << 4) + 4 * (in_n & 3);
+  }
+  auto take_stage = [&](uint32_t slot, int stage, uint32_t seen, auto with_care) __attribute__((always_inline)) {
     constexpr bool kCareful = decltype(with_care)::value;
     const bool tree = stage < st.tree;
-    const int ln = made_anew(lane) & 63, in_n = ln % kN, g = ln / kN;
+    const uint32_t k_at = made_anew(k_read + slot), v_at = made_anew(v_read + slot);
     float sc[kScores];
 #pragma unroll
     for (int tile = 0; tile < 32 / kN; ++tile) {
       Acc<kN> acc;
       clear(acc);
-      const int row = tile * kN + in_n;
 #pragma unroll
       for (int x = 0; x < kQf; ++x) {
-        const u32x4 a = *reinterpret_cast<const u32x4 *>(from + row * kRowBytes + (((kGroups * x + g) ^ G::k_key(row)) << 4));
+        const u32x4 a = lds_from<u32x4>((k_at ^ (((kGroups * x) ^ G::k_key(tile * kN)) << 4)) + tile * kN * kRowBytes);
         if constexpr (kBf16) {
           acc = product<kN>(a, qf[x], acc);
         } else {
@@ -388,13 +443,24 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
       for (int r = 0; r < kAcc; ++r) sc[tile * kAcc + r] = acc[r];
     }
     mfma_settle();
-    // ---- scores in the exponent's (log2) domain
+    // ---- scores; times `unit_of` they are in the exponent's (log2) domain
+    float unit_of = p.scale_log2e;
     if (p.cap_in > 0.f) {
+      unit_of = 1.f;
+      // cap tanh(x / cap) as in capped(), whose fraction alone does where no score of the wave is beyond 3/4 of the cap
+      float most = 0.f;
 #pragma unroll
-      for (int x = 0; x < kScores; ++x) sc[x] = capped(sc[x], p.cap_log2e, p.cap_in);
-    } else {
+      for (int x = 0; x < kScores; ++x) most = fmaxf(most, fabsf(sc[x]));
+      if (__builtin_amdgcn_ballot_w64(!(most * p.cap_in < .75f)) == 0) {
 #pragma unroll
-      for (int x = 0; x < kScores; ++x) sc[x] *= p.scale_log2e;
+        for (int x = 0; x < kScores; ++x) {
+          const float y = sc[x] * p.cap_in, y2 = y * y;
+          sc[x] = sc[x] * p.scale_log2e * fmaf(y2, y2 + 105.f, 945.f) * __builtin_amdgcn_rcpf(fmaf(y2, fmaf(15.f, y2, 420.f), 945.f));
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < kScores; ++x) sc[x] = capped(sc[x], p.cap_log2e, p.cap_in);
+      }
     }
     const float first = tree ? 0.f : (float)(cached_row(stage) - L);  // place of the stage's first cached row
     if (p.slopes || first < all_see) {
@@ -405,10 +471,11 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
         if (tree) place = *reinterpret_cast<const f32x4 *>(tree_place + stage * kStageRows + row);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          if (p.slopes) sc[4 * x4 + j] = fmaf(slope, place[j] - depth, sc[4 * x4 + j]);
+          if (p.slopes) sc[4 * x4 + j] = fmaf(slope, place[j] - depth, sc[4 * x4 + j] * unit_of);
           sc[4 * x4 + j] = place[j] >= lowest ? sc[4 * x4 + j] : -INFINITY;
         }
       }
+      if (p.slopes) unit_of = 1.f;
     }
     if (tree) seen &= stage == 0 ? anc.x : stage == 1 ? anc.y : stage == 2 ? anc.z : anc.w;
     if (tree || seen != ~0u) {  // uniform
@@ -425,6 +492,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
       m_blk = fmaxf(__uint_as_float(lo), __uint_as_float(hi));
       if constexpr (kN == 16) m_blk = fmaxf(m_blk, __shfl_xor(m_blk, 16, kWave));
     }
+    m_blk *= unit_of;
     // A new reference is adopted only when the maximum exceeds the old one by 2^8: weights then exceed 1, by a factor that fp32 sums and bf16
     // weights hold, and O is hardly ever scaled.  With care they are at most kBack as they meet V: no sum exceeds its largest value.
     if (__builtin_amdgcn_ballot_w64(m_blk > (kCareful ? m_run : m_run + kTau)) != 0) {
@@ -440,11 +508,10 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
     const float neg_m = -(m_run == -INFINITY ? 0.f : m_run);
 #pragma unroll
     for (int x = 0; x < kScores; ++x) {
-      sc[x] = fast_exp2(sc[x] + neg_m);
+      sc[x] = fast_exp2(fmaf(sc[x], unit_of, neg_m));
       l_run += sc[x];  // of the weights as they are: lse is an fp32 result
       if constexpr (kCareful) sc[x] *= kBack;
     }
-    const unsigned char *const v_from = from + G::kPart;
     if constexpr (kBf16) {
 #pragma unroll
       for (int half = 0; half < kScores / 8; ++half) {  // a product's rows are those of 8 scores
@@ -465,10 +532,9 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
           u32x4 vt;
 #pragma unroll
           for (int hi = 0; hi < 2; ++hi) {
-            const int r = 4 * kGroups * (2 * half + hi) + 4 * g + ((ln & 15) >> 2);
-            const int chunk = db * (kN / 8) + (kN == 32 ? 2 * ((ln >> 4) & 1) : 0) + ((ln & 3) >> 1);
-            const unsigned char *at = v_from + r * kRowBytes + ((chunk ^ G::v_key(r)) << 4) + 8 * (ln & 1);
-            const u32x2 t = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at));
+            const int row = 4 * kGroups * (2 * half + hi);
+            const uint32_t at = (v_at ^ (((db * (kN / 8)) ^ G::v_key(row)) << 4)) + row * kRowBytes;
+            const u32x2 t = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LdsPtr<s16x4>>((uintptr_t)at)));
             vt[2 * hi] = t.x;
             vt[2 * hi + 1] = t.y;
           }
@@ -501,8 +567,8 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
         if constexpr (kCareful) clear(codes);
 #pragma unroll
         for (int x = 0; x < kScores; ++x) {  // the product's rows are those of score x of the column's lanes
-          const int row = 4 * kGroups * (x >> 2) + 4 * g + (x & 3), c = db * (kN / 4) + (in_n >> 2);
-          float v = *reinterpret_cast<const float *>(v_from + row * kRowBytes + ((c ^ G::v_key(row)) << 4) + 4 * (in_n & 3));
+          const int row = 4 * kGroups * (x >> 2) + (x & 3);
+          float v = lds_from<float>((v_at ^ (((db * (kN / 4)) ^ G::v_key(row)) << 4)) + row * kRowBytes);
           if constexpr (kCareful) {
             const float code = not_finite_code(__float_as_uint(v));
             v = code == 0.f ? v : 0.f;
@@ -533,7 +599,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
     first_there = rows_there;
     for (int step = 0; step < n_steps; ++step) {
       const int stage = stage_at(step);
-      unsigned char *const to = group_lds + (G::kSlots == 2 ? (step & 1) * G::kStage : 0);
+      const uint32_t to = G::kSlots == 2 ? (step & 1) * G::kStage : 0;
       uint32_t seen = 0;
       if (stage < st.tree) {
         land_tree(to, stage);
@@ -618,7 +684,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
     for (int x = 0; x < kOwn; ++x) store_quad<kBf16>(p.out, row_out * D + 4 * kGroups * (first_quad + x) + 4 * (lane / kN), mine[x], inv);
     if (p.lse && rw == 0 && lane < kN) p.lse[row_out] = (m_run + __builtin_amdgcn_logf(l_run)) * kLn2;
   } else {
-    const size_t part = (size_t)first_slot * kCw + cw;
+    const size_t part = (size_t)slot * kCw + cw;
 #pragma unroll
     for (int x = 0; x < kOwn; ++x) *reinterpret_cast<f32x4 *>(p.part_o + ((part * G::kQuads + first_quad + x) * kWave + lane) * 4) = mine[x];
     if (rw == 0) {
@@ -717,23 +783,24 @@ __global__ __launch_bounds__(kWaves *kWave) void paged_merge_kernel(PagedParams 
 // ------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------
-// Partial results of a call, at most: a slot per range, of 32 * kCw columns.  More units than that are not cut.
-constexpr int kPagedResident = 512, kPagedRanges = 1024;
+// Partial results of a call, at most: as many ranges as run at once, of units that are left over, and twice as many of units that come first (a unit that
+// is cut is longer than an equal share: it has fewer pieces than twice its shares).
+constexpr int kPagedResident = 512, kPagedSlots = 3 * kPagedResident;
+constexpr long long kPagedUnits = 8 * kPagedResident;  // more are not cut: the last round is an eighth of the call at most
 
-// Ranges of a call whose units are cut, a bound that needs no device.  (Smaller trees and other shapes of the waves have more units of fewer columns.)
-static long long paged_ranges(int B, int H, int L_max) {
+static long long paged_slots(int B, int H, int L_max) {
   const long long stages = (L_max + kStageRows - 1ll) / kStageRows + PROPD_MAX_TREE / kStageRows;
-  const long long most = (long long)B * H * stages * 4;  // blocks of a unit: no more than four per head
-  return most < kPagedRanges ? most : kPagedRanges;
+  const long long most = (long long)B * H * 4 * stages;  // blocks of a unit: no more than four per head
+  return most < kPagedSlots ? most : kPagedSlots;
 }
 
 size_t paged_attention_workspace_bytes(int B, int H, int L_max, int T_max) {
-  const size_t ranges = (size_t)paged_ranges(B, H, L_max), blocks = (size_t)(T_max + 31) / 32;
-  return ranges * (4 * 16 * kWave * 4 * 4) + ranges * (4 * 2 * kWave * 4) + align_up((size_t)B * H * blocks * 16, 256);
+  const size_t slots = (size_t)paged_slots(B, H, L_max), blocks = (size_t)(T_max + 31) / 32;
+  return slots * (4 * 16 * kWave * 4 * 4) + slots * (4 * 2 * kWave * 4) + align_up((size_t)B * H * blocks * 16, 256);
 }
 
 template <bool kBf16, bool kCodes, int D, int kN, int kCw>
-static bool launch_paged(PagedParams p, long long ranges, int L_max, hipStream_t st) {
+static bool launch_paged(PagedParams p, int L_max, hipStream_t st) {
   using G = PagedGeo<kBf16, D, kN, kCw>;
   static std::atomic<uint64_t> set{0};
   if (!allow_lds(reinterpret_cast<const void *>(&paged_attn_kernel<kBf16, kCodes, D, kN, kCw>), G::kLds, set)) return false;
@@ -741,11 +808,15 @@ static bool launch_paged(PagedParams p, long long ranges, int L_max, hipStream_t
   const long long units = (long long)p.B * p.H_kv * p.blocks;
   const int resident = (kBf16 ? 2 : 1) * compute_units();
   p.resident = resident < kPagedResident ? resident : kPagedResident;
-  p.most_ranges = (int)ranges;
-  if (p.resident > p.most_ranges) p.resident = p.most_ranges;
   const long long steps = ((L_max + kStageRows - 1ll) / kStageRows + (p.T_max + kStageRows - 1) / kStageRows + G::kRw - 1) / G::kRw;
-  p.may_split = units < p.most_ranges && steps > 1 ? 1 : 0;
-  const long long grid = !p.may_split ? units : units * steps < p.most_ranges ? units * steps : p.most_ranges;
+  p.least = G::kRw == 1 ? 2 : 1;
+  p.may_split = units < kPagedUnits && steps > p.least ? 1 : 0;
+  // (ranges that come first: units, and the pieces of those that are cut; then the others')
+  long long grid = units;
+  if (p.may_split) {
+    grid += units <= p.resident ? p.resident : 3ll * p.resident;
+    if (grid > units * steps) grid = units * steps;
+  }
   hipLaunchKernelGGL((paged_attn_kernel<kBf16, kCodes, D, kN, kCw>), dim3((unsigned)grid), dim3(kPagedThreads), G::kLds, st, p);
   if (!launch_ok()) return false;
   if (!p.may_split) return true;
@@ -756,11 +827,11 @@ static bool launch_paged(PagedParams p, long long ranges, int L_max, hipStream_t
 }
 
 template <bool kBf16, bool kCodes, int D>
-static bool launch_paged(const PagedParams &p, long long ranges, int L_max, hipStream_t st) {
+static bool launch_paged(const PagedParams &p, int L_max, hipStream_t st) {
   const int columns = p.group * p.T_max;
-  return columns <= 16 ? launch_paged<kBf16, kCodes, D, 16, 1>(p, ranges, L_max, st)
-         : columns <= 64 ? launch_paged<kBf16, kCodes, D, 16, 4>(p, ranges, L_max, st)
-                         : launch_paged<kBf16, kCodes, D, 32, 4>(p, ranges, L_max, st);
+  return columns <= 16 ? launch_paged<kBf16, kCodes, D, 16, 1>(p, L_max, st)
+         : columns <= 64 ? launch_paged<kBf16, kCodes, D, 16, 4>(p, L_max, st)
+                         : launch_paged<kBf16, kCodes, D, 32, 4>(p, L_max, st);
 }
 
 }  // namespace propd
@@ -805,23 +876,23 @@ extern "C" propd_status propd_paged_attention(const propd_tree *tree, propd_dtyp
   p.scale_log2e = rule->scale * kLog2e;
   p.cap_in = rule->cap > 0.f ? rule->scale / rule->cap : 0.f;
   p.cap_log2e = rule->cap * kLog2e;
-  const long long ranges = paged_ranges(p.B, H, L_max);
+  const long long slots = paged_slots(p.B, H, L_max);
   char *ws = reinterpret_cast<char *>(workspace);
   p.part_o = reinterpret_cast<float *>(ws);
-  ws += (size_t)ranges * (4 * 16 * kWave * 4 * 4);
+  ws += (size_t)slots * (4 * 16 * kWave * 4 * 4);
   p.part_ml = reinterpret_cast<float *>(ws);
-  ws += (size_t)ranges * (4 * 2 * kWave * 4);
+  ws += (size_t)slots * (4 * 2 * kWave * 4);
   p.records = reinterpret_cast<int32_t *>(ws);
-  p.resident = p.most_ranges = p.may_split = 0;  // by the shape of the waves
+  p.resident = p.least = p.may_split = 0;  // by the shape of the waves
   hipStream_t st = as_stream(hip_stream);
   const bool bf16 = dt == PROPD_BF16, codes = cache->dt == PROPD_E4M3;
   bool ok;
   if (d == 128) {
-    ok = bf16 ? (codes ? launch_paged<true, true, 128>(p, ranges, L_max, st) : launch_paged<true, false, 128>(p, ranges, L_max, st))
-              : (codes ? launch_paged<false, true, 128>(p, ranges, L_max, st) : launch_paged<false, false, 128>(p, ranges, L_max, st));
+    ok = bf16 ? (codes ? launch_paged<true, true, 128>(p, L_max, st) : launch_paged<true, false, 128>(p, L_max, st))
+              : (codes ? launch_paged<false, true, 128>(p, L_max, st) : launch_paged<false, false, 128>(p, L_max, st));
   } else {
-    ok = bf16 ? (codes ? launch_paged<true, true, 64>(p, ranges, L_max, st) : launch_paged<true, false, 64>(p, ranges, L_max, st))
-              : (codes ? launch_paged<false, true, 64>(p, ranges, L_max, st) : launch_paged<false, false, 64>(p, ranges, L_max, st));
+    ok = bf16 ? (codes ? launch_paged<true, true, 64>(p, L_max, st) : launch_paged<true, false, 64>(p, L_max, st))
+              : (codes ? launch_paged<false, true, 64>(p, L_max, st) : launch_paged<false, false, 64>(p, L_max, st));
   }
   return ok ? PROPD_OK : PROPD_ERR_DEVICE;
 }

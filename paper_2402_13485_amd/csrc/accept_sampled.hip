@@ -120,6 +120,28 @@ __device__ __forceinline__ T block_reduce(T v, T *room, F &&join) {
   return r;
 }
 
+// The sum over the threads before this one, and over all, in a fixed order.
+__device__ __forceinline__ double block_before(double v, double *room, double &total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+  double upto = v;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const double x = __shfl_up(upto, o, kWave);
+    upto += lane >= o ? x : 0.0;
+  }
+  __syncthreads();
+  if (lane == 63) room[wave] = upto;
+  __syncthreads();
+  double before = 0.0;
+  total = 0.0;
+  for (int w = 0; w < waves; ++w) {
+    before += w < wave ? room[w] : 0.0;
+    total += room[w];
+  }
+  const double shifted = __shfl_up(upto, 1, kWave);
+  return before + (lane > 0 ? shifted : 0.0);
+}
+
 __device__ __forceinline__ int tree_size(const SampledParams &p, int b) {
   const int T = p.n_nodes[b];
   return T < 1 ? 1 : (T > p.T_max ? p.T_max : T);
@@ -183,17 +205,25 @@ struct RowStat {
   float most;
   double scale;  // 1 / sum; 0 where the row has no probability
 };
+// Of all slices of a row; eight of them are requested together.
 __device__ __forceinline__ RowStat row_stat(const SliceStat *s, int slices, double inv) {
   float most = -INFINITY;
-  for (int i = 0; i < slices; ++i) most = fmaxf(most, s[i].most);
   double sum = 0.0;
-  if (most > -INFINITY)
-    for (int i = 0; i < slices; ++i) sum += s[i].sum * weight_of(s[i].most, most, inv);
+  for (int i0 = 0; i0 < slices; i0 += 8) {
+    SliceStat x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = s[i0 + i < slices ? i0 + i : i0];
+    float top = most;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i].most);
+    if (top == -INFINITY) continue;
+    sum = most == -INFINITY ? 0.0 : sum * weight_of(most, top, inv);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += i0 + i < slices ? x[i].sum * weight_of(x[i].most, top, inv) : 0.0;
+    most = top;
+  }
   return {most, sum > 0.0 ? 1.0 / sum : 0.0};
 }
-
-// Nodes before i, as a set
-__device__ __forceinline__ bool in_set(const uint64_t (&s)[2], int i) { return (s[i >> 6] >> (i & 63)) & 1; }
 
 template <bool kBf16, bool kDraft>
 __global__ __launch_bounds__(kDraft ? 1024 : PROPD_MAX_TREE) void sampled_walk_kernel(SampledParams p) {
@@ -360,7 +390,7 @@ __global__ __launch_bounds__(kSampledThreads) void sampled_next_kernel(SampledPa
   __shared__ float f_room[kSampledThreads / kWave];
   __shared__ double d_room[kSampledThreads / kWave];
   __shared__ uint32_t s_refused[kSliceTokens / 32];
-  __shared__ double s_upto[kSampledThreads];
+  __shared__ double s_goal;
   __shared__ int s_last, s_found;
   const int b = blockIdx.x / p.slices, own = blockIdx.x - b * p.slices, tid = threadIdx.x;
   const WalkEnd e = p.end[b];
@@ -389,7 +419,7 @@ __global__ __launch_bounds__(kSampledThreads) void sampled_next_kernel(SampledPa
     for (int i = 0; i < 16; ++i) sum += w[i];
     return sum;
   };
-  const double total_here = block_reduce(chunk(own), d_room, [](double a, double b) { return a + b; });
+  const double own_sum = chunk(own), total_here = block_reduce(own_sum, d_room, [](double a, double b) { return a + b; });
   if (tid == 0) {
     SliceStat *to = p.left + (size_t)b * p.slices + own;
     __hip_atomic_store(&to->most, e.much > 0.0 ? 0.f : most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -408,15 +438,9 @@ __global__ __launch_bounds__(kSampledThreads) void sampled_next_kernel(SampledPa
   }
   const float top = block_reduce(mine.sum > 0.0 ? mine.most : -INFINITY, f_room, [](float a, float b) { return fmaxf(a, b); });
   const double share = mine.sum > 0.0 ? mine.sum * weight_of(mine.most, top, p.inv) : 0.0;
-  s_upto[tid] = share;
   if (tid == 0) s_found = -1;
-  __syncthreads();
-  // prefix sums, in order
-  double total = 0.0, before = 0.0;
-  for (int c = 0; c < p.slices; ++c) {
-    before = c == tid ? total : before;
-    total += s_upto[c];
-  }
+  double total;
+  const double before = block_before(share, d_room, total);
   const double goal = (double)p.u_next[b] * total;
   // the first chunk whose end lies beyond the goal; where rounding leaves none, the last that has anything
   if (share > 0.0 && before + share > goal) atomicMin(reinterpret_cast<unsigned int *>(&s_found), (unsigned)tid);
@@ -448,17 +472,14 @@ __global__ __launch_bounds__(kSampledThreads) void sampled_next_kernel(SampledPa
     return;
   }
   __syncthreads();
-  s_upto[tid] = before;  // (of chunk tid)
-  if (tid == found) d_room[0] = weight_of(mine.most, top, p.inv);
+  if (tid == found) {
+    s_goal = (goal - before) / weight_of(mine.most, top, p.inv);  // in the chunk's own measure
+    s_found = 0x7fffffff;
+  }
   __syncthreads();
-  const double in_chunk = (goal - s_upto[found]) / d_room[0];  // in the chunk's own measure
-  const double sum = chunk(found);
-  __syncthreads();
-  s_upto[tid] = sum;
-  if (tid == 0) s_found = 0x7fffffff;
-  __syncthreads();
-  double here = 0.0;
-  for (int j = 0; j < tid; ++j) here += s_upto[j];
+  const double in_chunk = s_goal, sum = found == own ? own_sum : chunk(found);
+  double all;
+  double here = block_before(sum, d_room, all);
   int first = 0x7fffffff, final = -1;
   const int v0 = found * kSliceTokens + 16 * tid;
 #pragma unroll

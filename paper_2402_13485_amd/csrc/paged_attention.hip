@@ -583,7 +583,6 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
         }
       }
     }
-    mfma_settle();  // O is read by the next stage's rescale, or after the last
   };
   auto walk = [&](auto with_care) __attribute__((always_inline)) {
     m_run = -INFINITY;
@@ -614,6 +613,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
       if constexpr (kCw > 1) lds_barrier();
       if (active && stage < n_stages && seen != 0) take_stage(to, stage, seen, with_care);
     }
+    mfma_settle();  // O is read by what follows (within the loop it is read behind the next scores' wait)
   };
   walk(std::false_type{});
   bool careful;

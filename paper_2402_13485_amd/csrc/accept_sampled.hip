@@ -17,7 +17,10 @@
 
 namespace propd {
 
-constexpr int kSampledThreads = 256, kSliceTokens = 16 * kSampledThreads;
+// (four tokens per thread: what little code there is runs once, and is fetched meanwhile; with 16 per thread of 256 the kernel of the last token took 15.8 us
+// instead of NEXT_US for one sequence of 32000 tokens)
+constexpr int kOf = 8, kSampledThreads = 512, kSliceTokens = kOf * kSampledThreads;
+constexpr int kWalkThreads = 1024;  // where the draft's distributions take part
 constexpr int kMostVocab = 1 << 20;
 constexpr float kMostInverse = 0x1p20f;
 
@@ -81,65 +84,102 @@ __device__ __forceinline__ float logit_at(const void *rows, size_t row, int V, i
   return no_nan(kBf16 ? bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(rows)[at]) : reinterpret_cast<const float *>(rows)[at]);
 }
 
-// A thread's 16 neighbouring values of slice `slice` of a row; -inf beyond the vocabulary.
+// Neighbouring values of a row; -inf beyond the vocabulary.
 template <bool kBf16>
-__device__ __forceinline__ void load_slice(const SampledParams &p, const void *rows, size_t row, int slice, float (&x)[16]) {
-  const int first = slice * kSliceTokens + 16 * (int)threadIdx.x;
-  if (p.aligned && first + 16 <= p.V) {
+__device__ __forceinline__ void load_tokens(const SampledParams &p, const void *rows, size_t row, int first, float (&x)[kOf]) {
+  if (p.aligned && first + kOf <= p.V) {
     if constexpr (kBf16) {
-      const u32x4 *src = reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint16_t *>(rows) + row * (size_t)p.V + first);
-      const u32x4 a[2] = {src[0], src[1]};
+      typedef uint32_t Pairs __attribute__((ext_vector_type(kOf / 2)));
+      const Pairs a = *reinterpret_cast<const Pairs *>(reinterpret_cast<const uint16_t *>(rows) + row * (size_t)p.V + first);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[2 * i] = no_nan(__uint_as_float(a[i / 4][i % 4] << 16));
-        x[2 * i + 1] = no_nan(__uint_as_float(a[i / 4][i % 4] & 0xffff0000u));
+      for (int i = 0; i < kOf / 2; ++i) {
+        x[2 * i] = no_nan(__uint_as_float(a[i] << 16));
+        x[2 * i + 1] = no_nan(__uint_as_float(a[i] & 0xffff0000u));
       }
     } else {
       const f32x4 *src = reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(rows) + row * (size_t)p.V + first);
-      const f32x4 a[4] = {src[0], src[1], src[2], src[3]};
+      f32x4 a[kOf / 4];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = no_nan(a[i / 4][i % 4]);
+      for (int i = 0; i < kOf / 4; ++i) a[i] = src[i];
+#pragma unroll
+      for (int i = 0; i < kOf; ++i) x[i] = no_nan(a[i / 4][i % 4]);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = first + i < p.V ? logit_at<kBf16>(rows, row, p.V, first + i) : -INFINITY;
+    for (int i = 0; i < kOf; ++i) x[i] = first + i < p.V ? logit_at<kBf16>(rows, row, p.V, first + i) : -INFINITY;
   }
 }
 
-// Over the workgroup, in a fixed order; every thread gets the result.  `room`: one entry per wave, used by one call at a time.
+// Sums and extremes over the lanes up to each, by data-parallel moves between registers (a few cycles a step, a tenth of what one through LDS
+// takes); `idle` fills the lanes that a step does not reach.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t v, uint32_t idle) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)idle, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved(float v, float idle) {
+  return __uint_as_float(moved<CTRL, ROWS>(__float_as_uint(v), __float_as_uint(idle)));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int v, int idle) {
+  return (int)moved<CTRL, ROWS>((uint32_t)v, (uint32_t)idle);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double v, double idle) {
+  const uint64_t a = __builtin_bit_cast(uint64_t, v), z = __builtin_bit_cast(uint64_t, idle);
+  const uint64_t lo = moved<CTRL, ROWS>((uint32_t)a, (uint32_t)z), hi = moved<CTRL, ROWS>((uint32_t)(a >> 32), (uint32_t)(z >> 32));
+  return __builtin_bit_cast(double, lo | hi << 32);
+}
 template <class T, class F>
-__device__ __forceinline__ T block_reduce(T v, T *room, F &&join) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = join(v, __shfl_xor(v, o, kWave));
-  const int waves = blockDim.x / kWave;
+__device__ __forceinline__ T scan_of_16(T v, T idle, F &&join) {  // within each row of 16 lanes
+  v = join(v, moved<0x111, 0xf>(v, idle));  // row_shr:1
+  v = join(v, moved<0x112, 0xf>(v, idle));  // row_shr:2
+  v = join(v, moved<0x114, 0xf>(v, idle));  // row_shr:4
+  return join(v, moved<0x118, 0xf>(v, idle));  // row_shr:8
+}
+template <class T, class F>
+__device__ __forceinline__ T scan_of_wave(T v, T idle, F &&join) {
+  v = scan_of_16(v, idle, join);
+  v = join(v, moved<0x142, 0xa>(v, idle));  // row_bcast:15 into rows 1 and 3
+  return join(v, moved<0x143, 0xc>(v, idle));  // row_bcast:31 into rows 2 and 3
+}
+__device__ __forceinline__ int of_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ float of_lane(float v, int lane) { return __uint_as_float((uint32_t)of_lane((int)__float_as_uint(v), lane)); }
+__device__ __forceinline__ double of_lane(double v, int lane) {
+  const uint64_t a = __builtin_bit_cast(uint64_t, v);
+  const uint64_t lo = (uint32_t)of_lane((int)(uint32_t)a, lane), hi = (uint32_t)of_lane((int)(uint32_t)(a >> 32), lane);
+  return __builtin_bit_cast(double, lo | hi << 32);
+}
+
+// Over the workgroup (of up to 16 waves), in a fixed order; every thread gets the result.  `room`: one entry per wave, used by one call at a time.
+template <class T, class F>
+__device__ __forceinline__ T block_reduce(T v, T idle, T *room, F &&join) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+  v = scan_of_wave(v, idle, join);
   __syncthreads();  // whoever read the room before is done
-  if ((threadIdx.x & 63) == 0) room[threadIdx.x / kWave] = v;
+  if (lane == 63) room[wave] = v;
   __syncthreads();
-  T r = room[0];
-  for (int w = 1; w < waves; ++w) r = join(r, room[w]);
-  return r;
+  return of_lane(scan_of_16((lane & 15) < waves ? room[lane & 15] : idle, idle, join), 15);
+}
+__device__ __forceinline__ float block_max(float v, float *room) {
+  return block_reduce(v, -INFINITY, room, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ double block_sum(double v, double *room) {
+  return block_reduce(v, 0.0, room, [](double a, double b) { return a + b; });
 }
 
 // The sum over the threads before this one, and over all, in a fixed order.
 __device__ __forceinline__ double block_before(double v, double *room, double &total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
-  double upto = v;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const double x = __shfl_up(upto, o, kWave);
-    upto += lane >= o ? x : 0.0;
-  }
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
+  auto add = [](double a, double b) { return a + b; };
+  const double upto = scan_of_wave(v, 0.0, add);
   __syncthreads();
   if (lane == 63) room[wave] = upto;
   __syncthreads();
-  double before = 0.0;
-  total = 0.0;
-  for (int w = 0; w < waves; ++w) {
-    before += w < wave ? room[w] : 0.0;
-    total += room[w];
-  }
-  const double shifted = __shfl_up(upto, 1, kWave);
-  return before + (lane > 0 ? shifted : 0.0);
+  const double waves_upto = scan_of_16((lane & 15) < waves ? room[lane & 15] : 0.0, 0.0, add);
+  total = of_lane(waves_upto, 15);
+  const double before = wave > 0 ? of_lane(waves_upto, wave - 1) : 0.0;
+  return before + moved<0x138, 0xf>(upto, 0.0);  // wave_shr:1
 }
 
 __device__ __forceinline__ int tree_size(const SampledParams &p, int b) {
@@ -151,18 +191,18 @@ __device__ __forceinline__ int tree_size(const SampledParams &p, int b) {
 template <bool kBf16>
 __device__ __forceinline__ SliceStat slice_stat(const SampledParams &p, const void *rows, size_t row, int slice, double inv, float *f_room,
                                                 double *d_room) {
-  float x[16];
-  load_slice<kBf16>(p, rows, row, slice, x);
+  float x[kOf];
+  load_tokens<kBf16>(p, rows, row, slice * kSliceTokens + kOf * (int)threadIdx.x, x);
   float most = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) most = fmaxf(most, x[i]);
-  most = block_reduce(most, f_room, [](float a, float b) { return fmaxf(a, b); });
+  for (int i = 0; i < kOf; ++i) most = fmaxf(most, x[i]);
+  most = block_max(most, f_room);
   double sum = 0.0;
   if (most > -INFINITY) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sum += weight_of(x[i], most, inv);
+    for (int i = 0; i < kOf; ++i) sum += weight_of(x[i], most, inv);
   }
-  sum = block_reduce(sum, d_room, [](double a, double b) { return a + b; });
+  sum = block_sum(sum, d_room);
   return {most, 0.f, sum};
 }
 
@@ -225,11 +265,23 @@ __device__ __forceinline__ RowStat row_stat(const SliceStat *s, int slices, doub
   return {most, sum > 0.0 ? 1.0 / sum : 0.0};
 }
 
+struct NodeSet {
+  uint64_t w[2];
+};
+__device__ __forceinline__ int take_first(NodeSet &s) {  // the lowest node of a set that has one
+  const int i = s.w[0] ? __ffsll((unsigned long long)s.w[0]) - 1 : 63 + __ffsll((unsigned long long)s.w[1]);
+  if (s.w[0]) s.w[0] &= s.w[0] - 1;
+  else s.w[1] &= s.w[1] - 1;
+  return i;
+}
+__device__ __forceinline__ bool some(const NodeSet &s) { return (s.w[0] | s.w[1]) != 0; }
+
 template <bool kBf16, bool kDraft>
-__global__ __launch_bounds__(kDraft ? 1024 : PROPD_MAX_TREE) void sampled_walk_kernel(SampledParams p) {
-  __shared__ int s_parent[PROPD_MAX_TREE], s_token[PROPD_MAX_TREE], s_path[PROPD_MAX_TREE], s_next[PROPD_MAX_TREE];
+__global__ __launch_bounds__(kDraft ? kWalkThreads : PROPD_MAX_TREE) void sampled_walk_kernel(SampledParams p) {
+  __shared__ int s_token[PROPD_MAX_TREE], s_path[PROPD_MAX_TREE], s_next[PROPD_MAX_TREE];
   __shared__ double s_p[PROPD_MAX_TREE], s_q[PROPD_MAX_TREE];
   __shared__ float s_u[PROPD_MAX_TREE];
+  __shared__ NodeSet s_children[PROPD_MAX_TREE];
   __shared__ uint64_t s_passes[2];
   __shared__ double d_room[16];
   __shared__ int s_full;
@@ -245,17 +297,20 @@ __global__ __launch_bounds__(kDraft ? 1024 : PROPD_MAX_TREE) void sampled_walk_k
   }
   const bool inside = child && token >= 0 && token < V;
   if (i < PROPD_MAX_TREE) {
-    s_parent[i] = child ? above : -1;
     s_token[i] = token;
     s_next[i] = -1;
+    s_children[i].w[0] = s_children[i].w[1] = 0;
+  }
+  __syncthreads();
+  if (kDraft ? inside : child) atomicOr(reinterpret_cast<unsigned long long *>(&s_children[above].w[i >> 6]), 1ull << (i & 63));
+  if (i < PROPD_MAX_TREE) {
     double pc = 0.0, qc = 0.0;
     if (inside) {
       const size_t row = base + above;
-      const float x = logit_at<kBf16>(p.logits, row, V, token);
+      const float x = logit_at<kBf16>(p.logits, row, V, token), y = kDraft ? logit_at<kBf16>(p.draft, row, V, token) : 0.f;
       const RowStat s = row_stat(p.p_stat + row * p.slices, p.slices, p.inv);
       pc = s.scale > 0.0 ? weight_of(x, s.most, p.inv) * s.scale : 0.0;
       if constexpr (kDraft) {
-        const float y = logit_at<kBf16>(p.draft, row, V, token);
         const RowStat t = row_stat(p.q_stat + row * p.slices, p.slices, p.draft_inv);
         qc = t.scale > 0.0 ? weight_of(y, t.most, p.draft_inv) * t.scale : 0.0;
       }
@@ -264,36 +319,30 @@ __global__ __launch_bounds__(kDraft ? 1024 : PROPD_MAX_TREE) void sampled_walk_k
     s_q[i] = qc;
     s_u[i] = child ? p.u[base + i] : 0.f;
   }
-  if (i < 2) s_passes[i] = 0;
   __syncthreads();
   double much = 0.0;
   int last = 0, full = 1;
   if constexpr (!kDraft) {
     // every candidate's test, as if its siblings before it had been refused: the first that passes is taken
-    uint64_t before[2] = {0, 0};
+    NodeSet before = {{0, 0}};
     bool again = false;
-    double left = 1.0;
     if (child) {
-      for (int j = above + 1; j < i; ++j)
-        if (s_parent[j] == above) {
-          before[j >> 6] |= 1ull << (j & 63);
-          again = again || s_token[j] == token;
-        }
+      uint64_t lo, hi;
+      mask_below(i, lo, hi);
+      before = {{s_children[above].w[0] & lo, s_children[above].w[1] & hi}};
+      for (NodeSet m = before; some(m);) again = s_token[take_first(m)] == token || again;
     }
     const double mine = again ? 0.0 : s_p[i];
     __syncthreads();
     s_p[i] = mine;  // (a token refused before has nothing left)
     __syncthreads();
-    if (child) {
-      for (int w = 0; w < 2; ++w)
-        for (uint64_t m = before[w]; m; m &= m - 1) left -= s_p[64 * w + __ffsll((unsigned long long)m) - 1];
-      left = left > 0.0 ? left : 0.0;
-    }
-    const bool passes = child && (double)s_u[i] * left < mine;
+    double left = 1.0;
+    for (NodeSet m = before; some(m);) left -= s_p[take_first(m)];
+    const bool passes = child && (double)s_u[i] * (left > 0.0 ? left : 0.0) < mine;
     const uint64_t word = __ballot(passes);
     if ((i & 63) == 0) s_passes[i >> 6] = word;
     __syncthreads();
-    if (passes && ((before[0] & s_passes[0]) | (before[1] & s_passes[1])) == 0) s_next[above] = i;
+    if (passes && ((before.w[0] & s_passes[0]) | (before.w[1] & s_passes[1])) == 0) s_next[above] = i;
     __syncthreads();
     if (i == 0) {
       int node = 0, n = 0;
@@ -318,20 +367,24 @@ __global__ __launch_bounds__(kDraft ? 1024 : PROPD_MAX_TREE) void sampled_walk_k
       double mass = 1.0;
       int taken = -1;
       bool known = true;  // mass belongs to much
-      RowStat ps = {0.f, 0.0}, qs = {0.f, 0.0};
       const size_t row = base + node;
-      for (int j = node + 1; j < T; ++j) {
-        if (s_parent[j] != node || s_token[j] < 0 || s_token[j] >= V) continue;
+      for (NodeSet m = s_children[node]; some(m);) {
+        const int j = take_first(m);
         if (!known) {
-          ps = row_stat(p.p_stat + row * p.slices, p.slices, p.inv);
-          qs = row_stat(p.q_stat + row * p.slices, p.slices, p.draft_inv);
+          const RowStat ps = row_stat(p.p_stat + row * p.slices, p.slices, p.inv), qs = row_stat(p.q_stat + row * p.slices, p.slices, p.draft_inv);
           double sum = 0.0;
-          for (int v = i; v < V; v += blockDim.x) {
-            const float x = logit_at<kBf16>(p.logits, row, V, v), y = logit_at<kBf16>(p.draft, row, V, v);
-            const double left = weight_of(x, ps.most, p.inv) * ps.scale - much * (weight_of(y, qs.most, p.draft_inv) * qs.scale);
-            sum += left > 0.0 ? left : 0.0;
+#pragma unroll 2
+          for (int first = kOf * i; first < V; first += kOf * kWalkThreads) {
+            float x[kOf], y[kOf];
+            load_tokens<kBf16>(p, p.logits, row, first, x);
+            load_tokens<kBf16>(p, p.draft, row, first, y);
+#pragma unroll
+            for (int e = 0; e < kOf; ++e) {
+              const double left = weight_of(x[e], ps.most, p.inv) * ps.scale - much * (weight_of(y[e], qs.most, p.draft_inv) * qs.scale);
+              sum += left > 0.0 && x[e] > -INFINITY ? left : 0.0;
+            }
           }
-          mass = block_reduce(sum, d_room, [](double x, double y) { return x + y; });
+          mass = block_sum(sum, d_room);
           known = true;
         }
         const double left = s_p[j] - much * s_q[j];
@@ -366,26 +419,26 @@ __global__ __launch_bounds__(kDraft ? 1024 : PROPD_MAX_TREE) void sampled_walk_k
   }
 }
 
-// What is left of a thread's 16 tokens of a chunk.  refused: a bit per token of the chunk.
-template <bool kBf16>
-__device__ __forceinline__ void left_of(const SampledParams &p, const WalkEnd &e, const float (&x)[16], size_t row, int chunk, float most,
-                                        const uint32_t *refused, double (&w)[16]) {
-  if (e.much > 0.0) {
-    float y[16];
-    load_slice<kBf16>(p, p.draft, row, chunk, y);
+// What is left of a thread's tokens of a chunk.  refused: a bit per token of the chunk.
+template <bool kBf16, bool kDraft>
+__device__ __forceinline__ void left_of(const SampledParams &p, const WalkEnd &e, const float (&x)[kOf], size_t row, int chunk, float most,
+                                        const uint32_t *refused, double (&w)[kOf]) {
+  if (kDraft && e.much > 0.0) {
+    float y[kOf];
+    load_tokens<kBf16>(p, p.draft, row, chunk * kSliceTokens + kOf * (int)threadIdx.x, y);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < kOf; ++i) {
       const double left = weight_of(x[i], e.p_most, p.inv) * e.p_scale - e.much * (weight_of(y[i], e.q_most, p.draft_inv) * e.q_scale);
       w[i] = left > 0.0 && x[i] > -INFINITY ? left : 0.0;
     }
   } else {
-    const uint32_t gone = refused[threadIdx.x >> 1] >> (16 * (threadIdx.x & 1));
+    const uint32_t gone = kDraft ? 0 : refused[threadIdx.x * kOf / 32] >> (threadIdx.x * kOf % 32);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) w[i] = x[i] > -INFINITY && !((gone >> i) & 1) ? weight_of(x[i], most, p.inv) : 0.0;
+    for (int i = 0; i < kOf; ++i) w[i] = x[i] > -INFINITY && !((gone >> i) & 1) ? weight_of(x[i], most, p.inv) : 0.0;
   }
 }
 
-template <bool kBf16>
+template <bool kBf16, bool kDraft>
 __global__ __launch_bounds__(kSampledThreads) void sampled_next_kernel(SampledParams p) {
   __shared__ float f_room[kSampledThreads / kWave];
   __shared__ double d_room[kSampledThreads / kWave];
@@ -397,101 +450,105 @@ __global__ __launch_bounds__(kSampledThreads) void sampled_next_kernel(SampledPa
   if (e.cut) return;
   const int T = tree_size(p, b);
   const size_t base = (size_t)b * p.T_max, row = base + e.node;
-  float x[16], most = -INFINITY;
-  double w[16];
-  // what is left in a chunk, by token; relative to its largest logit where p itself is left
-  auto chunk = [&](int c) -> double {
-    load_slice<kBf16>(p, p.logits, row, c, x);
-    __syncthreads();
-    for (int j = tid; j < kSliceTokens / 32; j += kSampledThreads) s_refused[j] = 0;
-    __syncthreads();
-    if (!p.draft && tid > e.node && tid < T && p.parent[base + tid] == e.node) {
-      const int t = p.token[base + tid] - c * kSliceTokens;
-      if (p.token[base + tid] >= 0 && t >= 0 && t < kSliceTokens) atomicOr(s_refused + (t >> 5), 1u << (t & 31));
-    }
-    most = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) most = fmaxf(most, x[i]);
-    most = block_reduce(most, f_room, [](float a, float b) { return fmaxf(a, b); });  // (its barriers stand behind the set)
-    left_of<kBf16>(p, e, x, row, c, most, s_refused, w);
-    double sum = 0.0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sum += w[i];
-    return sum;
-  };
-  const double own_sum = chunk(own), total_here = block_reduce(own_sum, d_room, [](double a, double b) { return a + b; });
-  if (tid == 0) {
-    SliceStat *to = p.left + (size_t)b * p.slices + own;
-    __hip_atomic_store(&to->most, e.much > 0.0 ? 0.f : most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(&to->sum, total_here, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s_last = __hip_atomic_fetch_add(p.arrived + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == p.slices - 1;
-  }
-  __syncthreads();
-  if (!s_last) return;
-
-  // ---- the last workgroup of the sequence: which chunk, then which token
-  SliceStat mine = {-INFINITY, 0.f, 0.0};
-  if (tid < p.slices) {
-    const SliceStat *from = p.left + (size_t)b * p.slices + tid;
-    mine.most = __hip_atomic_load(&from->most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    mine.sum = __hip_atomic_load(&from->sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  const float top = block_reduce(mine.sum > 0.0 ? mine.most : -INFINITY, f_room, [](float a, float b) { return fmaxf(a, b); });
-  const double share = mine.sum > 0.0 ? mine.sum * weight_of(mine.most, top, p.inv) : 0.0;
-  if (tid == 0) s_found = -1;
-  double total;
-  const double before = block_before(share, d_room, total);
-  const double goal = (double)p.u_next[b] * total;
-  // the first chunk whose end lies beyond the goal; where rounding leaves none, the last that has anything
-  if (share > 0.0 && before + share > goal) atomicMin(reinterpret_cast<unsigned int *>(&s_found), (unsigned)tid);
-  __syncthreads();
-  int found = s_found;
-  if (found < 0) {
-    __syncthreads();
-    if (share > 0.0) atomicMax(&s_found, tid);
-    __syncthreads();
-    found = s_found;
-  }
-  if (found < 0) {  // nothing is left: the likeliest token
-    float best = -INFINITY;
-    int at = 0x7fffffff;
-    for (int v = tid; v < p.V; v += kSampledThreads) {
-      const float y = logit_at<kBf16>(p.logits, row, p.V, v);
-      if (y > best || at == 0x7fffffff) {
-        best = y;
-        at = v;
+  const bool relative = !(kDraft && e.much > 0.0);  // what is left is p itself, in a chunk relative to its largest logit
+  double w[kOf], sum;
+  int c = own;
+#pragma nounroll
+  for (bool all = true;; all = false) {  // all workgroups, a chunk each; then the last of them, the token's chunk
+    float x[kOf], most = -INFINITY;
+    load_tokens<kBf16>(p, p.logits, row, c * kSliceTokens + kOf * tid, x);
+    if constexpr (!kDraft) {
+      for (int j = tid; j < kSliceTokens / 32; j += kSampledThreads) s_refused[j] = 0;
+      __syncthreads();
+      if (tid > e.node && tid < T && p.parent[base + tid] == e.node) {
+        const int token = p.token[base + tid], t = token - c * kSliceTokens;
+        if (token >= 0 && t >= 0 && t < kSliceTokens) atomicOr(s_refused + (t >> 5), 1u << (t & 31));
       }
     }
-    const float top_logit = block_reduce(best, f_room, [](float a, float b) { return fmaxf(a, b); });
-    __syncthreads();
-    if (tid == 0) s_found = 0x7fffffff;
-    __syncthreads();
-    if (best == top_logit) atomicMin(&s_found, at);
-    __syncthreads();
-    if (tid == 0) p.next_token[b] = s_found < p.V ? s_found : 0;
-    return;
-  }
-  __syncthreads();
-  if (tid == found) {
-    s_goal = (goal - before) / weight_of(mine.most, top, p.inv);  // in the chunk's own measure
-    s_found = 0x7fffffff;
-  }
-  __syncthreads();
-  const double in_chunk = s_goal, sum = found == own ? own_sum : chunk(found);
-  double all;
-  double here = block_before(sum, d_room, all);
-  int first = 0x7fffffff, final = -1;
-  const int v0 = found * kSliceTokens + 16 * tid;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < kOf; ++i) most = fmaxf(most, x[i]);
+    most = block_max(most, f_room);  // (its barriers stand behind the set)
+    left_of<kBf16, kDraft>(p, e, x, row, c, most, s_refused, w);
+    sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kOf; ++i) sum += w[i];
+    if (!all) break;
+    const double here = block_sum(sum, d_room);
+    if (tid == 0) {
+      SliceStat *to = p.left + (size_t)b * p.slices + own;
+      __hip_atomic_store(&to->most, relative ? most : 0.f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(&to->sum, here, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      s_last = __hip_atomic_fetch_add(p.arrived + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == p.slices - 1;
+      s_found = -1;
+    }
+    __syncthreads();
+    if (!s_last) return;
+
+    // ---- the last workgroup of the sequence: which chunk
+    SliceStat mine = {-INFINITY, 0.f, 0.0};
+    if (tid < p.slices) {
+      const SliceStat *from = p.left + (size_t)b * p.slices + tid;
+      mine.most = __hip_atomic_load(&from->most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      mine.sum = __hip_atomic_load(&from->sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    const float top = block_max(mine.sum > 0.0 ? mine.most : -INFINITY, f_room);
+    const double scale = mine.sum > 0.0 ? weight_of(mine.most, top, p.inv) : 0.0, share = mine.sum * scale;
+    double total;
+    const double before = block_before(share, d_room, total);
+    const double goal = (double)p.u_next[b] * total;
+    // the first chunk whose end lies beyond the goal; where rounding leaves none, the last that has anything
+    if (share > 0.0 && before + share > goal) atomicMin(reinterpret_cast<unsigned int *>(&s_found), (unsigned)tid);
+    __syncthreads();
+    c = s_found;
+    if (c < 0) {
+      __syncthreads();
+      if (share > 0.0) atomicMax(&s_found, tid);
+      __syncthreads();
+      c = s_found;
+    }
+    if (c < 0) {  // nothing is left: the likeliest token
+      float best = -INFINITY;
+      int at = 0x7fffffff;
+      for (int v = tid; v < p.V; v += kSampledThreads) {
+        const float y = logit_at<kBf16>(p.logits, row, p.V, v);
+        if (y > best || at == 0x7fffffff) {
+          best = y;
+          at = v;
+        }
+      }
+      const float top_logit = block_max(best, f_room);
+      __syncthreads();
+      if (tid == 0) s_found = 0x7fffffff;
+      __syncthreads();
+      if (best == top_logit) atomicMin(&s_found, at);
+      __syncthreads();
+      if (tid == 0) p.next_token[b] = s_found < p.V ? s_found : 0;
+      return;
+    }
+    __syncthreads();
+    if (tid == c) {
+      s_goal = (goal - before) / scale;  // in the chunk's own measure
+      s_found = 0x7fffffff;
+    }
+    __syncthreads();
+    if (c == own) break;  // (its weights are at hand)
+  }
+
+  // ---- and which token of it
+  double all_of_it;
+  double here = block_before(sum, d_room, all_of_it);
+  int first = 0x7fffffff, final = -1;
+  const int v0 = c * kSliceTokens + kOf * tid;
+#pragma unroll
+  for (int i = 0; i < kOf; ++i) {
     here += w[i];
     if (w[i] > 0.0) {
-      if (here > in_chunk && first == 0x7fffffff) first = v0 + i;
+      if (here > s_goal && first == 0x7fffffff) first = v0 + i;
       final = v0 + i;
     }
   }
   if (first != 0x7fffffff) atomicMin(&s_found, first);
-  const int end = block_reduce(final, reinterpret_cast<int *>(f_room), [](int a, int b) { return a > b ? a : b; });
+  const int end = block_reduce(final, -1, reinterpret_cast<int *>(f_room), [](int a, int b) { return a > b ? a : b; });
   if (tid == 0) p.next_token[b] = s_found != 0x7fffffff ? s_found : end;
 }
 
@@ -510,10 +567,12 @@ template <bool kBf16>
 static propd_status run_sampled(const SampledParams &p, hipStream_t st) {
   hipLaunchKernelGGL(sampled_stats_kernel<kBf16>, dim3((unsigned)(p.B * p.per_sequence)), dim3(kSampledThreads), 0, st, p);
   if (!launch_ok()) return PROPD_ERR_DEVICE;
-  if (p.draft) hipLaunchKernelGGL((sampled_walk_kernel<kBf16, true>), dim3((unsigned)p.B), dim3(1024), 0, st, p);
+  if (p.draft) hipLaunchKernelGGL((sampled_walk_kernel<kBf16, true>), dim3((unsigned)p.B), dim3(kWalkThreads), 0, st, p);
   else hipLaunchKernelGGL((sampled_walk_kernel<kBf16, false>), dim3((unsigned)p.B), dim3(PROPD_MAX_TREE), 0, st, p);
   if (!launch_ok()) return PROPD_ERR_DEVICE;
-  hipLaunchKernelGGL(sampled_next_kernel<kBf16>, dim3((unsigned)(p.B * p.slices)), dim3(kSampledThreads), 0, st, p);
+  const dim3 grid((unsigned)(p.B * p.slices));
+  if (p.draft) hipLaunchKernelGGL((sampled_next_kernel<kBf16, true>), grid, dim3(kSampledThreads), 0, st, p);
+  else hipLaunchKernelGGL((sampled_next_kernel<kBf16, false>), grid, dim3(kSampledThreads), 0, st, p);
   return launch_ok() ? PROPD_OK : PROPD_ERR_DEVICE;
 }
 
@@ -566,7 +625,7 @@ extern "C" propd_status propd_accept_sampled(const propd_tree *tree, propd_dtype
   p.accept_path = accept_path;
   p.next_token = next_token;
   // workgroups of a sequence: about as many as run at once, no more than there can be slices of nodes with children
-  const long long most = (long long)(p.T_max > 1 ? p.T_max - 1 : 1) * p.slices, fair = 2048 / p.B > 1 ? 2048 / p.B : 1;
+  const long long most = (long long)(p.T_max > 1 ? p.T_max - 1 : 1) * p.slices, fair = 512 / p.B > 1 ? 512 / p.B : 1;
   p.per_sequence = (int)(most < fair ? most : fair);
   return dt == PROPD_BF16 ? run_sampled<true>(p, as_stream(hip_stream)) : run_sampled<false>(p, as_stream(hip_stream));
 }

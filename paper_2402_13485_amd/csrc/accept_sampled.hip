@@ -13,6 +13,8 @@
 // The rows are read at memory speed; the exponentials (20 fp64 instructions each, at the rate of fp32 ones) take as long.
 #include <math.h>
 
+#include <type_traits>
+
 #include "common.h"
 
 namespace propd {
@@ -50,31 +52,40 @@ struct SampledParams {
   int32_t *accept_len, *accept_path, *next_token;
 };
 
-// exp(x) for x <= 0: x = n log 2 + r with |r| <= log(2) / 2, the exponential series of r up to r^12 (3e-16 off).
-__device__ __forceinline__ double exp_below(double x) {
-  const double n = rint(x * 1.4426950408889634);
-  double r = fma(n, -0.693147180559945309, x);
-  r = fma(n, -2.319046813846299558e-17, r);  // what log 2 is beyond its double
-  double s = 1.0 / 479001600.0;
-  s = fma(s, r, 1.0 / 39916800.0);
-  s = fma(s, r, 1.0 / 3628800.0);
-  s = fma(s, r, 1.0 / 362880.0);
-  s = fma(s, r, 1.0 / 40320.0);
-  s = fma(s, r, 1.0 / 5040.0);
-  s = fma(s, r, 1.0 / 720.0);
-  s = fma(s, r, 1.0 / 120.0);
-  s = fma(s, r, 1.0 / 24.0);
-  s = fma(s, r, 1.0 / 6.0);
-  s = fma(s, r, 0.5);
-  s = fma(s, r, 1.0);
-  s = fma(s, r, 1.0);
-  return x < -745.0 ? 0.0 : __builtin_amdgcn_ldexp(s, (int)n);
+// 2^t for t up to about 0: t = n + f with |f| <= 1/2, the series of 2^f = exp(f log 2) up to f^11 (6e-15 off).  Below 2^-1074 it is 0.
+__device__ __forceinline__ double exp2_below(double t) {
+  t = fmax(t, -1100.0);
+  const double n = rint(t), f = t - n;
+  double s = 4.4455382718708116e-10;  // log(2)^k / k! for k = 11, 10, ..., 1
+  s = fma(s, f, 7.0549116208011233e-09);
+  s = fma(s, f, 1.0178086009239699e-07);
+  s = fma(s, f, 1.3215486790144307e-06);
+  s = fma(s, f, 1.5252733804059841e-05);
+  s = fma(s, f, 1.5403530393381608e-04);
+  s = fma(s, f, 1.3333558146428443e-03);
+  s = fma(s, f, 9.6181291076284772e-03);
+  s = fma(s, f, 5.5504108664821580e-02);
+  s = fma(s, f, 2.4022650695910071e-01);
+  s = fma(s, f, 6.9314718055994531e-01);
+  s = fma(s, f, 1.0);
+  return __builtin_amdgcn_ldexp(s, (int)n);
 }
 
-// exp((x - most) * inv), 1 for the largest itself (infinite or not)
-__device__ __forceinline__ double weight_of(float x, float most, double inv) {
-  return x == most ? 1.0 : exp_below(((double)x - (double)most) * inv);
-}
+// The weights of a row's tokens: exp((x - most) * inv) times a scale, as 2^(x * slope + offset).  Where `most` is infinite, those that
+// are it have the scale and the others nothing.
+struct Weights {
+  double slope, offset;
+  bool infinite;
+  __device__ __forceinline__ Weights(float most, double inv, double scale = 1.0) {
+    infinite = most == INFINITY;
+    slope = inv * 1.4426950408889634;
+    offset = most == -INFINITY || infinite ? 0.0 : -(double)most * slope;
+    offset = scale == 1.0 ? offset : scale > 0.0 ? offset + log2(scale) : -INFINITY;
+  }
+  __device__ __forceinline__ double operator()(float x) const {
+    return exp2_below(infinite ? (x == INFINITY ? offset : -INFINITY) : fma((double)x, slope, offset));
+  }
+};
 
 __device__ __forceinline__ float no_nan(float x) { return x == x ? x : -INFINITY; }
 
@@ -198,9 +209,10 @@ __device__ __forceinline__ SliceStat slice_stat(const SampledParams &p, const vo
   for (int i = 0; i < kOf; ++i) most = fmaxf(most, x[i]);
   most = block_max(most, f_room);
   double sum = 0.0;
+  const Weights weight(most, inv);
   if (most > -INFINITY) {
 #pragma unroll
-    for (int i = 0; i < kOf; ++i) sum += weight_of(x[i], most, inv);
+    for (int i = 0; i < kOf; ++i) sum += weight(x[i]);
   }
   sum = block_sum(sum, d_room);
   return {most, 0.f, sum};
@@ -214,6 +226,7 @@ __global__ __launch_bounds__(kSampledThreads) void sampled_stats_kernel(SampledP
   __shared__ double d_room[kSampledThreads / kWave];
   const int b = blockIdx.x / p.per_sequence, at = blockIdx.x - b * p.per_sequence, tid = threadIdx.x;
   const int T = tree_size(p, b);
+  if (at == 0 && tid == 0) p.arrived[b] = 0;  // of the last kernel
   if (tid < 2) s_inner[tid] = 0;
   __syncthreads();
   if (tid > 0 && tid < T) {
@@ -257,9 +270,10 @@ __device__ __forceinline__ RowStat row_stat(const SliceStat *s, int slices, doub
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i].most);
     if (top == -INFINITY) continue;
-    sum = most == -INFINITY ? 0.0 : sum * weight_of(most, top, inv);
+    const Weights weight(top, inv);
+    sum = most == -INFINITY ? 0.0 : sum * weight(most);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += i0 + i < slices ? x[i].sum * weight_of(x[i].most, top, inv) : 0.0;
+    for (int i = 0; i < 8; ++i) sum += i0 + i < slices && x[i].most > -INFINITY ? x[i].sum * weight(x[i].most) : 0.0;
     most = top;
   }
   return {most, sum > 0.0 ? 1.0 / sum : 0.0};
@@ -274,149 +288,201 @@ __device__ __forceinline__ int take_first(NodeSet &s) {  // the lowest node of a
   else s.w[1] &= s.w[1] - 1;
   return i;
 }
+__device__ __forceinline__ bool in_set(const NodeSet &s, int i) { return (s.w[i >> 6] >> (i & 63)) & 1; }
 __device__ __forceinline__ bool some(const NodeSet &s) { return (s.w[0] | s.w[1]) != 0; }
 
+// What a workgroup knows of its sequence's tree.
+struct Walk {
+  int token[PROPD_MAX_TREE], path[PROPD_MAX_TREE], next[PROPD_MAX_TREE];
+  NodeSet children[PROPD_MAX_TREE];
+  RowStat row_p[PROPD_MAX_TREE], row_q[PROPD_MAX_TREE];  // of nodes that have children
+  double p[PROPD_MAX_TREE], q[PROPD_MAX_TREE];           // of every candidate's token at its parent
+  float u[PROPD_MAX_TREE];
+  uint64_t passes[2];
+  int full;  // nodes of the path
+};
+
+// The probabilities of all candidates at once.  Threads from PROPD_MAX_TREE on only meet the barriers; returns the parent of node threadIdx.x, -1 if
+// it is no candidate (kDraft: if its token lies outside the vocabulary).
 template <bool kBf16, bool kDraft>
-__global__ __launch_bounds__(kDraft ? kWalkThreads : PROPD_MAX_TREE) void sampled_walk_kernel(SampledParams p) {
-  __shared__ int s_token[PROPD_MAX_TREE], s_path[PROPD_MAX_TREE], s_next[PROPD_MAX_TREE];
-  __shared__ double s_p[PROPD_MAX_TREE], s_q[PROPD_MAX_TREE];
-  __shared__ float s_u[PROPD_MAX_TREE];
-  __shared__ NodeSet s_children[PROPD_MAX_TREE];
-  __shared__ uint64_t s_passes[2];
-  __shared__ double d_room[16];
-  __shared__ int s_full;
-  const int b = blockIdx.x, i = threadIdx.x, T = tree_size(p, b), V = p.V;
+__device__ __forceinline__ int meet_candidates(const SampledParams &p, int b, int T, Walk &s) {
+  const int i = threadIdx.x;
   const size_t base = (size_t)b * p.T_max;
-  if (i == 0) p.arrived[b] = 0;  // of the next kernel
   bool child = i > 0 && i < T;
   int above = 0, token = -1;
+  float u = 0.f;
   if (child) {
     above = p.parent[base + i];
     token = p.token[base + i];
+    u = p.u[base + i];
     child = above >= 0 && above < i;
   }
-  const bool inside = child && token >= 0 && token < V;
+  const bool inside = child && token >= 0 && token < p.V;
+  child = kDraft ? inside : child;
+  float x = 0.f, y = 0.f;
+  if (inside) {  // (on its way meanwhile)
+    x = logit_at<kBf16>(p.logits, base + above, p.V, token);
+    if constexpr (kDraft) y = logit_at<kBf16>(p.draft, base + above, p.V, token);
+  }
   if (i < PROPD_MAX_TREE) {
-    s_token[i] = token;
-    s_next[i] = -1;
-    s_children[i].w[0] = s_children[i].w[1] = 0;
+    s.token[i] = token;
+    s.next[i] = -1;
+    s.children[i].w[0] = s.children[i].w[1] = 0;
+    s.u[i] = u;
   }
   __syncthreads();
-  if (kDraft ? inside : child) atomicOr(reinterpret_cast<unsigned long long *>(&s_children[above].w[i >> 6]), 1ull << (i & 63));
+  if (child) atomicOr(reinterpret_cast<unsigned long long *>(&s.children[above].w[i >> 6]), 1ull << (i & 63));
+  __syncthreads();
+  if (i < T && some(s.children[i])) {
+    s.row_p[i] = row_stat(p.p_stat + (base + i) * p.slices, p.slices, p.inv);
+    if constexpr (kDraft) s.row_q[i] = row_stat(p.q_stat + (base + i) * p.slices, p.slices, p.draft_inv);
+  }
+  __syncthreads();
   if (i < PROPD_MAX_TREE) {
     double pc = 0.0, qc = 0.0;
     if (inside) {
-      const size_t row = base + above;
-      const float x = logit_at<kBf16>(p.logits, row, V, token), y = kDraft ? logit_at<kBf16>(p.draft, row, V, token) : 0.f;
-      const RowStat s = row_stat(p.p_stat + row * p.slices, p.slices, p.inv);
-      pc = s.scale > 0.0 ? weight_of(x, s.most, p.inv) * s.scale : 0.0;
+      const RowStat r = s.row_p[above];
+      pc = r.scale > 0.0 ? Weights(r.most, p.inv)(x) * r.scale : 0.0;
       if constexpr (kDraft) {
-        const RowStat t = row_stat(p.q_stat + row * p.slices, p.slices, p.draft_inv);
-        qc = t.scale > 0.0 ? weight_of(y, t.most, p.draft_inv) * t.scale : 0.0;
+        const RowStat r2 = s.row_q[above];
+        qc = r2.scale > 0.0 ? Weights(r2.most, p.draft_inv)(y) * r2.scale : 0.0;
       }
     }
-    s_p[i] = pc;
-    s_q[i] = qc;
-    s_u[i] = child ? p.u[base + i] : 0.f;
+    s.p[i] = pc;
+    s.q[i] = qc;
   }
   __syncthreads();
-  double much = 0.0;
-  int last = 0, full = 1;
-  if constexpr (!kDraft) {
-    // every candidate's test, as if its siblings before it had been refused: the first that passes is taken
-    NodeSet before = {{0, 0}};
-    bool again = false;
-    if (child) {
-      uint64_t lo, hi;
-      mask_below(i, lo, hi);
-      before = {{s_children[above].w[0] & lo, s_children[above].w[1] & hi}};
-      for (NodeSet m = before; some(m);) again = s_token[take_first(m)] == token || again;
-    }
-    const double mine = again ? 0.0 : s_p[i];
-    __syncthreads();
-    s_p[i] = mine;  // (a token refused before has nothing left)
-    __syncthreads();
-    double left = 1.0;
-    for (NodeSet m = before; some(m);) left -= s_p[take_first(m)];
-    const bool passes = child && (double)s_u[i] * (left > 0.0 ? left : 0.0) < mine;
-    const uint64_t word = __ballot(passes);
-    if ((i & 63) == 0) s_passes[i >> 6] = word;
-    __syncthreads();
-    if (passes && ((before.w[0] & s_passes[0]) | (before.w[1] & s_passes[1])) == 0) s_next[above] = i;
-    __syncthreads();
-    if (i == 0) {
-      int node = 0, n = 0;
-      do {
-        s_path[n++] = node;
-        node = s_next[node];
-      } while (node >= 0);
-      s_full = n;
-    }
-    __syncthreads();
-    full = s_full;
-    last = s_path[full - 1];
-  } else {
-    // (every thread goes along; child and what it needs are the same for all)
-    full = 0;
-    int node = 0;
-    while (true) {
-      if (i == 0) s_path[full] = node;
-      ++full;
-      last = node;
-      much = 0.0;
-      double mass = 1.0;
-      int taken = -1;
-      bool known = true;  // mass belongs to much
-      const size_t row = base + node;
-      for (NodeSet m = s_children[node]; some(m);) {
-        const int j = take_first(m);
-        if (!known) {
-          const RowStat ps = row_stat(p.p_stat + row * p.slices, p.slices, p.inv), qs = row_stat(p.q_stat + row * p.slices, p.slices, p.draft_inv);
-          double sum = 0.0;
-#pragma unroll 2
-          for (int first = kOf * i; first < V; first += kOf * kWalkThreads) {
-            float x[kOf], y[kOf];
-            load_tokens<kBf16>(p, p.logits, row, first, x);
-            load_tokens<kBf16>(p, p.draft, row, first, y);
-#pragma unroll
-            for (int e = 0; e < kOf; ++e) {
-              const double left = weight_of(x[e], ps.most, p.inv) * ps.scale - much * (weight_of(y[e], qs.most, p.draft_inv) * qs.scale);
-              sum += left > 0.0 && x[e] > -INFINITY ? left : 0.0;
-            }
-          }
-          mass = block_sum(sum, d_room);
-          known = true;
-        }
-        const double left = s_p[j] - much * s_q[j];
-        if ((double)s_u[j] * mass * s_q[j] < left) {
-          taken = j;
-          break;
-        }
-        much += mass;
-        known = false;
-      }
-      if (taken < 0) break;
-      node = taken;
-    }
-    __syncthreads();
+  return child ? above : -1;
+}
+
+// The path of candidates that were not drawn, into s.path and s.full.
+template <bool kBf16>
+__device__ __forceinline__ void walk_given(const SampledParams &p, int b, int T, Walk &s) {
+  const int i = threadIdx.x, above = meet_candidates<kBf16, false>(p, b, T, s);
+  // every candidate's test, as if its siblings before it had been refused: the first that passes is taken
+  NodeSet before = {{0, 0}};
+  bool again = false;
+  if (above >= 0) {
+    uint64_t lo, hi;
+    mask_below(i, lo, hi);
+    before = {{s.children[above].w[0] & lo, s.children[above].w[1] & hi}};
+    for (NodeSet m = before; some(m);) again = s.token[take_first(m)] == s.token[i] || again;
   }
-  // A path buffer shorter than the path keeps its first nodes; the next node's token goes on with the same output.
-  const int len = full < p.stride ? full : p.stride;
-  for (int j = i; j < p.stride; j += blockDim.x) p.accept_path[(size_t)b * p.stride + j] = j < len ? s_path[j] : -1;
+  const double mine = above < 0 || again ? 0.0 : s.p[i];
+  __syncthreads();
+  if (i < PROPD_MAX_TREE) s.p[i] = mine;  // (a token refused before has nothing left)
+  __syncthreads();
+  double left = 1.0;
+  for (NodeSet m = before; some(m);) left -= s.p[take_first(m)];
+  const bool passes = above >= 0 && (double)s.u[i] * (left > 0.0 ? left : 0.0) < mine;
+  const uint64_t word = __ballot(passes);
+  if (i < PROPD_MAX_TREE && (i & 63) == 0) s.passes[i >> 6] = word;
+  __syncthreads();
+  if (passes && ((before.w[0] & s.passes[0]) | (before.w[1] & s.passes[1])) == 0) s.next[above] = i;
+  __syncthreads();
   if (i == 0) {
+    int node = 0, n = 0;
+    do {
+      s.path[n++] = node;
+      node = s.next[node];
+    } while (node >= 0);
+    s.full = n;
+  }
+  __syncthreads();
+}
+
+// Writes the path.  A path buffer shorter than it keeps its first nodes; the next node's token goes on with the same output.
+__device__ __forceinline__ bool write_path(const SampledParams &p, int b, const Walk &s, int full) {
+  const int len = full < p.stride ? full : p.stride;
+  for (int j = threadIdx.x; j < p.stride; j += blockDim.x) p.accept_path[(size_t)b * p.stride + j] = j < len ? s.path[j] : -1;
+  if (threadIdx.x == 0) {
     p.accept_len[b] = len;
-    if (full > len) p.next_token[b] = s_token[s_path[len]];
-    WalkEnd e = {last, full > len, 0.f, 0.f, 0.0, 0.0, much};
-    if (kDraft && much > 0.0) {
-      const RowStat s = row_stat(p.p_stat + (base + last) * p.slices, p.slices, p.inv);
-      const RowStat t = row_stat(p.q_stat + (base + last) * p.slices, p.slices, p.draft_inv);
-      e.p_most = s.most;
-      e.p_scale = s.scale;
-      e.q_most = t.most;
-      e.q_scale = t.scale;
+    if (full > len) p.next_token[b] = s.token[s.path[len]];
+  }
+  return full > len;
+}
+
+// The path of candidates that were drawn.
+template <bool kBf16>
+__global__ __launch_bounds__(kWalkThreads) void sampled_walk_kernel(SampledParams p) {
+  __shared__ Walk s;
+  __shared__ double d_room[kWalkThreads / kWave];
+  const int b = blockIdx.x, i = threadIdx.x, T = tree_size(p, b);
+  const size_t base = (size_t)b * p.T_max;
+  double much = 0.0;
+  int last = 0, full = 0;
+  meet_candidates<kBf16, true>(p, b, T, s);
+  // (every thread goes along; child and what it needs are the same for all)
+  int node = 0;
+  while (true) {
+    if (i == 0) s.path[full] = node;
+    ++full;
+    last = node;
+    much = 0.0;
+    double mass = 1.0;
+    int taken = -1;
+    bool known = true;  // mass belongs to much
+    const size_t row = base + node;
+    for (NodeSet m = s.children[node]; some(m);) {
+      const int j = take_first(m);
+      if (!known) {
+        const RowStat ps = s.row_p[node], qs = s.row_q[node];
+        const Weights weight_p(ps.most, p.inv, ps.scale), weight_q(qs.most, p.draft_inv, qs.scale);
+        double sum = 0.0;
+        for (int first = kOf * i; first < p.V; first += kOf * kWalkThreads) {
+          float x[kOf], y[kOf];
+          load_tokens<kBf16>(p, p.logits, row, first, x);
+          load_tokens<kBf16>(p, p.draft, row, first, y);
+#pragma unroll
+          for (int e = 0; e < kOf; ++e) sum += fmax(fma(-much, weight_q(y[e]), weight_p(x[e])), 0.0);
+        }
+        mass = block_sum(sum, d_room);
+        known = true;
+      }
+      const double left = s.p[j] - much * s.q[j];
+      if ((double)s.u[j] * mass * s.q[j] < left) {
+        taken = j;
+        break;
+      }
+      much += mass;
+      known = false;
+    }
+    if (taken < 0) break;
+    node = taken;
+  }
+  __syncthreads();
+  const bool cut = write_path(p, b, s, full);
+  if (i == 0) {
+    WalkEnd e = {last, cut, 0.f, 0.f, 0.0, 0.0, much};
+    if (much > 0.0) {
+      e.p_most = s.row_p[last].most;
+      e.p_scale = s.row_p[last].scale;
+      e.q_most = s.row_q[last].most;
+      e.q_scale = s.row_q[last].scale;
     }
     p.end[b] = e;
   }
+}
+
+// The likeliest token of a row, the lowest id among equal ones, by the workgroup.
+template <bool kBf16>
+__device__ __forceinline__ void likeliest_token(const SampledParams &p, size_t row, float *f_room, int *found, int32_t *to) {
+  float best = -INFINITY;
+  int at = 0x7fffffff;
+  for (int v = threadIdx.x; v < p.V; v += blockDim.x) {
+    const float y = logit_at<kBf16>(p.logits, row, p.V, v);
+    if (y > best || at == 0x7fffffff) {
+      best = y;
+      at = v;
+    }
+  }
+  const float top = block_max(best, f_room);
+  __syncthreads();
+  if (threadIdx.x == 0) *found = 0x7fffffff;
+  __syncthreads();
+  if (best == top) atomicMin(found, at);
+  __syncthreads();
+  if (threadIdx.x == 0) *to = *found < p.V ? *found : 0;
 }
 
 // What is left of a thread's tokens of a chunk.  refused: a bit per token of the chunk.
@@ -426,15 +492,14 @@ __device__ __forceinline__ void left_of(const SampledParams &p, const WalkEnd &e
   if (kDraft && e.much > 0.0) {
     float y[kOf];
     load_tokens<kBf16>(p, p.draft, row, chunk * kSliceTokens + kOf * (int)threadIdx.x, y);
+    const Weights weight_p(e.p_most, p.inv, e.p_scale), weight_q(e.q_most, p.draft_inv, e.q_scale);
 #pragma unroll
-    for (int i = 0; i < kOf; ++i) {
-      const double left = weight_of(x[i], e.p_most, p.inv) * e.p_scale - e.much * (weight_of(y[i], e.q_most, p.draft_inv) * e.q_scale);
-      w[i] = left > 0.0 && x[i] > -INFINITY ? left : 0.0;
-    }
+    for (int i = 0; i < kOf; ++i) w[i] = fmax(fma(-e.much, weight_q(y[i]), weight_p(x[i])), 0.0);
   } else {
+    const Weights weight(most, p.inv);
     const uint32_t gone = kDraft ? 0 : refused[threadIdx.x * kOf / 32] >> (threadIdx.x * kOf % 32);
 #pragma unroll
-    for (int i = 0; i < kOf; ++i) w[i] = x[i] > -INFINITY && !((gone >> i) & 1) ? weight_of(x[i], most, p.inv) : 0.0;
+    for (int i = 0; i < kOf; ++i) w[i] = x[i] > -INFINITY && !((gone >> i) & 1) ? weight(x[i]) : 0.0;
   }
 }
 
@@ -442,14 +507,24 @@ template <bool kBf16, bool kDraft>
 __global__ __launch_bounds__(kSampledThreads) void sampled_next_kernel(SampledParams p) {
   __shared__ float f_room[kSampledThreads / kWave];
   __shared__ double d_room[kSampledThreads / kWave];
-  __shared__ uint32_t s_refused[kSliceTokens / 32];
+  __shared__ uint32_t s_refused[kSliceTokens / 32];  // a bit per token
+  __shared__ std::conditional_t<kDraft, char, Walk> s_walk;
   __shared__ double s_goal;
   __shared__ int s_last, s_found;
   const int b = blockIdx.x / p.slices, own = blockIdx.x - b * p.slices, tid = threadIdx.x;
-  const WalkEnd e = p.end[b];
-  if (e.cut) return;
   const int T = tree_size(p, b);
-  const size_t base = (size_t)b * p.T_max, row = base + e.node;
+  const size_t base = (size_t)b * p.T_max;
+  WalkEnd e = {};
+  if constexpr (kDraft) {
+    e = p.end[b];
+    if (e.cut) return;
+  } else {  // every workgroup walks by itself: the path is short, and a kernel of its own takes longer
+    walk_given<kBf16>(p, b, T, s_walk);
+    e.node = s_walk.path[s_walk.full - 1];
+    if (own == 0) write_path(p, b, s_walk, s_walk.full);
+    if (s_walk.full > p.stride) return;
+  }
+  const size_t row = base + e.node;
   const bool relative = !(kDraft && e.much > 0.0);  // what is left is p itself, in a chunk relative to its largest logit
   double w[kOf], sum;
   int c = own;
@@ -460,8 +535,8 @@ __global__ __launch_bounds__(kSampledThreads) void sampled_next_kernel(SampledPa
     if constexpr (!kDraft) {
       for (int j = tid; j < kSliceTokens / 32; j += kSampledThreads) s_refused[j] = 0;
       __syncthreads();
-      if (tid > e.node && tid < T && p.parent[base + tid] == e.node) {
-        const int token = p.token[base + tid], t = token - c * kSliceTokens;
+      if (tid < T && in_set(s_walk.children[e.node], tid)) {  // all of them were refused
+        const int token = s_walk.token[tid], t = token - c * kSliceTokens;
         if (token >= 0 && t >= 0 && t < kSliceTokens) atomicOr(s_refused + (t >> 5), 1u << (t & 31));
       }
     }
@@ -492,7 +567,7 @@ __global__ __launch_bounds__(kSampledThreads) void sampled_next_kernel(SampledPa
       mine.sum = __hip_atomic_load(&from->sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     const float top = block_max(mine.sum > 0.0 ? mine.most : -INFINITY, f_room);
-    const double scale = mine.sum > 0.0 ? weight_of(mine.most, top, p.inv) : 0.0, share = mine.sum * scale;
+    const double scale = mine.sum > 0.0 ? (relative ? Weights(top, p.inv)(mine.most) : 1.0) : 0.0, share = mine.sum * scale;
     double total;
     const double before = block_before(share, d_room, total);
     const double goal = (double)p.u_next[b] * total;
@@ -507,22 +582,8 @@ __global__ __launch_bounds__(kSampledThreads) void sampled_next_kernel(SampledPa
       c = s_found;
     }
     if (c < 0) {  // nothing is left: the likeliest token
-      float best = -INFINITY;
-      int at = 0x7fffffff;
-      for (int v = tid; v < p.V; v += kSampledThreads) {
-        const float y = logit_at<kBf16>(p.logits, row, p.V, v);
-        if (y > best || at == 0x7fffffff) {
-          best = y;
-          at = v;
-        }
-      }
-      const float top_logit = block_max(best, f_room);
       __syncthreads();
-      if (tid == 0) s_found = 0x7fffffff;
-      __syncthreads();
-      if (best == top_logit) atomicMin(&s_found, at);
-      __syncthreads();
-      if (tid == 0) p.next_token[b] = s_found < p.V ? s_found : 0;
+      likeliest_token<kBf16>(p, row, f_room, &s_found, p.next_token + b);
       return;
     }
     __syncthreads();
@@ -567,9 +628,10 @@ template <bool kBf16>
 static propd_status run_sampled(const SampledParams &p, hipStream_t st) {
   hipLaunchKernelGGL(sampled_stats_kernel<kBf16>, dim3((unsigned)(p.B * p.per_sequence)), dim3(kSampledThreads), 0, st, p);
   if (!launch_ok()) return PROPD_ERR_DEVICE;
-  if (p.draft) hipLaunchKernelGGL((sampled_walk_kernel<kBf16, true>), dim3((unsigned)p.B), dim3(kWalkThreads), 0, st, p);
-  else hipLaunchKernelGGL((sampled_walk_kernel<kBf16, false>), dim3((unsigned)p.B), dim3(PROPD_MAX_TREE), 0, st, p);
-  if (!launch_ok()) return PROPD_ERR_DEVICE;
+  if (p.draft) {
+    hipLaunchKernelGGL(sampled_walk_kernel<kBf16>, dim3((unsigned)p.B), dim3(kWalkThreads), 0, st, p);
+    if (!launch_ok()) return PROPD_ERR_DEVICE;
+  }
   const dim3 grid((unsigned)(p.B * p.slices));
   if (p.draft) hipLaunchKernelGGL((sampled_next_kernel<kBf16, true>), grid, dim3(kSampledThreads), 0, st, p);
   else hipLaunchKernelGGL((sampled_next_kernel<kBf16, false>), grid, dim3(kSampledThreads), 0, st, p);
@@ -625,7 +687,7 @@ extern "C" propd_status propd_accept_sampled(const propd_tree *tree, propd_dtype
   p.accept_path = accept_path;
   p.next_token = next_token;
   // workgroups of a sequence: about as many as run at once, no more than there can be slices of nodes with children
-  const long long most = (long long)(p.T_max > 1 ? p.T_max - 1 : 1) * p.slices, fair = 512 / p.B > 1 ? 512 / p.B : 1;
+  const long long most = (long long)(p.T_max > 1 ? p.T_max - 1 : 1) * p.slices, fair = 2048 / p.B > 1 ? 2048 / p.B : 1;
   p.per_sequence = (int)(most < fair ? most : fair);
   return dt == PROPD_BF16 ? run_sampled<true>(p, as_stream(hip_stream)) : run_sampled<false>(p, as_stream(hip_stream));
 }

@@ -140,7 +140,7 @@ __device__ __forceinline__ int paged_sum(int v) { return __builtin_amdgcn_readla
 __device__ __forceinline__ float paged_sum(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
-  return v;
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));  // (what follows from it is the same for all lanes, in scalar registers)
 }
 
 // Units of a lane's sequence that come first, and the others; `before`: units of the sequences before those of the lanes.
@@ -283,7 +283,8 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
       *reinterpret_cast<u32x4 *>(p.records + 4 * (((size_t)b * p.H_kv + hk) * p.blocks + block)) =
           u32x4{(uint32_t)first_slot, (uint32_t)count, (uint32_t)pieces, 0};
   }
-  const int L = clamped(p.seq_lens[b], p.pages.capacity), T = clamped(p.n_nodes[b] - 1, p.T_max - 1) + 1;
+  const int L = __builtin_amdgcn_readfirstlane(clamped(p.seq_lens[b], p.pages.capacity));
+  const int T = __builtin_amdgcn_readfirstlane(clamped(p.n_nodes[b] - 1, p.T_max - 1) + 1);
   const PagedStages st = paged_stages(L, T, p.window);
   const int quot = steps / pieces, extra = steps - quot * pieces;
   const int step0 = piece * quot + (piece < extra ? piece : extra), n_steps = quot + (piece < extra ? 1 : 0);
@@ -329,13 +330,18 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
   int ids = -1, ids_from = -64;  // pages of the 16-row pieces of 32 steps' stages, a piece per lane
   auto stage_at = [&](int step) { return (step0 + step) * kRw + rw; };
   auto cached_row = [&](int stage) { return (stage - st.tree + st.first) * kStageRows; };
+  // this wave's steps: the tree's stages, then cached ones
+  const int steps_here = n_stages - rw - step0 * kRw <= 0 ? 0 : (n_stages - rw - step0 * kRw + kRw - 1) / kRw;  // to the unit's end
+  const int steps_own = steps_here < n_steps ? steps_here : n_steps;
+  const int tree_here = st.tree - rw - step0 * kRw <= 0 ? 0 : (st.tree - rw - step0 * kRw + kRw - 1) / kRw;
+  const int steps_tree = tree_here < steps_own ? tree_here : steps_own, steps_cached = steps_own - steps_tree;
   u32x4 data[kLoads];
   uint32_t scale_byte[kLoads];
   uint32_t rows_there = 0;  // of the stage on its way
+  // Requests a cached stage.  Without a branch around the loads: they stay on their way until their rows are stored.
   auto issue = [&](int step) __attribute__((always_inline)) {
     rows_there = 0;
     const int stage = stage_at(step);
-    if (step >= n_steps || stage < st.tree || stage >= n_stages) return;  // uniform
     if (step >= ids_from + 32) {
       ids_from = step;
       const int at = stage_at(step + (lane >> 1)), row = cached_row(at) + 16 * (lane & 1);
@@ -358,7 +364,10 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
       const bool second = kAtOnce >= 32 ? (ld_row & 16) != 0 : (first & 16) != 0;
       const size_t at = second ? row[1] : row[0];
       const int in_half = kAtOnce >= 16 ? 0 : first & 15;
-      data[i] = *reinterpret_cast<const u32x4 *>((v ? p.pages.v : p.pages.k) + at * kSrcRow + in_half * kSrcRow + ld_from);
+      const u32x4 *from = reinterpret_cast<const u32x4 *>((v ? p.pages.v : p.pages.k) + at * kSrcRow + in_half * kSrcRow + ld_from);
+      // Up to 64 columns no other workgroup reads these rows, and they need not stay in the caches: 32 x 8 heads of 8192 rows in 8 bits 108 -> 97 us.
+      // (Rows that blocks of columns share 327 -> 331.)
+      data[i] = kN == 16 ? __builtin_nontemporal_load(from) : *from;
       if constexpr (kCodes) scale_byte[i] = (v ? p.pages.v_scale : p.pages.k_scale)[at + in_half + (ld_row & 15)];
     }
   };
@@ -429,14 +438,22 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
     for (int tile = 0; tile < 32 / kN; ++tile) {
       Acc<kN> acc;
       clear(acc);
+      constexpr int kBatch = kQf < 8 ? kQf : 8;  // pieces that are requested together, so that products wait for LDS once
 #pragma unroll
-      for (int x = 0; x < kQf; ++x) {
-        const u32x4 a = lds_from<u32x4>((k_at ^ (((kGroups * x) ^ G::k_key(tile * kN)) << 4)) + tile * kN * kRowBytes);
-        if constexpr (kBf16) {
-          acc = product<kN>(a, qf[x], acc);
-        } else {
+      for (int x0 = 0; x0 < kQf; x0 += kBatch) {
+        u32x4 a[kBatch];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc = product<kN>(__uint_as_float(a[j]), __uint_as_float(qf[x][j]), acc);
+        for (int x = 0; x < kBatch; ++x)
+          a[x] = lds_from<u32x4>((k_at ^ (((kGroups * (x0 + x)) ^ G::k_key(tile * kN)) << 4)) + tile * kN * kRowBytes);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int x = 0; x < kBatch; ++x) {
+          if constexpr (kBf16) {
+            acc = product<kN>(a[x], qf[x0 + x], acc);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc = product<kN>(__uint_as_float(a[x][j]), __uint_as_float(qf[x0 + x][j]), acc);
+          }
         }
       }
 #pragma unroll
@@ -506,6 +523,22 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
       m_run = m_new;
     }
     const float neg_m = -(m_run == -INFINITY ? 0.f : m_run);
+    // V^T of the rows of 8 scores, requested ahead of what they are multiplied with
+    u32x4 vt[kBf16 ? 2 : 1][kBf16 ? kBlocks : 1];
+    auto read_v = [&](int half) __attribute__((always_inline)) {
+#pragma unroll
+      for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+          const int row = 4 * kGroups * (2 * half + hi);
+          const uint32_t at = (v_at ^ (((db * (kN / 8)) ^ G::v_key(row)) << 4)) + row * kRowBytes;
+          const u32x2 t = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LdsPtr<s16x4>>((uintptr_t)at)));
+          vt[half & 1][db][2 * hi] = t.x;
+          vt[half & 1][db][2 * hi + 1] = t.y;
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    if constexpr (kBf16) read_v(0);
 #pragma unroll
     for (int x = 0; x < kScores; ++x) {
       sc[x] = fast_exp2(fmaf(sc[x], unit_of, neg_m));
@@ -515,6 +548,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
     if constexpr (kBf16) {
 #pragma unroll
       for (int half = 0; half < kScores / 8; ++half) {  // a product's rows are those of 8 scores
+        if (half + 1 < kScores / 8) read_v(half + 1);
         uint32_t pw[kParts][4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
@@ -529,24 +563,16 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
         }
 #pragma unroll
         for (int db = 0; db < kBlocks; ++db) {
-          u32x4 vt;
-#pragma unroll
-          for (int hi = 0; hi < 2; ++hi) {
-            const int row = 4 * kGroups * (2 * half + hi);
-            const uint32_t at = (v_at ^ (((db * (kN / 8)) ^ G::v_key(row)) << 4)) + row * kRowBytes;
-            const u32x2 t = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LdsPtr<s16x4>>((uintptr_t)at)));
-            vt[2 * hi] = t.x;
-            vt[2 * hi + 1] = t.y;
-          }
+          u32x4 &v = vt[half & 1][db];
           if constexpr (kCareful) {
             u32x4 code, one;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const uint32_t w2 = pw[0][x];  // (zero only for weights below the least bf16 value)
               one[x] = (w2 & 0xffffu ? 0x3f80u : 0u) | (w2 >> 16 ? 0x3f800000u : 0u);
-              uint32_t pair = vt[x];
+              uint32_t pair = v[x];
               code[x] = take_not_finite(pair);
-              vt[x] = pair;
+              v[x] = pair;
             }
             Acc<kN> codes;
             clear(codes);
@@ -557,7 +583,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
           }
 #pragma unroll
           for (int part = kParts - 1; part >= 0; --part)  // the small part first
-            o_acc[db] = product<kN>(vt, u32x4{pw[part][0], pw[part][1], pw[part][2], pw[part][3]}, o_acc[db]);
+            o_acc[db] = product<kN>(v, u32x4{pw[part][0], pw[part][1], pw[part][2], pw[part][3]}, o_acc[db]);
         }
       }
     } else {
@@ -590,31 +616,25 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
 #pragma unroll
     for (int db = 0; db < kBlocks; ++db) clear(o_acc[db]);
     ids_from = -64;
-    uint32_t first_there = 0;
-    // (the first cached stage is requested before the tree's own rows are waited for)
-    int ahead = 0;
-    while (ahead < n_steps && stage_at(ahead) < st.tree) ++ahead;
-    issue(ahead);
-    first_there = rows_there;
-    for (int step = 0; step < n_steps; ++step) {
-      const int stage = stage_at(step);
-      const uint32_t to = G::kSlots == 2 ? (step & 1) * G::kStage : 0;
-      uint32_t seen = 0;
-      if (stage < st.tree) {
-        land_tree(to, stage);
-        const int left = T - stage * kStageRows;
-        seen = left >= 32 ? ~0u : (1u << left) - 1u;
-      } else if (stage < n_stages) {
-        seen = first_there;
-        land(to, seen);
-        issue(step + 1);
-        first_there = rows_there;
-      }
+    if (steps_cached > 0) issue(steps_tree);  // (before the tree's own rows are waited for)
+    for (int step = 0; step < steps_tree; ++step) {
+      const int stage = stage_at(step), left = T - stage * kStageRows;
+      const uint32_t slot = G::kSlots == 2 ? (step & 1) * G::kStage : 0;
+      land_tree(slot, stage);
       if constexpr (kCw > 1) lds_barrier();
-      if (active && stage < n_stages && seen != 0) take_stage(to, stage, seen, with_care);
+      if (active) take_stage(slot, stage, left >= 32 ? ~0u : (1u << left) - 1u, with_care);
+    }
+    for (int step = steps_tree; step < steps_tree + steps_cached; ++step) {
+      const uint32_t slot = G::kSlots == 2 ? (step & 1) * G::kStage : 0, seen = rows_there;
+      land(slot, seen);
+      issue(step + 1 < steps_tree + steps_cached ? step + 1 : step);  // behind the last: that once more, not used
+      if constexpr (kCw > 1) lds_barrier();
+      if (active && seen != 0) take_stage(slot, stage_at(step), seen, with_care);
     }
     mfma_settle();  // O is read by what follows (within the loop it is read behind the next scores' wait)
   };
+  // What was requested so far is here: the loops' waits are for their own requests alone.
+  __builtin_amdgcn_s_waitcnt(0);
   walk(std::false_type{});
   bool careful;
   {

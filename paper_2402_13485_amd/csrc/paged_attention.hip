@@ -238,7 +238,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
   if (tid == 0) s_any = 0;
 
   // ---- which range
-  int b = 0, hk, block, piece, pieces, slot, steps;
+  int b = 0, hk, block, piece, pieces, slot, steps, L, T;
   {
     const PagedSequence lanes = paged_sequence<kN, kCw>(p, lane);
     const PagedPlan plan = paged_plan<kN, kCw>(p, lanes);
@@ -268,9 +268,13 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
       cut_before += __builtin_amdgcn_readlane(cut_incl, 63);
       units_before += paged_sum(q.units);
     }
-    const PagedSequence q = paged_sequence<kN, kCw>(p, b);
-    steps = __builtin_amdgcn_readfirstlane(q.steps);
-    const int n_blocks = __builtin_amdgcn_readfirstlane(q.units) / p.H_kv, rest = at - start;
+    // (the lengths of the first 64 sequences are at hand)
+    const PagedSequence q = p.B <= kWave ? lanes : paged_sequence<kN, kCw>(p, b);
+    const int src = p.B <= kWave ? b : 0;
+    steps = __builtin_amdgcn_readlane(q.steps, src);
+    L = __builtin_amdgcn_readlane(q.L, src);
+    T = __builtin_amdgcn_readlane(q.T, src);
+    const int n_blocks = __builtin_amdgcn_readlane(q.units, src) / p.H_kv, rest = at - start;
     pieces = paged_pieces(steps, most);
     // units next to each other, blocks of one K/V head first, then pieces
     piece = rest / count;
@@ -283,8 +287,6 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
       *reinterpret_cast<u32x4 *>(p.records + 4 * (((size_t)b * p.H_kv + hk) * p.blocks + block)) =
           u32x4{(uint32_t)first_slot, (uint32_t)count, (uint32_t)pieces, 0};
   }
-  const int L = __builtin_amdgcn_readfirstlane(clamped(p.seq_lens[b], p.pages.capacity));
-  const int T = __builtin_amdgcn_readfirstlane(clamped(p.n_nodes[b] - 1, p.T_max - 1) + 1);
   const PagedStages st = paged_stages(L, T, p.window);
   const int quot = steps / pieces, extra = steps - quot * pieces;
   const int step0 = piece * quot + (piece < extra ? piece : extra), n_steps = quot + (piece < extra ? 1 : 0);
@@ -725,9 +727,9 @@ __global__ __launch_bounds__(kWaves *kWave) void paged_merge_kernel(PagedParams 
   const unsigned item = blockIdx.x / (kCw * kShare);
   const unsigned unit = item / (unsigned)p.blocks, b = unit / (unsigned)p.H_kv;
   const int block = (int)(item - unit * (unsigned)p.blocks), hk = (int)(unit - b * (unsigned)p.H_kv);
+  const u32x4 record = *reinterpret_cast<const u32x4 *>(p.records + 4 * (size_t)item);  // (on its way with the number of nodes; not looked at beyond the columns)
   const int T = clamped(p.n_nodes[b] - 1, p.T_max - 1) + 1, columns = p.group * T;
   if ((block * kCw + cw) * kN >= columns) return;
-  const u32x4 record = *reinterpret_cast<const u32x4 *>(p.records + 4 * (size_t)item);
   const int first = (int)record.x, stride = (int)record.y, P = (int)record.z;
   if (P <= 1) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = (block * kCw + cw) * kN + lane % kN;
@@ -849,9 +851,15 @@ static bool launch_paged(PagedParams p, int L_max, hipStream_t st) {
 template <bool kBf16, bool kCodes, int D>
 static bool launch_paged(const PagedParams &p, int L_max, hipStream_t st) {
   const int columns = p.group * p.T_max;
-  return columns <= 16 ? launch_paged<kBf16, kCodes, D, 16, 1>(p, L_max, st)
-         : columns <= 64 ? launch_paged<kBf16, kCodes, D, 16, 4>(p, L_max, st)
-                         : launch_paged<kBf16, kCodes, D, 32, 4>(p, L_max, st);
+  if (columns <= 16) return launch_paged<kBf16, kCodes, D, 16, 1>(p, L_max, st);
+  // Blocks of 64 columns read every row from LDS twice as often per product as those of 128, and there are more of them: better where all stages of a
+  // call hardly fill the chip.  Calls (sequences, query heads on K/V heads, nodes, rows; 8 bits, d = 128), us, 64 / 128 columns:
+  //   bf16  1, 32 on 8, 32, 500: 15.3 / 16.4     3, 64 on 8, 113, 12: 19.0 / 29.0     2, 16 on 4, 48, 1024: 26.0 / 23.7    4, 32 on 8, 64, 2048: 42 / 36
+  //   fp32                      20.3 / 24.6                          40.4 / 40.4                          29.2 / 32.1                          123 / 101
+  const long long blocks = (long long)p.B * p.H_kv * ((columns + 127) / 128);
+  const long long stages = (L_max + kStageRows - 1ll) / kStageRows + (p.T_max + kStageRows - 1) / kStageRows;
+  const bool few = blocks * stages <= 1024 && (!kBf16 || stages <= 20);
+  return columns <= 64 || few ? launch_paged<kBf16, kCodes, D, 16, 4>(p, L_max, st) : launch_paged<kBf16, kCodes, D, 32, 4>(p, L_max, st);
 }
 
 }  // namespace propd

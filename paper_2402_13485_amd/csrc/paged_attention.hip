@@ -130,7 +130,10 @@ __device__ __forceinline__ PagedSequence paged_sequence(const PagedParams &p, in
   return q;
 }
 
+// Pieces of a unit.  The second kernel takes 16 of them at a time, which costs as much as half a step: no more than make the two least together.
 __device__ __forceinline__ int paged_pieces(int steps, int most) {
+  const int enough = (int)ceilf(sqrtf((float)steps * (1.f / 24.f)));
+  most = most > enough ? most : enough;
   return most >= steps ? 1 : (int)((unsigned)(steps + most - 1) / (unsigned)most);
 }
 __device__ __forceinline__ int paged_scan(int v) {
@@ -831,8 +834,10 @@ static bool launch_paged(PagedParams p, int L_max, hipStream_t st) {
   const int resident = (kBf16 ? 2 : 1) * compute_units();
   p.resident = resident < kPagedResident ? resident : kPagedResident;
   const long long steps = ((L_max + kStageRows - 1ll) / kStageRows + (p.T_max + kStageRows - 1) / kStageRows + G::kRw - 1) / G::kRw;
-  p.least = G::kRw == 1 ? 2 : 1;
-  p.may_split = units < kPagedUnits && steps > p.least ? 1 : 0;
+  // Few steps are not worth a second kernel (8 units of two steps 9.0 us instead of 12.0), nor a short range of 128 columns its partial result of 64 KB: 32
+  // units of 20 steps in pieces of at least 6 / 4 / 2 steps 18.6 / 19.0 / 24.2, 80 of 11 23.5 / 26.7 / 27.7; fp32 products take longer: 24 of 34 23.5 / 21.3 / 20.6.
+  p.least = G::kRw > 1 ? 1 : kN == 32 && kBf16 ? 6 : 2;
+  p.may_split = units < kPagedUnits && steps > (G::kRw == 1 ? p.least : 2) ? 1 : 0;
   // (ranges that come first: units, and the pieces of those that are cut; then the others')
   long long grid = units;
   if (p.may_split) {

@@ -1,16 +1,17 @@
 // Acceptance by sampling: drafted tokens against the target's probabilities, with given random numbers.
 //
-// Three kernels:
+// Two kernels, and a third in front of the last where candidates were drawn:
 //   sampled_stats_kernel  largest value and sum of exponentials of the logits rows of nodes that have children (the target's, and the draft's
 //                         if it is given), in slices of 4096 values that stay in registers between the two
-//   sampled_walk_kernel   one workgroup per sequence: the probabilities of all candidates at once, then the tests along the path.  What a
+//   sampled_walk_kernel   (drawn candidates) one workgroup per sequence: the probabilities of all candidates at once, then the tests along the path.  What a
 //                         refused candidate leaves of the target needs no distribution of its own: after k refusals r = (p - s_k q)+ / W_k
 //                         with s_0 = 0, W_0 = 1, W_k = sum over the vocabulary of (p - s_k q)+ and s_{k+1} = s_k + W_k, since
 //                         ((p - s q)+ / W - q)+ = (p - (s + W) q)+ / W.  Only a candidate that has refused siblings before it needs the sum.
 //   sampled_next_kernel   the token after the path: what is left in chunks of 4096 tokens, by all workgroups of a sequence; the one that ends
-//                         last finds the chunk, and in it the token.
+//                         last finds the chunk, and in it the token.  Candidates that were not drawn need no sums: every workgroup walks by itself.
 // 64 bits throughout: a vocabulary has so many borders between tokens that an error of 2^-24 of a sum would move one token in a few hundred.
-// The rows are read at memory speed; the exponentials (20 fp64 instructions each, at the rate of fp32 ones) take as long.
+// What bounds it: latency.  One sequence of 16 nodes takes 18.8 us, of them 4.5 in the first kernel; 16 sequences of 64 nodes 29.3, 13 in the first, whose
+// exponentials (18 fp64 instructions each, at the rate of fp32 ones) take as long as its reads; drawn candidates of 4 sequences 49, 34 in the walk.
 #include <math.h>
 
 #include <type_traits>
@@ -19,8 +20,8 @@
 
 namespace propd {
 
-// (four tokens per thread: what little code there is runs once, and is fetched meanwhile; with 16 per thread of 256 the kernel of the last token took 15.8 us
-// instead of NEXT_US for one sequence of 32000 tokens)
+// Threads by tokens of each, us: one sequence of 16 nodes / 16 of 64 nodes (32000 tokens, three kernels): 256 x 16 22.1 / 37.0, 512 x 8 20.2 / 35.2,
+// 1024 x 4 22.2 / 39.0, 256 x 8 20.5 / 41.5.
 constexpr int kOf = 8, kSampledThreads = 512, kSliceTokens = kOf * kSampledThreads;
 constexpr int kWalkThreads = 1024;  // where the draft's distributions take part
 constexpr int kMostVocab = 1 << 20;

@@ -247,3 +247,22 @@ def test_frequencies(pb):
         first = np.where(a > 1, token[np.arange(B), np.clip(path[:, 1], 0, 3)], nxt)
         counts = np.bincount(first, minlength=V)
         assert (np.abs(counts - B * p[0]) < 5 * np.sqrt(B * p[0] * (1 - p[0]))).all()
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+def test_many_sequences(pb, drawn):
+    """More sequences than workgroups to go round, small and large trees side by side."""
+    rng = np.random.default_rng(12)
+    check(pb, make_case(rng, "f32", 700, 9, 30, drawn))
+    check(pb, make_case(rng, "bf16", 70, 60, 200, drawn, sharp=2.0))
+
+
+def test_numbers_that_are_no_numbers(pb):
+    """NaN in u refuses, NaN in u_next takes some token that is left; nothing is read or written out of range."""
+    rng = np.random.default_rng(13)
+    for drawn in (False, True):
+        x = make_case(rng, "f32", 4, 8, 5000, drawn)
+        x["u"][:], x["u_next"][:] = np.nan, np.nan
+        args, kw = dev_args(pb, x)
+        a, path, nxt = (to_host(t) for t in pb.propd_accept_sampled(*args, **kw))
+        assert (a == 1).all() and (path[:, 0] == 0).all() and (path[:, 1:] == -1).all() and ((nxt >= 0) & (nxt < 5000)).all()

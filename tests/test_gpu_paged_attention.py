@@ -313,3 +313,40 @@ def test_dense_and_paged_caches_agree(pb):
         # half a step of each, and 2^-15 for weights and sums
         assert ((a - b).float().abs()[:, :, :n] <= 2.0 ** -7 * b.float().abs()[:, :, :n] + 2.0 ** -12).all()
         assert ((al - bl).abs()[:, :, :n] <= 2.0 ** -18 * (1 + bl.abs()[:, :, :n])).all()
+
+
+@pytest.mark.parametrize("B,H,Hk,T,dtype,codes", [(84, 16, 4, 40, "bf16", True), (84, 16, 4, 40, "bf16", False), (70, 16, 4, 40, "f32", False), (150, 16, 4, 16, "bf16", True),
+                                                  (150, 16, 4, 4, "bf16", True), (90, 8, 4, 2, "f32", True)])
+def test_more_units_than_run_at_once(pb, B, H, Hk, T, dtype, codes):
+    """Whole units first and the others cut, in every shape of the waves, with one sequence so long that its units among the first are cut too."""
+    rng = np.random.default_rng(B + T)
+    lens = [int(x) for x in rng.integers(0, 60, B)]
+    lens[1], lens[B - 2] = 2500, 700
+    x = make_case(rng, dtype, codes, H, Hk, 64, [synth.chain_tree(min(T, 3 + b % T)) for b in range(B)], lens, 64, T_max=T)
+    check_attention(x, rule_of(64), *run_attention(pb, x, rule_of(64)))
+
+
+def test_two_streams_at_once(pb):
+    """Calls on two streams with workspaces of their own give the bits that they give alone."""
+    rng = np.random.default_rng(21)
+    calls = []
+    for T, L in ((1, 1500), (30, 900)):
+        x = make_case(rng, "bf16", True, 8, 2, 128, [synth.random_tree(rng, T)] * 3, [L, L // 2, 7], 32)
+        tree, cache = dev_tree(pb, x), dev_cache(pb, x)
+        q, kt, vt, lens = (to_dev(x[n]) for n in ("q", "k_tree", "v_tree", "seq_lens"))
+        out = torch.zeros_like(q)
+        ws = torch.empty(pb.workspace_bytes(pb.WS_PAGED_ATTENTION, 3, T, 8, 128, cache.capacity), dtype=torch.uint8, device="cuda")
+        calls.append((out, lambda a=(tree, q, cache, kt, vt, lens), o=out, w=ws: pb.propd_paged_attention(*a, 0.088, out=o, workspace=w)))
+    want = []
+    for out, call in calls:
+        call()
+        torch.cuda.synchronize()
+        want.append(out.clone())
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(10):
+        for (out, call), stream in zip(calls, streams):
+            with torch.cuda.stream(stream):
+                out.zero_()
+                call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out, w) for (out, _), w in zip(calls, want))

@@ -140,3 +140,21 @@ def test_tensors_in_host_memory_are_refused(pb):
                  lambda: pb.propd_accept_sampled(tree, torch.zeros((1, 4, 9)), torch.zeros((1, 4)), torch.zeros(1))):
         with pytest.raises(TypeError):
             call()
+
+
+def test_other_calls_refuse_the_type_of_8_bit_pages(pb):
+    lib, t, big = pb.load_library(), tree_of(pb), 1 << 40
+    out = ctypes.byref(pb._TreeOut(OK, OK, OK, OK, OK))
+    rule = ctypes.byref(pb._ScoreRule(0.1, 0.0, 0, None))
+    rows = ctypes.byref(pb._CacheRows(OK, OK, OK, OK))
+    e4m3 = pb.PROPD_E4M3
+    for status in (lib.propd_tree_attention(t, e4m3, 2, 128, 1.0, OK, OK, OK, OK, OK, OK, 64, OK, OK, big, None),
+                   lib.propd_early_prune(t, e4m3, 128, 1000, 4, OK, OK, OK, OK, OK, OK, OK, out, None, 0, None, OK, big, None),
+                   lib.propd_early_prune_prob(t, e4m3, 128, 1000, 0, 0.5, 0, OK, OK, OK, OK, OK, OK, OK, out, None, 0, None, OK, big, None),
+                   lib.propd_accept_path(t, e4m3, 100, OK, OK, OK, 8, OK, OK, big, None), lib.propd_accept_path_static(t, e4m3, 100, OK, OK, OK, 8, OK, None),
+                   lib.propd_commit_path(t, e4m3, 2, 128, OK, OK, 8, OK, OK, OK, OK, OK, 64, OK, OK, 8, None),
+                   lib.propd_grouped_attention(t, e4m3, 8, 2, 128, rule, OK, OK, OK, OK, OK, OK, None, None, 64, OK, None, OK, big, None),
+                   lib.propd_cache_observe(t, e4m3, 8, 2, 128, rule, 0.5, OK, OK, 8, OK, OK, OK, OK, OK, None, None, OK, 64, None, OK, None),
+                   lib.propd_cache_evict(2, e4m3, 2, 128, 64, 8, 1, 1, OK, 0x2000, rows, rows, OK, big, None),
+                   lib.propd_rotary(e4m3, 2, 4, 2, 2, 64, 64, 0, 1, None, OK, None, OK, 1, None, OK, OK, OK, OK, None)):
+        assert status == INVALID

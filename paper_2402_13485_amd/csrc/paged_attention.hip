@@ -2,14 +2,14 @@
 //
 // A unit is a (sequence, K/V head, block of query columns): the nodes of all query heads that read the K/V head lie side by side, column r is
 // node r % T of head r / T, so that a row is read once for all of them.  Its rows come in stages of 32, the tree's own first, then the cached ones.
-//   - A workgroup takes a range of a unit's stages.  Its four waves are kCw columns of 32 query columns by 4 / kCw rows of
-//     stages: a single token or a small tree has one column of waves, each of which streams stages of its own and waits for nobody; the
-//     row of waves of a large tree shares every stage.
+//   - A workgroup takes a range of a unit's stages.  Its four waves are kCw blocks of kN query columns by 4 / kCw rows of stages: up to 16 columns
+//     (a single token) each wave streams stages of its own and waits for nobody; up to 64 columns, and beyond with 32 a wave, four waves share
+//     every stage.
 //   - The next stage's rows are on their way to registers while a stage is multiplied; from there they go to LDS, 8-bit rows
 //     as the bf16 or fp32 values that they stand for (once per workgroup, not once per wave that multiplies them).
 //   - S^T = K . Q^T, so that a lane owns a column: running maximum and sum, position, slope and ancestor set are per-lane scalars, and the weights
-//     are the B operand of O^T += V^T . P^T as they are.  bf16: 32x32x16 products, V^T by transposing LDS reads, a weight as the sum of two bf16
-//     values (off by 2^-17; one alone would add 40 % to the result's own rounding).  fp32: 32x32x2 products.
+//     are the B operand of O^T += V^T . P^T as they are.  bf16: products of 32x32x16 or 16x16x32, V^T by transposing LDS reads, a weight as the sum
+//     of two bf16 values (off by 2^-17; one alone would add 40 % to the result's own rounding).  fp32: products of 32x32x2 or 16x16x4.
 //   - Ranges of a unit leave partial results, which a second kernel joins in their order.
 // What bounds it: a single token or few, memory (32 x 8 heads of 8192 rows in 8 bits 96 us, 5.6 TB/s); large trees, vector and matrix instructions that hardly
 // overlap (16 x 40 heads on 8, 128 nodes, 4096 rows 307 us, matrix unit busy 43 %); small calls, a chain of dependent reads (1 x 32 heads of 1024 rows 13 us).
@@ -30,7 +30,7 @@ struct PagedParams {
   const uint64_t *anc;
   const float *slopes;
   int B, H, H_kv, group, T_max;
-  int blocks;   // blocks of 32 * kCw columns of a unit's tree of T_max nodes
+  int blocks;   // blocks of kN * kCw columns of a unit's tree of T_max nodes
   int window;   // window_of
   float scale_log2e, cap_in, cap_log2e;  // cap_in: scale / cap
   float *part_o, *part_ml;
@@ -48,7 +48,7 @@ struct PagedGeo {
   static constexpr int kRowBytes = D * (kBf16 ? 2 : 4);
   static constexpr int kPart = kStageRows * kRowBytes;  // K part of a stage; the V part follows
   static constexpr int kStage = 2 * kPart;
-  static constexpr int kSlots = kCw == 1 ? 1 : 2;      // a wave's own stage needs one
+  static constexpr int kSlots = kCw == 1 ? 1 : 2;      // places for stages; a wave's own needs one
   static constexpr int kChunks = kRowBytes / 16;
   static constexpr int kGroups = 64 / kN;              // lanes that have a column
   static constexpr int kScores = 32 / kGroups;         // scores of a lane per stage; number x is of row 4 * kGroups * (x / 4) + 4 * group + x % 4

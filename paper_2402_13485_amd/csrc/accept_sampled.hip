@@ -53,7 +53,7 @@ struct SampledParams {
   int32_t *accept_len, *accept_path, *next_token;
 };
 
-// 2^t for t up to about 0: t = n + f with |f| <= 1/2, the series of 2^f = exp(f log 2) up to f^11 (6e-15 off).  Below 2^-1074 it is 0.
+// 2^t for t up to 0: t = n + f with |f| <= 1/2, the series of 2^f = exp(f log 2) up to f^11 (6e-15 off).  Below 2^-1074 it is 0.
 __device__ __forceinline__ double exp2_below(double t) {
   t = fmax(t, -1100.0);
   const double n = rint(t), f = t - n;
@@ -72,19 +72,20 @@ __device__ __forceinline__ double exp2_below(double t) {
   return __builtin_amdgcn_ldexp(s, (int)n);
 }
 
-// The weights of a row's tokens: exp((x - most) * inv) times a scale, as 2^(x * slope + offset).  Where `most` is infinite, those that
-// are it have the scale and the others nothing.
+// The weights of a row's tokens: exp((x - most) * inv) times a scale of at most 1, as 2^((x - most) * slope + log2(scale)).  The difference comes first: it is
+// exactly 0 at the row's largest logit and negative elsewhere, however large the logits are (most * slope alone is off by 1e22 for a row masked with
+// fp32's lowest value).  Where `most` is infinite, those that are it have the scale and the others nothing.
 struct Weights {
-  double slope, offset;
+  double most, slope, offset;
   bool infinite;
-  __device__ __forceinline__ Weights(float most, double inv, double scale = 1.0) {
-    infinite = most == INFINITY;
+  __device__ __forceinline__ Weights(float row_most, double inv, double scale = 1.0) {
+    infinite = row_most == INFINITY;
+    most = row_most == -INFINITY || infinite ? 0.0 : (double)row_most;  // (a row of -inf: every weight is 0)
     slope = inv * 1.4426950408889634;
-    offset = most == -INFINITY || infinite ? 0.0 : -(double)most * slope;
-    offset = scale == 1.0 ? offset : scale > 0.0 ? offset + log2(scale) : -INFINITY;
+    offset = scale == 1.0 ? 0.0 : scale > 0.0 ? log2(scale) : -INFINITY;
   }
   __device__ __forceinline__ double operator()(float x) const {
-    return exp2_below(infinite ? (x == INFINITY ? offset : -INFINITY) : fma((double)x, slope, offset));
+    return exp2_below(infinite ? (x == INFINITY ? offset : -INFINITY) : fma((double)x - most, slope, offset));
   }
 };
 

@@ -215,6 +215,10 @@ __device__ __forceinline__ void store_quad(unsigned char *out, size_t at, f32x4 
   else *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(out) + at) = f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
 }
 
+// A part of a result times a factor that may be zero: a row that is seen has a weight above zero, however little it is, so that what an infinity or a NaN
+// of V made stays, in whatever order rows and ranges come.
+__device__ __forceinline__ float weighed(float o, float f) { return fabsf(o) < INFINITY ? o * f : o; }
+
 __device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : l; }  // NaN stays
 
 // LDS written before is seen by the workgroup; loads from memory stay in flight.
@@ -526,10 +530,15 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
 #pragma unroll
       for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
-        for (int r = 0; r < kAcc; ++r) o_acc[db][r] *= alpha;
+        for (int r = 0; r < kAcc; ++r) o_acc[db][r] = kCareful ? weighed(o_acc[db][r], alpha) : o_acc[db][r] * alpha;
       m_run = m_new;
     }
     const float neg_m = -(m_run == -INFINITY ? 0.f : m_run);
+    uint32_t live = 0;  // scores of rows that are seen
+    if constexpr (kCareful) {
+#pragma unroll
+      for (int x = 0; x < kScores; ++x) live |= sc[x] > -INFINITY ? 1u << x : 0u;
+    }
     // V^T of the rows of 8 scores, requested ahead of what they are multiplied with
     u32x4 vt[kBf16 ? 2 : 1][kBf16 ? kBlocks : 1];
     auto read_v = [&](int half) __attribute__((always_inline)) {
@@ -575,8 +584,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
             u32x4 code, one;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-              const uint32_t w2 = pw[0][x];  // (zero only for weights below the least bf16 value)
-              one[x] = (w2 & 0xffffu ? 0x3f80u : 0u) | (w2 >> 16 ? 0x3f800000u : 0u);
+              one[x] = (live >> (8 * half + 2 * x) & 1 ? 0x3f80u : 0u) | (live >> (8 * half + 2 * x + 1) & 1 ? 0x3f800000u : 0u);
               uint32_t pair = v[x];
               code[x] = take_not_finite(pair);
               v[x] = pair;
@@ -605,7 +613,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
           if constexpr (kCareful) {
             const float code = not_finite_code(__float_as_uint(v));
             v = code == 0.f ? v : 0.f;
-            codes = product<kN>(code, sc[x] == 0.f ? 0.f : 1.f, codes);
+            codes = product<kN>(code, live >> x & 1 ? 1.f : 0.f, codes);
           }
           o_acc[db] = product<kN>(v, sc[x], o_acc[db]);
         }
@@ -689,7 +697,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
 #pragma unroll
     for (int x = 0; x < G::kQuads; ++x) {
       const f32x4 v = quad_of(x);
-      room[(wave * G::kQuads + x) * kWave + lane] = f == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : v * f;
+      room[(wave * G::kQuads + x) * kWave + lane] = f32x4{weighed(v[0], f), weighed(v[1], f), weighed(v[2], f), weighed(v[3], f)};
     }
     lds_barrier();
 #pragma unroll
@@ -753,7 +761,7 @@ __global__ __launch_bounds__(kWaves *kWave) void paged_merge_kernel(PagedParams 
     a_new *= careful && !theirs ? kBack : 1.f;
     careful = careful || theirs;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = (a_old == 0.f ? 0.f : acc[r] * a_old) + (a_new == 0.f ? 0.f : o[r] * a_new);
+    for (int r = 0; r < 16; ++r) acc[r] = weighed(acc[r], a_old) + weighed(o[r], a_new);
     M = M_new;
   };
   constexpr int kTogether = 4;  // pieces of a wave that are requested together

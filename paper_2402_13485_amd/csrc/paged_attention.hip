@@ -689,8 +689,7 @@ __global__ __launch_bounds__(kPagedThreads, kBf16 ? 2 : 1) void paged_attn_kerne
     const float safe = M == -INFINITY ? 0.f : M;
 #pragma unroll
     for (int w = 0; w < kRw; ++w) {
-      const float f = fast_exp2(s_ml[w * kCw + cw][0][lane] - safe);
-      total += f == 0.f ? 0.f : f * s_ml[w * kCw + cw][1][lane];
+      total += fast_exp2(s_ml[w * kCw + cw][0][lane] - safe) * s_ml[w * kCw + cw][1][lane];  // (sums are finite, or NaN that stays)
     }
     const float f = fast_exp2(m_run - safe);
     f32x4 *const room = reinterpret_cast<f32x4 *>(smem);  // [4 waves][quads][lanes]
@@ -756,7 +755,7 @@ __global__ __launch_bounds__(kWaves *kWave) void paged_merge_kernel(PagedParams 
     const bool theirs = signbit(signed_l);
     const float M_new = fmaxf(M, m), safe = M_new == -INFINITY ? 0.f : M_new, l = fabsf(signed_l);
     float a_old = fast_exp2(M - safe), a_new = fast_exp2(m - safe);
-    total = total * a_old + (a_new == 0.f ? 0.f : l * a_new);
+    total = total * a_old + l * a_new;  // (finite, or NaN that stays)
     a_old *= theirs && !careful ? kBack : 1.f;
     a_new *= careful && !theirs ? kBack : 1.f;
     careful = careful || theirs;

@@ -61,3 +61,21 @@ def test_infinities_of_rows_that_weigh_next_to_nothing(pb, dtype, codes, T, L, o
     for column in (9, 17):
         assert np.isnan(got[..., column]).all()
     check_attention(x, rule_of(64), out, lse)
+
+
+@pytest.mark.parametrize("where", ["own row", "last row", "second half"])
+@pytest.mark.parametrize("T,L", [(1, 33), (1, 200), (1, 5000), (9, 65), (20, 4000), (70, 4000)])
+@pytest.mark.parametrize("dtype,codes", TYPES)
+def test_scores_that_are_no_numbers(pb, dtype, codes, T, L, where):
+    """NaN in K of rows that a query sees: its results are NaN, also where a range of rows or a wave has nothing but such rows."""
+    rng = np.random.default_rng(L + T)
+    x = make_case(rng, dtype, codes, 4, 2, 64, [synth.chain_tree(T), synth.chain_tree(T)], [L, L], 16)
+    clean = run_attention(pb, x, rule_of(64))
+    if where == "own row":  # of the first node, which all others see
+        x["k_tree"][0, :, 0, 7] = synth.from_float(np.array([np.nan], np.float32), dtype)[0]
+    for j in {"own row": [], "last row": [L - 1], "second half": range(L // 2, L)}[where]:
+        page, at = x["page_table"][0, j // 16], j % 16
+        x["k_pages"][page, :, at, 7] = 0x7f if codes else synth.from_float(np.array([np.nan], np.float32), dtype)[0]
+    out, lse = run_attention(pb, x, rule_of(64))
+    assert np.isnan(synth.as_float(out[0])).all() and np.isnan(lse[0]).all()
+    assert (out[1].view(np.uint8) == clean[0][1].view(np.uint8)).all() and (lse[1] == clean[1][1]).all()

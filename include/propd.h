@@ -472,6 +472,8 @@ typedef struct propd_paged_cache {
  *              2^-17) for PROPD_BF16
  *   seq_lens   [B], clamped to [0, table_pages * page_rows]
  *   out and lse rows i >= n_nodes[b] are left untouched
+ *   v          an infinity or a NaN in a row reaches the nodes that see the row with a score above -inf, however little it weighs, and no others;
+ *              a score that is NaN makes a node's results NaN
  *   workspace  propd_workspace_bytes(PROPD_WS_PAGED_ATTENTION, B, T_max, H, d, table_pages * page_rows, 0, 0) bytes
  * q, pages, k_tree, v_tree, out, anc and workspace must be 16-byte aligned.
  */
@@ -522,7 +524,8 @@ PROPD_API propd_status propd_paged_read(propd_dtype dt, int32_t B, int32_t S, in
  * without the tokens refused, or r): the lowest v with r(0) + ... + r(v) > u_next[b].  If nothing is left, it is the likeliest token of p_l (the lowest id among equal ones).
  * As there, a path buffer shorter than the path keeps its first path_stride nodes, and next_token is then the token of the next node.
  *   logits, draft_logits  dt = PROPD_BF16 or PROPD_F32, read for nodes that have children, and logits at the path's end.
- *            NaN counts as -inf (probability 0); several +inf share the probability; a row of -inf alone gives probability 0 throughout.
+ *            NaN counts as -inf (probability 0); several +inf share the probability; a row of -inf alone gives probability 0 throughout.  Finite logits
+ *            may be of any size: only their differences to the row's largest count, so that a mask may be the type's lowest value.
  *            16-byte aligned rows are read faster, others are allowed
  *   u        [B,T_max], u_next [B]   fp32 in [0,1); the entries of node 0 and of padding are not used
  *   tree     n_nodes, parent, token are read; a token outside [0, vocab) is refused and changes nothing

@@ -10,8 +10,9 @@
 //   sampled_next_kernel   the token after the path: what is left in chunks of 4096 tokens, by all workgroups of a sequence; the one that ends
 //                         last finds the chunk, and in it the token.  Candidates that were not drawn need no sums: every workgroup walks by itself.
 // 64 bits throughout: a vocabulary has so many borders between tokens that an error of 2^-24 of a sum would move one token in a few hundred.
-// What bounds it: latency.  One sequence of 16 nodes takes 18.8 us, of them 4.5 in the first kernel; 16 sequences of 64 nodes 29.3, 13 in the first, whose
-// exponentials (18 fp64 instructions each, at the rate of fp32 ones) take as long as its reads; drawn candidates of 4 sequences 49, 34 in the walk.
+// What bounds it: latency.  One sequence of 16 nodes takes 18.4 us, of them 4.5 in the first kernel; 16 sequences of 64 nodes 29.1, 13 in the first, whose
+// exponentials (19 fp64 instructions each, at the rate of fp32 ones) take as long as its reads; drawn candidates of 4 sequences 50 to 60, 35 and more in the walk by how many
+// of them are refused.
 #include <math.h>
 
 #include <type_traits>

@@ -11,8 +11,10 @@
 //     are the B operand of O^T += V^T . P^T as they are.  bf16: products of 32x32x16 or 16x16x32, V^T by transposing LDS reads, a weight as the sum
 //     of two bf16 values (off by 2^-17; one alone would add 40 % to the result's own rounding).  fp32: products of 32x32x2 or 16x16x4.
 //   - Ranges of a unit leave partial results, which a second kernel joins in their order.
+//   - A range whose sums are not finite, or could leave fp32 when joined, is done once more with care: values of V that are not finite are taken out of the
+//     products and counted by sign for the columns that see their rows, and weights are small enough that no sum exceeds its largest value.
 // What bounds it: a single token or few, memory (32 x 8 heads of 8192 rows in 8 bits 96 us, 5.6 TB/s); large trees, vector and matrix instructions that hardly
-// overlap (16 x 40 heads on 8, 128 nodes, 4096 rows 307 us, matrix unit busy 43 %); small calls, a chain of dependent reads (1 x 32 heads of 1024 rows 13 us).
+// overlap (16 x 40 heads on 8, 128 nodes, 4096 rows 300 us, matrix unit busy 43 %); small calls, a chain of dependent reads (1 x 32 heads of 1024 rows 13 us).
 #include "attention_device.h"
 #include "paged_cache.h"
 #include "score_rule.h"
@@ -820,7 +822,7 @@ __global__ __launch_bounds__(kWaves *kWave) void paged_merge_kernel(PagedParams 
 // Partial results of a call, at most: as many ranges as run at once, of units that are left over, and twice as many of units that come first (a unit that
 // is cut is longer than an equal share: it has fewer pieces than twice its shares).
 constexpr int kPagedResident = 512, kPagedSlots = 3 * kPagedResident;
-constexpr long long kPagedUnits = 8 * kPagedResident;  // more are not cut: the last round is an eighth of the call at most
+constexpr long long kPagedUnits = 8 * kPagedResident;  // from so many on none is cut: the last round is an eighth of the call at most
 
 static long long paged_slots(int B, int H, int L_max) {
   const long long stages = (L_max + kStageRows - 1ll) / kStageRows + PROPD_MAX_TREE / kStageRows;
@@ -872,6 +874,8 @@ static bool launch_paged(const PagedParams &p, int L_max, hipStream_t st) {
   //   fp32                      20.3 / 24.6                          40.4 / 40.4                          29.2 / 32.1                          123 / 101
   const long long blocks = (long long)p.B * p.H_kv * ((columns + 127) / 128);
   const long long stages = (L_max + kStageRows - 1ll) / kStageRows + (p.T_max + kStageRows - 1) / kStageRows;
+  // The lengths are on the device: stages are those that the table has room for, here and where a second kernel is chosen.  In tables of 8192 rows (and of
+  // 131072) the first of these takes 19.0 (bf16) and 24.6 (fp32), one token over 40 rows 10.0 instead of 7.7, calls of more stages what they take otherwise.
   const bool few = blocks * stages <= 1024 && (!kBf16 || stages <= 20);
   return columns <= 64 || few ? launch_paged<kBf16, kCodes, D, 16, 4>(p, L_max, st) : launch_paged<kBf16, kCodes, D, 32, 4>(p, L_max, st);
 }
